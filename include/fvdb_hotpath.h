@@ -449,6 +449,102 @@ fx_status fx_sparse_conv_leaf_bwd_weight(const fx_grid* g, const void* d_feat, c
                                          int32_t C_in, int32_t C_out, void* d_gw, fx_dtype out_dt, void* stream);
 
 /* ---------------------------------------------------------------------------------------
+ * What stands around a convolution in a network: a recurrence that reaches along all of a grid's voxels, the norms,
+ * gate and residual connection of a block, and dropout.  Features are rows of C channels as everywhere in this
+ * library; here every tensor of rows also has a row stride ld_* in elements (>= C), so that a column range of a wider
+ * tensor -- features and gate out of one projection -- needs no copy.  Elements of a row follow each other; pointers
+ * are aligned to an element, no more.  Arithmetic and sums are fp32, every output is rounded once (RNE) to its type.
+ * Vectors over the channels (norm weights, scale) and their gradients have a dtype of their own, vec_dt: the rows' or
+ * FX_F32.  None of these calls synchronises, except fx_build_sequences.  No atomics are used on results: a call
+ * gives the same bits every time.
+ *
+ * Sequences: which rows follow each other.  h_joffsets [B,2] (host) as for a grid -- the voxel ranges of a batch of
+ * grids (fx_grid_info) make every grid one sequence in index order --, but the ranges must follow each other without
+ * gaps from row 0 to row `rows` (FX_EINVAL); ranges without rows, B == 0 and rows == 0 are valid.
+ * Synchronises `stream`; afterwards the handle may be used on any stream.  Destroy it when no work that uses it is
+ * in flight on a stream other than the one it was built on. */
+typedef struct fx_sequences fx_sequences;
+fx_status fx_build_sequences(const int64_t* h_joffsets, int32_t B, int64_t rows, void* stream, fx_sequences** out);
+void fx_sequences_destroy(fx_sequences* q);
+
+/* Gated linear recurrence.  For every sequence and channel, t running over its rows in order, or against it where
+ * `reverse` is not 0:
+ *     h_t = f_t h_(t-1) + (1 - f_t) x_t,   f = sigmoid(gate),   h before the first row = h0
+ *   d_x, d_gate  device [rows, C], dtype dt
+ *   d_h0         device [B, C] fp32, or NULL for zeros
+ *   d_h          device [rows, C], dtype dt; must not be d_x or d_gate (FX_EINVAL) nor overlap them
+ *   d_last       device [B, C] fp32, or NULL: the unrounded state behind every sequence's last row; h0 (or zeros) for a
+ *                sequence without rows.  Fed as h0 to the rows that come later, it continues the recurrence.
+ * 1 - f is computed as sigmoid(-gate), to its own precision where f is near 1.  An infinity or NaN stays in its
+ * sequence and channel; a sequence's rows do not depend on any other's.
+ * Backward, with gh = dL/dh and glast = dL/dlast (fp32 [B, C], NULL for zeros): d_h is what the forward call wrote
+ * (the states enter the gate's gradient as they were rounded then), d_h0 what it was given.
+ *     lambda_t = gh_t + f_(t+1) lambda_(t+1)  (glast in the place of the second term at the last row)
+ *     gx_t = (1 - f_t) lambda_t,  ggate_t = lambda_t (h_(t-1) - x_t) f_t (1 - f_t),  gh0 = f_first lambda_first
+ *   d_gx, d_ggate [rows, C] dtype dt, neither where an input lies; d_gh0 [B, C] fp32 or NULL (glast or zeros for a
+ *   sequence without rows).
+ * Step, for rows that arrive one at a time: rows r of d_x and d_gate are the next rows of `rows` running sequences with
+ * states d_state [rows, C] fp32; d_new_state may be d_state. */
+fx_status fx_gated_scan_fwd(const fx_sequences* q, const void* d_x, int64_t ld_x, const void* d_gate, int64_t ld_gate, fx_dtype dt,
+                            int32_t C, int32_t reverse, const float* d_h0, void* d_h, int64_t ld_h, float* d_last, void* stream);
+fx_status fx_gated_scan_bwd(const fx_sequences* q, const void* d_x, int64_t ld_x, const void* d_gate, int64_t ld_gate, const void* d_h,
+                            int64_t ld_h, const void* d_gh, int64_t ld_gh, fx_dtype dt, int32_t C, int32_t reverse, const float* d_h0,
+                            const float* d_glast, void* d_gx, int64_t ld_gx, void* d_ggate, int64_t ld_ggate, float* d_gh0, void* stream);
+fx_status fx_gated_scan_step(const void* d_x, int64_t ld_x, const void* d_gate, int64_t ld_gate, fx_dtype dt, int64_t rows, int32_t C,
+                             const float* d_state, float* d_new_state, void* d_h, int64_t ld_h, void* stream);
+
+/* Norm in front of a block:  out[r,c] = x[r,c] / sqrt(mean_c x[r,c]^2 + eps) * weight[c]   (weight NULL: ones), and its
+ * gradients:  gx = (g w - xh mean_c(g w xh)) / sqrt(mean x^2 + eps),  gweight = sum over rows of g xh,  xh the row
+ * without its weight.  d_gx or d_gweight may be NULL (not computed); d_out may be d_x, d_gx may be d_gout or d_x.
+ * C up to 4096, rows up to 2^31-1 (FX_ERANGE), here and in the calls below. */
+fx_status fx_rms_norm_fwd(const void* d_x, int64_t ld_x, fx_dtype dt, int64_t rows, int32_t C, const void* d_weight,
+                          fx_dtype vec_dt, float eps, void* d_out, int64_t ld_out, void* stream);
+fx_status fx_rms_norm_bwd(const void* d_gout, int64_t ld_gout, const void* d_x, int64_t ld_x, fx_dtype dt, int64_t rows,
+                          int32_t C, const void* d_weight, fx_dtype vec_dt, float eps, void* d_gx, int64_t ld_gx, void* d_gweight,
+                          void* stream);
+
+/* A block's output y joined with the residual stream x, in one pass with the norm for the block that follows:
+ *     r = rms_norm(y; post),  out = x + scale * drop(r * act(gate)),  norm = rms_norm(out; next)
+ * Whatever of post, gate, scale and next is NULL is left out (r = y, act = 1, scale = 1, no second output); p = 0 leaves
+ * drop out.  The second norm is taken of out before its rounding.  d_out may be d_x or d_y with the same stride.
+ * Backward: d_out is what the forward call wrote and is read only with d_gnorm; one of d_gout and d_gnorm may be NULL
+ * (FX_EINVAL for both); any gradient may be NULL (not computed), and one of an absent input has to be.  gx is the
+ * gradient of out through both outputs; d_gx may be d_gout, d_gy may be d_y, d_ggate may be d_gate. */
+typedef enum { FX_GATE_SIGMOID = 0, FX_GATE_SILU = 1 } fx_gate_act;
+typedef struct {
+    int64_t rows;
+    int32_t C;
+    fx_dtype dt;              /* of all rows */
+    fx_dtype vec_dt;          /* of post, scale, next and their gradients */
+    fx_gate_act act;
+    const void* d_y;
+    const void* d_gate;
+    int64_t ld_y, ld_gate;
+    const void *d_post, *d_scale, *d_next;
+    const uint64_t* d_offset; /* dropout, as in fx_dropout */
+    uint64_t seed, offset;
+    double p;
+    float eps;
+} fx_block_join;
+fx_status fx_block_join_fwd(const fx_block_join* b, const void* d_x, int64_t ld_x, void* d_out, int64_t ld_out, void* d_norm,
+                            int64_t ld_norm, void* stream);
+fx_status fx_block_join_bwd(const fx_block_join* b, const void* d_gout, int64_t ld_gout, const void* d_gnorm, int64_t ld_gnorm,
+                            const void* d_out, int64_t ld_out, void* d_gx, int64_t ld_gx, void* d_gy, int64_t ld_gy,
+                            void* d_ggate, int64_t ld_ggate, void* d_gpost, void* d_gscale, void* d_gnext, void* stream);
+
+/* Dropout:  out = residual + (keep ? x * 65536 / (65536 - t) : 0),  t = round(65536 p)  (residual NULL: 0; 0 <= p <= 1;
+ * everything is dropped where t = 65536).  Channel c of row r is kept where number c & 7 of the eight 16-bit halves of
+ * Philox4x32-7's four words (Salmon et al., "Parallel random numbers: as easy as 1, 2, 3", 2011; word by word, low half
+ * first) is at least t, at counter (c >> 3, r, offset, offset >> 32) and key (seed, seed >> 32).  The mask is never
+ * stored: it depends on (seed, offset, r, c) alone, the same in every call, dtype and layout, and the gradient of x is
+ * this same call on the gradient of out.  p is a multiple of 2^-16 in effect, and the factor is exact for it.
+ *   d_offset  device uint64 added to `offset` when the kernel runs, or NULL: a captured graph whose owner raises it
+ *             between replays draws a new mask every time
+ * A dropped value leaves 0 whatever it was, an infinity or NaN too.  d_out may be d_x or d_residual with the same stride. */
+fx_status fx_dropout(const void* d_x, int64_t ld_x, fx_dtype dt, int64_t rows, int32_t C, double p, uint64_t seed, uint64_t offset,
+                     const uint64_t* d_offset, const void* d_residual, int64_t ld_residual, void* d_out, int64_t ld_out, void* stream);
+
+/* ---------------------------------------------------------------------------------------
  * Measurement support (the paper's protocol, Sec. 4.1: per-operator times).  While enabled,
  * every kernel launch of the library is bracketed by hipEvents on its launch stream;
  * fx_profile_read waits for the recorded events and returns the summed time and launch count

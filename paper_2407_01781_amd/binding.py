@@ -32,6 +32,14 @@ class FxError(RuntimeError):
         self.status = status
 
 
+class _BlockJoin(C.Structure):
+    """fx_block_join"""
+    _fields_ = [("rows", C.c_int64), ("C", C.c_int32), ("dt", C.c_int32), ("vec_dt", C.c_int32), ("act", C.c_int32),
+                ("d_y", C.c_void_p), ("d_gate", C.c_void_p), ("ld_y", C.c_int64), ("ld_gate", C.c_int64),
+                ("d_post", C.c_void_p), ("d_scale", C.c_void_p), ("d_next", C.c_void_p), ("d_offset", C.c_void_p),
+                ("seed", C.c_uint64), ("offset", C.c_uint64), ("p", C.c_double), ("eps", C.c_float)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(
@@ -99,6 +107,21 @@ def _load():
     L.fx_upsample2_bwd.argtypes = [vp, vp, C.c_int, i32, vp, vp]
     L.fx_upsample2.restype = C.c_int
     L.fx_upsample2.argtypes = [vp, vp, C.c_int, i32, vp, vp]
+    f32, f64, u64 = C.c_float, C.c_double, C.c_uint64
+    for name, args in (
+            ("fx_build_sequences", [vp, i32, i64, vp, C.POINTER(vp)]),
+            ("fx_gated_scan_fwd", [vp, vp, i64, vp, i64, C.c_int, i32, i32, vp, vp, i64, vp, vp]),
+            ("fx_gated_scan_bwd", [vp, vp, i64, vp, i64, vp, i64, vp, i64, C.c_int, i32, i32, vp, vp, vp, i64, vp, i64, vp, vp]),
+            ("fx_gated_scan_step", [vp, i64, vp, i64, C.c_int, i64, i32, vp, vp, vp, i64, vp]),
+            ("fx_rms_norm_fwd", [vp, i64, C.c_int, i64, i32, vp, C.c_int, f32, vp, i64, vp]),
+            ("fx_rms_norm_bwd", [vp, i64, vp, i64, C.c_int, i64, i32, vp, C.c_int, f32, vp, i64, vp, vp]),
+            ("fx_block_join_fwd", [C.POINTER(_BlockJoin), vp, i64, vp, i64, vp, i64, vp]),
+            ("fx_block_join_bwd", [C.POINTER(_BlockJoin), vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp]),
+            ("fx_dropout", [vp, i64, C.c_int, i64, i32, f64, u64, u64, vp, vp, i64, vp, i64, vp])):
+        getattr(L, name).restype = C.c_int
+        getattr(L, name).argtypes = args
+    L.fx_sequences_destroy.restype = None
+    L.fx_sequences_destroy.argtypes = [vp]
     L.fx_set_option.restype = C.c_int
     L.fx_set_option.argtypes = [C.c_char_p, i32]
     L.fx_get_option.restype = C.c_int
@@ -491,3 +514,198 @@ def upsample2_bwd(kmap: KernelMap, grad_out: torch.Tensor) -> torch.Tensor:
     gin = torch.empty((kmap.n_out, grad_out.shape[1]), dtype=grad_out.dtype, device="cuda")
     _check(lib.fx_upsample2_bwd(kmap._h, _ptr(grad_out), _TORCH_DT[grad_out.dtype], grad_out.shape[1], _ptr(gin), _stream()))
     return gin
+
+
+# ------------------------------------------------------------------------------------------ around the convolution
+class Sequences:
+    """Handle on the rows' division into sequences (fx_build_sequences)."""
+
+    def __init__(self, handle: int, batch_size: int, rows: int):
+        self._h = C.c_void_p(handle)
+        self.batch_size, self.rows = batch_size, rows
+
+    def __del__(self):
+        h = getattr(self, "_h", None)
+        if h is not None and h.value:
+            lib.fx_sequences_destroy(h)
+            self._h = None
+
+
+def build_sequences(joffsets) -> Sequences:
+    """joffsets: host int64 [B,2], ranges that follow each other from row 0 on (IndexGrid.voxel_joffsets() makes every
+    grid of a batch one sequence)."""
+    jo = np.ascontiguousarray(np.asarray(joffsets, dtype=np.int64).reshape(-1, 2))
+    rows = int(jo[-1, 1]) if len(jo) else 0
+    h = C.c_void_p()
+    _check(lib.fx_build_sequences(jo.ctypes.data_as(C.c_void_p), jo.shape[0], rows, _stream(), C.byref(h)))
+    return Sequences(h.value, jo.shape[0], rows)
+
+
+def _rows(t: torch.Tensor, shape, dtype, name: str) -> torch.Tensor:
+    """A tensor of rows: any row stride, channels next to each other."""
+    assert t.is_cuda and t.dtype == dtype and t.shape == shape, f"{name}: {tuple(shape)} {dtype} on the GPU expected"
+    assert t.stride(1) == 1 or t.shape[1] <= 1 or t.numel() == 0, f"{name}: the channels of a row have to lie next to each other"
+    return t
+
+
+def _ld(t: Optional[torch.Tensor]) -> int:
+    # the stride of a single row says nothing; rows of a broadcast tensor (stride 0) are refused by the library
+    return 0 if t is None else t.stride(0) if t.shape[0] > 1 and t.numel() else max(t.shape[1], 1)
+
+
+def _states(t: Optional[torch.Tensor], shape, name: str) -> Optional[torch.Tensor]:
+    assert t is None or (t.is_cuda and t.dtype == torch.float32 and t.shape == shape and t.is_contiguous()), \
+        f"{name}: contiguous float32 {tuple(shape)} on the GPU expected"
+    return t
+
+
+def _vector(t: Optional[torch.Tensor], c: int, dtype, name: str) -> Optional[torch.Tensor]:
+    assert t is None or (t.is_cuda and t.shape == (c,) and t.is_contiguous() and t.dtype in (dtype, torch.float32)), \
+        f"{name}: contiguous ({c},) of {dtype} or float32 on the GPU expected"
+    return t
+
+
+def gated_scan_fwd(seqs: Sequences, x: torch.Tensor, gate: torch.Tensor, h0: Optional[torch.Tensor] = None, reverse: bool = False,
+                   out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """h_t = f_t h_(t-1) + (1 - f_t) x_t with f = sigmoid(gate) along every sequence, against the rows' order where
+    `reverse`; x, gate [rows, C], h0 [B, C] float32 (zeros without).  Returns h [rows, C] and the states [B, C] float32
+    behind the last rows."""
+    assert x.dim() == 2 and x.dtype in _TORCH_DT and x.shape[0] == seqs.rows
+    _rows(x, x.shape, x.dtype, "x"), _rows(gate, x.shape, x.dtype, "gate")
+    states = (seqs.batch_size, x.shape[1])
+    _states(h0, states, "h0")
+    h = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _rows(out, x.shape, x.dtype, "out")
+    last = torch.empty(states, dtype=torch.float32, device=x.device)
+    _check(lib.fx_gated_scan_fwd(seqs._h, _ptr(x), _ld(x), _ptr(gate), _ld(gate), _TORCH_DT[x.dtype], x.shape[1], int(reverse),
+                                 _ptr(h0), _ptr(h), _ld(h), _ptr(last), _stream()))
+    return h, last
+
+
+def gated_scan_bwd(seqs: Sequences, x: torch.Tensor, gate: torch.Tensor, h: torch.Tensor, grad_h: torch.Tensor,
+                   h0: Optional[torch.Tensor] = None, grad_last: Optional[torch.Tensor] = None,
+                   reverse: bool = False) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Gradients of gated_scan_fwd's x, gate [rows, C] and h0 [B, C]; h is its output, grad_last the gradient of its
+    second output (zeros without)."""
+    assert x.dim() == 2 and x.dtype in _TORCH_DT and x.shape[0] == seqs.rows
+    for t, name in ((x, "x"), (gate, "gate"), (h, "h"), (grad_h, "grad_h")):
+        _rows(t, x.shape, x.dtype, name)
+    states = (seqs.batch_size, x.shape[1])
+    _states(h0, states, "h0"), _states(grad_last, states, "grad_last")
+    gx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    ggate = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    gh0 = torch.empty(states, dtype=torch.float32, device=x.device)
+    _check(lib.fx_gated_scan_bwd(seqs._h, _ptr(x), _ld(x), _ptr(gate), _ld(gate), _ptr(h), _ld(h), _ptr(grad_h), _ld(grad_h),
+                                 _TORCH_DT[x.dtype], x.shape[1], int(reverse), _ptr(h0), _ptr(grad_last), _ptr(gx), _ld(gx),
+                                 _ptr(ggate), _ld(ggate), _ptr(gh0), _stream()))
+    return gx, ggate, gh0
+
+
+def gated_scan_step(x: torch.Tensor, gate: torch.Tensor, state: torch.Tensor,
+                    new_state: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The next row of each of x.shape[0] running sequences: h [n, C] and the states behind it [n, C] float32
+    (new_state may be `state`)."""
+    assert x.dim() == 2 and x.dtype in _TORCH_DT
+    _rows(x, x.shape, x.dtype, "x"), _rows(gate, x.shape, x.dtype, "gate")
+    _states(state, x.shape, "state"), _states(new_state, x.shape, "new_state")
+    h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if new_state is None:
+        new_state = torch.empty(x.shape, dtype=torch.float32, device=x.device)
+    _check(lib.fx_gated_scan_step(_ptr(x), _ld(x), _ptr(gate), _ld(gate), _TORCH_DT[x.dtype], x.shape[0], x.shape[1], _ptr(state),
+                                  _ptr(new_state), _ptr(h), _ld(h), _stream()))
+    return h, new_state
+
+
+def rms_norm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x / sqrt(mean over the channels of x^2 + eps) * weight; x [rows, C], weight [C] of x's dtype or float32."""
+    assert x.dim() == 2 and x.dtype in _TORCH_DT
+    _rows(x, x.shape, x.dtype, "x"), _vector(weight, x.shape[1], x.dtype, "weight")
+    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _rows(out, x.shape, x.dtype, "out")
+    _check(lib.fx_rms_norm_fwd(_ptr(x), _ld(x), _TORCH_DT[x.dtype], x.shape[0], x.shape[1], _ptr(weight),
+                               0 if weight is None else _TORCH_DT[weight.dtype], eps, _ptr(out), _ld(out), _stream()))
+    return out
+
+
+def rms_norm_bwd(grad_out: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                 eps: float = 1e-6) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Gradients of rms_norm_fwd's x and weight (None without one)."""
+    assert x.dim() == 2 and x.dtype in _TORCH_DT
+    _rows(x, x.shape, x.dtype, "x"), _rows(grad_out, x.shape, x.dtype, "grad_out"), _vector(weight, x.shape[1], x.dtype, "weight")
+    gx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    gw = None if weight is None else torch.empty_like(weight)
+    _check(lib.fx_rms_norm_bwd(_ptr(grad_out), _ld(grad_out), _ptr(x), _ld(x), _TORCH_DT[x.dtype], x.shape[0], x.shape[1], _ptr(weight),
+                               0 if weight is None else _TORCH_DT[weight.dtype], eps, _ptr(gx), _ld(gx), _ptr(gw), _stream()))
+    return gx, gw
+
+
+_GATES = {"sigmoid": 0, "silu": 1}
+
+
+def _block(y, gate, act, post_weight, scale, next_weight, eps, p, seed, offset, d_offset) -> _BlockJoin:
+    assert y.dim() == 2 and y.dtype in _TORCH_DT
+    _rows(y, y.shape, y.dtype, "y")
+    if gate is not None:
+        _rows(gate, y.shape, y.dtype, "gate")
+    vectors = [_vector(v, y.shape[1], y.dtype, n) for v, n in ((post_weight, "post_weight"), (scale, "scale"), (next_weight, "next_weight"))]
+    kinds = {v.dtype for v in vectors if v is not None}
+    assert len(kinds) <= 1, "post_weight, scale and next_weight have one dtype"
+    return _BlockJoin(rows=y.shape[0], C=y.shape[1], dt=_TORCH_DT[y.dtype], vec_dt=_TORCH_DT[kinds.pop()] if kinds else 0,
+                      act=_GATES[act], d_y=y.data_ptr(), d_gate=None if gate is None else gate.data_ptr(), ld_y=_ld(y), ld_gate=_ld(gate),
+                      d_post=None if post_weight is None else post_weight.data_ptr(), d_scale=None if scale is None else scale.data_ptr(),
+                      d_next=None if next_weight is None else next_weight.data_ptr(), d_offset=_offset(d_offset),
+                      seed=seed, offset=offset, p=p, eps=eps)
+
+
+def _offset(t: Optional[torch.Tensor]):
+    assert t is None or (t.is_cuda and t.dtype == torch.int64 and t.numel() == 1), "d_offset: one int64 on the GPU"
+    return None if t is None else t.data_ptr()
+
+
+def block_join_fwd(x: torch.Tensor, y: torch.Tensor, gate: Optional[torch.Tensor] = None, act: str = "silu",
+                   post_weight: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                   next_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, p: float = 0.0, seed: int = 0, offset: int = 0,
+                   d_offset: Optional[torch.Tensor] = None,
+                   out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """x + scale * drop(rms_norm(y; post_weight) * act(gate)), and that sum's rms_norm by next_weight (None without one).
+    Rows [n, C] of one dtype, vectors [C] of that dtype or float32; drop is dropout's mask of (seed, offset)."""
+    b = _block(y, gate, act, post_weight, scale, next_weight, eps, p, seed, offset, d_offset)
+    _rows(x, y.shape, y.dtype, "x")
+    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _rows(out, x.shape, x.dtype, "out")
+    norm = None if next_weight is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _check(lib.fx_block_join_fwd(C.byref(b), _ptr(x), _ld(x), _ptr(out), _ld(out), _ptr(norm), _ld(norm), _stream()))
+    return out, norm
+
+
+def block_join_bwd(grad_out: Optional[torch.Tensor], grad_norm: Optional[torch.Tensor], out: Optional[torch.Tensor], y: torch.Tensor,
+                   gate: Optional[torch.Tensor] = None, act: str = "silu", post_weight: Optional[torch.Tensor] = None,
+                   scale: Optional[torch.Tensor] = None, next_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, p: float = 0.0,
+                   seed: int = 0, offset: int = 0, d_offset: Optional[torch.Tensor] = None) -> dict:
+    """Gradients of block_join_fwd's inputs: {"x", "y", "gate", "post", "scale", "next"}, None for those that are absent.
+    grad_out and grad_norm are the gradients of its two outputs (one may be None), `out` its first output (needed with
+    grad_norm)."""
+    b = _block(y, gate, act, post_weight, scale, next_weight, eps, p, seed, offset, d_offset)
+    for t, name in ((grad_out, "grad_out"), (grad_norm, "grad_norm"), (out, "out")):
+        if t is not None:
+            _rows(t, y.shape, y.dtype, name)
+    rows = lambda t: None if t is None else torch.empty(y.shape, dtype=y.dtype, device=y.device)
+    vec = lambda t: None if t is None else torch.empty_like(t)
+    g = {"x": rows(y), "y": rows(y), "gate": rows(gate), "post": vec(post_weight), "scale": vec(scale), "next": vec(next_weight)}
+    _check(lib.fx_block_join_bwd(C.byref(b), _ptr(grad_out), _ld(grad_out), _ptr(grad_norm), _ld(grad_norm), _ptr(out), _ld(out),
+                                 _ptr(g["x"]), _ld(g["x"]), _ptr(g["y"]), _ld(g["y"]), _ptr(g["gate"]), _ld(g["gate"]), _ptr(g["post"]),
+                                 _ptr(g["scale"]), _ptr(g["next"]), _stream()))
+    return g
+
+
+def dropout(x: torch.Tensor, p: float, seed: int, offset: int, residual: Optional[torch.Tensor] = None,
+            d_offset: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x [rows, C] with a share p of its values dropped and the others scaled by 1 / (1 - p), plus the residual if there
+    is one.  The mask depends on (seed, offset, row, channel) alone and is never stored; the gradient of x is the same
+    call on the output's gradient.  Take another offset for every call that wants a mask of its own."""
+    assert x.dim() == 2 and x.dtype in _TORCH_DT
+    _rows(x, x.shape, x.dtype, "x")
+    if residual is not None:
+        _rows(residual, x.shape, x.dtype, "residual")
+    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _rows(out, x.shape, x.dtype, "out")
+    _check(lib.fx_dropout(_ptr(x), _ld(x), _TORCH_DT[x.dtype], x.shape[0], x.shape[1], p, seed, offset, _offset(d_offset),
+                          _ptr(residual), _ld(residual), _ptr(out), _ld(out), _stream()))
+    return out

@@ -60,7 +60,8 @@ enum ProfSlot {
     kProfBucketSort = 0, kProfBucketLeaves, kProfVoxelsToLeaves, kProfFindTiles, kProfRankTiles, kProfInsertUpper, kProfScanUpper, kProfInsertLower, kProfScanLower,
     kProfInsertLeaf, kProfScanLeaf, kProfGridIjk, kProfNbmap, kProfLeafNeighbors, kProfBuildTiles,
     kProfPackWeights, kProfConvMfma, kProfConvGather, kProfConvLowdepth, kProfConvScalar, kProfMemset,
-    kProfDgradStrided, kProfWgrad, kProfWgradReduce, kProfPool, kProfUpsample, kProfConvLeaf, kProfSmallGrid, kProfSlotCount
+    kProfDgradStrided, kProfWgrad, kProfWgradReduce, kProfPool, kProfUpsample, kProfConvLeaf, kProfSmallGrid,
+    kProfScanFwd, kProfScanBwd, kProfBlockFwd, kProfBlockBwd, kProfBlockSums, kProfDropout, kProfSlotCount
 };
 bool prof_enabled();
 void prof_begin(int slot, hipStream_t s);
