@@ -14,9 +14,11 @@
 // negative), and the composition selects, so that nothing of one sequence, an infinity or NaN neither, reaches the
 // next.  All of it is fp32.
 //
-// A tile is `groups` x 8 rows of up to 64 channels: 8 lanes hold a row (8 channels each, 128 bytes of a 16-bit type), and
-// every lane takes 8 rows that follow each other.  Three launches where a call has more than one tile: the tiles' (A, H);
-// the value before every tile; the rows.
+// One pass over the data.  A tile is some hundred rows of up to 64 channels: 8 lanes hold a row (8 channels each, 128
+// bytes of a 16-bit type), and every lane takes a few rows that follow each other, in registers from the load to the
+// store.  A workgroup scans its tile's runs in LDS, publishes the tile's (A, H), looks back over the tiles before it for
+// the value that its first row starts from, and finishes its rows.  Tiles are taken in scan order by ticket, so whatever
+// a workgroup waits for belongs to a workgroup that already runs, and that one waits for earlier tiles only.
 #include "rows.h"
 
 #include <mutex>
@@ -37,13 +39,18 @@ struct fx_sequences {
 
 namespace fx {
 
-constexpr int kScanRows = 8;            // rows of a lane
 constexpr int kScanThreads = 512;       // most threads of a workgroup
+constexpr int kGroupTiles = 16;         // tiles whose joint (A, H) is published as one
+constexpr int kLookWindow = 16;         // groups looked at together
+
+// Rows of a lane: as many as leave a workgroup's registers (gate, input and, backward, state and x of all its rows) room
+// for a second one on the compute unit.
+template <int DT, bool BWD> struct ScanRows { static constexpr int n = BWD && DT == FX_F32 ? 2 : 4; };
 
 struct ScanArgs {
     int64_t rows;
     int32_t C, lanes_log2;              // lanes of a row within the slab
-    int32_t slabs, tiles;
+    int32_t slabs, tiles, groups;       // 64 channels; tiles of a slab; groups of tiles
     const unsigned char *x, *gate, *h, *gh;
     unsigned char *out, *gx, *ggate;
     int64_t ld_x, ld_gate, ld_h, ld_gh, ld_out, ld_gx, ld_ggate;      // bytes from row to row
@@ -52,8 +59,10 @@ struct ScanArgs {
     const float* h0;                    // backward: the states before the sequences' first rows
     const uint64_t* begin;
     const int32_t *rank, *id;
-    float2* sums;                       // [slabs][tiles][64] (A, H) of every tile
-    float* before;                      // [slabs][tiles][64] value before every tile
+    // what workgroups tell each other, where there is more than one tile: kNothing until it is written
+    uint64_t* tile_runs;                // [slabs][tiles][64] (A, H) of every tile
+    uint64_t* group_runs;               // [slabs][groups][64] (A, H) of every group, then the value behind it as (-1, H)
+    uint32_t* ticket;
 };
 
 struct Run { float A, H; };
@@ -66,24 +75,17 @@ __device__ __forceinline__ Run then(const Run& l, const Run& r) {
 // the value behind a run
 __device__ __forceinline__ float through(const Run& r, float v) { return r.A < 0.f ? r.H : r.A * v + r.H; }
 
-// A lane's eight rows: u0 .. u0 + 7 in scan order, rows lo .. lo + 7 of the tensors (in turn or against it).
+// A lane's rows: u0 .. u0 + n - 1 in scan order, rows lo .. lo + n - 1 of the tensors (in turn or against it).
 struct LaneRows {
-    int64_t u0, lo;
+    int64_t lo;
     uint32_t begin, stop;               // bit i: the sequence of row u0 + i begins / ends there, in scan order
     int n;                              // rows that exist
 };
 
-template <bool UP>
-__device__ __forceinline__ int64_t row_at(const ScanArgs& a, int64_t u) {
-    const int64_t c = u < a.rows ? u : a.rows - 1;
-    return UP ? c : a.rows - 1 - c;
-}
-
-template <bool UP>
+template <bool UP, int R>
 __device__ __forceinline__ LaneRows lane_rows(const ScanArgs& a, int64_t u0) {
     LaneRows r;
-    r.u0 = u0;
-    r.n = (int)max((int64_t)0, min((int64_t)kScanRows, a.rows - u0));
+    r.n = (int)max((int64_t)0, min((int64_t)R, a.rows - u0));
     r.begin = r.stop = 0;
     r.lo = 0;
     if (r.n == 0) return r;
@@ -100,28 +102,38 @@ __device__ __forceinline__ LaneRows lane_rows(const ScanArgs& a, int64_t u0) {
     return r;
 }
 
+// does a sequence begin, in scan order, at row u
+template <bool UP>
+__device__ __forceinline__ bool begins_at(const ScanArgs& a, int64_t u) {
+    const int64_t r = UP ? u : a.rows - u;         // the row's own bit, or that of the row behind it
+    return a.begin[r >> 6] >> (r & 63) & 1;
+}
+
 __device__ __forceinline__ int sequence_of(const ScanArgs& a, int64_t row) {
     const uint64_t w = a.begin[row >> 6] & ((2ull << (row & 63)) - 1);
     return a.id[a.rank[row >> 6] + __popcll(w) - 1];
 }
 
-// v of eight channels of a row of a [B, C] table, zeros without one
+// eight channels of a row of a [B, C] table, zeros without one
+template <int KIND>
 __device__ __forceinline__ void load_states(const float* t, int seq, int col, int C, float (&v)[kPiece]) {
 #pragma unroll
-    for (int e = 0; e < kPiece; ++e) v[e] = t && col + e < C ? t[(int64_t)seq * C + col + e] : 0.f;
+    for (int e = 0; e < kPiece; ++e) v[e] = 0.f;
+    if (t) unpack<FX_F32>(load_piece<FX_F32, KIND>(reinterpret_cast<const unsigned char*>(t + (int64_t)seq * C), col, C), v);
 }
+template <int KIND>
 __device__ __forceinline__ void store_states(float* t, int seq, int col, int C, const float (&v)[kPiece]) {
-#pragma unroll
-    for (int e = 0; e < kPiece; ++e)
-        if (col + e < C) t[(int64_t)seq * C + col + e] = v[e];
+    store_piece<FX_F32, KIND>(reinterpret_cast<unsigned char*>(t + (int64_t)seq * C), col, C, pack<FX_F32>(v));
 }
 
-// The scan over the lanes' runs within a workgroup.  Runs of all groups in LDS; a thread takes one channel of eight
-// groups and leaves in their place what stands before each within the eight; the eights' own runs lie in seg.
+// The scan over the lanes' runs within a workgroup.  Runs of all groups of lanes in LDS; a thread takes one channel of
+// eight groups and leaves in their place what stands before each within the eight; the eights' own runs lie in seg.
 struct ScanLds {
-    float A[kScanThreads * kPiece], H[kScanThreads * kPiece];      // [group][channel of the slab]
+    float A[kScanThreads * kPiece], H[kScanThreads * kPiece];      // [group of lanes][channel of the slab]
     float seg_A[kScanThreads], seg_H[kScanThreads];                // [eight groups][channel]
     float before[kScanThreads];                                    // value before every eight groups
+    uint64_t seen[kGroupTiles][64];                                // what a look back found, [tile or group][channel]
+    int ticket;
 };
 
 __device__ __forceinline__ void put_run(ScanLds& s, int t, const float (&A)[kPiece], const float (&H)[kPiece]) {
@@ -147,116 +159,192 @@ __device__ __forceinline__ void scan_eights(ScanLds& s, int width_log2) {
     s.seg_H[t] = run.H;
 }
 
-// what a lane's rows are scanned with: the gates and the inputs, as loaded
-template <int DT> struct ScanRaw { Piece<DT> gate[kScanRows], in[kScanRows]; };
+// ---- what workgroups tell each other
+// One 64-bit word a channel holds both numbers of a run, so a reader has all or nothing of it and nothing needs to be
+// ordered around it.  No number has the bits of kNothing: a NaN is written with the same bits always.
+constexpr uint32_t kNothing = 0xFFFFFFFFu;
+constexpr int kMostPolls = 1 << 22;     // seconds; a wait ends long before, see the tickets
 
-template <int DT, int KIND, bool UP>
-__device__ __forceinline__ void load_rows(const ScanArgs& a, int64_t u0, int col, const unsigned char* in, int64_t ld_in, ScanRaw<DT>& raw) {
-#pragma unroll
-    for (int i = 0; i < kScanRows; ++i) {
-        const int64_t row = row_at<UP>(a, u0 + i);
-        raw.gate[i] = load_piece<DT, KIND>(a.gate + row * a.ld_gate, col, a.C);
-        raw.in[i] = load_piece<DT, KIND>(in + row * ld_in, col, a.C);
-    }
+__device__ __forceinline__ uint32_t plain_bits(float v) { return v == v ? __float_as_uint(v) : 0x7FC00000u; }
+__device__ __forceinline__ void publish(uint64_t* at, const Run& r) {
+    __hip_atomic_store(at, (uint64_t)plain_bits(r.A) << 32 | plain_bits(r.H), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
+__device__ __forceinline__ uint64_t look(const uint64_t* at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ bool is_there(uint64_t w) { return (uint32_t)(w >> 32) != kNothing; }
+__device__ __forceinline__ Run run_in(uint64_t w) { return Run{__uint_as_float((uint32_t)(w >> 32)), __uint_as_float((uint32_t)w)}; }
 
-// the run of a lane's rows; BWD: b = f in, else (1 - f) in
-template <int DT, bool UP, bool BWD>
-__device__ __forceinline__ void run_of(const ScanArgs& a, const LaneRows& lr, const ScanRaw<DT>& raw, int col, float (&A)[kPiece], float (&H)[kPiece]) {
+// Words `from`, `from` + step, ... of `n` (64 words from one to the next) for this thread's channel into s.seen, waiting
+// for those that are not there yet.  All threads of the workgroup take part; ends with a barrier.  A word that does not
+// come within the bound counts as NaN.
+__device__ __forceinline__ void gather_runs(ScanLds& s, const uint64_t* words, int64_t step, int n, int width_log2) {
+    const int c = threadIdx.x & ((1 << width_log2) - 1), first = threadIdx.x >> width_log2, stride = blockDim.x >> width_log2;
+    for (int i0 = first; i0 < n; i0 += 4 * stride) {
+        uint64_t w[4];
 #pragma unroll
-    for (int e = 0; e < kPiece; ++e) { A[e] = 1.f; H[e] = 0.f; }
+        for (int k = 0; k < 4; ++k) {
+            const int i = i0 + k * stride;
+            w[k] = i < n ? look(words + step * i + c) : 0;
+        }
+        for (int polls = 0; polls < kMostPolls; ++polls) {
+            bool all = true;
 #pragma unroll
-    for (int i = 0; i < kScanRows; ++i) {
-        if (i >= lr.n) break;
-        if (lr.begin >> i & 1) load_states(a.first, sequence_of(a, UP ? lr.lo + i : lr.lo + lr.n - 1 - i), col, a.C, H);
-        float z[kPiece], v[kPiece];
-        unpack<DT>(raw.gate[i], z);
-        unpack<DT>(raw.in[i], v);
+            for (int k = 0; k < 4; ++k) all = all && is_there(w[k]);
+            if (all) break;
+            __builtin_amdgcn_s_sleep(1);
 #pragma unroll
-        for (int e = 0; e < kPiece; ++e) {
-            float f, g;
-            sigmoids(z[e], f, g);
-            H[e] = BWD ? f * (v[e] + H[e]) : f * H[e] + g * v[e];
-            A[e] *= f;
+            for (int k = 0; k < 4; ++k)
+                if (!is_there(w[k])) w[k] = look(words + step * (i0 + k * stride) + c);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = i0 + k * stride;
+            if (i < n) s.seen[i][c] = is_there(w[k]) ? w[k] : (uint64_t)0xBF800000u << 32 | 0x7FC00000u;
         }
     }
-    if (lr.begin) {
-#pragma unroll
-        for (int e = 0; e < kPiece; ++e) A[e] = -1.f;
-    }
+    __syncthreads();
 }
 
-// The (A, H) of every tile.
+// The value before the tile for channel threadIdx.x (threads below `width`; others get 0), having published the tile's
+// run and, from the last tile of a group, the group's.
+__device__ __forceinline__ float look_back(const ScanArgs& a, ScanLds& s, int slab, int tile, bool begins, const Run& mine, int width_log2) {
+    const int t = threadIdx.x, width = 1 << width_log2, group = tile / kGroupTiles, in_group = tile % kGroupTiles;
+    const bool closes = in_group == kGroupTiles - 1;
+    uint64_t* tiles = a.tile_runs + ((int64_t)slab * a.tiles + (tile - in_group)) * 64;
+    uint64_t* groups = a.group_runs + (int64_t)slab * a.groups * 64;
+    if (t < width && !closes) publish(tiles + in_group * 64 + t, mine);
+    Run run{1.f, 0.f};                              // of the group's tiles before this one
+    if (in_group && (!begins || closes)) {
+        gather_runs(s, tiles, 64, in_group, width_log2);
+        if (t < width)
+#pragma unroll 2
+            for (int i = 0; i < in_group; ++i) run = then(run, run_in(s.seen[i][t]));
+    }
+    if (closes && t < width) publish(groups + group * 64 + t, then(run, mine));
+    float v = 0.f;
+    if (!begins) {
+        // backwards over the groups until the value behind one of them is known for every channel
+        Run back{1.f, 0.f};
+        for (int end = group; end > 0; end -= kLookWindow) {
+            const int n = min(end, kLookWindow);
+            __syncthreads();                        // the words of the turn before have been read
+            gather_runs(s, groups + (int64_t)(end - 1) * 64, -64, n, width_log2);
+            if (t < width)
+#pragma unroll 2
+                for (int i = 0; i < n && back.A >= 0.f; ++i) back = then(run_in(s.seen[i][t]), back);
+            if (!__syncthreads_or(t < width && !(back.A < 0.f))) break;
+        }
+        if (t < width) v = through(run, back.H);
+    }
+    if (closes && t < width) publish(groups + group * 64 + t, Run{-1.f, through(mine, v)});
+    return v;
+}
+
+__global__ void __launch_bounds__(256) k_scan_clear(uint64_t* words, int64_t n, uint32_t* ticket) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) words[i] = ~0ull;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
+}
+
+// The smaller of a row's two sigmoids, its sign saying which: what a lane keeps of a gate between the two passes over
+// its rows.
+__device__ __forceinline__ float keep_gate(float z, float& f, float& g) {
+    sigmoids(z, f, g);
+    return z > 0.f ? g : -f;
+}
+__device__ __forceinline__ void kept_gate(float k, float& f, float& g) {
+    const float small = fabsf(k), large = 1.f - small;
+    const bool up = (int)__float_as_uint(k) >= 0;       // the sign of a zero counts too
+    f = up ? large : small;
+    g = up ? small : large;
+}
+
 template <int DT, int KIND, bool UP, bool BWD>
-__global__ void __launch_bounds__(kScanThreads)
-k_scan_tiles(ScanArgs a) {
+__global__ void __launch_bounds__(kScanThreads, BWD ? 2 : 4)
+k_scan(ScanArgs a) {
+    constexpr int R = ScanRows<DT, BWD>::n;
     __shared__ ScanLds s;
     const int t = threadIdx.x, lanes = 1 << a.lanes_log2, width_log2 = a.lanes_log2 + 3, width = 1 << width_log2;
-    const int slab = blockIdx.x % a.slabs, tile = blockIdx.x / a.slabs;
+    const int group = t >> a.lanes_log2;
+    int turn = blockIdx.x;
+    if (a.tile_runs) {
+        if (t == 0) s.ticket = (int)atomicAdd(a.ticket, 1u);
+        __syncthreads();
+        turn = s.ticket;
+    }
+    const int slab = turn % a.slabs, tile = turn / a.slabs;
     const int col = slab * 64 + (t & (lanes - 1)) * kPiece;
-    const int64_t u0 = ((int64_t)tile * (blockDim.x >> a.lanes_log2) + (t >> a.lanes_log2)) * kScanRows;
-    ScanRaw<DT> raw;
-    load_rows<DT, KIND, UP>(a, u0, col, BWD ? a.gh : a.x, BWD ? a.ld_gh : a.ld_x, raw);
-    const LaneRows lr = lane_rows<UP>(a, u0);
-    float A[kPiece], H[kPiece];
-    run_of<DT, UP, BWD>(a, lr, raw, col, A, H);
-    put_run(s, t, A, H);
-    __syncthreads();
-    scan_eights(s, width_log2);
-    __syncthreads();
-    if (t < width) {
-        Run run{1.f, 0.f};
-        for (int i = t; i < (int)blockDim.x; i += width) run = then(run, Run{s.seg_A[i], s.seg_H[i]});
-        a.sums[((int64_t)slab * a.tiles + tile) * 64 + t] = make_float2(run.A, run.H);
-    }
-}
-
-// The value before every tile: 16 channels a workgroup, 64 ranges of tiles side by side.
-__global__ void __launch_bounds__(1024)
-k_scan_before(const float2* __restrict__ sums, float* __restrict__ before, int tiles) {
-    __shared__ float2 range[64][16];
-    const int c = blockIdx.x * 16 + (threadIdx.x & 15), r = threadIdx.x >> 4, per = (tiles + 63) / 64;
-    const float2* in = sums + (int64_t)blockIdx.y * tiles * 64 + c;
-    float* out = before + (int64_t)blockIdx.y * tiles * 64 + c;
-    const int from = min(tiles, r * per), to = min(tiles, from + per);
-    Run run{1.f, 0.f};
-#pragma unroll 8
-    for (int i = from; i < to; ++i) { const float2 v = in[(int64_t)i * 64]; run = then(run, Run{v.x, v.y}); }
-    range[r][threadIdx.x & 15] = make_float2(run.A, run.H);
-    __syncthreads();
-    float v = 0.f;                      // what stands before the first tile is never used: a sequence begins there
-    for (int i = 0; i < r; ++i) { const float2 q = range[i][threadIdx.x & 15]; v = through(Run{q.x, q.y}, v); }
-#pragma unroll 8
-    for (int i = from; i < to; ++i) {
-        const float2 q = in[(int64_t)i * 64];
-        out[(int64_t)i * 64] = v;
-        v = through(Run{q.x, q.y}, v);
-    }
-}
-
-// The rows.
-template <int DT, int KIND, bool UP, bool BWD>
-__global__ void __launch_bounds__(kScanThreads)
-k_scan_rows(ScanArgs a) {
-    __shared__ ScanLds s;
-    const int t = threadIdx.x, lanes = 1 << a.lanes_log2, width_log2 = a.lanes_log2 + 3, width = 1 << width_log2;
-    const int slab = blockIdx.x % a.slabs, tile = blockIdx.x / a.slabs;
-    const int col = slab * 64 + (t & (lanes - 1)) * kPiece, group = t >> a.lanes_log2;
-    const int64_t u0 = ((int64_t)tile * (blockDim.x >> a.lanes_log2) + group) * kScanRows;
-    ScanRaw<DT> raw;
-    load_rows<DT, KIND, UP>(a, u0, col, BWD ? a.gh : a.x, BWD ? a.ld_gh : a.ld_x, raw);
-    const LaneRows lr = lane_rows<UP>(a, u0);
+    const int64_t tile0 = (int64_t)tile * (blockDim.x >> a.lanes_log2) * R, u0 = tile0 + group * R;
+    const LaneRows lr = lane_rows<UP, R>(a, u0);
+    constexpr int64_t step = UP ? 1 : -1;
+    const int64_t r0 = UP ? lr.lo : lr.lo + max(lr.n, 1) - 1;        // the lane's first row in scan order
+    Piece<DT> in[R], px[BWD ? R : 1], pp[BWD ? R : 1];
+    float kept[R][kPiece];
     {
+        const unsigned char *pg = a.gate + r0 * a.ld_gate, *pi = (BWD ? a.gh : a.x) + r0 * (BWD ? a.ld_gh : a.ld_x);
+        Piece<DT> gate[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {       // rows that do not exist: the last that does once more
+            gate[i] = load_piece<DT, KIND>(pg, col, a.C);
+            in[i] = load_piece<DT, KIND>(pi, col, a.C);
+            if (i + 1 < lr.n) { pg += step * a.ld_gate; pi += step * (BWD ? a.ld_gh : a.ld_x); }
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            float z[kPiece];
+            unpack<DT>(gate[i], z);
+#pragma unroll
+            for (int e = 0; e < kPiece; ++e) kept[i][e] = z[e];
+        }
+    }
+    {
+        // the run of this lane's rows
         float A[kPiece], H[kPiece];
-        run_of<DT, UP, BWD>(a, lr, raw, col, A, H);
+#pragma unroll
+        for (int e = 0; e < kPiece; ++e) { A[e] = 1.f; H[e] = 0.f; }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            if (lr.begin >> i & 1) load_states<KIND>(a.first, sequence_of(a, r0 + step * i), col, a.C, H);
+            float v[kPiece];
+            unpack<DT>(in[i], v);
+#pragma unroll
+            for (int e = 0; e < kPiece; ++e) {
+                float f, g;
+                kept[i][e] = keep_gate(kept[i][e], f, g);
+                asm volatile("" : "+v"(kept[i][e]));        // one number is kept: f and g of all rows do not fit the registers
+                H[e] = BWD ? f * (v[e] + H[e]) : f * H[e] + g * v[e];
+                A[e] *= f;
+            }
+            __builtin_amdgcn_sched_barrier(0);      // a row after the other: the gates of all rows at once do not fit the registers
+        }
+        if (lr.begin) {
+#pragma unroll
+            for (int e = 0; e < kPiece; ++e) A[e] = -1.f;
+        }
         put_run(s, t, A, H);
     }
+    if (BWD) {
+        // The rows run against the sequence: the state before a row lies at the row that comes next here.
+        const unsigned char *p = a.x + r0 * a.ld_x, *q = a.h + r0 * a.ld_h;
+        const bool more = UP ? r0 + lr.n < a.rows : r0 - lr.n >= 0;        // a row behind the lane's last
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            px[i] = load_piece<DT, KIND>(p, col, a.C);
+            if (i + 1 < lr.n) p += step * a.ld_x;
+            if (i + 1 < lr.n || (i + 1 == lr.n && more)) q += step * a.ld_h;
+            pp[i] = load_piece<DT, KIND>(q, col, a.C);
+        }
+    }
     __syncthreads();
     scan_eights(s, width_log2);
     __syncthreads();
-    if (t < width) {
-        float v = a.before ? a.before[((int64_t)slab * a.tiles + tile) * 64 + t] : 0.f;
-        for (int i = t; i < (int)blockDim.x; i += width) { s.before[i] = v; v = through(Run{s.seg_A[i], s.seg_H[i]}, v); }
+    {
+        Run run{1.f, 0.f};
+        if (t < width)
+#pragma unroll 2
+            for (int i = t; i < (int)blockDim.x; i += width) run = then(run, Run{s.seg_A[i], s.seg_H[i]});
+        float v = a.tile_runs ? look_back(a, s, slab, tile, begins_at<UP>(a, tile0), run, width_log2) : 0.f;
+        if (t < width)
+#pragma unroll 2
+            for (int i = t; i < (int)blockDim.x; i += width) { s.before[i] = v; v = through(Run{s.seg_A[i], s.seg_H[i]}, v); }
     }
     __syncthreads();
     float v[kPiece];
@@ -264,33 +352,31 @@ k_scan_rows(ScanArgs a) {
     for (int e = 0; e < kPiece; ++e)
         v[e] = through(Run{s.A[t * kPiece + e], s.H[t * kPiece + e]}, s.before[((group >> 3) << width_log2) + (t & (lanes - 1)) * kPiece + e]);
 #pragma unroll
-    for (int i = 0; i < kScanRows; ++i) {
+    for (int i = 0; i < R; ++i) {
         if (i >= lr.n) break;
-        const int64_t row = UP ? lr.lo + i : lr.lo + lr.n - 1 - i;
+        const int64_t row = r0 + step * i;
         const bool begins = lr.begin >> i & 1, ends = lr.stop >> i & 1;
-        if (begins) load_states(a.first, sequence_of(a, row), col, a.C, v);
-        float z[kPiece], in[kPiece];
-        unpack<DT>(raw.gate[i], z);
-        unpack<DT>(raw.in[i], in);
+        if (begins) load_states<KIND>(a.first, sequence_of(a, row), col, a.C, v);
+        float w[kPiece];
+        unpack<DT>(in[i], w);
         if (!BWD) {
 #pragma unroll
             for (int e = 0; e < kPiece; ++e) {
                 float f, g;
-                sigmoids(z[e], f, g);
-                v[e] = f * v[e] + g * in[e];
+                kept_gate(kept[i][e], f, g);
+                v[e] = f * v[e] + g * w[e];
             }
             store_piece<DT, KIND>(a.out + row * a.ld_out, col, a.C, pack<DT>(v));
         } else {
-            // the rows run against the sequence: the state before a row lies at the row that comes next here, h0 at the end
             float x[kPiece], p[kPiece], gx[kPiece], gz[kPiece];
-            unpack<DT>(load_piece<DT, KIND>(a.x + row * a.ld_x, col, a.C), x);
-            if (ends) load_states(a.h0, sequence_of(a, row), col, a.C, p);
-            else unpack<DT>(load_piece<DT, KIND>(a.h + (UP ? row + 1 : row - 1) * a.ld_h, col, a.C), p);
+            unpack<DT>(px[i], x);
+            unpack<DT>(pp[i], p);
+            if (ends) load_states<KIND>(a.h0, sequence_of(a, row), col, a.C, p);
 #pragma unroll
             for (int e = 0; e < kPiece; ++e) {
                 float f, g;
-                sigmoids(z[e], f, g);
-                const float lam = in[e] + v[e];
+                kept_gate(kept[i][e], f, g);
+                const float lam = w[e] + v[e];
                 gx[e] = g * lam;
                 gz[e] = lam * (p[e] - x[e]) * (f * g);
                 v[e] = f * lam;
@@ -298,7 +384,8 @@ k_scan_rows(ScanArgs a) {
             store_piece<DT, KIND>(a.gx + row * a.ld_gx, col, a.C, pack<DT>(gx));
             store_piece<DT, KIND>(a.ggate + row * a.ld_ggate, col, a.C, pack<DT>(gz));
         }
-        if (ends && a.last) store_states(a.last, sequence_of(a, row), col, a.C, v);
+        if (ends && a.last) store_states<KIND>(a.last, sequence_of(a, row), col, a.C, v);
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
@@ -368,20 +455,29 @@ static void scan_args(ScanArgs* a, const fx_sequences* q, int32_t C) {
 
 template <int DT, int KIND, bool UP, bool BWD>
 static fx_status launch_scan(ScanArgs& a, hipStream_t st) {
-    const int threads = kScanThreads;
-    const int64_t rows_a_tile = (int64_t)(threads >> a.lanes_log2) * kScanRows, tiles = (a.rows + rows_a_tile - 1) / rows_a_tile;
-    if (tiles * a.slabs > 0x7FFFFFFF) { set_error("gated scan: too many tiles for one launch"); return FX_ERANGE; }
-    a.tiles = (int)tiles;
-    void* work = nullptr;
-    if (tiles > 1) {
-        FX_TRY(dev_alloc(&work, (size_t)tiles * a.slabs * 64 * 12, st));
-        a.sums = (float2*)work;
-        a.before = (float*)(a.sums + tiles * a.slabs * 64);
-        k_scan_tiles<DT, KIND, UP, BWD><<<(unsigned)(tiles * a.slabs), threads, 0, st>>>(a);
-        const int width = 8 << a.lanes_log2;
-        k_scan_before<<<dim3((width + 15) / 16, a.slabs), 1024, 0, st>>>(a.sums, a.before, a.tiles);
+    // As many threads as leave every compute unit a tile, from a wave on.
+    int threads = kScanThreads;
+    int64_t rows_a_tile, tiles;
+    for (;; threads /= 2) {
+        rows_a_tile = (int64_t)(threads >> a.lanes_log2) * ScanRows<DT, BWD>::n;
+        tiles = (a.rows + rows_a_tile - 1) / rows_a_tile;
+        if (threads == 64 || tiles * a.slabs >= 2 * compute_units()) break;
     }
-    k_scan_rows<DT, KIND, UP, BWD><<<(unsigned)(tiles * a.slabs), threads, 0, st>>>(a);
+    if (tiles * a.slabs > 0x3FFFFFFF) { set_error("gated scan: too many tiles for one launch"); return FX_ERANGE; }
+    a.tiles = (int)tiles;
+    a.groups = (int)((tiles + kGroupTiles - 1) / kGroupTiles);
+    void* work = nullptr;
+    unsigned nb = (unsigned)a.slabs;
+    if (tiles > 1) {
+        const int64_t words = (int64_t)a.slabs * 64 * (a.tiles + a.groups);
+        FX_TRY(dev_alloc(&work, (size_t)words * 8 + 256, st));
+        a.tile_runs = (uint64_t*)work;
+        a.group_runs = a.tile_runs + (int64_t)a.slabs * 64 * a.tiles;
+        a.ticket = (uint32_t*)(a.tile_runs + words);
+        k_scan_clear<<<(unsigned)std::min<int64_t>((words + 255) / 256, 1024), 256, 0, st>>>(a.tile_runs, words, a.ticket);
+        nb = (unsigned)(tiles * a.slabs);
+    }
+    k_scan<DT, KIND, UP, BWD><<<nb, threads, 0, st>>>(a);
     const hipError_t e = hipGetLastError();
     dev_free(work, st);
     if (e != hipSuccess) { set_error("launch of the gated scan failed: %s", hipGetErrorString(e)); return FX_EDEVICE; }
