@@ -83,9 +83,9 @@ k_block_fwd(BlockArgs a) {
         const bool real = mine < a.rows;
         const int64_t row = real ? mine : a.rows - 1;
         Piece<DT> px, py, pg;
-        if (MODE == kModeNorm || a.x) px = load_piece<DT, KIND>(a.x + row * a.ld_x, col, C);
-        if (MODE != kModeNorm) py = load_piece<DT, KIND>(a.y + row * a.ld_y, col, C);
-        if (MODE == kModeJoin && a.gate) pg = load_piece<DT, KIND>(a.gate + row * a.ld_gate, col, C);
+        if (MODE == kModeNorm || a.x) px = load_piece<DT, KIND>(a.x + row * a.ld_x, 0, col, C);
+        if (MODE != kModeNorm) py = load_piece<DT, KIND>(a.y + row * a.ld_y, 0, col, C);
+        if (MODE == kModeJoin && a.gate) pg = load_piece<DT, KIND>(a.gate + row * a.ld_gate, 0, col, C);
         float v[kPiece];
         unpack<DT>(MODE == kModeNorm ? px : py, v);
         if (MODE == kModeJoin && a.post) {
@@ -122,7 +122,7 @@ k_block_fwd(BlockArgs a) {
                 if (a.x) v[e] += x[e];
             }
             if (WIDE) __syncthreads();      // an output may lie where an input lies: all waves have their pieces of the row
-            if (real) store_piece<DT, KIND>(a.out + row * a.ld_out, col, C, pack<DT>(v));
+            if (real) store_piece<DT, KIND>(a.out + row * a.ld_out, 0, col, C, pack<DT>(v));
         }
         if (MODE == kModeNorm || (MODE == kModeJoin && a.next)) {
             float s[1] = {0.f};
@@ -132,7 +132,7 @@ k_block_fwd(BlockArgs a) {
             const float rs = inv_rms(s[0], a.inv_C, a.eps);
 #pragma unroll
             for (int e = 0; e < kPiece; ++e) v[e] *= rs * wn[e];
-            if (real) store_piece<DT, KIND>(a.norm + row * a.ld_norm, col, C, pack<DT>(v));
+            if (real) store_piece<DT, KIND>(a.norm + row * a.ld_norm, 0, col, C, pack<DT>(v));
         }
     }
 }
@@ -185,12 +185,12 @@ k_block_bwd(BlockArgs a) {
         const int64_t row = real ? mine : a.rows - 1;
         Piece<DT> px, py, pg, pgo, pgn;
         if (a.gnorm) {
-            px = load_piece<DT, KIND>(a.x + row * a.ld_x, col, C);
-            pgn = load_piece<DT, KIND>(a.gnorm + row * a.ld_gnorm, col, C);
+            px = load_piece<DT, KIND>(a.x + row * a.ld_x, 0, col, C);
+            pgn = load_piece<DT, KIND>(a.gnorm + row * a.ld_gnorm, 0, col, C);
         }
-        if (a.gout) pgo = load_piece<DT, KIND>(a.gout + row * a.ld_gout, col, C);
-        if (MODE == kModeJoin) py = load_piece<DT, KIND>(a.y + row * a.ld_y, col, C);
-        if (MODE == kModeJoin && a.gate) pg = load_piece<DT, KIND>(a.gate + row * a.ld_gate, col, C);
+        if (a.gout) pgo = load_piece<DT, KIND>(a.gout + row * a.ld_gout, 0, col, C);
+        if (MODE == kModeJoin) py = load_piece<DT, KIND>(a.y + row * a.ld_y, 0, col, C);
+        if (MODE == kModeJoin && a.gate) pg = load_piece<DT, KIND>(a.gate + row * a.ld_gate, 0, col, C);
         float sums[3] = {0.f, 0.f, 0.f};         // x'^2, gnorm w x', y^2
         float x[kPiece], g[kPiece], D[kPiece], y[kPiece];
         if (a.gnorm) {
@@ -217,7 +217,7 @@ k_block_bwd(BlockArgs a) {
                 acc_next[e] += real ? g[e] * (x[e] * rx) : 0.f;
             }
         }
-        if (real && a.gx) store_piece<DT, KIND>(a.gx + row * a.ld_gx, col, C, pack<DT>(D));
+        if (real && a.gx) store_piece<DT, KIND>(a.gx + row * a.ld_gx, 0, col, C, pack<DT>(D));
         if (MODE == kModeJoin) {
             uint32_t w[4];
             if (a.drop.below) philox8((uint32_t)lane, (uint32_t)row, offset, a.drop.seed, w);
@@ -241,14 +241,14 @@ k_block_bwd(BlockArgs a) {
                 y[e] = yh;
                 D[e] = t;
             }
-            if (real && a.ggate) store_piece<DT, KIND>(a.ggate + row * a.ld_ggate, col, C, pack<DT>(z));
+            if (real && a.ggate) store_piece<DT, KIND>(a.ggate + row * a.ld_ggate, 0, col, C, pack<DT>(z));
             if (a.post) {
                 group_sums<WIDE>(dot, lanes, lds_sum);
                 const float cy = dot[0] * a.inv_C;
 #pragma unroll
                 for (int e = 0; e < kPiece; ++e) D[e] = ry * (D[e] - y[e] * cy);
             }
-            if (real && a.gy) store_piece<DT, KIND>(a.gy + row * a.ld_gy, col, C, pack<DT>(D));
+            if (real && a.gy) store_piece<DT, KIND>(a.gy + row * a.ld_gy, 0, col, C, pack<DT>(D));
         }
     }
     const int64_t vec = (int64_t)gridDim.x * C;

@@ -11,44 +11,46 @@ constexpr int kMaxRowChannels = 4096;   // widest row of the norms
 // Kind of row: channels in whole pieces; a ragged last piece; fewer channels than a piece
 enum RowKind { kRowsWhole = 0, kRowsRagged = 1, kRowsNarrow = 2 };
 
-template <int DT> struct RowType { static constexpr int kBytes = DT == FX_F32 ? 4 : 2, kWords = DT == FX_F32 ? 8 : 4; };
+// N channels as they lie in memory
+template <int DT, int N = kPiece> struct Piece {
+    static constexpr int kBytes = DT == FX_F32 ? 4 : 2, kWords = N * kBytes / 4;
+    uint32_t w[kWords];
+};
 
-// eight channels as they lie in memory
-template <int DT> struct Piece { uint32_t w[RowType<DT>::kWords]; };
-
-// Sixteen bytes at any address that is a multiple of the element's size: rows of an odd number of channels, and columns
+// A few bytes at any address that is a multiple of the element's size: rows of an odd number of channels, and columns
 // of a wider tensor, start anywhere.  One load or store instruction all the same.
-struct __attribute__((packed, aligned(2))) Bytes16 { uint32_t w[4]; };
-struct __attribute__((packed, aligned(2))) Bytes8 { uint32_t w[2]; };
-struct __attribute__((packed, aligned(2))) Bytes4 { uint32_t w; };
+template <int WORDS> struct __attribute__((packed, aligned(2))) Bytes { uint32_t w[WORDS]; };
 
-// The piece that begins at channel `col` of the row at `row`; channels from C on come as zeros.  A ragged row's last
-// piece is loaded as the row's last eight channels and moved into place, so that no load passes the row's end and every
+// The piece that begins at channel `col` of the row `off` bytes behind `base`; channels from C on come as zeros (the
+// offset apart from the base: where the base is the same in all lanes, it stays in scalar registers; without ZEROS, a lane
+// that has no channel at all gets some that are not its own).  A ragged row's last
+// piece is loaded as the row's last N channels and moved into place, so that no load passes the row's end and every
 // lane, one without channels too, loads from inside the row.
-template <int DT, int KIND>
-__device__ __forceinline__ Piece<DT> load_piece(const unsigned char* row, int col, int C) {
-    Piece<DT> p;
-    constexpr int ES = RowType<DT>::kBytes, NW = RowType<DT>::kWords;
+template <int DT, int KIND, int N = kPiece, bool ZEROS = true>
+__device__ __forceinline__ Piece<DT, N> load_piece(const unsigned char* base, uint32_t off, int col, int C) {
+    Piece<DT, N> p;
+    constexpr int ES = Piece<DT, N>::kBytes, NW = Piece<DT, N>::kWords, LW = NW < 4 ? NW : 4;
     if (KIND == kRowsNarrow) {
+        const unsigned char* row = base + off;
 #pragma unroll
         for (int i = 0; i < NW; ++i) p.w[i] = 0;
 #pragma unroll
-        for (int e = 0; e < kPiece - 1; ++e)
+        for (int e = 0; e < N - 1; ++e)
             if (col + e < C) {
                 if (DT == FX_F32) p.w[e % NW] = reinterpret_cast<const uint32_t*>(row)[col + e];
                 else p.w[e >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[col + e] << (16 * (e & 1));
             }
         return p;
     }
-    const int at = min(col, C - kPiece);
-    const unsigned char* src = row + (int64_t)at * ES;
+    const int at = min(col, C - N);
+    const unsigned char* src = base + (uint32_t)(off + at * ES);
 #pragma unroll
-    for (int i = 0; i < NW / 4; ++i) {
-        const Bytes16 b = reinterpret_cast<const Bytes16*>(src)[i];
+    for (int i = 0; i < NW / LW; ++i) {
+        const Bytes<LW> b = reinterpret_cast<const Bytes<LW>*>(src)[i];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) p.w[4 * i + j] = b.w[j];
+        for (int j = 0; j < LW; ++j) p.w[LW * i + j] = b.w[j];
     }
-    if (KIND == kRowsRagged) {      // move by col - at channels, 0 .. 7 and more where the lane has no channel at all
+    if (KIND == kRowsRagged) {      // move by col - at channels, 0 .. N - 1 and more where the lane has no channel at all
         const int bits = (col - at) * 8 * ES;
 #pragma unroll
         for (int step = NW / 2; step >= 1; step >>= 1) {
@@ -63,64 +65,64 @@ __device__ __forceinline__ Piece<DT> load_piece(const unsigned char* row, int co
 #pragma unroll
             for (int i = 0; i < NW; ++i) p.w[i] = (p.w[i] >> 16) | (i + 1 < NW ? p.w[i + 1] << 16 : 0u);
         }
-        if (col >= C) {
-#pragma unroll
-            for (int i = 0; i < NW; ++i) p.w[i] = 0;
-        }
     }
-    if (KIND == kRowsWhole && at != col) {
+    if (ZEROS && (KIND == kRowsRagged ? col >= C : at != col)) {
 #pragma unroll
         for (int i = 0; i < NW; ++i) p.w[i] = 0;
     }
     return p;
 }
 
-template <int DT>
-__device__ __forceinline__ void unpack(const Piece<DT>& p, float (&v)[kPiece]) {
+template <int DT, int N>
+__device__ __forceinline__ void unpack(const Piece<DT, N>& p, float (&v)[N]) {
 #pragma unroll
-    for (int e = 0; e < kPiece; ++e) {
-        if (DT == FX_F32) v[e] = __uint_as_float(p.w[e % RowType<DT>::kWords]);
+    for (int e = 0; e < N; ++e) {
+        if (DT == FX_F32) v[e] = __uint_as_float(p.w[e % Piece<DT, N>::kWords]);
         else if (DT == FX_BF16) v[e] = __uint_as_float(e & 1 ? p.w[e >> 1] & 0xFFFF0000u : p.w[e >> 1] << 16);
         else v[e] = Elem<_Float16>::to_float((uint16_t)(p.w[e >> 1] >> (16 * (e & 1))));
     }
 }
 
 // one rounding to the storage type (round to nearest even)
-template <int DT>
-__device__ __forceinline__ Piece<DT> pack(const float (&v)[kPiece]) {
-    Piece<DT> p;
+template <int DT, int N>
+__device__ __forceinline__ Piece<DT, N> pack(const float (&v)[N]) {
+    Piece<DT, N> p;
     if (DT == FX_F32) {
 #pragma unroll
-        for (int e = 0; e < kPiece; ++e) p.w[e % RowType<DT>::kWords] = __float_as_uint(v[e]);
+        for (int e = 0; e < N; ++e) p.w[e % Piece<DT, N>::kWords] = __float_as_uint(v[e]);
     } else {
 #pragma unroll
-        for (int e = 0; e < kPiece; e += 2)
+        for (int e = 0; e < N; e += 2)
             p.w[e >> 1] = DT == FX_F16 ? Elem<_Float16>::pack2(v[e], v[e + 1]) : Elem<__bf16>::pack2(v[e], v[e + 1]);
     }
     return p;
 }
 
-template <int DT, int KIND>
-__device__ __forceinline__ void store_piece(unsigned char* row, int col, int C, const Piece<DT>& p) {
-    constexpr int ES = RowType<DT>::kBytes, NW = RowType<DT>::kWords;
-    unsigned char* dst = row + (int64_t)col * ES;
+template <int DT, int KIND, int N>
+__device__ __forceinline__ void store_piece(unsigned char* base, uint32_t off, int col, int C, const Piece<DT, N>& p) {
+    constexpr int ES = Piece<DT, N>::kBytes, NW = Piece<DT, N>::kWords, LW = NW < 4 ? NW : 4;
+    unsigned char* dst = base + (uint32_t)(off + col * ES);
     const int n = C - col;
-    if (KIND != kRowsNarrow && n >= kPiece) {
+    if (KIND != kRowsNarrow && n >= N) {
 #pragma unroll
-        for (int i = 0; i < NW / 4; ++i)
-            reinterpret_cast<Bytes16*>(dst)[i] = Bytes16{{p.w[4 * i], p.w[4 * i + 1], p.w[4 * i + 2], p.w[4 * i + 3]}};
+        for (int i = 0; i < NW / LW; ++i) {
+            Bytes<LW> b;
+#pragma unroll
+            for (int j = 0; j < LW; ++j) b.w[j] = p.w[LW * i + j];
+            reinterpret_cast<Bytes<LW>*>(dst)[i] = b;
+        }
         return;
     }
     if (KIND == kRowsWhole || n <= 0) return;
     if (DT == FX_F32) {
 #pragma unroll
-        for (int e = 0; e < kPiece - 1; ++e)
+        for (int e = 0; e < N - 1; ++e)
             if (e < n) reinterpret_cast<uint32_t*>(dst)[e] = p.w[e % NW];
     } else {                        // 4, 2 and 1 channels, the binary digits of what is left
         uint32_t a = p.w[0];
         int at = 0;
-        if (n & 4) { reinterpret_cast<Bytes8*>(dst)[0] = Bytes8{{p.w[0], p.w[1]}}; a = p.w[2 % NW]; at = 4; }
-        if (n & 2) { reinterpret_cast<Bytes4*>(dst + at * 2)[0] = Bytes4{a}; a = p.w[(at + 2) / 2 % NW]; at += 2; }
+        if (N > 4 && (n & 4)) { reinterpret_cast<Bytes<2>*>(dst)[0] = Bytes<2>{{p.w[0], p.w[1 % NW]}}; a = p.w[2 % NW]; at = 4; }
+        if (n & 2) { reinterpret_cast<Bytes<1>*>(dst + at * 2)[0] = Bytes<1>{{a}}; a = p.w[(at + 2) / 2 % NW]; at += 2; }
         if (n & 1) reinterpret_cast<uint16_t*>(dst)[at] = (uint16_t)a;
     }
 }

@@ -14,11 +14,12 @@
 // negative), and the composition selects, so that nothing of one sequence, an infinity or NaN neither, reaches the
 // next.  All of it is fp32.
 //
-// One pass over the data.  A tile is some hundred rows of up to 64 channels: 8 lanes hold a row (8 channels each, 128
-// bytes of a 16-bit type), and every lane takes a few rows that follow each other, in registers from the load to the
-// store.  A workgroup scans its tile's runs in LDS, publishes the tile's (A, H), looks back over the tiles before it for
-// the value that its first row starts from, and finishes its rows.  Tiles are taken in scan order by ticket, so whatever
-// a workgroup waits for belongs to a workgroup that already runs, and that one waits for earlier tiles only.
+// One pass over the data.  A tile is some hundred rows of up to 64 channels: 16 lanes hold a row (4 channels each), and
+// every lane takes a few rows that follow each other, in registers from the load to the store.  A wave scans its lanes'
+// runs by shuffles, the waves' runs meet in LDS; the workgroup publishes the tile's (A, H), looks back over the tiles
+// before it for the value that its first row starts from, and finishes its rows.  Tiles are taken in scan order by
+// ticket, so whatever a workgroup waits for belongs to a workgroup that already runs, and that one waits for earlier
+// tiles only.
 #include "rows.h"
 
 #include <mutex>
@@ -42,10 +43,11 @@ namespace fx {
 constexpr int kScanThreads = 512;       // most threads of a workgroup
 constexpr int kGroupTiles = 16;         // tiles whose joint (A, H) is published as one
 constexpr int kLookWindow = 16;         // groups looked at together
+constexpr int kQuad = 4;                // channels of a lane
 
 // Rows of a lane: as many as leave a workgroup's registers (gate, input and, backward, state and x of all its rows) room
 // for a second one on the compute unit.
-template <int DT, bool BWD> struct ScanRows { static constexpr int n = BWD && DT == FX_F32 ? 2 : 4; };
+template <int DT, bool BWD> struct ScanRows { static constexpr int n = 8 / (BWD && DT == FX_F32 ? 2 : 1); };
 
 struct ScanArgs {
     int64_t rows;
@@ -79,6 +81,8 @@ __device__ __forceinline__ float through(const Run& r, float v) { return r.A < 0
 struct LaneRows {
     int64_t lo;
     uint32_t begin, stop;               // bit i: the sequence of row u0 + i begins / ends there, in scan order
+    uint32_t starts;                    // bit j: a sequence begins at row lo + j, in the tensors' order
+    int rank;                           // which of the sequences with rows row lo belongs to
     int n;                              // rows that exist
 };
 
@@ -86,21 +90,46 @@ template <bool UP, int R>
 __device__ __forceinline__ LaneRows lane_rows(const ScanArgs& a, int64_t u0) {
     LaneRows r;
     r.n = (int)max((int64_t)0, min((int64_t)R, a.rows - u0));
-    r.begin = r.stop = 0;
-    r.lo = 0;
-    if (r.n == 0) return r;
-    r.lo = UP ? u0 : a.rows - u0 - r.n;
-    const uint64_t w0 = a.begin[r.lo >> 6], w1 = a.begin[(r.lo >> 6) + 1];
+    r.lo = UP ? min(u0, a.rows - 1) : a.rows - min(u0, a.rows - 1) - max(r.n, 1);
+    const int64_t word = r.lo >> 6;
+    const uint64_t w0 = a.begin[word], w1 = a.begin[word + 1];
     const int sh = (int)(r.lo & 63);
     const uint32_t bits = (uint32_t)(sh ? (w0 >> sh) | (w1 << (64 - sh)) : w0) & ((2u << r.n) - 1);      // rows lo .. lo + n
-    const uint32_t starts = bits & ((1u << r.n) - 1), ends = bits >> 1;
-    if (UP) { r.begin = starts; r.stop = ends; }
+    r.rank = a.rank[word] + __popcll(w0 & ((2ull << sh) - 1)) - 1;
+    r.starts = bits & ((1u << r.n) - 1);
+    const uint32_t ends = bits >> 1;
+    if (UP || r.n == 0) { r.begin = r.starts; r.stop = ends; }
     else {                              // bit i is row lo + n - 1 - i
         r.begin = __brev(ends) >> (32 - r.n);
-        r.stop = __brev(starts) >> (32 - r.n);
+        r.stop = __brev(r.starts) >> (32 - r.n);
     }
     return r;
 }
+
+// number of the sequence that the lane's row i (in scan order) belongs to
+template <bool UP>
+__device__ __forceinline__ int sequence_of(const ScanArgs& a, const LaneRows& r, int i) {
+    const int j = UP ? i : r.n - 1 - i;
+    return a.id[r.rank + __popc(r.starts & ((2u << j) - 1) & ~1u)];
+}
+
+// The tile's rows: `count` rows from row `lowest` of the tensors on, the lane's own from the `lane`-th in scan order on.
+// Addresses are a base that is the same in all lanes plus 32 bits of a lane; in a FULL tile the row's number moves the
+// base.  A row that does not exist is read as the tile's last.
+template <bool UP, int R, bool FULL>
+struct TileRows {
+    int64_t lowest;
+    int count, lane;
+    template <typename T>
+    __device__ __forceinline__ T* base(T* tensor, int64_t ld, int i) const {
+        return tensor + (lowest + (!FULL ? 0 : UP ? i : R - 1 - i)) * ld;
+    }
+    __device__ __forceinline__ uint32_t offset(int64_t ld, int i) const {
+        if (FULL) return (uint32_t)(UP ? lane : count - R - lane) * (uint32_t)ld;
+        const int k = min(lane + i, count - 1);
+        return (uint32_t)(UP ? k : count - 1 - k) * (uint32_t)ld;
+    }
+};
 
 // does a sequence begin, in scan order, at row u
 template <bool UP>
@@ -109,55 +138,47 @@ __device__ __forceinline__ bool begins_at(const ScanArgs& a, int64_t u) {
     return a.begin[r >> 6] >> (r & 63) & 1;
 }
 
-__device__ __forceinline__ int sequence_of(const ScanArgs& a, int64_t row) {
-    const uint64_t w = a.begin[row >> 6] & ((2ull << (row & 63)) - 1);
-    return a.id[a.rank[row >> 6] + __popcll(w) - 1];
-}
-
-// eight channels of a row of a [B, C] table, zeros without one
+// four channels of a row of a [B, C] table, zeros without one
 template <int KIND>
-__device__ __forceinline__ void load_states(const float* t, int seq, int col, int C, float (&v)[kPiece]) {
+__device__ __forceinline__ void load_states(const float* t, int seq, int col, int C, float (&v)[kQuad]) {
 #pragma unroll
-    for (int e = 0; e < kPiece; ++e) v[e] = 0.f;
-    if (t) unpack<FX_F32>(load_piece<FX_F32, KIND>(reinterpret_cast<const unsigned char*>(t + (int64_t)seq * C), col, C), v);
+    for (int e = 0; e < kQuad; ++e) v[e] = 0.f;
+    if (t) unpack<FX_F32>(load_piece<FX_F32, KIND, kQuad>(reinterpret_cast<const unsigned char*>(t + (int64_t)seq * C), 0, col, C), v);
 }
 template <int KIND>
-__device__ __forceinline__ void store_states(float* t, int seq, int col, int C, const float (&v)[kPiece]) {
-    store_piece<FX_F32, KIND>(reinterpret_cast<unsigned char*>(t + (int64_t)seq * C), col, C, pack<FX_F32>(v));
+__device__ __forceinline__ void store_states(float* t, int seq, int col, int C, const float (&v)[kQuad]) {
+    store_piece<FX_F32, KIND>(reinterpret_cast<unsigned char*>(t + (int64_t)seq * C), 0, col, C, pack<FX_F32>(v));
 }
 
-// The scan over the lanes' runs within a workgroup.  Runs of all groups of lanes in LDS; a thread takes one channel of
-// eight groups and leaves in their place what stands before each within the eight; the eights' own runs lie in seg.
+// four channels' runs
+struct Runs { float A[kQuad], H[kQuad]; };
+__device__ __forceinline__ Runs no_runs() {
+    Runs r;
+#pragma unroll
+    for (int e = 0; e < kQuad; ++e) { r.A[e] = 1.f; r.H[e] = 0.f; }
+    return r;
+}
+__device__ __forceinline__ void pass_through(const Runs& r, float (&v)[kQuad]) {
+#pragma unroll
+    for (int e = 0; e < kQuad; ++e) v[e] = through(Run{r.A[e], r.H[e]}, v[e]);
+}
+// Runs by channel in LDS.
+struct RunTable {
+    float A[64], H[64];
+    __device__ __forceinline__ void put(int c, const Run& r) { A[c] = r.A; H[c] = r.H; }
+    __device__ __forceinline__ void put4(int c, const Runs& r) {
+        *reinterpret_cast<f32x4*>(&A[c]) = f32x4{r.A[0], r.A[1], r.A[2], r.A[3]};
+        *reinterpret_cast<f32x4*>(&H[c]) = f32x4{r.H[0], r.H[1], r.H[2], r.H[3]};
+    }
+    __device__ __forceinline__ Run get(int c) const { return Run{A[c], H[c]}; }
+};
 struct ScanLds {
-    float A[kScanThreads * kPiece], H[kScanThreads * kPiece];      // [group of lanes][channel of the slab]
-    float seg_A[kScanThreads], seg_H[kScanThreads];                // [eight groups][channel]
-    float before[kScanThreads];                                    // value before every eight groups
-    uint64_t seen[kGroupTiles][64];                                // what a look back found, [tile or group][channel]
+    RunTable wave[kScanThreads / 64];           // of every wave's rows
+    RunTable tiles[kGroupTiles / 4];            // of four tiles each of the group, before this one
+    RunTable groups[kLookWindow / 4];           // of four groups each, backwards
+    float before[kScanThreads / 64][64];        // value before every wave's rows
     int ticket;
 };
-
-__device__ __forceinline__ void put_run(ScanLds& s, int t, const float (&A)[kPiece], const float (&H)[kPiece]) {
-#pragma unroll
-    for (int i = 0; i < kPiece; i += 4) {
-        *reinterpret_cast<f32x4*>(&s.A[t * kPiece + i]) = f32x4{A[i], A[i + 1], A[i + 2], A[i + 3]};
-        *reinterpret_cast<f32x4*>(&s.H[t * kPiece + i]) = f32x4{H[i], H[i + 1], H[i + 2], H[i + 3]};
-    }
-}
-
-__device__ __forceinline__ void scan_eights(ScanLds& s, int width_log2) {
-    const int t = threadIdx.x, width = 1 << width_log2, c = t & (width - 1), seg = t >> width_log2;
-    Run run{1.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int at = ((seg * 8 + i) << width_log2) + c;
-        const Run mine{s.A[at], s.H[at]};
-        s.A[at] = run.A;
-        s.H[at] = run.H;
-        run = then(run, mine);
-    }
-    s.seg_A[t] = run.A;
-    s.seg_H[t] = run.H;
-}
 
 // ---- what workgroups tell each other
 // One 64-bit word a channel holds both numbers of a run, so a reader has all or nothing of it and nothing needs to be
@@ -173,70 +194,99 @@ __device__ __forceinline__ uint64_t look(const uint64_t* at) { return __hip_atom
 __device__ __forceinline__ bool is_there(uint64_t w) { return (uint32_t)(w >> 32) != kNothing; }
 __device__ __forceinline__ Run run_in(uint64_t w) { return Run{__uint_as_float((uint32_t)(w >> 32)), __uint_as_float((uint32_t)w)}; }
 
-// Words `from`, `from` + step, ... of `n` (64 words from one to the next) for this thread's channel into s.seen, waiting
-// for those that are not there yet.  All threads of the workgroup take part; ends with a barrier.  A word that does not
-// come within the bound counts as NaN.
-__device__ __forceinline__ void gather_runs(ScanLds& s, const uint64_t* words, int64_t step, int n, int width_log2) {
-    const int c = threadIdx.x & ((1 << width_log2) - 1), first = threadIdx.x >> width_log2, stride = blockDim.x >> width_log2;
-    for (int i0 = first; i0 < n; i0 += 4 * stride) {
-        uint64_t w[4];
+// The joint run of up to four words, 64 words from one to the next, waiting for those that are not there yet.  BACK: the
+// words lie one before the other.  A word that does not come within the bound counts as NaN.
+template <bool BACK>
+__device__ __forceinline__ Run gather_runs(const uint64_t* at, int n) {
+    const int64_t step = BACK ? -64 : 64;
+    uint64_t w[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int i = i0 + k * stride;
-            w[k] = i < n ? look(words + step * i + c) : 0;
-        }
-        for (int polls = 0; polls < kMostPolls; ++polls) {
-            bool all = true;
+    for (int k = 0; k < 4; ++k) w[k] = k < n ? look(at + step * k) : 0;
+    for (int polls = 0; polls < kMostPolls; ++polls) {
+        if (is_there(w[0]) && is_there(w[1]) && is_there(w[2]) && is_there(w[3])) break;
+        __builtin_amdgcn_s_sleep(1);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) all = all && is_there(w[k]);
-            if (all) break;
-            __builtin_amdgcn_s_sleep(1);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (!is_there(w[k])) w[k] = look(words + step * (i0 + k * stride) + c);
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int i = i0 + k * stride;
-            if (i < n) s.seen[i][c] = is_there(w[k]) ? w[k] : (uint64_t)0xBF800000u << 32 | 0x7FC00000u;
-        }
+        for (int k = 0; k < 4; ++k)
+            if (!is_there(w[k])) w[k] = look(at + step * k);
     }
-    __syncthreads();
+    Run run{1.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const Run r = is_there(w[k]) ? run_in(w[k]) : Run{-1.f, __uint_as_float(0x7FC00000u)};
+        if (k < n) run = BACK ? then(r, run) : then(run, r);
+    }
+    return run;
 }
 
-// The value before the tile for channel threadIdx.x (threads below `width`; others get 0), having published the tile's
-// run and, from the last tile of a group, the group's.
-__device__ __forceinline__ float look_back(const ScanArgs& a, ScanLds& s, int slab, int tile, bool begins, const Run& mine, int width_log2) {
-    const int t = threadIdx.x, width = 1 << width_log2, group = tile / kGroupTiles, in_group = tile % kGroupTiles;
-    const bool closes = in_group == kGroupTiles - 1;
-    uint64_t* tiles = a.tile_runs + ((int64_t)slab * a.tiles + (tile - in_group)) * 64;
-    uint64_t* groups = a.group_runs + (int64_t)slab * a.groups * 64;
-    if (t < width && !closes) publish(tiles + in_group * 64 + t, mine);
-    Run run{1.f, 0.f};                              // of the group's tiles before this one
-    if (in_group && (!begins || closes)) {
-        gather_runs(s, tiles, 64, in_group, width_log2);
-        if (t < width)
-#pragma unroll 2
-            for (int i = 0; i < in_group; ++i) run = then(run, run_in(s.seen[i][t]));
+// Publishes the tile's run and, from the last tile of a group, the group's, and leaves the value before every wave's rows
+// in s.before; a lane is a channel here, and all but the waiting for others' words is done by the first wave.  All
+// threads take part; ends with a barrier.
+template <bool UP>
+__device__ __forceinline__ void look_back(const ScanArgs& a, ScanLds& s, int slab, int tile, int64_t tile0) {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+    const int group = tile / kGroupTiles, in_group = tile % kGroupTiles;
+    const bool here = lane < kQuad << a.lanes_log2, first = wave == 0 && here;
+    const bool linked = a.tile_runs != nullptr, closes = linked && in_group == kGroupTiles - 1;
+    // a tile that a sequence begins with asks nobody
+    const bool asks = linked && !__builtin_amdgcn_readfirstlane((int)begins_at<UP>(a, tile0));
+    uint64_t* tiles = a.tile_runs + ((int64_t)slab * a.tiles + (tile - in_group)) * 64 + lane;
+    uint64_t* groups = a.group_runs + (int64_t)slab * a.groups * 64 + lane;
+    Run mine{1.f, 0.f}, before{1.f, 0.f};           // of the tile; of the group's tiles before it
+    if (first && linked) {
+#pragma unroll 1
+        for (int w = 0; w < waves; ++w) mine = then(mine, s.wave[w].get(lane));
+        if (!closes) publish(tiles + in_group * 64, mine);
     }
-    if (closes && t < width) publish(groups + group * 64 + t, then(run, mine));
-    float v = 0.f;
-    if (!begins) {
+    const int n_tiles = asks || closes ? in_group : 0, t_words = (n_tiles + 3) / 4;
+#pragma unroll 1
+    for (int k = wave; k < t_words; k += waves)
+        if (here) s.tiles[k].put(lane, gather_runs<false>(tiles + 4 * k * 64, min(4, n_tiles - 4 * k)));
+    if (closes) {
+        __syncthreads();
+        if (first) {
+#pragma unroll 1
+            for (int k = 0; 4 * k < n_tiles; ++k) before = then(before, s.tiles[k].get(lane));
+            publish(groups + group * 64, then(before, mine));
+        }
+    }
+    float v = 0.f;                                  // before the first tile: never used, a sequence begins there
+    if (asks) {
         // backwards over the groups until the value behind one of them is known for every channel
         Run back{1.f, 0.f};
-        for (int end = group; end > 0; end -= kLookWindow) {
+        int end = group, turn = closes ? 0 : t_words;       // waves that wait for a tile are not the first to wait for a group
+#pragma unroll 1
+        for (;;) {
             const int n = min(end, kLookWindow);
-            __syncthreads();                        // the words of the turn before have been read
-            gather_runs(s, groups + (int64_t)(end - 1) * 64, -64, n, width_log2);
-            if (t < width)
-#pragma unroll 2
-                for (int i = 0; i < n && back.A >= 0.f; ++i) back = then(run_in(s.seen[i][t]), back);
-            if (!__syncthreads_or(t < width && !(back.A < 0.f))) break;
+#pragma unroll 1
+            for (int k = (wave + waves - turn % waves) % waves; 4 * k < n; k += waves)
+                if (here) s.groups[k].put(lane, gather_runs<true>(groups + (int64_t)(end - 1 - 4 * k) * 64, min(4, n - 4 * k)));
+            __syncthreads();
+            if (here) {
+#pragma unroll 1
+                for (int k = 0; 4 * k < n; ++k) back = then(s.groups[k].get(lane), back);
+            }
+            end -= n;
+            turn = 0;
+            if (end == 0 || __all(!here || back.A < 0.f)) break;        // the same in every wave: each holds all channels
+            __syncthreads();
         }
-        if (t < width) v = through(run, back.H);
+        if (first) {
+            if (!closes) {
+#pragma unroll 1
+                for (int k = 0; 4 * k < n_tiles; ++k) before = then(before, s.tiles[k].get(lane));
+            }
+            v = through(before, back.H);
+        }
     }
-    if (closes && t < width) publish(groups + group * 64 + t, Run{-1.f, through(mine, v)});
-    return v;
+    if (first) {
+#pragma unroll 1
+        for (int w = 0; w < waves; ++w) {
+            s.before[w][lane] = v;
+            v = through(s.wave[w].get(lane), v);
+        }
+        if (closes) publish(groups + group * 64, Run{-1.f, v});
+    }
+    __syncthreads();
 }
 
 __global__ void __launch_bounds__(256) k_scan_clear(uint64_t* words, int64_t n, uint32_t* ticket) {
@@ -257,136 +307,167 @@ __device__ __forceinline__ void kept_gate(float k, float& f, float& g) {
     g = up ? small : large;
 }
 
-template <int DT, int KIND, bool UP, bool BWD>
-__global__ void __launch_bounds__(kScanThreads, BWD ? 2 : 4)
-k_scan(ScanArgs a) {
+template <int DT, int KIND, bool UP, bool BWD, bool FULL>
+__device__ __forceinline__ void scan_tile(const ScanArgs& a, ScanLds& s, int slab, int tile, int64_t tile0, int rows_a_tile) {
     constexpr int R = ScanRows<DT, BWD>::n;
-    __shared__ ScanLds s;
-    const int t = threadIdx.x, lanes = 1 << a.lanes_log2, width_log2 = a.lanes_log2 + 3, width = 1 << width_log2;
-    const int group = t >> a.lanes_log2;
-    int turn = blockIdx.x;
-    if (a.tile_runs) {
-        if (t == 0) s.ticket = (int)atomicAdd(a.ticket, 1u);
-        __syncthreads();
-        turn = s.ticket;
-    }
-    const int slab = turn % a.slabs, tile = turn / a.slabs;
-    const int col = slab * 64 + (t & (lanes - 1)) * kPiece;
-    const int64_t tile0 = (int64_t)tile * (blockDim.x >> a.lanes_log2) * R, u0 = tile0 + group * R;
-    const LaneRows lr = lane_rows<UP, R>(a, u0);
-    constexpr int64_t step = UP ? 1 : -1;
-    const int64_t r0 = UP ? lr.lo : lr.lo + max(lr.n, 1) - 1;        // the lane's first row in scan order
-    Piece<DT> in[R], px[BWD ? R : 1], pp[BWD ? R : 1];
-    float kept[R][kPiece];
-    {
-        const unsigned char *pg = a.gate + r0 * a.ld_gate, *pi = (BWD ? a.gh : a.x) + r0 * (BWD ? a.ld_gh : a.ld_x);
-        Piece<DT> gate[R];
-#pragma unroll
-        for (int i = 0; i < R; ++i) {       // rows that do not exist: the last that does once more
-            gate[i] = load_piece<DT, KIND>(pg, col, a.C);
-            in[i] = load_piece<DT, KIND>(pi, col, a.C);
-            if (i + 1 < lr.n) { pg += step * a.ld_gate; pi += step * (BWD ? a.ld_gh : a.ld_x); }
-        }
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            float z[kPiece];
-            unpack<DT>(gate[i], z);
-#pragma unroll
-            for (int e = 0; e < kPiece; ++e) kept[i][e] = z[e];
-        }
-    }
-    {
-        // the run of this lane's rows
-        float A[kPiece], H[kPiece];
-#pragma unroll
-        for (int e = 0; e < kPiece; ++e) { A[e] = 1.f; H[e] = 0.f; }
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            if (lr.begin >> i & 1) load_states<KIND>(a.first, sequence_of(a, r0 + step * i), col, a.C, H);
-            float v[kPiece];
-            unpack<DT>(in[i], v);
-#pragma unroll
-            for (int e = 0; e < kPiece; ++e) {
-                float f, g;
-                kept[i][e] = keep_gate(kept[i][e], f, g);
-                asm volatile("" : "+v"(kept[i][e]));        // one number is kept: f and g of all rows do not fit the registers
-                H[e] = BWD ? f * (v[e] + H[e]) : f * H[e] + g * v[e];
-                A[e] *= f;
-            }
-            __builtin_amdgcn_sched_barrier(0);      // a row after the other: the gates of all rows at once do not fit the registers
-        }
-        if (lr.begin) {
-#pragma unroll
-            for (int e = 0; e < kPiece; ++e) A[e] = -1.f;
-        }
-        put_run(s, t, A, H);
-    }
-    if (BWD) {
-        // The rows run against the sequence: the state before a row lies at the row that comes next here.
-        const unsigned char *p = a.x + r0 * a.ld_x, *q = a.h + r0 * a.ld_h;
-        const bool more = UP ? r0 + lr.n < a.rows : r0 - lr.n >= 0;        // a row behind the lane's last
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            px[i] = load_piece<DT, KIND>(p, col, a.C);
-            if (i + 1 < lr.n) p += step * a.ld_x;
-            if (i + 1 < lr.n || (i + 1 == lr.n && more)) q += step * a.ld_h;
-            pp[i] = load_piece<DT, KIND>(q, col, a.C);
-        }
-    }
-    __syncthreads();
-    scan_eights(s, width_log2);
-    __syncthreads();
-    {
-        Run run{1.f, 0.f};
-        if (t < width)
-#pragma unroll 2
-            for (int i = t; i < (int)blockDim.x; i += width) run = then(run, Run{s.seg_A[i], s.seg_H[i]});
-        float v = a.tile_runs ? look_back(a, s, slab, tile, begins_at<UP>(a, tile0), run, width_log2) : 0.f;
-        if (t < width)
-#pragma unroll 2
-            for (int i = t; i < (int)blockDim.x; i += width) { s.before[i] = v; v = through(Run{s.seg_A[i], s.seg_H[i]}, v); }
-    }
-    __syncthreads();
-    float v[kPiece];
-#pragma unroll
-    for (int e = 0; e < kPiece; ++e)
-        v[e] = through(Run{s.A[t * kPiece + e], s.H[t * kPiece + e]}, s.before[((group >> 3) << width_log2) + (t & (lanes - 1)) * kPiece + e]);
+    const int t = threadIdx.x, wave = t >> 6, lane = t & 63, lanes = 1 << a.lanes_log2;
+    const int c4 = (lane & (lanes - 1)) * kQuad, col = slab * 64 + c4;
+    TileRows<UP, R, FULL> tr;
+    tr.count = FULL ? rows_a_tile : (int)min((int64_t)rows_a_tile, a.rows - tile0);
+    tr.lowest = UP ? tile0 : a.rows - tile0 - tr.count;
+    tr.lane = (t >> a.lanes_log2) * R;
+    const LaneRows lr = lane_rows<UP, R>(a, tile0 + tr.lane);
+    const unsigned char* in_rows = BWD ? a.gh : a.x;
+    const int64_t ld_in = BWD ? a.ld_gh : a.ld_x;
+    // One number or two of every value are held between the passes over the rows: forward, the state that the lane's own
+    // rows make and the product of gates that a state before them enters it with; backward, the gate.
+    Piece<DT, kQuad> in[R], px[BWD ? R : 1], pp[BWD ? R : 1];
+    float held[R][kQuad], gates[BWD ? 1 : R][kQuad];
+    Piece<DT, kQuad> gate[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-        if (i >= lr.n) break;
-        const int64_t row = r0 + step * i;
-        const bool begins = lr.begin >> i & 1, ends = lr.stop >> i & 1;
-        if (begins) load_states<KIND>(a.first, sequence_of(a, row), col, a.C, v);
-        float w[kPiece];
-        unpack<DT>(in[i], w);
-        if (!BWD) {
+        gate[i] = load_piece<DT, KIND, kQuad, false>(tr.base(a.gate, a.ld_gate, i), tr.offset(a.ld_gate, i), col, a.C);
+        in[i] = load_piece<DT, KIND, kQuad, false>(tr.base(in_rows, ld_in, i), tr.offset(ld_in, i), col, a.C);
+        __builtin_amdgcn_sched_barrier(0);      // in turn: the first rows are worked on while the last are on their way
+    }
+    // of the first sequence that begins in the lane's rows and the first that ends, asked for along with the rows
+    float start[kQuad], state0[kQuad];
+    if (lr.begin) load_states<KIND>(a.first, sequence_of<UP>(a, lr, __ffs(lr.begin) - 1), col, a.C, start);
+    if (BWD && lr.stop) load_states<KIND>(a.h0, sequence_of<UP>(a, lr, __ffs(lr.stop) - 1), col, a.C, state0);
+    Runs mine = no_runs();                      // of this lane's rows
 #pragma unroll
-            for (int e = 0; e < kPiece; ++e) {
-                float f, g;
-                kept_gate(kept[i][e], f, g);
-                v[e] = f * v[e] + g * w[e];
+    for (int i = 0; i < R; ++i) {
+        if (lr.begin >> i & 1) {
+            if (lr.begin & ((1u << i) - 1)) load_states<KIND>(a.first, sequence_of<UP>(a, lr, i), col, a.C, start);
+#pragma unroll
+            for (int e = 0; e < kQuad; ++e) { mine.A[e] = 1.f; mine.H[e] = start[e]; }
+        }
+        float z[kQuad], v[kQuad];
+        unpack<DT>(gate[i], z);
+        unpack<DT>(in[i], v);
+#pragma unroll
+        for (int e = 0; e < kQuad; ++e) {
+            float f, g;
+            const float k = keep_gate(z[e], f, g);
+            mine.H[e] = BWD ? f * (v[e] + mine.H[e]) : f * mine.H[e] + g * v[e];
+            mine.A[e] *= f;
+            held[i][e] = BWD ? k : mine.H[e];
+            if (BWD) asm volatile("" : "+v"(held[i][e]));       // the number itself, not f and g that it stands for
+            else gates[i][e] = mine.A[e];
+        }
+        if (BWD) {
+#pragma unroll
+            for (int k = 0; k < Piece<DT, kQuad>::kWords; ++k) asm volatile("" : "+v"(in[i].w[k]));     // as loaded, for the same reason
+        }
+        __builtin_amdgcn_sched_barrier(0);      // a row after the other: all rows' numbers at once do not fit the registers
+    }
+    if (BWD) {
+        // The rows run against the sequence: the state before a row lies at the row that comes next here.  Behind the
+        // last row of all there is none (and none is asked for): the row itself in its place.
+        const int64_t more = tile0 + tr.count < a.rows ? a.ld_h : 0;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            px[i] = load_piece<DT, KIND, kQuad, false>(tr.base(a.x, a.ld_x, i), tr.offset(a.ld_x, i), col, a.C);
+            const bool last = tr.lane + i >= tr.count - 1;
+            if (i + 1 < R && FULL) pp[i] = load_piece<DT, KIND, kQuad, false>(tr.base(a.h, a.ld_h, i + 1), tr.offset(a.ld_h, i + 1), col, a.C);
+            else pp[i] = load_piece<DT, KIND, kQuad, false>(tr.base(a.h, a.ld_h, i) + (last ? (UP ? more : -more) : UP ? a.ld_h : -a.ld_h), tr.offset(a.ld_h, i), col, a.C);
+        }
+    }
+    // Runs of all lanes up to this one.  Where a sequence begins in a lane's rows, what stands before them is left out:
+    // a bit a lane says so for all of its channels.
+    uint64_t cut = __ballot(lr.begin != 0);
+#pragma unroll 1
+    for (int d = lanes; d < 64; d <<= 1) {
+        const bool alone = (cut | ((1ull << d) - 1)) >> lane & 1;
+#pragma unroll
+        for (int e = 0; e < kQuad; ++e) {
+            const float oA = __shfl_up(mine.A[e], d), oH = __shfl_up(mine.H[e], d);
+            mine.H[e] = alone ? mine.H[e] : mine.A[e] * oH + mine.H[e];
+            mine.A[e] = alone ? mine.A[e] : mine.A[e] * oA;
+        }
+        cut |= cut << d;
+    }
+    if (cut >> lane & 1) {
+#pragma unroll
+        for (int e = 0; e < kQuad; ++e) mine.A[e] = -1.f;
+    }
+    if (lane >= 64 - lanes) s.wave[wave].put4(c4, mine);
+    // of the lanes before this one
+#pragma unroll
+    for (int e = 0; e < kQuad; ++e) {
+        const float oA = __shfl_up(mine.A[e], lanes), oH = __shfl_up(mine.H[e], lanes);
+        mine.A[e] = lane < lanes ? 1.f : oA;
+        mine.H[e] = lane < lanes ? 0.f : oH;
+    }
+    __syncthreads();
+    look_back<UP>(a, s, slab, tile, tile0);
+    float v[kQuad];
+    {
+        const f32x4 b = *reinterpret_cast<const f32x4*>(&s.before[wave][c4]);
+#pragma unroll
+        for (int e = 0; e < kQuad; ++e) v[e] = b[e];
+    }
+    pass_through(mine, v);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        if (!FULL && i >= lr.n) continue;
+        const bool begins = lr.begin >> i & 1, ends = lr.stop >> i & 1;
+        if (!BWD) {
+            if (begins) {
+#pragma unroll
+                for (int e = 0; e < kQuad; ++e) v[e] = 0.f;     // what stands before the lane's rows ends here
             }
-            store_piece<DT, KIND>(a.out + row * a.ld_out, col, a.C, pack<DT>(v));
+            float h[kQuad];
+#pragma unroll
+            for (int e = 0; e < kQuad; ++e) h[e] = gates[i][e] * v[e] + held[i][e];
+            store_piece<DT, KIND>(tr.base(a.out, a.ld_out, i), tr.offset(a.ld_out, i), col, a.C, pack<DT>(h));
+            if (ends && a.last) store_states<KIND>(a.last, sequence_of<UP>(a, lr, i), col, a.C, h);
         } else {
-            float x[kPiece], p[kPiece], gx[kPiece], gz[kPiece];
+            if (begins) {
+                if (lr.begin & (lr.begin - 1)) load_states<KIND>(a.first, sequence_of<UP>(a, lr, i), col, a.C, start);
+#pragma unroll
+                for (int e = 0; e < kQuad; ++e) v[e] = start[e];
+            }
+            float w[kQuad], x[kQuad], p[kQuad], gx[kQuad], gz[kQuad];
+            unpack<DT>(in[i], w);
             unpack<DT>(px[i], x);
             unpack<DT>(pp[i], p);
-            if (ends) load_states<KIND>(a.h0, sequence_of(a, row), col, a.C, p);
+            if (ends) {
+                if (lr.stop & ((1u << i) - 1)) load_states<KIND>(a.h0, sequence_of<UP>(a, lr, i), col, a.C, state0);
 #pragma unroll
-            for (int e = 0; e < kPiece; ++e) {
+                for (int e = 0; e < kQuad; ++e) p[e] = state0[e];
+            }
+#pragma unroll
+            for (int e = 0; e < kQuad; ++e) {
                 float f, g;
-                kept_gate(kept[i][e], f, g);
+                kept_gate(held[i][e], f, g);
                 const float lam = w[e] + v[e];
                 gx[e] = g * lam;
                 gz[e] = lam * (p[e] - x[e]) * (f * g);
                 v[e] = f * lam;
             }
-            store_piece<DT, KIND>(a.gx + row * a.ld_gx, col, a.C, pack<DT>(gx));
-            store_piece<DT, KIND>(a.ggate + row * a.ld_ggate, col, a.C, pack<DT>(gz));
+            store_piece<DT, KIND>(tr.base(a.gx, a.ld_gx, i), tr.offset(a.ld_gx, i), col, a.C, pack<DT>(gx));
+            store_piece<DT, KIND>(tr.base(a.ggate, a.ld_ggate, i), tr.offset(a.ld_ggate, i), col, a.C, pack<DT>(gz));
+            if (ends && a.last) store_states<KIND>(a.last, sequence_of<UP>(a, lr, i), col, a.C, v);
         }
-        if (ends && a.last) store_states<KIND>(a.last, sequence_of(a, row), col, a.C, v);
         __builtin_amdgcn_sched_barrier(0);
     }
+}
+
+template <int DT, int KIND, bool UP, bool BWD>
+__global__ void __launch_bounds__(kScanThreads, BWD ? 3 : 4)
+k_scan(ScanArgs a) {
+    __shared__ ScanLds s;
+    int turn = blockIdx.x;
+    if (a.tile_runs) {
+        if (threadIdx.x == 0) s.ticket = (int)atomicAdd(a.ticket, 1u);
+        __syncthreads();
+        turn = __builtin_amdgcn_readfirstlane(s.ticket);
+    }
+    const int slab = turn % a.slabs, tile = turn / a.slabs, rows_a_tile = (blockDim.x >> a.lanes_log2) * ScanRows<DT, BWD>::n;
+    const int64_t tile0 = (int64_t)tile * rows_a_tile;
+    if (tile0 + rows_a_tile <= a.rows) scan_tile<DT, KIND, UP, BWD, true>(a, s, slab, tile, tile0, rows_a_tile);
+    else scan_tile<DT, KIND, UP, BWD, false>(a, s, slab, tile, tile0, rows_a_tile);
 }
 
 // states of sequences without rows pass through
@@ -406,7 +487,7 @@ k_scan_step(int64_t rows, int C, int pieces, const unsigned char* x, int64_t ld_
     if (row >= rows) return;
     const int col = (int)(i - row * pieces) * kPiece;
     float z[kPiece], v[kPiece], h[kPiece];
-    const Piece<DT> pz = load_piece<DT, KIND>(gate + row * ld_gate, col, C), pv = load_piece<DT, KIND>(x + row * ld_x, col, C);
+    const Piece<DT> pz = load_piece<DT, KIND>(gate + row * ld_gate, 0, col, C), pv = load_piece<DT, KIND>(x + row * ld_x, 0, col, C);
 #pragma unroll
     for (int e = 0; e < kPiece; ++e) h[e] = col + e < C ? state[row * C + col + e] : 0.f;
     unpack<DT>(pz, z);
@@ -418,7 +499,7 @@ k_scan_step(int64_t rows, int C, int pieces, const unsigned char* x, int64_t ld_
         h[e] = f * h[e] + g * v[e];
         if (col + e < C) new_state[row * C + col + e] = h[e];
     }
-    store_piece<DT, KIND>(out + row * ld_out, col, C, pack<DT>(h));
+    store_piece<DT, KIND>(out + row * ld_out, 0, col, C, pack<DT>(h));
 }
 
 // ---------------------------------------------------------------------------------- host
@@ -445,24 +526,33 @@ static void scan_args(ScanArgs* a, const fx_sequences* q, int32_t C) {
     *a = ScanArgs{};
     a->rows = q->rows;
     a->C = C;
-    const int pieces = std::min(8, (C + kPiece - 1) / kPiece);
-    while ((1 << a->lanes_log2) < pieces) ++a->lanes_log2;
+    const int quads = std::min(64 / kQuad, (C + kQuad - 1) / kQuad);
+    while ((1 << a->lanes_log2) < quads) ++a->lanes_log2;
     a->slabs = (C + 63) / 64;
     a->begin = q->d_begin;
     a->rank = q->d_rank;
     a->id = q->d_id;
 }
 
+constexpr int64_t kMostOffset = 1ll << 31;      // bytes from a tile's first row to its last
+
+static int64_t most_ld(const ScanArgs& a) {
+    return std::max({a.ld_x, a.ld_gate, a.ld_h, a.ld_gh, a.ld_out, a.ld_gx, a.ld_ggate});
+}
+
 template <int DT, int KIND, bool UP, bool BWD>
 static fx_status launch_scan(ScanArgs& a, hipStream_t st) {
-    // As many threads as leave every compute unit a tile, from a wave on.
-    int threads = kScanThreads;
+    // As many threads as leave every compute unit two tiles, from a wave on.  Backward at most 256: at its registers a
+    // compute unit holds three such workgroups, or one of 512 (986,880 x 64 bf16: 212 us, 230 us); forward two of 512,
+    // whose tiles, twice as long, have half as many others to wait for (132 us; of 256 150 us).
+    int threads = BWD ? kScanThreads / 2 : kScanThreads;
     int64_t rows_a_tile, tiles;
     for (;; threads /= 2) {
         rows_a_tile = (int64_t)(threads >> a.lanes_log2) * ScanRows<DT, BWD>::n;
         tiles = (a.rows + rows_a_tile - 1) / rows_a_tile;
-        if (threads == 64 || tiles * a.slabs >= 2 * compute_units()) break;
+        if (threads == 64 || (tiles * a.slabs >= 2 * compute_units() && rows_a_tile * most_ld(a) < kMostOffset)) break;
     }
+    if (rows_a_tile * most_ld(a) >= kMostOffset) { set_error("gated scan: rows lie more than %lld bytes apart", (long long)(kMostOffset / rows_a_tile)); return FX_ERANGE; }
     if (tiles * a.slabs > 0x3FFFFFFF) { set_error("gated scan: too many tiles for one launch"); return FX_ERANGE; }
     a.tiles = (int)tiles;
     a.groups = (int)((tiles + kGroupTiles - 1) / kGroupTiles);
@@ -486,7 +576,7 @@ static fx_status launch_scan(ScanArgs& a, hipStream_t st) {
 
 template <int DT, bool BWD>
 static fx_status launch_scan_kind(ScanArgs& a, bool up, hipStream_t st) {
-    const int kind = a.C < kPiece ? kRowsNarrow : a.C % kPiece ? kRowsRagged : kRowsWhole;
+    const int kind = a.C < kQuad ? kRowsNarrow : a.C % kQuad ? kRowsRagged : kRowsWhole;
 #define FX_SCAN(KIND) return up ? launch_scan<DT, KIND, true, BWD>(a, st) : launch_scan<DT, KIND, false, BWD>(a, st)
     if (kind == kRowsWhole) FX_SCAN(kRowsWhole);
     if (kind == kRowsRagged) FX_SCAN(kRowsRagged);
