@@ -60,11 +60,23 @@ __device__ __forceinline__ void group_sums(float (&v)[N], int lanes, float* lds)
 __device__ __forceinline__ float inv_rms(float sum_sq, float inv_C, float eps) { return 1.f / sqrtf(sum_sq * inv_C + eps); }
 
 // act(z) and its derivative
-__device__ __forceinline__ void gate_factor(int act, float z, float& a, float& da) {
-    float up, down;
-    sigmoids(z, up, down);
-    if (act == FX_GATE_SILU) { a = z * up; da = up * (1.f + z * down); }
-    else { a = up; da = up * down; }
+__device__ __forceinline__ void gate_factors(int act, const float (&z)[kPiece], float (&f)[kPiece], float (&df)[kPiece]) {
+    if (act == FX_GATE_SILU) {
+#pragma unroll
+        for (int e = 0; e < kPiece; ++e) {
+            float up, down;
+            sigmoids(z[e], up, down);
+            f[e] = z[e] * up;
+            df[e] = up * (1.f + z[e] * down);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < kPiece; ++e) {
+            float down;
+            sigmoids(z[e], f[e], down);
+            df[e] = f[e] * down;
+        }
+    }
 }
 
 template <int DT, int KIND, bool WIDE, int MODE>
@@ -73,11 +85,12 @@ k_block_fwd(BlockArgs a) {
     __shared__ float lds[WIDE ? kWideThreads / 64 : 1];
     const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1), C = a.C, col = lane * kPiece;
     const int rows_here = WIDE ? 1 : kBlockThreads >> a.lanes_log2;
+    const uint32_t mask = lane_mask(col, C);
     const uint64_t offset = a.drop.offset + (a.drop.d_more ? *a.drop.d_more : 0);
     float wp[kPiece], ws[kPiece], wn[kPiece];
-    if (MODE == kModeJoin) load_vector(a.post, a.vec_f32, DT, col, C, 1.f, wp);
-    if (MODE == kModeJoin) load_vector(a.scale, a.vec_f32, DT, col, C, 1.f, ws);
-    if (MODE != kModeDrop) load_vector(a.next, a.vec_f32, DT, col, C, 1.f, wn);
+    if (MODE == kModeJoin) load_vector<DT, KIND>(a.post, a.vec_f32, col, C, 1.f, wp);
+    if (MODE == kModeJoin) load_vector<DT, KIND>(a.scale, a.vec_f32, col, C, 1.f, ws);
+    if (MODE != kModeDrop) load_vector<DT, KIND>(a.next, a.vec_f32, col, C, 1.f, wn);
     for (int64_t r0 = (int64_t)blockIdx.x * rows_here; r0 < a.rows; r0 += (int64_t)gridDim.x * rows_here) {
         const int64_t mine = WIDE ? r0 : r0 + (threadIdx.x >> a.lanes_log2);
         const bool real = mine < a.rows;
@@ -87,7 +100,7 @@ k_block_fwd(BlockArgs a) {
         if (MODE != kModeNorm) py = load_piece<DT, KIND>(a.y + row * a.ld_y, 0, col, C);
         if (MODE == kModeJoin && a.gate) pg = load_piece<DT, KIND>(a.gate + row * a.ld_gate, 0, col, C);
         float v[kPiece];
-        unpack<DT>(MODE == kModeNorm ? px : py, v);
+        unpack<DT>(masked(MODE == kModeNorm ? px : py, mask), v);
         if (MODE == kModeJoin && a.post) {
             float s[1] = {0.f};
 #pragma unroll
@@ -98,14 +111,11 @@ k_block_fwd(BlockArgs a) {
             for (int e = 0; e < kPiece; ++e) v[e] *= rs * wp[e];
         }
         if (MODE == kModeJoin && a.gate) {
-            float z[kPiece];
+            float z[kPiece], f[kPiece], df[kPiece];
             unpack<DT>(pg, z);
+            gate_factors(a.act, z, f, df);
 #pragma unroll
-            for (int e = 0; e < kPiece; ++e) {
-                float f, df;
-                gate_factor(a.act, z[e], f, df);
-                v[e] *= f;
-            }
+            for (int e = 0; e < kPiece; ++e) v[e] *= f[e];
         }
         if (MODE != kModeNorm) {
             if (a.drop.below) {
@@ -114,12 +124,15 @@ k_block_fwd(BlockArgs a) {
 #pragma unroll
                 for (int e = 0; e < kPiece; ++e) v[e] = drop_value(w, e, a.drop, v[e]);
             }
-            float x[kPiece];
-            if (a.x) unpack<DT>(px, x);
+            if (MODE == kModeJoin) {
 #pragma unroll
-            for (int e = 0; e < kPiece; ++e) {
-                if (MODE == kModeJoin) v[e] *= ws[e];
-                if (a.x) v[e] += x[e];
+                for (int e = 0; e < kPiece; ++e) v[e] *= ws[e];
+            }
+            if (a.x) {
+                float x[kPiece];
+                unpack<DT>(masked(px, mask), x);
+#pragma unroll
+                for (int e = 0; e < kPiece; ++e) v[e] += x[e];
             }
             if (WIDE) __syncthreads();      // an output may lie where an input lies: all waves have their pieces of the row
             if (real) store_piece<DT, KIND>(a.out + row * a.ld_out, 0, col, C, pack<DT>(v));
@@ -172,11 +185,12 @@ k_block_bwd(BlockArgs a) {
     __shared__ float lds[WIDE ? 1 : 4][64 * kPiece];
     const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1), C = a.C, col = lane * kPiece;
     const int rows_here = WIDE ? 1 : kBlockThreads >> a.lanes_log2;
+    const uint32_t mask = lane_mask(col, C);
     const uint64_t offset = a.drop.offset + (a.drop.d_more ? *a.drop.d_more : 0);
     float wp[kPiece], ws[kPiece], wn[kPiece], acc_post[kPiece], acc_scale[kPiece], acc_next[kPiece];
-    if (MODE == kModeJoin) load_vector(a.post, a.vec_f32, DT, col, C, 1.f, wp);
-    if (MODE == kModeJoin) load_vector(a.scale, a.vec_f32, DT, col, C, 1.f, ws);
-    load_vector(a.next, a.vec_f32, DT, col, C, 1.f, wn);
+    if (MODE == kModeJoin) load_vector<DT, KIND>(a.post, a.vec_f32, col, C, 1.f, wp);
+    if (MODE == kModeJoin) load_vector<DT, KIND>(a.scale, a.vec_f32, col, C, 1.f, ws);
+    load_vector<DT, KIND>(a.next, a.vec_f32, col, C, 1.f, wn);
 #pragma unroll
     for (int e = 0; e < kPiece; ++e) acc_post[e] = acc_scale[e] = acc_next[e] = 0.f;
     for (int64_t r0 = (int64_t)blockIdx.x * rows_here; r0 < a.rows; r0 += (int64_t)gridDim.x * rows_here) {
@@ -191,57 +205,64 @@ k_block_bwd(BlockArgs a) {
         if (a.gout) pgo = load_piece<DT, KIND>(a.gout + row * a.ld_gout, 0, col, C);
         if (MODE == kModeJoin) py = load_piece<DT, KIND>(a.y + row * a.ld_y, 0, col, C);
         if (MODE == kModeJoin && a.gate) pg = load_piece<DT, KIND>(a.gate + row * a.ld_gate, 0, col, C);
+        // a row that does not exist counts as zeros, and as if its norms were 1
+        const uint32_t m = real ? mask : 0;
         float sums[3] = {0.f, 0.f, 0.f};         // x'^2, gnorm w x', y^2
         float x[kPiece], g[kPiece], D[kPiece], y[kPiece];
         if (a.gnorm) {
-            unpack<DT>(px, x);
-            unpack<DT>(pgn, g);
+            unpack<DT>(masked(px, m), x);
+            unpack<DT>(masked(pgn, m), g);
 #pragma unroll
             for (int e = 0; e < kPiece; ++e) { sums[0] += x[e] * x[e]; sums[1] += g[e] * wn[e] * x[e]; }
         }
         if (MODE == kModeJoin) {
-            unpack<DT>(py, y);
+            unpack<DT>(masked(py, m), y);
 #pragma unroll
             for (int e = 0; e < kPiece; ++e) sums[2] += y[e] * y[e];
         }
         group_sums<WIDE>(sums, lanes, lds_sum);
-        const float rx = inv_rms(sums[0], a.inv_C, a.eps), ry = inv_rms(sums[2], a.inv_C, a.eps);
+        const float rx = real ? inv_rms(sums[0], a.inv_C, a.eps) : 1.f;
+        const float ry = real && a.post ? inv_rms(sums[2], a.inv_C, a.eps) : 1.f;       // without post, r is y
         const float cx = sums[1] * a.inv_C * rx * rx;
 #pragma unroll
         for (int e = 0; e < kPiece; ++e) D[e] = 0.f;
-        if (a.gout) unpack<DT>(pgo, D);
+        if (a.gout) unpack<DT>(masked(pgo, m), D);
         if (a.gnorm) {
 #pragma unroll
             for (int e = 0; e < kPiece; ++e) {
                 D[e] += rx * (g[e] * wn[e] - x[e] * cx);
-                acc_next[e] += real ? g[e] * (x[e] * rx) : 0.f;
+                acc_next[e] += g[e] * (x[e] * rx);
             }
         }
         if (real && a.gx) store_piece<DT, KIND>(a.gx + row * a.ld_gx, 0, col, C, pack<DT>(D));
         if (MODE == kModeJoin) {
-            uint32_t w[4];
-            if (a.drop.below) philox8((uint32_t)lane, (uint32_t)row, offset, a.drop.seed, w);
-            float z[kPiece];
-            if (a.gate) unpack<DT>(pg, z);
+            if (a.drop.below) {
+                uint32_t w[4];
+                philox8((uint32_t)lane, (uint32_t)row, offset, a.drop.seed, w);
+#pragma unroll
+                for (int e = 0; e < kPiece; ++e) D[e] = drop_value(w, e, a.drop, D[e]);
+            }
+            float f[kPiece], df[kPiece];
+#pragma unroll
+            for (int e = 0; e < kPiece; ++e) { f[e] = 1.f; df[e] = 0.f; }
+            if (a.gate) {
+                float z[kPiece];
+                unpack<DT>(pg, z);
+                gate_factors(a.act, z, f, df);
+            }
             float dot[1] = {0.f};                // u post yh
 #pragma unroll
             for (int e = 0; e < kPiece; ++e) {
-                float f = 1.f, df = 0.f;
-                if (a.gate) gate_factor(a.act, z[e], f, df);
-                const float yh = y[e] * ry, r = a.post ? yh * wp[e] : y[e];
-                float t = D[e];
-                if (a.drop.below) t = drop_value(w, e, a.drop, t);
-                acc_scale[e] += real ? t * (r * f) : 0.f;
-                t *= ws[e];
-                z[e] = t * (r * df);
-                t *= f;
-                acc_post[e] += real ? t * yh : 0.f;
-                t *= wp[e];
-                dot[0] += t * yh;
-                y[e] = yh;
-                D[e] = t;
+                y[e] *= ry;                      // yh
+                const float r = y[e] * wp[e];
+                acc_scale[e] += D[e] * (r * f[e]);
+                const float t = D[e] * ws[e], u = t * f[e];
+                df[e] *= t * r;
+                acc_post[e] += u * y[e];
+                D[e] = u * wp[e];
+                dot[0] += D[e] * y[e];
             }
-            if (real && a.ggate) store_piece<DT, KIND>(a.ggate + row * a.ld_ggate, 0, col, C, pack<DT>(z));
+            if (real && a.ggate) store_piece<DT, KIND>(a.ggate + row * a.ld_ggate, 0, col, C, pack<DT>(df));
             if (a.post) {
                 group_sums<WIDE>(dot, lanes, lds_sum);
                 const float cy = dot[0] * a.inv_C;
@@ -258,26 +279,27 @@ k_block_bwd(BlockArgs a) {
     if (a.want & 4) write_partial<WIDE>(acc_next, lanes, C, mine + 2 * vec, lds);
 }
 
-// out[c] = sum over the workgroups' partial sums, in index order within each of eight slices and then over the slices
+// out[c] = sum over the workgroups' partial sums: 64 slices of them in index order, then the slices
 template <int DT>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
 k_block_sums(const float* __restrict__ partial, int n, int C, void* out0, void* out1, void* out2) {
-    __shared__ float lds[8][32];
+    __shared__ float lds[64][16];
     void* out = blockIdx.y == 0 ? out0 : blockIdx.y == 1 ? out1 : out2;
     if (!out) return;
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5, per = (n + 7) / 8;
-    const int64_t base = (int64_t)blockIdx.y * n * C;
+    const int c = blockIdx.x * 16 + (threadIdx.x & 15), slice = threadIdx.x >> 4, per = (n + 63) / 64;
     float s = 0.f;
     if (c < C) {
+        const float* in = partial + (int64_t)blockIdx.y * n * C + c;
         const int end = min(n, (slice + 1) * per);
-#pragma unroll 8
-        for (int i = slice * per; i < end; ++i) s += partial[base + (int64_t)i * C + c];
+#pragma unroll 16
+        for (int i = slice * per; i < end; ++i) s += in[(int64_t)i * C];
     }
-    lds[slice][threadIdx.x & 31] = s;
+    lds[slice][threadIdx.x & 15] = s;
     __syncthreads();
     if (slice == 0 && c < C) {
-#pragma unroll
-        for (int i = 1; i < 8; ++i) s += lds[i][threadIdx.x];
+        s = 0.f;
+#pragma unroll 16
+        for (int i = 0; i < 64; ++i) s += lds[i][threadIdx.x];
         if (DT == FX_F32) reinterpret_cast<float*>(out)[c] = s;
         else if (DT == FX_F16) reinterpret_cast<uint16_t*>(out)[c] = Elem<_Float16>::from_float(s);
         else reinterpret_cast<uint16_t*>(out)[c] = Elem<__bf16>::from_float(s);
@@ -338,7 +360,7 @@ static void launch_block(bool bwd, fx_dtype dt, const BlockArgs& a, const RowSha
     else launch_block_kind<FX_BF16, MODE>(bwd, a, s, nb, st);
 }
 
-constexpr int kFwdWaves = 32, kBwdWaves = 16;     // of a compute unit in one launch
+constexpr int kFwdWaves = 128, kBwdWaves = 8, kNormBwdWaves = 16;     // of a compute unit in one launch
 
 static fx_status check_rows(const char* who, int64_t rows, int32_t C, fx_dtype dt) {
     if (rows < 0 || C < 1 || !known(dt)) { set_error("%s: negative rows, no channels or unknown dtype", who); return FX_EINVAL; }
@@ -383,10 +405,10 @@ static fx_status drop_args(const char* who, double p, uint64_t seed, uint64_t of
 // The last step of both backward calls: vectors over the workgroups' partial sums, zeros where there are no rows.
 static fx_status finish_sums(fx_dtype vec_dt, const BlockArgs& a, unsigned nb, void* gpost, void* gscale, void* gnext, hipStream_t st) {
     ProfScope ps(kProfBlockSums, st);
-    const dim3 grid((a.C + 31) / 32, 3);
-    if (vec_dt == FX_F32) k_block_sums<FX_F32><<<grid, 256, 0, st>>>(a.partial, (int)nb, a.C, gpost, gscale, gnext);
-    else if (vec_dt == FX_F16) k_block_sums<FX_F16><<<grid, 256, 0, st>>>(a.partial, (int)nb, a.C, gpost, gscale, gnext);
-    else k_block_sums<FX_BF16><<<grid, 256, 0, st>>>(a.partial, (int)nb, a.C, gpost, gscale, gnext);
+    const dim3 grid((a.C + 15) / 16, 3);
+    if (vec_dt == FX_F32) k_block_sums<FX_F32><<<grid, 1024, 0, st>>>(a.partial, (int)nb, a.C, gpost, gscale, gnext);
+    else if (vec_dt == FX_F16) k_block_sums<FX_F16><<<grid, 1024, 0, st>>>(a.partial, (int)nb, a.C, gpost, gscale, gnext);
+    else k_block_sums<FX_BF16><<<grid, 1024, 0, st>>>(a.partial, (int)nb, a.C, gpost, gscale, gnext);
     FX_HIP_TRY(hipGetLastError());
     return FX_OK;
 }
@@ -394,7 +416,7 @@ static fx_status finish_sums(fx_dtype vec_dt, const BlockArgs& a, unsigned nb, v
 template <int MODE>
 static fx_status run_bwd(fx_dtype dt, fx_dtype vec_dt, BlockArgs& a, void* gpost, void* gscale, void* gnext, hipStream_t st) {
     const RowShape shape = row_shape(a.C);
-    const unsigned nb = row_blocks(a.rows, shape, kBwdWaves);
+    const unsigned nb = row_blocks(a.rows, shape, MODE == kModeNorm ? kNormBwdWaves : kBwdWaves);
     a.lanes_log2 = shape.lanes_log2;
     a.want = (gpost ? 1 : 0) | (gscale ? 2 : 0) | (gnext ? 4 : 0);
     void* partial = nullptr;

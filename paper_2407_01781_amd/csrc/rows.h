@@ -21,12 +21,12 @@ template <int DT, int N = kPiece> struct Piece {
 // of a wider tensor, start anywhere.  One load or store instruction all the same.
 template <int WORDS> struct __attribute__((packed, aligned(2))) Bytes { uint32_t w[WORDS]; };
 
-// The piece that begins at channel `col` of the row `off` bytes behind `base`; channels from C on come as zeros (the
-// offset apart from the base: where the base is the same in all lanes, it stays in scalar registers; without ZEROS, a lane
-// that has no channel at all gets some that are not its own).  A ragged row's last
+// The piece that begins at channel `col` of the row `off` bytes behind `base` (apart from the base: where that is the same
+// in all lanes, it stays in scalar registers).  Channels from C on come as zeros, but for a lane that has no channel at
+// all: it gets some of the row's, for the caller to mask where they would count.  A ragged row's last
 // piece is loaded as the row's last N channels and moved into place, so that no load passes the row's end and every
 // lane, one without channels too, loads from inside the row.
-template <int DT, int KIND, int N = kPiece, bool ZEROS = true>
+template <int DT, int KIND, int N = kPiece>
 __device__ __forceinline__ Piece<DT, N> load_piece(const unsigned char* base, uint32_t off, int col, int C) {
     Piece<DT, N> p;
     constexpr int ES = Piece<DT, N>::kBytes, NW = Piece<DT, N>::kWords, LW = NW < 4 ? NW : 4;
@@ -61,15 +61,25 @@ __device__ __forceinline__ Piece<DT, N> load_piece(const unsigned char* base, ui
                 p.w[i] = on ? from : p.w[i];
             }
         }
-        if (ES == 2 && (bits & 16)) {
+        if (ES == 2) {
 #pragma unroll
-            for (int i = 0; i < NW; ++i) p.w[i] = (p.w[i] >> 16) | (i + 1 < NW ? p.w[i + 1] << 16 : 0u);
+            for (int i = 0; i < NW; ++i) p.w[i] = __builtin_amdgcn_alignbit(i + 1 < NW ? p.w[i + 1] : 0u, p.w[i], bits & 16);
         }
     }
-    if (ZEROS && (KIND == kRowsRagged ? col >= C : at != col)) {
+    return p;
+}
+
+// All bits for a lane that has channels, none for one that has not.  Opaque: a test in its place becomes a branch behind
+// every load, which waits for it.
+__device__ __forceinline__ uint32_t lane_mask(int col, int C) {
+    uint32_t m = col < C ? ~0u : 0u;
+    asm volatile("" : "+v"(m));
+    return m;
+}
+template <int DT, int N>
+__device__ __forceinline__ Piece<DT, N> masked(Piece<DT, N> p, uint32_t mask) {
 #pragma unroll
-        for (int i = 0; i < NW; ++i) p.w[i] = 0;
-    }
+    for (int i = 0; i < Piece<DT, N>::kWords; ++i) p.w[i] &= mask;
     return p;
 }
 
@@ -127,17 +137,14 @@ __device__ __forceinline__ void store_piece(unsigned char* base, uint32_t off, i
     }
 }
 
-// a vector of C values of type DT (FX_F32 or the rows' own) by channel; `absent` where there is none, zeros from C on
-__device__ __forceinline__ void load_vector(const void* p, int is_f32, int dt, int col, int C, float absent, float (&v)[kPiece]) {
+// a vector of C values, FX_F32 or of the rows' type, by channel; `absent` where there is none
+template <int DT, int KIND>
+__device__ __forceinline__ void load_vector(const void* p, int is_f32, int col, int C, float absent, float (&v)[kPiece]) {
+    const unsigned char* b = reinterpret_cast<const unsigned char*>(p);
 #pragma unroll
-    for (int e = 0; e < kPiece; ++e) {
-        v[e] = col + e < C ? absent : 0.f;
-        if (p && col + e < C) {
-            if (is_f32) v[e] = reinterpret_cast<const float*>(p)[col + e];
-            else if (dt == FX_F16) v[e] = Elem<_Float16>::to_float(reinterpret_cast<const uint16_t*>(p)[col + e]);
-            else v[e] = Elem<__bf16>::to_float(reinterpret_cast<const uint16_t*>(p)[col + e]);
-        }
-    }
+    for (int e = 0; e < kPiece; ++e) v[e] = absent;
+    if (p && is_f32) unpack<FX_F32>(load_piece<FX_F32, KIND>(b, 0, col, C), v);
+    else if (p) unpack<DT>(load_piece<DT, KIND>(b, 0, col, C), v);
 }
 
 template <int CTRL>

@@ -326,8 +326,8 @@ __device__ __forceinline__ void scan_tile(const ScanArgs& a, ScanLds& s, int sla
     Piece<DT, kQuad> gate[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-        gate[i] = load_piece<DT, KIND, kQuad, false>(tr.base(a.gate, a.ld_gate, i), tr.offset(a.ld_gate, i), col, a.C);
-        in[i] = load_piece<DT, KIND, kQuad, false>(tr.base(in_rows, ld_in, i), tr.offset(ld_in, i), col, a.C);
+        gate[i] = load_piece<DT, KIND, kQuad>(tr.base(a.gate, a.ld_gate, i), tr.offset(a.ld_gate, i), col, a.C);
+        in[i] = load_piece<DT, KIND, kQuad>(tr.base(in_rows, ld_in, i), tr.offset(ld_in, i), col, a.C);
         __builtin_amdgcn_sched_barrier(0);      // in turn: the first rows are worked on while the last are on their way
     }
     // of the first sequence that begins in the lane's rows and the first that ends, asked for along with the rows
@@ -367,10 +367,10 @@ __device__ __forceinline__ void scan_tile(const ScanArgs& a, ScanLds& s, int sla
         const int64_t more = tile0 + tr.count < a.rows ? a.ld_h : 0;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            px[i] = load_piece<DT, KIND, kQuad, false>(tr.base(a.x, a.ld_x, i), tr.offset(a.ld_x, i), col, a.C);
+            px[i] = load_piece<DT, KIND, kQuad>(tr.base(a.x, a.ld_x, i), tr.offset(a.ld_x, i), col, a.C);
             const bool last = tr.lane + i >= tr.count - 1;
-            if (i + 1 < R && FULL) pp[i] = load_piece<DT, KIND, kQuad, false>(tr.base(a.h, a.ld_h, i + 1), tr.offset(a.ld_h, i + 1), col, a.C);
-            else pp[i] = load_piece<DT, KIND, kQuad, false>(tr.base(a.h, a.ld_h, i) + (last ? (UP ? more : -more) : UP ? a.ld_h : -a.ld_h), tr.offset(a.ld_h, i), col, a.C);
+            if (i + 1 < R && FULL) pp[i] = load_piece<DT, KIND, kQuad>(tr.base(a.h, a.ld_h, i + 1), tr.offset(a.ld_h, i + 1), col, a.C);
+            else pp[i] = load_piece<DT, KIND, kQuad>(tr.base(a.h, a.ld_h, i) + (last ? (UP ? more : -more) : UP ? a.ld_h : -a.ld_h), tr.offset(a.ld_h, i), col, a.C);
         }
     }
     // Runs of all lanes up to this one.  Where a sequence begins in a lane's rows, what stands before them is left out:
