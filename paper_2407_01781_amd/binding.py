@@ -146,8 +146,14 @@ def _check(status: int):
         raise FxError(status, lib.fx_last_error().decode())
 
 
+# the current stream's handle without the Stream object around it (2.8 us a call, of some 10 for a small operator)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device())
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -526,7 +532,7 @@ class Sequences:
 
     def __del__(self):
         h = getattr(self, "_h", None)
-        if h is not None and h.value:
+        if h is not None and h.value and lib is not None:        # None when the interpreter ends
             lib.fx_sequences_destroy(h)
             self._h = None
 
@@ -541,28 +547,51 @@ def build_sequences(joffsets) -> Sequences:
     return Sequences(h.value, jo.shape[0], rows)
 
 
-def _rows(t: torch.Tensor, shape, dtype, name: str) -> torch.Tensor:
-    """A tensor of rows: any row stride, channels next to each other."""
-    assert t.is_cuda and t.dtype == dtype and t.shape == shape, f"{name}: {tuple(shape)} {dtype} on the GPU expected"
-    assert t.stride(1) == 1 or t.shape[1] <= 1 or t.numel() == 0, f"{name}: the channels of a row have to lie next to each other"
-    return t
+def _rows(t: torch.Tensor, like: torch.Tensor, name: str) -> int:
+    """The address of a tensor of rows, of the shape and dtype of `like`: any row stride, channels next to each other."""
+    if t.dtype != like.dtype or t.shape != like.shape or not t.is_cuda:
+        raise AssertionError(f"{name}: {tuple(like.shape)} {like.dtype} on the GPU expected")
+    if t.stride(1) != 1 and t.shape[1] > 1 and t.numel():
+        raise AssertionError(f"{name}: the channels of a row have to lie next to each other")
+    return t.data_ptr()
+
+
+def _opt_rows(t: Optional[torch.Tensor], like: torch.Tensor, name: str):
+    return None if t is None else _rows(t, like, name)
 
 
 def _ld(t: Optional[torch.Tensor]) -> int:
     # the stride of a single row says nothing; rows of a broadcast tensor (stride 0) are refused by the library
-    return 0 if t is None else t.stride(0) if t.shape[0] > 1 and t.numel() else max(t.shape[1], 1)
+    if t is None:
+        return 0
+    return t.stride(0) if t.shape[0] > 1 and t.shape[1] else max(t.shape[1], 1)
 
 
-def _states(t: Optional[torch.Tensor], shape, name: str) -> Optional[torch.Tensor]:
-    assert t is None or (t.is_cuda and t.dtype == torch.float32 and t.shape == shape and t.is_contiguous()), \
+def _new_rows(like: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(like, memory_format=torch.contiguous_format)
+
+
+def _out_rows(out: Optional[torch.Tensor], like: torch.Tensor) -> torch.Tensor:
+    if out is None:
+        return _new_rows(like)
+    _rows(out, like, "out")
+    return out
+
+
+def _states(t: Optional[torch.Tensor], shape, name: str):
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == torch.float32 and t.shape == shape and t.is_contiguous(), \
         f"{name}: contiguous float32 {tuple(shape)} on the GPU expected"
-    return t
+    return t.data_ptr()
 
 
-def _vector(t: Optional[torch.Tensor], c: int, dtype, name: str) -> Optional[torch.Tensor]:
-    assert t is None or (t.is_cuda and t.shape == (c,) and t.is_contiguous() and t.dtype in (dtype, torch.float32)), \
-        f"{name}: contiguous ({c},) of {dtype} or float32 on the GPU expected"
-    return t
+def _vector(t: Optional[torch.Tensor], like: torch.Tensor, name: str):
+    if t is None:
+        return None
+    assert t.is_cuda and t.shape == like.shape[1:] and t.is_contiguous() and t.dtype in (like.dtype, torch.float32), \
+        f"{name}: contiguous ({like.shape[1]},) of {like.dtype} or float32 on the GPU expected"
+    return t.data_ptr()
 
 
 def gated_scan_fwd(seqs: Sequences, x: torch.Tensor, gate: torch.Tensor, h0: Optional[torch.Tensor] = None, reverse: bool = False,
@@ -571,13 +600,13 @@ def gated_scan_fwd(seqs: Sequences, x: torch.Tensor, gate: torch.Tensor, h0: Opt
     `reverse`; x, gate [rows, C], h0 [B, C] float32 (zeros without).  Returns h [rows, C] and the states [B, C] float32
     behind the last rows."""
     assert x.dim() == 2 and x.dtype in _TORCH_DT and x.shape[0] == seqs.rows
-    _rows(x, x.shape, x.dtype, "x"), _rows(gate, x.shape, x.dtype, "gate")
+    xp, gp = _rows(x, x, "x"), _rows(gate, x, "gate")
     states = (seqs.batch_size, x.shape[1])
-    _states(h0, states, "h0")
-    h = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _rows(out, x.shape, x.dtype, "out")
+    h0p = _states(h0, states, "h0")
+    h = _out_rows(out, x)
     last = torch.empty(states, dtype=torch.float32, device=x.device)
-    _check(lib.fx_gated_scan_fwd(seqs._h, _ptr(x), _ld(x), _ptr(gate), _ld(gate), _TORCH_DT[x.dtype], x.shape[1], int(reverse),
-                                 _ptr(h0), _ptr(h), _ld(h), _ptr(last), _stream()))
+    _check(lib.fx_gated_scan_fwd(seqs._h, xp, _ld(x), gp, _ld(gate), _TORCH_DT[x.dtype], x.shape[1], int(reverse), h0p, h.data_ptr(),
+                                 _ld(h), last.data_ptr(), _stream()))
     return h, last
 
 
@@ -587,16 +616,13 @@ def gated_scan_bwd(seqs: Sequences, x: torch.Tensor, gate: torch.Tensor, h: torc
     """Gradients of gated_scan_fwd's x, gate [rows, C] and h0 [B, C]; h is its output, grad_last the gradient of its
     second output (zeros without)."""
     assert x.dim() == 2 and x.dtype in _TORCH_DT and x.shape[0] == seqs.rows
-    for t, name in ((x, "x"), (gate, "gate"), (h, "h"), (grad_h, "grad_h")):
-        _rows(t, x.shape, x.dtype, name)
+    xp, gp, hp, ghp = _rows(x, x, "x"), _rows(gate, x, "gate"), _rows(h, x, "h"), _rows(grad_h, x, "grad_h")
     states = (seqs.batch_size, x.shape[1])
-    _states(h0, states, "h0"), _states(grad_last, states, "grad_last")
-    gx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    ggate = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    h0p, glp = _states(h0, states, "h0"), _states(grad_last, states, "grad_last")
+    gx, ggate = _new_rows(x), _new_rows(x)
     gh0 = torch.empty(states, dtype=torch.float32, device=x.device)
-    _check(lib.fx_gated_scan_bwd(seqs._h, _ptr(x), _ld(x), _ptr(gate), _ld(gate), _ptr(h), _ld(h), _ptr(grad_h), _ld(grad_h),
-                                 _TORCH_DT[x.dtype], x.shape[1], int(reverse), _ptr(h0), _ptr(grad_last), _ptr(gx), _ld(gx),
-                                 _ptr(ggate), _ld(ggate), _ptr(gh0), _stream()))
+    _check(lib.fx_gated_scan_bwd(seqs._h, xp, _ld(x), gp, _ld(gate), hp, _ld(h), ghp, _ld(grad_h), _TORCH_DT[x.dtype], x.shape[1],
+                                 int(reverse), h0p, glp, gx.data_ptr(), _ld(gx), ggate.data_ptr(), _ld(ggate), gh0.data_ptr(), _stream()))
     return gx, ggate, gh0
 
 
@@ -605,13 +631,13 @@ def gated_scan_step(x: torch.Tensor, gate: torch.Tensor, state: torch.Tensor,
     """The next row of each of x.shape[0] running sequences: h [n, C] and the states behind it [n, C] float32
     (new_state may be `state`)."""
     assert x.dim() == 2 and x.dtype in _TORCH_DT
-    _rows(x, x.shape, x.dtype, "x"), _rows(gate, x.shape, x.dtype, "gate")
-    _states(state, x.shape, "state"), _states(new_state, x.shape, "new_state")
-    h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    xp, gp = _rows(x, x, "x"), _rows(gate, x, "gate")
+    sp = _states(state, x.shape, "state")
+    h = _new_rows(x)
     if new_state is None:
-        new_state = torch.empty(x.shape, dtype=torch.float32, device=x.device)
-    _check(lib.fx_gated_scan_step(_ptr(x), _ld(x), _ptr(gate), _ld(gate), _TORCH_DT[x.dtype], x.shape[0], x.shape[1], _ptr(state),
-                                  _ptr(new_state), _ptr(h), _ld(h), _stream()))
+        new_state = torch.empty_like(state)
+    _check(lib.fx_gated_scan_step(xp, _ld(x), gp, _ld(gate), _TORCH_DT[x.dtype], x.shape[0], x.shape[1], sp,
+                                  _states(new_state, x.shape, "new_state"), h.data_ptr(), _ld(h), _stream()))
     return h, new_state
 
 
@@ -619,10 +645,10 @@ def rms_norm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: fl
                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x / sqrt(mean over the channels of x^2 + eps) * weight; x [rows, C], weight [C] of x's dtype or float32."""
     assert x.dim() == 2 and x.dtype in _TORCH_DT
-    _rows(x, x.shape, x.dtype, "x"), _vector(weight, x.shape[1], x.dtype, "weight")
-    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _rows(out, x.shape, x.dtype, "out")
-    _check(lib.fx_rms_norm_fwd(_ptr(x), _ld(x), _TORCH_DT[x.dtype], x.shape[0], x.shape[1], _ptr(weight),
-                               0 if weight is None else _TORCH_DT[weight.dtype], eps, _ptr(out), _ld(out), _stream()))
+    xp, wp = _rows(x, x, "x"), _vector(weight, x, "weight")
+    out = _out_rows(out, x)
+    _check(lib.fx_rms_norm_fwd(xp, _ld(x), _TORCH_DT[x.dtype], x.shape[0], x.shape[1], wp, 0 if weight is None else _TORCH_DT[weight.dtype],
+                               eps, out.data_ptr(), _ld(out), _stream()))
     return out
 
 
@@ -630,35 +656,34 @@ def rms_norm_bwd(grad_out: torch.Tensor, x: torch.Tensor, weight: Optional[torch
                  eps: float = 1e-6) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """Gradients of rms_norm_fwd's x and weight (None without one)."""
     assert x.dim() == 2 and x.dtype in _TORCH_DT
-    _rows(x, x.shape, x.dtype, "x"), _rows(grad_out, x.shape, x.dtype, "grad_out"), _vector(weight, x.shape[1], x.dtype, "weight")
-    gx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    xp, gp, wp = _rows(x, x, "x"), _rows(grad_out, x, "grad_out"), _vector(weight, x, "weight")
+    gx = _new_rows(x)
     gw = None if weight is None else torch.empty_like(weight)
-    _check(lib.fx_rms_norm_bwd(_ptr(grad_out), _ld(grad_out), _ptr(x), _ld(x), _TORCH_DT[x.dtype], x.shape[0], x.shape[1], _ptr(weight),
-                               0 if weight is None else _TORCH_DT[weight.dtype], eps, _ptr(gx), _ld(gx), _ptr(gw), _stream()))
+    _check(lib.fx_rms_norm_bwd(gp, _ld(grad_out), xp, _ld(x), _TORCH_DT[x.dtype], x.shape[0], x.shape[1], wp,
+                               0 if weight is None else _TORCH_DT[weight.dtype], eps, gx.data_ptr(), _ld(gx),
+                               None if gw is None else gw.data_ptr(), _stream()))
     return gx, gw
 
 
 _GATES = {"sigmoid": 0, "silu": 1}
 
 
+def _offset(t: Optional[torch.Tensor]):
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == torch.int64 and t.numel() == 1, "d_offset: one int64 on the GPU"
+    return t.data_ptr()
+
+
 def _block(y, gate, act, post_weight, scale, next_weight, eps, p, seed, offset, d_offset) -> _BlockJoin:
     assert y.dim() == 2 and y.dtype in _TORCH_DT
-    _rows(y, y.shape, y.dtype, "y")
-    if gate is not None:
-        _rows(gate, y.shape, y.dtype, "gate")
-    vectors = [_vector(v, y.shape[1], y.dtype, n) for v, n in ((post_weight, "post_weight"), (scale, "scale"), (next_weight, "next_weight"))]
-    kinds = {v.dtype for v in vectors if v is not None}
-    assert len(kinds) <= 1, "post_weight, scale and next_weight have one dtype"
-    return _BlockJoin(rows=y.shape[0], C=y.shape[1], dt=_TORCH_DT[y.dtype], vec_dt=_TORCH_DT[kinds.pop()] if kinds else 0,
-                      act=_GATES[act], d_y=y.data_ptr(), d_gate=None if gate is None else gate.data_ptr(), ld_y=_ld(y), ld_gate=_ld(gate),
-                      d_post=None if post_weight is None else post_weight.data_ptr(), d_scale=None if scale is None else scale.data_ptr(),
-                      d_next=None if next_weight is None else next_weight.data_ptr(), d_offset=_offset(d_offset),
-                      seed=seed, offset=offset, p=p, eps=eps)
-
-
-def _offset(t: Optional[torch.Tensor]):
-    assert t is None or (t.is_cuda and t.dtype == torch.int64 and t.numel() == 1), "d_offset: one int64 on the GPU"
-    return None if t is None else t.data_ptr()
+    some = post_weight if post_weight is not None else scale if scale is not None else next_weight
+    vec = torch.float32 if some is None else some.dtype
+    assert all(v is None or v.dtype == vec for v in (scale, next_weight)), "post_weight, scale and next_weight have one dtype"
+    # in the order of the members
+    return _BlockJoin(y.shape[0], y.shape[1], _TORCH_DT[y.dtype], _TORCH_DT[vec], _GATES[act], _rows(y, y, "y"),
+                      _opt_rows(gate, y, "gate"), _ld(y), _ld(gate), _vector(post_weight, y, "post_weight"), _vector(scale, y, "scale"),
+                      _vector(next_weight, y, "next_weight"), _offset(d_offset), seed, offset, p, eps)
 
 
 def block_join_fwd(x: torch.Tensor, y: torch.Tensor, gate: Optional[torch.Tensor] = None, act: str = "silu",
@@ -669,10 +694,10 @@ def block_join_fwd(x: torch.Tensor, y: torch.Tensor, gate: Optional[torch.Tensor
     """x + scale * drop(rms_norm(y; post_weight) * act(gate)), and that sum's rms_norm by next_weight (None without one).
     Rows [n, C] of one dtype, vectors [C] of that dtype or float32; drop is dropout's mask of (seed, offset)."""
     b = _block(y, gate, act, post_weight, scale, next_weight, eps, p, seed, offset, d_offset)
-    _rows(x, y.shape, y.dtype, "x")
-    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _rows(out, x.shape, x.dtype, "out")
-    norm = None if next_weight is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _check(lib.fx_block_join_fwd(C.byref(b), _ptr(x), _ld(x), _ptr(out), _ld(out), _ptr(norm), _ld(norm), _stream()))
+    xp = _rows(x, y, "x")
+    out = _out_rows(out, x)
+    norm = None if next_weight is None else _new_rows(x)
+    _check(lib.fx_block_join_fwd(b, xp, _ld(x), out.data_ptr(), _ld(out), None if norm is None else norm.data_ptr(), _ld(norm), _stream()))
     return out, norm
 
 
@@ -684,15 +709,15 @@ def block_join_bwd(grad_out: Optional[torch.Tensor], grad_norm: Optional[torch.T
     grad_out and grad_norm are the gradients of its two outputs (one may be None), `out` its first output (needed with
     grad_norm)."""
     b = _block(y, gate, act, post_weight, scale, next_weight, eps, p, seed, offset, d_offset)
+    ins = []
     for t, name in ((grad_out, "grad_out"), (grad_norm, "grad_norm"), (out, "out")):
-        if t is not None:
-            _rows(t, y.shape, y.dtype, name)
-    rows = lambda t: None if t is None else torch.empty(y.shape, dtype=y.dtype, device=y.device)
+        ins += (_opt_rows(t, y, name), _ld(t))
+    rows = lambda t: None if t is None else _new_rows(y)
     vec = lambda t: None if t is None else torch.empty_like(t)
-    g = {"x": rows(y), "y": rows(y), "gate": rows(gate), "post": vec(post_weight), "scale": vec(scale), "next": vec(next_weight)}
-    _check(lib.fx_block_join_bwd(C.byref(b), _ptr(grad_out), _ld(grad_out), _ptr(grad_norm), _ld(grad_norm), _ptr(out), _ld(out),
-                                 _ptr(g["x"]), _ld(g["x"]), _ptr(g["y"]), _ld(g["y"]), _ptr(g["gate"]), _ld(g["gate"]), _ptr(g["post"]),
-                                 _ptr(g["scale"]), _ptr(g["next"]), _stream()))
+    g = {"x": _new_rows(y), "y": _new_rows(y), "gate": rows(gate), "post": vec(post_weight), "scale": vec(scale), "next": vec(next_weight)}
+    ptr = [None if t is None else t.data_ptr() for t in g.values()]
+    ld = max(y.shape[1], 1)
+    _check(lib.fx_block_join_bwd(b, *ins, ptr[0], ld, ptr[1], ld, ptr[2], ld, *ptr[3:], _stream()))
     return g
 
 
@@ -702,10 +727,8 @@ def dropout(x: torch.Tensor, p: float, seed: int, offset: int, residual: Optiona
     is one.  The mask depends on (seed, offset, row, channel) alone and is never stored; the gradient of x is the same
     call on the output's gradient.  Take another offset for every call that wants a mask of its own."""
     assert x.dim() == 2 and x.dtype in _TORCH_DT
-    _rows(x, x.shape, x.dtype, "x")
-    if residual is not None:
-        _rows(residual, x.shape, x.dtype, "residual")
-    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _rows(out, x.shape, x.dtype, "out")
-    _check(lib.fx_dropout(_ptr(x), _ld(x), _TORCH_DT[x.dtype], x.shape[0], x.shape[1], p, seed, offset, _offset(d_offset),
-                          _ptr(residual), _ld(residual), _ptr(out), _ld(out), _stream()))
+    xp, rp = _rows(x, x, "x"), _opt_rows(residual, x, "residual")
+    out = _out_rows(out, x)
+    _check(lib.fx_dropout(xp, _ld(x), _TORCH_DT[x.dtype], x.shape[0], x.shape[1], p, seed, offset, _offset(d_offset), rp, _ld(residual),
+                          out.data_ptr(), _ld(out), _stream()))
     return out
