@@ -42,7 +42,7 @@ namespace fx {
 
 constexpr int kScanThreads = 512;       // most threads of a workgroup
 constexpr int kGroupTiles = 16;         // tiles whose joint (A, H) is published as one
-constexpr int kLookWindow = 16;         // groups looked at together
+constexpr int kLookWindow = 16;         // groups looked back over
 constexpr int kQuad = 4;                // channels of a lane
 
 // Rows of a lane: as many as leave a workgroup's registers (gate, input and, backward, state and x of all its rows) room
@@ -175,7 +175,7 @@ struct RunTable {
 struct ScanLds {
     RunTable wave[kScanThreads / 64];           // of every wave's rows
     RunTable tiles[kGroupTiles / 4];            // of four tiles each of the group, before this one
-    RunTable groups[kLookWindow / 4];           // of four groups each, backwards
+    RunTable groups[kLookWindow];               // of the groups before this one, backwards
     float before[kScanThreads / 64][64];        // value before every wave's rows
     int ticket;
 };
@@ -194,10 +194,10 @@ __device__ __forceinline__ uint64_t look(const uint64_t* at) { return __hip_atom
 __device__ __forceinline__ bool is_there(uint64_t w) { return (uint32_t)(w >> 32) != kNothing; }
 __device__ __forceinline__ Run run_in(uint64_t w) { return Run{__uint_as_float((uint32_t)(w >> 32)), __uint_as_float((uint32_t)w)}; }
 
-// The joint run of up to four words, 64 words from one to the next, waiting for those that are not there yet.  BACK: the
-// words lie one before the other.  A word that does not come within the bound counts as NaN.
+// Up to four words, 64 words from one to the next, waiting for those that are not there yet.  BACK: the words lie one
+// before the other.  A word that does not come within the bound counts as NaN.
 template <bool BACK>
-__device__ __forceinline__ Run gather_runs(const uint64_t* at, int n) {
+__device__ __forceinline__ void gather_runs(const uint64_t* at, int n, Run (&r)[4]) {
     const int64_t step = BACK ? -64 : 64;
     uint64_t w[4];
 #pragma unroll
@@ -209,13 +209,8 @@ __device__ __forceinline__ Run gather_runs(const uint64_t* at, int n) {
         for (int k = 0; k < 4; ++k)
             if (!is_there(w[k])) w[k] = look(at + step * k);
     }
-    Run run{1.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const Run r = is_there(w[k]) ? run_in(w[k]) : Run{-1.f, __uint_as_float(0x7FC00000u)};
-        if (k < n) run = BACK ? then(r, run) : then(run, r);
-    }
-    return run;
+    for (int k = 0; k < 4; ++k) r[k] = is_there(w[k]) ? run_in(w[k]) : Run{-1.f, __uint_as_float(0x7FC00000u)};
 }
 
 // Publishes the tile's run and, from the last tile of a group, the group's, and leaves the value before every wave's rows
@@ -240,51 +235,64 @@ __device__ __forceinline__ void look_back(const ScanArgs& a, ScanLds& s, int sla
     const int n_tiles = asks || closes ? in_group : 0, t_words = (n_tiles + 3) / 4;
 #pragma unroll 1
     for (int k = wave; k < t_words; k += waves)
-        if (here) s.tiles[k].put(lane, gather_runs<false>(tiles + 4 * k * 64, min(4, n_tiles - 4 * k)));
+        if (here) {
+            const int n = min(4, n_tiles - 4 * k);
+            Run r[4], run{1.f, 0.f};
+            gather_runs<false>(tiles + 4 * k * 64, n, r);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < n) run = then(run, r[i]);
+            s.tiles[k].put(lane, run);
+        }
     if (closes) {
         __syncthreads();
         if (first) {
 #pragma unroll 1
-            for (int k = 0; 4 * k < n_tiles; ++k) before = then(before, s.tiles[k].get(lane));
+            for (int k = 0; k < t_words; ++k) before = then(before, s.tiles[k].get(lane));
             publish(groups + group * 64, then(before, mine));
         }
     }
-    float v = 0.f;                                  // before the first tile: never used, a sequence begins there
+    float v = 0.f, reach = 0.f;                     // before the tile, and before its group; of the first tile never used
     if (asks) {
-        // backwards over the groups until the value behind one of them is known for every channel
-        Run back{1.f, 0.f};
-        int end = group, turn = closes ? 0 : t_words;       // waves that wait for a tile are not the first to wait for a group
+        // The value behind the nearest group that knows it, through the groups after that one, one at a time: a group
+        // that publishes what is behind it has come to the same bits, so it does not matter which one is found.
+        const int n = min(group, kLookWindow), turn = closes ? 0 : t_words;     // waves that wait for a tile are not the first to wait for a group
 #pragma unroll 1
-        for (;;) {
-            const int n = min(end, kLookWindow);
+        for (int polls = 0;; ++polls) {
 #pragma unroll 1
             for (int k = (wave + waves - turn % waves) % waves; 4 * k < n; k += waves)
-                if (here) s.groups[k].put(lane, gather_runs<true>(groups + (int64_t)(end - 1 - 4 * k) * 64, min(4, n - 4 * k)));
+                if (here) {
+                    Run r[4];
+                    gather_runs<true>(groups + (int64_t)(group - 1 - 4 * k) * 64, min(4, n - 4 * k), r);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (4 * k + i < n) s.groups[4 * k + i].put(lane, r[i]);
+                }
             __syncthreads();
-            if (here) {
-#pragma unroll 1
-                for (int k = 0; 4 * k < n; ++k) back = then(s.groups[k].get(lane), back);
-            }
-            end -= n;
-            turn = 0;
-            if (end == 0 || __all(!here || back.A < 0.f)) break;        // the same in every wave: each holds all channels
+            bool known = n == 0 || !here || polls == kMostPolls;
+#pragma unroll 4
+            for (int k = 0; k < n; ++k) known = known || s.groups[k].A[lane] < 0.f;
+            if (__all(known)) break;                // the same in every wave: each looks at all channels
             __syncthreads();
         }
         if (first) {
+            if (n) reach = __uint_as_float(0x7FC00000u);        // from groups behind which nothing is known
+#pragma unroll 4
+            for (int k = n - 1; k >= 0; --k) reach = through(s.groups[k].get(lane), reach);
             if (!closes) {
 #pragma unroll 1
-                for (int k = 0; 4 * k < n_tiles; ++k) before = then(before, s.tiles[k].get(lane));
+                for (int k = 0; k < t_words; ++k) before = then(before, s.tiles[k].get(lane));
             }
-            v = through(before, back.H);
+            v = through(before, reach);
         }
     }
+    if (closes && first) publish(groups + group * 64, Run{-1.f, through(then(before, mine), reach)});
     if (first) {
 #pragma unroll 1
         for (int w = 0; w < waves; ++w) {
             s.before[w][lane] = v;
             v = through(s.wave[w].get(lane), v);
         }
-        if (closes) publish(groups + group * 64, Run{-1.f, v});
     }
     __syncthreads();
 }
@@ -311,7 +319,10 @@ template <int DT, int KIND, bool UP, bool BWD, bool FULL>
 __device__ __forceinline__ void scan_tile(const ScanArgs& a, ScanLds& s, int slab, int tile, int64_t tile0, int rows_a_tile) {
     constexpr int R = ScanRows<DT, BWD>::n;
     const int t = threadIdx.x, wave = t >> 6, lane = t & 63, lanes = 1 << a.lanes_log2;
-    const int c4 = (lane & (lanes - 1)) * kQuad, col = slab * 64 + c4;
+    // The last lane of a row whose channels are not a multiple of four takes the last four: some of them a second time,
+    // with the same bits, and so do the lanes that are left over, which store nothing.
+    const int c4 = (lane & (lanes - 1)) * kQuad, col = KIND == kRowsNarrow ? c4 : min(slab * 64 + c4, a.C - kQuad);
+    const bool stores = slab * 64 + c4 < a.C;
     TileRows<UP, R, FULL> tr;
     tr.count = FULL ? rows_a_tile : (int)min((int64_t)rows_a_tile, a.rows - tile0);
     tr.lowest = UP ? tile0 : a.rows - tile0 - tr.count;
@@ -420,8 +431,8 @@ __device__ __forceinline__ void scan_tile(const ScanArgs& a, ScanLds& s, int sla
             float h[kQuad];
 #pragma unroll
             for (int e = 0; e < kQuad; ++e) h[e] = gates[i][e] * v[e] + held[i][e];
-            store_piece<DT, KIND>(tr.base(a.out, a.ld_out, i), tr.offset(a.ld_out, i), col, a.C, pack<DT>(h));
-            if (ends && a.last) store_states<KIND>(a.last, sequence_of<UP>(a, lr, i), col, a.C, h);
+            if (stores) store_piece<DT, KIND>(tr.base(a.out, a.ld_out, i), tr.offset(a.ld_out, i), col, a.C, pack<DT>(h));
+            if (ends && a.last && stores) store_states<KIND>(a.last, sequence_of<UP>(a, lr, i), col, a.C, h);
         } else {
             if (begins) {
                 if (lr.begin & (lr.begin - 1)) load_states<KIND>(a.first, sequence_of<UP>(a, lr, i), col, a.C, start);
@@ -446,9 +457,11 @@ __device__ __forceinline__ void scan_tile(const ScanArgs& a, ScanLds& s, int sla
                 gz[e] = lam * (p[e] - x[e]) * (f * g);
                 v[e] = f * lam;
             }
-            store_piece<DT, KIND>(tr.base(a.gx, a.ld_gx, i), tr.offset(a.ld_gx, i), col, a.C, pack<DT>(gx));
-            store_piece<DT, KIND>(tr.base(a.ggate, a.ld_ggate, i), tr.offset(a.ld_ggate, i), col, a.C, pack<DT>(gz));
-            if (ends && a.last) store_states<KIND>(a.last, sequence_of<UP>(a, lr, i), col, a.C, v);
+            if (stores) {
+                store_piece<DT, KIND>(tr.base(a.gx, a.ld_gx, i), tr.offset(a.ld_gx, i), col, a.C, pack<DT>(gx));
+                store_piece<DT, KIND>(tr.base(a.ggate, a.ld_ggate, i), tr.offset(a.ld_ggate, i), col, a.C, pack<DT>(gz));
+            }
+            if (ends && a.last && stores) store_states<KIND>(a.last, sequence_of<UP>(a, lr, i), col, a.C, v);
         }
         __builtin_amdgcn_sched_barrier(0);
     }
@@ -542,17 +555,22 @@ static int64_t most_ld(const ScanArgs& a) {
 
 template <int DT, int KIND, bool UP, bool BWD>
 static fx_status launch_scan(ScanArgs& a, hipStream_t st) {
-    // As many threads as leave every compute unit two tiles, from a wave on.  Backward at most 256: at its registers a
-    // compute unit holds three such workgroups, or one of 512 (986,880 x 64 bf16: 212 us, 230 us); forward two of 512,
-    // whose tiles, twice as long, have half as many others to wait for (132 us; of 256 150 us).
+    // Threads of a workgroup: one tile for everything if that can be, else at least 16 tiles if that can be, else as many
+    // as there are.  Backward at most 256: at its registers a compute unit holds three such workgroups, or one of 512
+    // (986,880 x 64 bf16: 212 us, 230 us); forward two of 512, whose tiles, twice as long, have half as many others to
+    // wait for (132 us; of 256 150 us).  Fewer and longer tiles from there on down: 10,000 x 64 bf16 in 10 tiles a 1/16
+    // of the compute units 12.7 us, in two a unit 17.1 us.
     int threads = BWD ? kScanThreads / 2 : kScanThreads;
     int64_t rows_a_tile, tiles;
+    const int64_t ld = most_ld(a);
     for (;; threads /= 2) {
         rows_a_tile = (int64_t)(threads >> a.lanes_log2) * ScanRows<DT, BWD>::n;
         tiles = (a.rows + rows_a_tile - 1) / rows_a_tile;
-        if (threads == 64 || (tiles * a.slabs >= 2 * compute_units() && rows_a_tile * most_ld(a) < kMostOffset)) break;
+        if (threads == 64) break;
+        if (rows_a_tile * ld >= kMostOffset) continue;
+        if (tiles == 1 ? 2 * a.rows > rows_a_tile : tiles * a.slabs * 16 >= compute_units()) break;
     }
-    if (rows_a_tile * most_ld(a) >= kMostOffset) { set_error("gated scan: rows lie more than %lld bytes apart", (long long)(kMostOffset / rows_a_tile)); return FX_ERANGE; }
+    if (rows_a_tile * ld >= kMostOffset) { set_error("gated scan: rows lie more than %lld bytes apart", (long long)(kMostOffset / rows_a_tile)); return FX_ERANGE; }
     if (tiles * a.slabs > 0x3FFFFFFF) { set_error("gated scan: too many tiles for one launch"); return FX_ERANGE; }
     a.tiles = (int)tiles;
     a.groups = (int)((tiles + kGroupTiles - 1) / kGroupTiles);
@@ -576,12 +594,8 @@ static fx_status launch_scan(ScanArgs& a, hipStream_t st) {
 
 template <int DT, bool BWD>
 static fx_status launch_scan_kind(ScanArgs& a, bool up, hipStream_t st) {
-    const int kind = a.C < kQuad ? kRowsNarrow : a.C % kQuad ? kRowsRagged : kRowsWhole;
-#define FX_SCAN(KIND) return up ? launch_scan<DT, KIND, true, BWD>(a, st) : launch_scan<DT, KIND, false, BWD>(a, st)
-    if (kind == kRowsWhole) FX_SCAN(kRowsWhole);
-    if (kind == kRowsRagged) FX_SCAN(kRowsRagged);
-    FX_SCAN(kRowsNarrow);
-#undef FX_SCAN
+    if (a.C >= kQuad) return up ? launch_scan<DT, kRowsWhole, true, BWD>(a, st) : launch_scan<DT, kRowsWhole, false, BWD>(a, st);
+    return up ? launch_scan<DT, kRowsNarrow, true, BWD>(a, st) : launch_scan<DT, kRowsNarrow, false, BWD>(a, st);
 }
 
 template <bool BWD>
