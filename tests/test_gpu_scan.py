@@ -207,6 +207,20 @@ def test_on_another_stream():
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+def test_the_same_bits_from_every_call():
+    """Many tiles in flight, so that what a tile finds of those before it is never the same twice."""
+    n, c = 300_000, 64
+    seqs = fx.build_sequences([[0, n]])
+    x, _ = _draw(91, n, c, "bf16")
+    z, _ = _draw(92, n, c, "bf16", mean=4.0)
+    h, last = fx.gated_scan_fwd(seqs, x, z)
+    g = fx.gated_scan_bwd(seqs, x, z, h, x)
+    for _ in range(10):
+        again = fx.gated_scan_fwd(seqs, x, z)
+        assert torch.equal(again[0], h) and torch.equal(again[1], last)
+        assert all(torch.equal(a, b) for a, b in zip(fx.gated_scan_bwd(seqs, x, z, h, x), g))
+
+
 def test_sequences_of_a_grid():
     """Every grid of a batch is one sequence of its voxels in index order."""
     from workloads import generators as G
