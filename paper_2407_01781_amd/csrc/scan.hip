@@ -228,7 +228,7 @@ __device__ __forceinline__ void look_back(const ScanArgs& a, ScanLds& s, int sla
     uint64_t* groups = a.group_runs + (int64_t)slab * a.groups * 64 + lane;
     Run mine{1.f, 0.f}, before{1.f, 0.f};           // of the tile; of the group's tiles before it
     if (first && linked) {
-#pragma unroll 1
+#pragma unroll 4
         for (int w = 0; w < waves; ++w) mine = then(mine, s.wave[w].get(lane));
         if (!closes) publish(tiles + in_group * 64, mine);
     }
@@ -247,7 +247,7 @@ __device__ __forceinline__ void look_back(const ScanArgs& a, ScanLds& s, int sla
     if (closes) {
         __syncthreads();
         if (first) {
-#pragma unroll 1
+#pragma unroll 4
             for (int k = 0; k < t_words; ++k) before = then(before, s.tiles[k].get(lane));
             publish(groups + group * 64, then(before, mine));
         }
@@ -280,7 +280,7 @@ __device__ __forceinline__ void look_back(const ScanArgs& a, ScanLds& s, int sla
 #pragma unroll 4
             for (int k = n - 1; k >= 0; --k) reach = through(s.groups[k].get(lane), reach);
             if (!closes) {
-#pragma unroll 1
+#pragma unroll 4
                 for (int k = 0; k < t_words; ++k) before = then(before, s.tiles[k].get(lane));
             }
             v = through(before, reach);
@@ -288,7 +288,7 @@ __device__ __forceinline__ void look_back(const ScanArgs& a, ScanLds& s, int sla
     }
     if (closes && first) publish(groups + group * 64, Run{-1.f, through(then(before, mine), reach)});
     if (first) {
-#pragma unroll 1
+#pragma unroll 4
         for (int w = 0; w < waves; ++w) {
             s.before[w][lane] = v;
             v = through(s.wave[w].get(lane), v);
@@ -344,7 +344,11 @@ __device__ __forceinline__ void scan_tile(const ScanArgs& a, ScanLds& s, int sla
     // of the first sequence that begins in the lane's rows and the first that ends, asked for along with the rows
     float start[kQuad], state0[kQuad];
     if (lr.begin) load_states<KIND>(a.first, sequence_of<UP>(a, lr, __ffs(lr.begin) - 1), col, a.C, start);
-    if (BWD && lr.stop) load_states<KIND>(a.h0, sequence_of<UP>(a, lr, __ffs(lr.stop) - 1), col, a.C, state0);
+    int stopped = 0;
+    if (lr.stop) {
+        stopped = sequence_of<UP>(a, lr, __ffs(lr.stop) - 1);
+        if (BWD) load_states<KIND>(a.h0, stopped, col, a.C, state0);
+    }
     Runs mine = no_runs();                      // of this lane's rows
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -432,7 +436,7 @@ __device__ __forceinline__ void scan_tile(const ScanArgs& a, ScanLds& s, int sla
 #pragma unroll
             for (int e = 0; e < kQuad; ++e) h[e] = gates[i][e] * v[e] + held[i][e];
             if (stores) store_piece<DT, KIND>(tr.base(a.out, a.ld_out, i), tr.offset(a.ld_out, i), col, a.C, pack<DT>(h));
-            if (ends && a.last && stores) store_states<KIND>(a.last, sequence_of<UP>(a, lr, i), col, a.C, h);
+            if (ends && a.last && stores) store_states<KIND>(a.last, lr.stop & ((1u << i) - 1) ? sequence_of<UP>(a, lr, i) : stopped, col, a.C, h);
         } else {
             if (begins) {
                 if (lr.begin & (lr.begin - 1)) load_states<KIND>(a.first, sequence_of<UP>(a, lr, i), col, a.C, start);
@@ -461,7 +465,7 @@ __device__ __forceinline__ void scan_tile(const ScanArgs& a, ScanLds& s, int sla
                 store_piece<DT, KIND>(tr.base(a.gx, a.ld_gx, i), tr.offset(a.ld_gx, i), col, a.C, pack<DT>(gx));
                 store_piece<DT, KIND>(tr.base(a.ggate, a.ld_ggate, i), tr.offset(a.ld_ggate, i), col, a.C, pack<DT>(gz));
             }
-            if (ends && a.last && stores) store_states<KIND>(a.last, sequence_of<UP>(a, lr, i), col, a.C, v);
+            if (ends && a.last && stores) store_states<KIND>(a.last, lr.stop & ((1u << i) - 1) ? sequence_of<UP>(a, lr, i) : stopped, col, a.C, v);
         }
         __builtin_amdgcn_sched_barrier(0);
     }
