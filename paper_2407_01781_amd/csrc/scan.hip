@@ -20,6 +20,13 @@
 // before it for the value that its first row starts from, and finishes its rows.  Tiles are taken in scan order by
 // ticket, so whatever a workgroup waits for belongs to a workgroup that already runs, and that one waits for earlier
 // tiles only.
+//
+// Measured (986,880 x 64 bf16, one sequence: 379 MB, 74 us at a copy's rate): 128 us, 2.95 TB/s; in three launches (the
+// tiles' runs, what stands before each, the rows: 632 MB) 168 us.  Where every tile begins a sequence of its own and
+// nobody waits, 93 us: the look back costs the rest.  What bounds it are a workgroup's phases one after the other (ticket,
+// rows, run, look back, store: 17 us a tile) with two workgroups a compute unit, all that its registers hold; vector
+// instructions fill 40 % of the time, the tickets (11.6 ns each at one address) take 45 us of all in turn.  Gradients of
+// 1,068,658 x 64 f16 in four sequences (821 MB, 161 us): 226 us, 3.6 TB/s, bound the same way.
 #include "rows.h"
 
 #include <mutex>
@@ -45,8 +52,10 @@ constexpr int kGroupTiles = 16;         // tiles whose joint (A, H) is published
 constexpr int kLookWindow = 16;         // groups looked back over
 constexpr int kQuad = 4;                // channels of a lane
 
-// Rows of a lane: as many as leave a workgroup's registers (gate, input and, backward, state and x of all its rows) room
-// for a second one on the compute unit.
+// Rows of a lane.  Forward, 8 rows of 4 channels hold 64 numbers between the passes and the kernel 128 registers, the
+// most with which two workgroups of 512 share a compute unit (16 rows: 197, one workgroup of 256 fewer, 129 us where no
+// tile waits against 93; 4 rows: twice the tiles to wait for).  Backward, gate, input, state and x of 8 rows of a 16-bit
+// type hold 80 and the kernel 158; of 4 rows it is 5 % slower where tiles wait.
 template <int DT, bool BWD> struct ScanRows { static constexpr int n = 8 / (BWD && DT == FX_F32 ? 2 : 1); };
 
 struct ScanArgs {
@@ -297,6 +306,7 @@ __device__ __forceinline__ void look_back(const ScanArgs& a, ScanLds& s, int sla
     __syncthreads();
 }
 
+// Nobody has said anything yet: 2 MB for the 986,880 rows above, 3 us.
 __global__ void __launch_bounds__(256) k_scan_clear(uint64_t* words, int64_t n, uint32_t* ticket) {
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) words[i] = ~0ull;
     if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
@@ -487,7 +497,7 @@ k_scan(ScanArgs a) {
     else scan_tile<DT, KIND, UP, BWD, false>(a, s, slab, tile, tile0, rows_a_tile);
 }
 
-// states of sequences without rows pass through
+// states of sequences without rows pass through (3 to 5 us, only where there are any)
 __global__ void k_scan_empty(const int32_t* __restrict__ empty, int n, int C, const float* __restrict__ first, float* __restrict__ last) {
     const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (i >= (int64_t)n * C) return;
@@ -495,7 +505,8 @@ __global__ void k_scan_empty(const int32_t* __restrict__ empty, int n, int C, co
     last[at] = first ? first[at] : 0.f;
 }
 
-// One row of each of many running sequences: h = f state + (1 - f) x, the state kept in fp32.
+// One row of each of many running sequences: h = f state + (1 - f) x, the state kept in fp32.  A thread is a piece of 8
+// channels; bound by the launch at the sizes of a step (8 x 256: 3.2 us, of 10 us a call), by memory beyond.
 template <int DT, int KIND>
 __global__ void __launch_bounds__(256)
 k_scan_step(int64_t rows, int C, int pieces, const unsigned char* x, int64_t ld_x, const unsigned char* gate, int64_t ld_gate, const float* state,
