@@ -12,6 +12,9 @@ SOURCES = ["conv_wgrad_bf16.hip", "conv_wgrad_f16.hip", "conv.hip", "conv_bwd.hi
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument"]
+# Sources whose kernels must not spill registers: their rows sit in registers across divergent branches, and a spill in
+# such a branch has been stored for the branch's lanes only (wrong gradients at 3 channels).
+NO_SCRATCH = {"scan.hip", "block.hip"}
 
 
 def _newest_source_mtime() -> float:
@@ -36,6 +39,8 @@ def build(force: bool = True, verbose: bool = False) -> str:
     def compile_one(src):
         obj = os.path.join(objdir, src.replace(".hip", ".o"))
         cmd = [hipcc] + compile_flags + ["-c", os.path.join(CSRC, src), "-o", obj]
+        if src in NO_SCRATCH:
+            cmd.append("-Rpass-analysis=kernel-resource-usage")
         if verbose:
             print(" ".join(cmd))
         return obj, subprocess.run(cmd, capture_output=True, text=True)
@@ -43,8 +48,14 @@ def build(force: bool = True, verbose: bool = False) -> str:
     with ThreadPoolExecutor(min(8, len(SOURCES))) as ex:
         results = list(ex.map(compile_one, SOURCES))
     errs = []
-    for obj, res in results:
-        err = "\n".join(l for l in res.stderr.splitlines() if "packed-fp32-ops" not in l)
+    for src, (obj, res) in zip(SOURCES, results):
+        lines = [l for l in res.stderr.splitlines() if "packed-fp32-ops" not in l]
+        if src in NO_SCRATCH and res.returncode == 0:
+            spills = [l for l in lines if "ScratchSize [bytes/lane]:" in l and not l.split("ScratchSize [bytes/lane]:")[1].strip().startswith("0")]
+            if spills:
+                raise RuntimeError(f"{src}: a kernel spills registers\n" + "\n".join(spills))
+            lines = []
+        err = "\n".join(lines)
         if res.returncode != 0:
             raise RuntimeError("hipcc failed:\n" + err)
         if err.strip():

@@ -23,10 +23,10 @@
 //
 // Measured (986,880 x 64 bf16, one sequence: 379 MB, 74 us at a copy's rate): 128 us, 2.95 TB/s; in three launches (the
 // tiles' runs, what stands before each, the rows: 632 MB) 168 us.  Where every tile begins a sequence of its own and
-// nobody waits, 93 us: the look back costs the rest.  What bounds it are a workgroup's phases one after the other (ticket,
+// nobody waits, 93 us (gradients 157): the look back costs the rest.  What bounds it are a workgroup's phases one after the other (ticket,
 // rows, run, look back, store: 17 us a tile) with two workgroups a compute unit, all that its registers hold; vector
 // instructions fill 40 % of the time, the tickets (11.6 ns each at one address) take 45 us of all in turn.  Gradients of
-// 1,068,658 x 64 f16 in four sequences (821 MB, 161 us): 226 us, 3.6 TB/s, bound the same way.
+// 1,068,658 x 64 f16 in four sequences (821 MB, 161 us): 208 us, 3.9 TB/s.
 #include "rows.h"
 
 #include <mutex>
@@ -52,10 +52,11 @@ constexpr int kGroupTiles = 16;         // tiles whose joint (A, H) is published
 constexpr int kLookWindow = 16;         // groups looked back over
 constexpr int kQuad = 4;                // channels of a lane
 
-// Rows of a lane.  Forward, 8 rows of 4 channels hold 64 numbers between the passes and the kernel 128 registers, the
-// most with which two workgroups of 512 share a compute unit (16 rows: 197, one workgroup of 256 fewer, 129 us where no
-// tile waits against 93; 4 rows: twice the tiles to wait for).  Backward, gate, input, state and x of 8 rows of a 16-bit
-// type hold 80 and the kernel 158; of 4 rows it is 5 % slower where tiles wait.
+// Rows of a lane, such that the kernel has 128 registers at most: two workgroups of 512 then share a compute unit.
+// Forward, 8 rows of 4 channels hold 64 numbers between the passes (16 rows: 197 registers; the gates and inputs held as
+// loaded and worked on twice, 16 rows: 136 us where 8 as they are take 133; 4 rows: twice the tiles to wait for).  Backward,
+// gate and gradient of 8 rows of a 16-bit type hold 48; state and x are asked for behind the look back (asked for before
+// it they hold 32 more: 158 registers, 212 us at 986,880 x 64 bf16 for 193).
 template <int DT, bool BWD> struct ScanRows { static constexpr int n = 8 / (BWD && DT == FX_F32 ? 2 : 1); };
 
 struct ScanArgs {
@@ -186,6 +187,7 @@ struct ScanLds {
     RunTable tiles[kGroupTiles / 4];            // of four tiles each of the group, before this one
     RunTable groups[kLookWindow];               // of the groups before this one, backwards
     float before[kScanThreads / 64][64];        // value before every wave's rows
+    f32x4 own_A[kScanThreads], own_H[kScanThreads];     // of the lanes before a lane in its wave: kept here while a tile waits, the registers are needed
     int ticket;
 };
 
@@ -386,18 +388,6 @@ __device__ __forceinline__ void scan_tile(const ScanArgs& a, ScanLds& s, int sla
         }
         __builtin_amdgcn_sched_barrier(0);      // a row after the other: all rows' numbers at once do not fit the registers
     }
-    if (BWD) {
-        // The rows run against the sequence: the state before a row lies at the row that comes next here.  Behind the
-        // last row of all there is none (and none is asked for): the row itself in its place.
-        const int64_t more = tile0 + tr.count < a.rows ? a.ld_h : 0;
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            px[i] = load_piece<DT, KIND, kQuad>(tr.base(a.x, a.ld_x, i), tr.offset(a.ld_x, i), col, a.C);
-            const bool last = tr.lane + i >= tr.count - 1;
-            if (i + 1 < R && FULL) pp[i] = load_piece<DT, KIND, kQuad>(tr.base(a.h, a.ld_h, i + 1), tr.offset(a.ld_h, i + 1), col, a.C);
-            else pp[i] = load_piece<DT, KIND, kQuad>(tr.base(a.h, a.ld_h, i) + (last ? (UP ? more : -more) : UP ? a.ld_h : -a.ld_h), tr.offset(a.ld_h, i), col, a.C);
-        }
-    }
     // Runs of all lanes up to this one.  Where a sequence begins in a lane's rows, what stands before them is left out:
     // a bit a lane says so for all of its channels.
     uint64_t cut = __ballot(lr.begin != 0);
@@ -424,15 +414,29 @@ __device__ __forceinline__ void scan_tile(const ScanArgs& a, ScanLds& s, int sla
         mine.A[e] = lane < lanes ? 1.f : oA;
         mine.H[e] = lane < lanes ? 0.f : oH;
     }
+    s.own_A[t] = f32x4{mine.A[0], mine.A[1], mine.A[2], mine.A[3]};
+    s.own_H[t] = f32x4{mine.H[0], mine.H[1], mine.H[2], mine.H[3]};
     __syncthreads();
     look_back<UP>(a, s, slab, tile, tile0);
+    if (BWD) {
+        // The rows run against the sequence: the state before a row lies at the row that comes next here.  Behind the
+        // last row of all there is none (and none is asked for): the row itself in its place.
+        const int64_t more = tile0 + tr.count < a.rows ? a.ld_h : 0;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            px[i] = load_piece<DT, KIND, kQuad>(tr.base(a.x, a.ld_x, i), tr.offset(a.ld_x, i), col, a.C);
+            const bool last = tr.lane + i >= tr.count - 1;
+            if (i + 1 < R && FULL) pp[i] = load_piece<DT, KIND, kQuad>(tr.base(a.h, a.ld_h, i + 1), tr.offset(a.ld_h, i + 1), col, a.C);
+            else pp[i] = load_piece<DT, KIND, kQuad>(tr.base(a.h, a.ld_h, i) + (last ? (UP ? more : -more) : UP ? a.ld_h : -a.ld_h), tr.offset(a.ld_h, i), col, a.C);
+        }
+    }
     float v[kQuad];
     {
         const f32x4 b = *reinterpret_cast<const f32x4*>(&s.before[wave][c4]);
 #pragma unroll
         for (int e = 0; e < kQuad; ++e) v[e] = b[e];
     }
-    pass_through(mine, v);
+    pass_through(Runs{{s.own_A[t][0], s.own_A[t][1], s.own_A[t][2], s.own_A[t][3]}, {s.own_H[t][0], s.own_H[t][1], s.own_H[t][2], s.own_H[t][3]}}, v);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         if (!FULL && i >= lr.n) continue;
@@ -482,7 +486,9 @@ __device__ __forceinline__ void scan_tile(const ScanArgs& a, ScanLds& s, int sla
 }
 
 template <int DT, int KIND, bool UP, bool BWD>
-__global__ void __launch_bounds__(kScanThreads, BWD ? 3 : 4)
+// No register may be spilled here (the build refuses it): the compiler has stored one under the lanes of a branch that all
+// lanes had taken it through.  Rows of fewer than four channels, whose pieces are loaded by tests, get more of them.
+__global__ void __launch_bounds__(kScanThreads, KIND == kRowsNarrow && BWD ? 3 : 4)
 k_scan(ScanArgs a) {
     __shared__ ScanLds s;
     int turn = blockIdx.x;
@@ -571,11 +577,9 @@ static int64_t most_ld(const ScanArgs& a) {
 template <int DT, int KIND, bool UP, bool BWD>
 static fx_status launch_scan(ScanArgs& a, hipStream_t st) {
     // Threads of a workgroup: one tile for everything if that can be, else at least 16 tiles if that can be, else as many
-    // as there are.  Backward at most 256: at its registers a compute unit holds three such workgroups, or one of 512
-    // (986,880 x 64 bf16: 212 us, 230 us); forward two of 512, whose tiles, twice as long, have half as many others to
-    // wait for (132 us; of 256 150 us).  Fewer and longer tiles from there on down: 10,000 x 64 bf16 in 10 tiles a 1/16
-    // of the compute units 12.7 us, in two a unit 17.1 us.
-    int threads = BWD ? kScanThreads / 2 : kScanThreads;
+    // as there are.  Fewer and longer tiles have fewer others to wait for (986,880 x 64 bf16, 512 threads 133 us, 256 150 us;
+    // 10,000 x 64 in 10 tiles a 1/16 of the compute units 12.7 us, in two a unit 17.1 us).
+    int threads = kScanThreads;
     int64_t rows_a_tile, tiles;
     const int64_t ld = most_ld(a);
     for (;; threads /= 2) {
