@@ -475,6 +475,8 @@ void fx_sequences_destroy(fx_sequences* q);
  *   d_h          device [rows, C], dtype dt; must not be d_x or d_gate (FX_EINVAL) nor overlap them
  *   d_last       device [B, C] fp32, or NULL: the unrounded state behind every sequence's last row; h0 (or zeros) for a
  *                sequence without rows.  Fed as h0 to the rows that come later, it continues the recurrence.
+ * Rows up to 4 MiB apart are always served; FX_ERANGE where the rows that one workgroup takes would reach over 2 GiB, and
+ * beyond 2^24 channels.
  * 1 - f is computed as sigmoid(-gate), to its own precision where f is near 1.  An infinity or NaN stays in its
  * sequence and channel; a sequence's rows do not depend on any other's.
  * Backward, with gh = dL/dh and glast = dL/dlast (fp32 [B, C], NULL for zeros): d_h is what the forward call wrote

@@ -70,7 +70,8 @@ struct ScanArgs {
     float* last;                        // [B, C] values behind the last
     const float* h0;                    // backward: the states before the sequences' first rows
     const uint64_t* begin;
-    const int32_t *rank, *id;
+    const int32_t *rank, *id, *empty;
+    int32_t n_empty;
     // what workgroups tell each other, where there is more than one tile: kNothing until it is written
     uint64_t* tile_runs;                // [slabs][tiles][64] (A, H) of every tile
     uint64_t* group_runs;               // [slabs][groups][64] (A, H) of every group, then the value behind it as (-1, H)
@@ -308,10 +309,18 @@ __device__ __forceinline__ void look_back(const ScanArgs& a, ScanLds& s, int sla
     __syncthreads();
 }
 
-// Nobody has said anything yet: 2 MB for the 986,880 rows above, 3 us.
-__global__ void __launch_bounds__(256) k_scan_clear(uint64_t* words, int64_t n, uint32_t* ticket) {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) words[i] = ~0ull;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
+// Before the tiles: nobody has said anything yet (2 MB of words for the 986,880 rows above, 3 us), and the states of
+// sequences without rows pass through.
+__global__ void __launch_bounds__(256)
+k_scan_prepare(uint64_t* words, int64_t n, uint32_t* ticket, const int32_t* __restrict__ empty, int n_empty, int C, const float* __restrict__ first,
+               float* __restrict__ last) {
+    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+    for (int64_t i = t; i < n; i += step) words[i] = ~0ull;
+    if (n && t == 0) *ticket = 0;
+    for (int64_t i = t; i < (int64_t)n_empty * C; i += step) {
+        const int64_t at = (int64_t)empty[i / C] * C + i % C;
+        last[at] = first ? first[at] : 0.f;
+    }
 }
 
 // The smaller of a row's two sigmoids, its sign saying which: what a lane keeps of a gate between the two passes over
@@ -503,14 +512,6 @@ k_scan(ScanArgs a) {
     else scan_tile<DT, KIND, UP, BWD, false>(a, s, slab, tile, tile0, rows_a_tile);
 }
 
-// states of sequences without rows pass through (3 to 5 us, only where there are any)
-__global__ void k_scan_empty(const int32_t* __restrict__ empty, int n, int C, const float* __restrict__ first, float* __restrict__ last) {
-    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i >= (int64_t)n * C) return;
-    const int64_t at = (int64_t)empty[i / C] * C + i % C;
-    last[at] = first ? first[at] : 0.f;
-}
-
 // One row of each of many running sequences: h = f state + (1 - f) x, the state kept in fp32.  A thread is a piece of 8
 // channels; bound by the launch at the sizes of a step (8 x 256: 3.2 us, of 10 us a call), by memory beyond.
 template <int DT, int KIND>
@@ -548,11 +549,14 @@ static fx_status check_rows_of(const char* who, const char* name, const void* p,
     return FX_OK;
 }
 
+constexpr int32_t kMostChannels = 1 << 24;      // a row's bytes and a tile's rows meet in 32 bits
+
 static fx_status check_scan(const char* who, const fx_sequences* q, int32_t C, fx_dtype dt) {
     if (!q || C < 1 || (dt != FX_F32 && dt != FX_F16 && dt != FX_BF16)) {
         set_error("%s: null sequences, no channels or unknown dtype", who);
         return FX_EINVAL;
     }
+    if (C > kMostChannels) { set_error("%s: more than %d channels", who, kMostChannels); return FX_ERANGE; }
     return FX_OK;
 }
 
@@ -566,12 +570,20 @@ static void scan_args(ScanArgs* a, const fx_sequences* q, int32_t C) {
     a->begin = q->d_begin;
     a->rank = q->d_rank;
     a->id = q->d_id;
+    a->empty = q->d_empty;
+    a->n_empty = q->n_empty;
 }
 
 constexpr int64_t kMostOffset = 1ll << 31;      // bytes from a tile's first row to its last
 
 static int64_t most_ld(const ScanArgs& a) {
     return std::max({a.ld_x, a.ld_gate, a.ld_h, a.ld_gh, a.ld_out, a.ld_gx, a.ld_ggate});
+}
+
+static void launch_prepare(const ScanArgs& a, int64_t words, hipStream_t st) {
+    const int64_t states = a.last ? (int64_t)a.n_empty * a.C : 0;
+    k_scan_prepare<<<(unsigned)std::min<int64_t>((std::max(words, states) + 255) / 256, 1024), 256, 0, st>>>(
+        a.tile_runs, words, a.ticket, a.empty, a.last ? a.n_empty : 0, a.C, a.first, a.last);
 }
 
 template <int DT, int KIND, bool UP, bool BWD>
@@ -595,13 +607,14 @@ static fx_status launch_scan(ScanArgs& a, hipStream_t st) {
     a.groups = (int)((tiles + kGroupTiles - 1) / kGroupTiles);
     void* work = nullptr;
     unsigned nb = (unsigned)a.slabs;
+    if (tiles <= 1 && a.last && a.n_empty) launch_prepare(a, 0, st);
     if (tiles > 1) {
         const int64_t words = (int64_t)a.slabs * 64 * (a.tiles + a.groups);
         FX_TRY(dev_alloc(&work, (size_t)words * 8 + 256, st));
         a.tile_runs = (uint64_t*)work;
         a.group_runs = a.tile_runs + (int64_t)a.slabs * 64 * a.tiles;
         a.ticket = (uint32_t*)(a.tile_runs + words);
-        k_scan_clear<<<(unsigned)std::min<int64_t>((words + 255) / 256, 1024), 256, 0, st>>>(a.tile_runs, words, a.ticket);
+        launch_prepare(a, words, st);
         nb = (unsigned)(tiles * a.slabs);
     }
     k_scan<DT, KIND, UP, BWD><<<nb, threads, 0, st>>>(a);
@@ -618,13 +631,13 @@ static fx_status launch_scan_kind(ScanArgs& a, bool up, hipStream_t st) {
 }
 
 template <bool BWD>
-static fx_status run_scan(const fx_sequences* q, ScanArgs& a, fx_dtype dt, bool up, hipStream_t st) {
+static fx_status run_scan(ScanArgs& a, fx_dtype dt, bool up, hipStream_t st) {
     ProfScope ps(BWD ? kProfScanBwd : kProfScanFwd, st);
-    if (a.last && q->n_empty) {
-        k_scan_empty<<<(unsigned)(((int64_t)q->n_empty * a.C + 255) / 256), 256, 0, st>>>(q->d_empty, q->n_empty, a.C, a.first, a.last);
+    if (a.rows == 0) {
+        if (a.last && a.n_empty) launch_prepare(a, 0, st);
         FX_HIP_TRY(hipGetLastError());
+        return FX_OK;
     }
-    if (a.rows == 0) return FX_OK;
     if (dt == FX_F32) return launch_scan_kind<FX_F32, BWD>(a, up, st);
     if (dt == FX_F16) return launch_scan_kind<FX_F16, BWD>(a, up, st);
     return launch_scan_kind<FX_BF16, BWD>(a, up, st);
@@ -711,7 +724,7 @@ extern "C" fx_status fx_gated_scan_fwd(const fx_sequences* q, const void* d_x, i
     a.out = (unsigned char*)d_h; a.ld_out = ld_h * es;
     a.first = d_h0;
     a.last = d_last;
-    return run_scan<false>(q, a, dt, !reverse, (hipStream_t)stream);
+    return run_scan<false>(a, dt, !reverse, (hipStream_t)stream);
 }
 
 extern "C" fx_status fx_gated_scan_bwd(const fx_sequences* q, const void* d_x, int64_t ld_x, const void* d_gate, int64_t ld_gate, const void* d_h,
@@ -741,7 +754,7 @@ extern "C" fx_status fx_gated_scan_bwd(const fx_sequences* q, const void* d_x, i
     a.h0 = d_h0;
     a.first = d_glast;
     a.last = d_gh0;
-    return run_scan<true>(q, a, dt, reverse != 0, (hipStream_t)stream);
+    return run_scan<true>(a, dt, reverse != 0, (hipStream_t)stream);
 }
 
 extern "C" fx_status fx_gated_scan_step(const void* d_x, int64_t ld_x, const void* d_gate, int64_t ld_gate, fx_dtype dt, int64_t rows, int32_t C,
@@ -751,6 +764,7 @@ extern "C" fx_status fx_gated_scan_step(const void* d_x, int64_t ld_x, const voi
         set_error("%s: negative rows, no channels, unknown dtype or null state", who);
         return FX_EINVAL;
     }
+    if (C > kMostChannels) { set_error("%s: more than %d channels", who, kMostChannels); return FX_ERANGE; }
     FX_TRY(check_rows_of(who, "d_x", d_x, ld_x, rows, C, dt));
     FX_TRY(check_rows_of(who, "d_gate", d_gate, ld_gate, rows, C, dt));
     FX_TRY(check_rows_of(who, "d_h", d_h, ld_h, rows, C, dt));

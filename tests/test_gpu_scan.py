@@ -259,5 +259,9 @@ def test_refusals():
         fx.gated_scan_fwd(seqs, x, x.half())
     with pytest.raises(AssertionError):
         fx.gated_scan_fwd(seqs, x, x.clone(), h0=torch.zeros((2, 8), device="cuda"))
+    far = torch.empty(9 * (1 << 26) + 32, dtype=torch.int8, device="cuda").view(torch.float32).as_strided((10, 8), (1 << 24, 1))      # 64 MiB apart
+    with pytest.raises(fx.FxError) as e:
+        fx.gated_scan_fwd(seqs, far, x)
+    assert e.value.status == -5
     # and the call works after the refusals
     assert torch.equal(fx.gated_scan_fwd(seqs, x, x.clone())[0], x)

@@ -40,6 +40,7 @@ def test_scan():
     _refused(-1, "fx_gated_scan_fwd", None, P, 8, P, 8, 0, 8, 0, None, P, 8, None, None)
     _refused(-1, "fx_gated_scan_bwd", None, P, 8, P, 8, P, 8, P, 8, 0, 8, 0, None, None, P, 8, P, 8, None, None)
     step = lambda x=P, ld=8, dt=0, rows=2, c=8, s=P, n=P, h=P: ("fx_gated_scan_step", x, ld, P, 8, dt, rows, c, s, n, h, 8, None)
+    _refused(-5, *step(ld=1 << 25, c=(1 << 24) + 1))
     for bad in (step(x=None), step(x=ODD), step(ld=7), step(dt=3), step(rows=-1), step(c=0), step(s=None), step(n=None), step(h=None)):
         _refused(-1, *bad)
 
