@@ -228,14 +228,13 @@ __device__ __forceinline__ void gather_runs(const uint64_t* at, int n, Run (&r)[
 // Publishes the tile's run and, from the last tile of a group, the group's, and leaves the value before every wave's rows
 // in s.before; a lane is a channel here, and all but the waiting for others' words is done by the first wave.  All
 // threads take part; ends with a barrier.
-template <bool UP>
-__device__ __forceinline__ void look_back(const ScanArgs& a, ScanLds& s, int slab, int tile, int64_t tile0) {
+__device__ __forceinline__ void look_back(const ScanArgs& a, ScanLds& s, int slab, int tile, int begins) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
     const int group = tile / kGroupTiles, in_group = tile % kGroupTiles;
     const bool here = lane < kQuad << a.lanes_log2, first = wave == 0 && here;
     const bool linked = a.tile_runs != nullptr, closes = linked && in_group == kGroupTiles - 1;
     // a tile that a sequence begins with asks nobody
-    const bool asks = linked && !__builtin_amdgcn_readfirstlane((int)begins_at<UP>(a, tile0));
+    const bool asks = linked && !__builtin_amdgcn_readfirstlane(begins);
     uint64_t* tiles = a.tile_runs + ((int64_t)slab * a.tiles + (tile - in_group)) * 64 + lane;
     uint64_t* groups = a.group_runs + (int64_t)slab * a.groups * 64 + lane;
     Run mine{1.f, 0.f}, before{1.f, 0.f};           // of the tile; of the group's tiles before it
@@ -349,6 +348,7 @@ __device__ __forceinline__ void scan_tile(const ScanArgs& a, ScanLds& s, int sla
     tr.lowest = UP ? tile0 : a.rows - tile0 - tr.count;
     tr.lane = (t >> a.lanes_log2) * R;
     const LaneRows lr = lane_rows<UP, R>(a, tile0 + tr.lane);
+    const int begins = begins_at<UP>(a, tile0);     // asked for here: in front of the tile's word to the others it would hold all of them up
     const unsigned char* in_rows = BWD ? a.gh : a.x;
     const int64_t ld_in = BWD ? a.ld_gh : a.ld_x;
     // One number or two of every value are held between the passes over the rows: forward, the state that the lane's own
@@ -426,7 +426,7 @@ __device__ __forceinline__ void scan_tile(const ScanArgs& a, ScanLds& s, int sla
     s.own_A[t] = f32x4{mine.A[0], mine.A[1], mine.A[2], mine.A[3]};
     s.own_H[t] = f32x4{mine.H[0], mine.H[1], mine.H[2], mine.H[3]};
     __syncthreads();
-    look_back<UP>(a, s, slab, tile, tile0);
+    look_back(a, s, slab, tile, begins);
     if (BWD) {
         // The rows run against the sequence: the state before a row lies at the row that comes next here.  Behind the
         // last row of all there is none (and none is asked for): the row itself in its place.
