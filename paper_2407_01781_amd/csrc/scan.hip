@@ -21,12 +21,12 @@
 // ticket, so whatever a workgroup waits for belongs to a workgroup that already runs, and that one waits for earlier
 // tiles only.
 //
-// Measured (986,880 x 64 bf16, one sequence: 379 MB, 74 us at a copy's rate): 128 us, 2.95 TB/s; in three launches (the
+// Measured (986,880 x 64 bf16, one sequence: 379 MB, 74 us at a copy's rate): 127 us, 2.98 TB/s; in three launches (the
 // tiles' runs, what stands before each, the rows: 632 MB) 168 us.  Where every tile begins a sequence of its own and
 // nobody waits, 93 us (gradients 157): the look back costs the rest.  What bounds it are a workgroup's phases one after the other (ticket,
 // rows, run, look back, store: 17 us a tile) with two workgroups a compute unit, all that its registers hold; vector
 // instructions fill 40 % of the time, the tickets (11.6 ns each at one address) take 45 us of all in turn.  Gradients of
-// 1,068,658 x 64 f16 in four sequences (821 MB, 161 us): 208 us, 3.9 TB/s.
+// 1,068,658 x 64 f16 in four sequences (821 MB, 161 us): 207 us, 4.0 TB/s.
 #include "rows.h"
 
 #include <mutex>
@@ -48,7 +48,7 @@ struct fx_sequences {
 namespace fx {
 
 constexpr int kScanThreads = 512;       // most threads of a workgroup
-constexpr int kGroupTiles = 16;         // tiles whose joint (A, H) is published as one
+constexpr int kGroupTiles = 16;         // tiles whose joint (A, H) is published as one (8: 4 % slower at 986,880 x 64 bf16; 32, 64: +- 3 %)
 constexpr int kLookWindow = 16;         // groups looked back over
 constexpr int kQuad = 4;                // channels of a lane
 
