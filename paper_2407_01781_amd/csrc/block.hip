@@ -130,8 +130,10 @@ k_block_fwd(BlockArgs a) {
                 for (int e = 0; e < kPiece; ++e) v[e] = drop_value(w, e, a.drop, v[e]);
             }
             if (MODE == kModeJoin) {
+                // A lane without channels holds the gate and weights of the row's last piece under a mask of its own: its
+                // zeros times an infinite gate, which that piece may have dropped, must not enter the sum of the next norm.
 #pragma unroll
-                for (int e = 0; e < kPiece; ++e) v[e] *= ws[e];
+                for (int e = 0; e < kPiece; ++e) v[e] = kept(v[e] * ws[e], mask);
             }
             if (a.x) {
                 float x[kPiece];

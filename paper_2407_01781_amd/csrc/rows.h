@@ -83,6 +83,9 @@ __device__ __forceinline__ Piece<DT, N> masked(Piece<DT, N> p, uint32_t mask) {
     return p;
 }
 
+// v under a mask of all bits, zero under none, whatever v is: no product with a zero does that to an infinity or NaN
+__device__ __forceinline__ float kept(float v, uint32_t mask) { return __uint_as_float(__float_as_uint(v) & mask); }
+
 template <int DT, int N>
 __device__ __forceinline__ void unpack(const Piece<DT, N>& p, float (&v)[N]) {
 #pragma unroll
