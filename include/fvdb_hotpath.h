@@ -511,7 +511,10 @@ fx_status fx_rms_norm_bwd(const void* d_gout, int64_t ld_gout, const void* d_x, 
  * drop out.  The second norm is taken of out before its rounding.  d_out may be d_x or d_y with the same stride.
  * Backward: d_out is what the forward call wrote and is read only with d_gnorm; one of d_gout and d_gnorm may be NULL
  * (FX_EINVAL for both); any gradient may be NULL (not computed), and one of an absent input has to be.  gx is the
- * gradient of out through both outputs; d_gx may be d_gout, d_gy may be d_y, d_ggate may be d_gate. */
+ * gradient of out through both outputs; d_gx may be d_gout, d_gy may be d_y, d_ggate may be d_gate.
+ * What drop drops is selected out, forward and backward: an infinity or NaN of y or the gate leaves nothing there, in out
+ * and norm, in the vectors' gradients (0 added) and in ggate (0).  Under post, y enters its row's norm all the same: in a
+ * row with infinities r is 0 but where they lie, NaN there, and so is gy; a NaN makes all of the row's r and gy NaN. */
 typedef enum { FX_GATE_SIGMOID = 0, FX_GATE_SILU = 1 } fx_gate_act;
 typedef struct {
     int64_t rows;

@@ -247,11 +247,19 @@ k_block_bwd(BlockArgs a) {
         }
         if (real && a.gx) store_piece<DT, KIND>(a.gx + row * a.ld_gx, 0, col, C, pack<DT>(D));
         if (MODE == kModeJoin) {
+            // What was dropped, and what a lane without channels or a row that does not exist holds, is selected out of the
+            // products: its gate or its norm may be infinite or NaN, and zero times either is not zero.
+            uint32_t keep[kPiece];
+#pragma unroll
+            for (int e = 0; e < kPiece; ++e) keep[e] = m;
             if (a.drop.below) {
                 uint32_t w[4];
                 philox8((uint32_t)lane, (uint32_t)row, offset, a.drop.seed, w);
 #pragma unroll
-                for (int e = 0; e < kPiece; ++e) D[e] = drop_value(w, e, a.drop, D[e]);
+                for (int e = 0; e < kPiece; ++e) {
+                    D[e] = drop_value(w, e, a.drop, D[e]);
+                    keep[e] = drop_keeps(w, e, a.drop.below) ? m : 0u;
+                }
             }
             float f[kPiece], df[kPiece];
 #pragma unroll
@@ -259,19 +267,21 @@ k_block_bwd(BlockArgs a) {
             if (a.gate) {
                 float z[kPiece];
                 unpack<DT>(pg, z);
+#pragma unroll
+                for (int e = 0; e < kPiece; ++e) z[e] = kept(z[e], keep[e]);
                 gate_factors(a.act, z, f, df);
             }
             float dot[1] = {0.f};                // u post yh
 #pragma unroll
             for (int e = 0; e < kPiece; ++e) {
                 y[e] *= ry;                      // yh
-                const float r = y[e] * wp[e];
+                const float yk = kept(y[e], keep[e]), r = kept(yk * wp[e], keep[e]);
                 acc_scale[e] += D[e] * (r * f[e]);
                 const float t = D[e] * ws[e], u = t * f[e];
                 df[e] *= t * r;
-                acc_post[e] += u * y[e];
+                acc_post[e] += u * yk;
                 D[e] = u * wp[e];
-                dot[0] += D[e] * y[e];
+                dot[0] += D[e] * yk;
             }
             if (real && a.ggate) store_piece<DT, KIND>(a.ggate + row * a.ld_ggate, 0, col, C, pack<DT>(df));
             if (a.post) {
