@@ -574,7 +574,7 @@ static void scan_args(ScanArgs* a, const fx_sequences* q, int32_t C) {
     a->n_empty = q->n_empty;
 }
 
-constexpr int64_t kMostOffset = 1ll << 31;      // bytes from a tile's first row to its last
+constexpr int64_t kMostOffset = 1ll << 31;      // bytes of a tile's rows: its last begins a row's distance before that
 
 static int64_t most_ld(const ScanArgs& a) {
     return std::max({a.ld_x, a.ld_gate, a.ld_h, a.ld_gh, a.ld_out, a.ld_gx, a.ld_ggate});
@@ -598,10 +598,10 @@ static fx_status launch_scan(ScanArgs& a, hipStream_t st) {
         rows_a_tile = (int64_t)(threads >> a.lanes_log2) * ScanRows<DT, BWD>::n;
         tiles = (a.rows + rows_a_tile - 1) / rows_a_tile;
         if (threads == 64) break;
-        if (rows_a_tile * ld >= kMostOffset) continue;
+        if (ld > kMostOffset / rows_a_tile) continue;
         if (tiles == 1 ? 2 * a.rows > rows_a_tile : tiles * a.slabs * 16 >= compute_units()) break;
     }
-    if (rows_a_tile * ld >= kMostOffset) { set_error("gated scan: rows lie more than %lld bytes apart", (long long)(kMostOffset / rows_a_tile)); return FX_ERANGE; }
+    if (ld > kMostOffset / rows_a_tile) { set_error("gated scan: rows lie more than %lld bytes apart", (long long)(kMostOffset / rows_a_tile)); return FX_ERANGE; }
     if (tiles * a.slabs > 0x3FFFFFFF) { set_error("gated scan: too many tiles for one launch"); return FX_ERANGE; }
     a.tiles = (int)tiles;
     a.groups = (int)((tiles + kGroupTiles - 1) / kGroupTiles);
