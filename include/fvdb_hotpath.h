@@ -474,7 +474,8 @@ void fx_sequences_destroy(fx_sequences* q);
  *   d_h0         device [B, C] fp32, or NULL for zeros
  *   d_h          device [rows, C], dtype dt; must not be d_x or d_gate (FX_EINVAL) nor overlap them
  *   d_last       device [B, C] fp32, or NULL: the unrounded state behind every sequence's last row; h0 (or zeros) for a
- *                sequence without rows.  Fed as h0 to the rows that come later, it continues the recurrence.
+ *                sequence without rows.  Fed as h0 to the rows that come later, it continues the recurrence; must not
+ *                overlap d_h0 (FX_EINVAL): two tables in turn.
  * Rows up to 4 MiB apart are always served; FX_ERANGE where the rows that one workgroup takes would reach over 2 GiB, and
  * beyond 2^24 channels.
  * 1 - f is computed as sigmoid(-gate), to its own precision where f is near 1.  An infinity or NaN stays in its
@@ -483,8 +484,8 @@ void fx_sequences_destroy(fx_sequences* q);
  * (the states enter the gate's gradient as they were rounded then), d_h0 what it was given.
  *     lambda_t = gh_t + f_(t+1) lambda_(t+1)  (glast in the place of the second term at the last row)
  *     gx_t = (1 - f_t) lambda_t,  ggate_t = lambda_t (h_(t-1) - x_t) f_t (1 - f_t),  gh0 = f_first lambda_first
- *   d_gx, d_ggate [rows, C] dtype dt, neither where an input lies; d_gh0 [B, C] fp32 or NULL (glast or zeros for a
- *   sequence without rows).
+ *   d_gx, d_ggate [rows, C] dtype dt, neither where an input or the other lies; d_gh0 [B, C] fp32 or NULL (glast or zeros
+ *   for a sequence without rows), not overlapping d_glast or d_h0 (FX_EINVAL).
  * Step, for rows that arrive one at a time: rows r of d_x and d_gate are the next rows of `rows` running sequences with
  * states d_state [rows, C] fp32; d_new_state may be d_state. */
 fx_status fx_gated_scan_fwd(const fx_sequences* q, const void* d_x, int64_t ld_x, const void* d_gate, int64_t ld_gate, fx_dtype dt,

@@ -560,6 +560,14 @@ static fx_status check_scan(const char* who, const fx_sequences* q, int32_t C, f
     return FX_OK;
 }
 
+// Do two [rows, C] tables of fp32 share memory?  States are read by the workgroups of other channels (a slab of fewer than
+// four takes the last of the slab before it along) and, backward, after others have written theirs: none may lie where one
+// is written.
+static bool share(const float* p, const float* q, int64_t rows, int32_t C) {
+    const uintptr_t bytes = (uintptr_t)rows * C * sizeof(float), a = (uintptr_t)p, b = (uintptr_t)q;
+    return p && q && (a < b ? b - a : a - b) < bytes;
+}
+
 static void scan_args(ScanArgs* a, const fx_sequences* q, int32_t C) {
     *a = ScanArgs{};
     a->rows = q->rows;
@@ -716,6 +724,7 @@ extern "C" fx_status fx_gated_scan_fwd(const fx_sequences* q, const void* d_x, i
     FX_TRY(check_rows_of(who, "d_gate", d_gate, ld_gate, q->rows, C, dt));
     FX_TRY(check_rows_of(who, "d_h", d_h, ld_h, q->rows, C, dt));
     if (q->rows > 0 && (d_h == d_x || d_h == d_gate)) { set_error("%s: d_h must not be an input", who); return FX_EINVAL; }
+    if (share(d_last, d_h0, q->B, C)) { set_error("%s: d_last must not lie where d_h0 lies", who); return FX_EINVAL; }
     ScanArgs a;
     scan_args(&a, q, C);
     const int es = esize(dt);
@@ -742,6 +751,8 @@ extern "C" fx_status fx_gated_scan_bwd(const fx_sequences* q, const void* d_x, i
     const void* in[4] = {d_x, d_gate, d_h, d_gh};
     for (const void* p : in)
         if (q->rows > 0 && (p == d_gx || p == d_ggate)) { set_error("%s: a gradient must not lie where an input lies", who); return FX_EINVAL; }
+    if (q->rows > 0 && d_gx == d_ggate) { set_error("%s: d_gx and d_ggate are the same", who); return FX_EINVAL; }
+    if (share(d_gh0, d_glast, q->B, C) || share(d_gh0, d_h0, q->B, C)) { set_error("%s: d_gh0 must not lie where d_glast or d_h0 lies", who); return FX_EINVAL; }
     ScanArgs a;
     scan_args(&a, q, C);
     const int es = esize(dt);
