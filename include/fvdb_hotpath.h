@@ -487,7 +487,8 @@ void fx_sequences_destroy(fx_sequences* q);
  *   d_gx, d_ggate [rows, C] dtype dt, neither where an input or the other lies; d_gh0 [B, C] fp32 or NULL (glast or zeros
  *   for a sequence without rows), not overlapping d_glast or d_h0 (FX_EINVAL).
  * Step, for rows that arrive one at a time: rows r of d_x and d_gate are the next rows of `rows` running sequences with
- * states d_state [rows, C] fp32; d_new_state may be d_state. */
+ * states d_state [rows, C] fp32; d_new_state may be d_state and must not overlap it otherwise, d_h must not be d_x or d_gate
+ * (FX_EINVAL) nor overlap them. */
 fx_status fx_gated_scan_fwd(const fx_sequences* q, const void* d_x, int64_t ld_x, const void* d_gate, int64_t ld_gate, fx_dtype dt,
                             int32_t C, int32_t reverse, const float* d_h0, void* d_h, int64_t ld_h, float* d_last, void* stream);
 fx_status fx_gated_scan_bwd(const fx_sequences* q, const void* d_x, int64_t ld_x, const void* d_gate, int64_t ld_gate, const void* d_h,

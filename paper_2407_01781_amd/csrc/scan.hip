@@ -780,6 +780,9 @@ extern "C" fx_status fx_gated_scan_step(const void* d_x, int64_t ld_x, const voi
     FX_TRY(check_rows_of(who, "d_gate", d_gate, ld_gate, rows, C, dt));
     FX_TRY(check_rows_of(who, "d_h", d_h, ld_h, rows, C, dt));
     if (rows == 0) return FX_OK;
+    // A row's last piece, where it is not whole, is read as the row's last eight channels: some are another thread's.
+    if (d_h == d_x || d_h == d_gate) { set_error("%s: d_h must not be an input", who); return FX_EINVAL; }
+    if (d_new_state != d_state && share(d_new_state, d_state, rows, C)) { set_error("%s: d_new_state overlaps d_state and is not d_state", who); return FX_EINVAL; }
     const int pieces = (C + kPiece - 1) / kPiece, es = esize(dt);
     const int64_t blocks = (rows * pieces + 255) / 256;
     if (blocks > 0x7FFFFFFF) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }
