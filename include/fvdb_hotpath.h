@@ -499,7 +499,8 @@ fx_status fx_gated_scan_step(const void* d_x, int64_t ld_x, const void* d_gate, 
 
 /* Norm in front of a block:  out[r,c] = x[r,c] / sqrt(mean_c x[r,c]^2 + eps) * weight[c]   (weight NULL: ones), and its
  * gradients:  gx = (g w - xh mean_c(g w xh)) / sqrt(mean x^2 + eps),  gweight = sum over rows of g xh,  xh the row
- * without its weight.  d_gx or d_gweight may be NULL (not computed); d_out may be d_x, d_gx may be d_gout or d_x.
+ * without its weight.  d_gx or d_gweight may be NULL (not computed); d_out may be d_x, d_gx may be d_gout or d_x, with
+ * the same stride.
  * C up to 4096, rows up to 2^31-1 (FX_ERANGE), here and in the calls below. */
 fx_status fx_rms_norm_fwd(const void* d_x, int64_t ld_x, fx_dtype dt, int64_t rows, int32_t C, const void* d_weight,
                           fx_dtype vec_dt, float eps, void* d_out, int64_t ld_out, void* stream);
@@ -510,10 +511,12 @@ fx_status fx_rms_norm_bwd(const void* d_gout, int64_t ld_gout, const void* d_x, 
 /* A block's output y joined with the residual stream x, in one pass with the norm for the block that follows:
  *     r = rms_norm(y; post),  out = x + scale * drop(r * act(gate)),  norm = rms_norm(out; next)
  * Whatever of post, gate, scale and next is NULL is left out (r = y, act = 1, scale = 1, no second output); p = 0 leaves
- * drop out.  The second norm is taken of out before its rounding.  d_out may be d_x or d_y with the same stride.
+ * drop out.  The second norm is taken of out before its rounding.  d_out may be d_x or d_y with the same stride, not
+ * d_norm (FX_EINVAL).
  * Backward: d_out is what the forward call wrote and is read only with d_gnorm; one of d_gout and d_gnorm may be NULL
  * (FX_EINVAL for both); any gradient may be NULL (not computed), and one of an absent input has to be.  gx is the
- * gradient of out through both outputs; d_gx may be d_gout, d_gy may be d_y, d_ggate may be d_gate.
+ * gradient of out through both outputs; d_gx may be d_gout, d_gy may be d_y, d_ggate may be d_gate, each with the same
+ * stride; no two of them may be the same (FX_EINVAL).
  * What drop drops is selected out, forward and backward: an infinity or NaN of y or the gate leaves nothing there, in out
  * and norm, in the vectors' gradients (0 added) and in ggate (0).  Under post, y enters its row's norm all the same: in a
  * row with infinities r is 0 but where they lie, NaN there, and so is gy; a NaN makes all of the row's r and gy NaN. */

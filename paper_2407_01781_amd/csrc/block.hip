@@ -547,6 +547,7 @@ extern "C" fx_status fx_block_join_fwd(const fx_block_join* b, const void* d_x, 
     FX_TRY(check_tensor(who, "d_out", d_out, ld_out, b->rows, b->C, b->dt, true));
     FX_TRY(check_tensor(who, "d_norm", d_norm, ld_norm, b->rows, b->C, b->dt, b->d_next != nullptr));
     if (d_norm && !b->d_next) { set_error("%s: d_norm without d_next", who); return FX_EINVAL; }
+    if (b->rows > 0 && d_norm == d_out) { set_error("%s: d_out and d_norm are the same", who); return FX_EINVAL; }
     if (b->rows == 0) return FX_OK;
     const int es = esize(b->dt);
     a.x = (const unsigned char*)d_x; a.ld_x = ld_x * es;
@@ -581,6 +582,10 @@ extern "C" fx_status fx_block_join_bwd(const fx_block_join* b, const void* d_gou
     FX_TRY(check_tensor(who, "d_gx", d_gx, ld_gx, rows, C, b->dt, false));
     FX_TRY(check_tensor(who, "d_gy", d_gy, ld_gy, rows, C, b->dt, false));
     FX_TRY(check_tensor(who, "d_ggate", d_ggate, ld_ggate, rows, C, b->dt, false));
+    if (rows > 0 && ((d_gx && (d_gx == d_gy || d_gx == d_ggate)) || (d_gy && d_gy == d_ggate))) {
+        set_error("%s: two of d_gx, d_gy and d_ggate are the same", who);
+        return FX_EINVAL;
+    }
     FX_TRY(check_vector(who, "d_gpost", d_gpost, b->vec_dt));
     FX_TRY(check_vector(who, "d_gscale", d_gscale, b->vec_dt));
     FX_TRY(check_vector(who, "d_gnext", d_gnext, b->vec_dt));

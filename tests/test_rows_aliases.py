@@ -26,3 +26,11 @@ def test_step(c):
     for off in (4, 4 * 5 * c - 4):
         _refused(-1, *_step(n=C.c_void_p(AT[3].value + off), c=c))
         _refused(-1, *_step(n=C.c_void_p(AT[3].value - off), c=c))
+
+
+def test_join():
+    b = B._BlockJoin(rows=3, C=8, dt=0, vec_dt=0, act=1, d_y=AT[0].value, d_gate=AT[1].value, ld_y=8, ld_gate=8, d_next=AT[7].value, eps=1e-6)
+    _refused(-1, "fx_block_join_fwd", C.byref(b), AT[2], 8, AT[3], 8, AT[3], 8, None)
+    bwd = lambda gx, gy, gg: ("fx_block_join_bwd", C.byref(b), AT[2], 8, AT[3], 8, AT[4], 8, gx, 8, gy, 8, gg, 8, None, None, None, None)
+    for which in ((AT[5], AT[5], None), (AT[5], AT[6], AT[5]), (None, AT[6], AT[6])):
+        _refused(-1, *bwd(*which))
