@@ -784,8 +784,8 @@ extern "C" fx_status fx_gated_scan_step(const void* d_x, int64_t ld_x, const voi
     if (d_h == d_x || d_h == d_gate) { set_error("%s: d_h must not be an input", who); return FX_EINVAL; }
     if (d_new_state != d_state && share(d_new_state, d_state, rows, C)) { set_error("%s: d_new_state overlaps d_state and is not d_state", who); return FX_EINVAL; }
     const int pieces = (C + kPiece - 1) / kPiece, es = esize(dt);
-    const int64_t blocks = (rows * pieces + 255) / 256;
-    if (blocks > 0x7FFFFFFF) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }
+    const int64_t blocks = rows > (0x7FFFFFFFll << 8) / pieces ? 0 : (rows * pieces + 255) / 256;
+    if (!blocks) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps(kProfScanFwd, st);
     const int kind = C < kPiece ? kRowsNarrow : C % kPiece ? kRowsRagged : kRowsWhole;
