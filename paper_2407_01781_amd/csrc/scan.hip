@@ -549,6 +549,7 @@ static fx_status check_rows_of(const char* who, const char* name, const void* p,
     return FX_OK;
 }
 
+constexpr int64_t kMostThreads = (1ll << 32) - 256;      // of a launch
 constexpr int32_t kMostChannels = 1 << 24;      // a row's bytes and a tile's rows meet in 32 bits
 
 static fx_status check_scan(const char* who, const fx_sequences* q, int32_t C, fx_dtype dt) {
@@ -784,20 +785,26 @@ extern "C" fx_status fx_gated_scan_step(const void* d_x, int64_t ld_x, const voi
     if (d_h == d_x || d_h == d_gate) { set_error("%s: d_h must not be an input", who); return FX_EINVAL; }
     if (d_new_state != d_state && share(d_new_state, d_state, rows, C)) { set_error("%s: d_new_state overlaps d_state and is not d_state", who); return FX_EINVAL; }
     const int pieces = (C + kPiece - 1) / kPiece, es = esize(dt);
-    const int64_t blocks = rows > (0x7FFFFFFFll << 8) / pieces ? 0 : (rows * pieces + 255) / 256;
-    if (!blocks) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }
+    if (rows > (0x7FFFFFFFll << 8) / pieces) { set_error("%s: too many rows", who); return FX_ERANGE; }
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps(kProfScanFwd, st);
     const int kind = C < kPiece ? kRowsNarrow : C % kPiece ? kRowsRagged : kRowsWhole;
-#define FX_STEP(DT, KIND) k_scan_step<DT, KIND><<<(unsigned)blocks, 256, 0, st>>>(rows, C, pieces, (const unsigned char*)d_x, ld_x * es, \
-        (const unsigned char*)d_gate, ld_gate * es, d_state, d_new_state, (unsigned char*)d_h, ld_h * es)
+    // One launch, for all rows that there is memory for but of a few channels: a launch's threads are counted in 32 bits,
+    // and more of them wrap without an error.
+    const int64_t most = kMostThreads / pieces;
+    for (int64_t r = 0; r < rows; r += most) {
+        const int64_t n = std::min(most, rows - r);
+        const unsigned blocks = (unsigned)((n * pieces + 255) / 256);
+#define FX_STEP(DT, KIND) k_scan_step<DT, KIND><<<blocks, 256, 0, st>>>(n, C, pieces, (const unsigned char*)d_x + r * ld_x * es, ld_x * es, \
+        (const unsigned char*)d_gate + r * ld_gate * es, ld_gate * es, d_state + r * C, d_new_state + r * C, (unsigned char*)d_h + r * ld_h * es, ld_h * es)
 #define FX_STEP_KIND(DT) do { if (kind == kRowsWhole) FX_STEP(DT, kRowsWhole); else if (kind == kRowsRagged) FX_STEP(DT, kRowsRagged); \
                               else FX_STEP(DT, kRowsNarrow); } while (0)
-    if (dt == FX_F32) FX_STEP_KIND(FX_F32);
-    else if (dt == FX_F16) FX_STEP_KIND(FX_F16);
-    else FX_STEP_KIND(FX_BF16);
+        if (dt == FX_F32) FX_STEP_KIND(FX_F32);
+        else if (dt == FX_F16) FX_STEP_KIND(FX_F16);
+        else FX_STEP_KIND(FX_BF16);
 #undef FX_STEP_KIND
 #undef FX_STEP
+    }
     FX_HIP_TRY(hipGetLastError());
     return FX_OK;
 }
