@@ -477,7 +477,7 @@ void fx_sequences_destroy(fx_sequences* q);
  *                sequence without rows.  Fed as h0 to the rows that come later, it continues the recurrence; must not
  *                overlap d_h0 (FX_EINVAL): two tables in turn.
  * Rows up to 4 MiB apart are always served; FX_ERANGE where the rows that one workgroup takes would reach over 2 GiB, and
- * beyond 2^24 channels.
+ * beyond 2^24 channels or 2^32 lanes of a launch (two a row of 33 to 64 channels in 16 bits).
  * 1 - f is computed as sigmoid(-gate), to its own precision where f is near 1.  An infinity or NaN stays in its
  * sequence and channel; a sequence's rows do not depend on any other's.
  * Backward, with gh = dL/dh and glast = dL/dlast (fp32 [B, C], NULL for zeros): d_h is what the forward call wrote

@@ -611,7 +611,7 @@ static fx_status launch_scan(ScanArgs& a, hipStream_t st) {
         if (tiles == 1 ? 2 * a.rows > rows_a_tile : tiles * a.slabs * 16 >= compute_units()) break;
     }
     if (ld > kMostOffset / rows_a_tile) { set_error("gated scan: rows lie more than %lld bytes apart", (long long)(kMostOffset / rows_a_tile)); return FX_ERANGE; }
-    if (tiles * a.slabs > 0x3FFFFFFF) { set_error("gated scan: too many tiles for one launch"); return FX_ERANGE; }
+    if (tiles * a.slabs > kMostThreads / threads) { set_error("gated scan: too many tiles for one launch"); return FX_ERANGE; }
     a.tiles = (int)tiles;
     a.groups = (int)((tiles + kGroupTiles - 1) / kGroupTiles);
     void* work = nullptr;

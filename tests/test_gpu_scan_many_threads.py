@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_2407_01781_amd as fx
+from paper_2407_01781_amd import binding as B
 
 pytestmark = pytest.mark.gpu
 
@@ -21,3 +22,13 @@ def test_steps_of_more_rows_than_threads():
         h[r] = s[r] = 1.0
     part = 1 << 28                          # comparisons of a part at a time: torch's own kernels count in 32 bits too
     assert all(bool((t[a:a + part] == 1).all()) for t in (h, s) for a in range(0, n, part))
+
+
+def test_more_tiles_than_threads():
+    """Refused on the host: of 2^31 - 1 rows of 129 channels nothing but the sequences' table is there."""
+    n, c = (1 << 31) - 1, 129
+    seqs = fx.build_sequences([[0, n]])
+    x = torch.empty(1, dtype=torch.bfloat16, device="cuda")
+    p = [x.data_ptr() + (i << 43) for i in range(3)]
+    assert B.lib.fx_gated_scan_fwd(seqs._h, p[0], c, p[1], c, 2, c, 0, None, p[2], c, None, None) == -5
+    assert b"too many tiles" in B.lib.fx_last_error()
