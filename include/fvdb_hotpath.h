@@ -455,8 +455,12 @@ fx_status fx_sparse_conv_leaf_bwd_weight(const fx_grid* g, const void* d_feat, c
  * tensor -- features and gate out of one projection -- needs no copy.  Elements of a row follow each other; pointers
  * are aligned to an element, no more.  Arithmetic and sums are fp32, every output is rounded once (RNE) to its type.
  * Vectors over the channels (norm weights, scale) and their gradients have a dtype of their own, vec_dt: the rows' or
- * FX_F32.  None of these calls synchronises, except fx_build_sequences.  No atomics are used on results: a call
- * gives the same bits every time.
+ * FX_F32.  No atomics are used on results: a call gives the same bits every time.
+ * All but fx_build_sequences are enqueued without waiting for the stream.  The recurrence over more rows than a workgroup
+ * holds and the gradients of vectors take scratch as the convolutions do: from the caller's allocator, or else from the
+ * library's cache, where a block that is not there yet costs a hipMalloc and one that another stream used last a
+ * hipDeviceSynchronize.  To be recorded into a graph these need the caller's allocator (FX_EUNSUPPORTED without one, see
+ * fx_set_allocator); the others, and any call that takes no scratch, do not.
  *
  * Sequences: which rows follow each other.  h_joffsets [B,2] (host) as for a grid -- the voxel ranges of a batch of
  * grids (fx_grid_info) make every grid one sequence in index order --, but the ranges must follow each other without

@@ -442,7 +442,7 @@ static fx_status run_bwd(fx_dtype dt, fx_dtype vec_dt, BlockArgs& a, void* gpost
     a.lanes_log2 = shape.lanes_log2;
     a.want = (gpost ? 1 : 0) | (gscale ? 2 : 0) | (gnext ? 4 : 0);
     void* partial = nullptr;
-    if (a.want) FX_TRY(dev_alloc(&partial, (size_t)3 * std::max(nb, 1u) * a.C * sizeof(float), st));
+    if (a.want) FX_TRY(scratch_alloc(MODE == kModeNorm ? "fx_rms_norm_bwd" : "fx_block_join_bwd", &partial, (size_t)3 * std::max(nb, 1u) * a.C * sizeof(float), st));
     a.partial = (float*)partial;
     fx_status s = FX_OK;
     if (nb) {

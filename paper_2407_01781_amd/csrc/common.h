@@ -41,6 +41,10 @@ int option(Option o);
 // From the caller's allocator when one is set (fx_set_allocator), else from the library's own cache of blocks.
 fx_status dev_alloc(void** p, size_t bytes, hipStream_t s);
 void dev_free(void* p, hipStream_t s);
+// Scratch of one call, to be freed by dev_free behind its launches.  Refused while the stream is recorded into a graph,
+// unless the caller's allocator is set, which keeps the graph's memory apart: a block of the library's cache would be
+// written at every replay, after others have been handed it or the driver has it back.
+fx_status scratch_alloc(const char* who, void** p, size_t bytes, hipStream_t s);
 
 // Pinned host staging owned by the library (per thread), at least `bytes` large.  Area 0 is
 // for read-backs (the caller synchronises before using the data), area 1 for uploads that stay

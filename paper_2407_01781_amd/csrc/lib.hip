@@ -189,6 +189,14 @@ int compute_units() {
     return n_cu;
 }
 
+fx_status scratch_alloc(const char* who, void** p, size_t bytes, hipStream_t s) {
+    if (!g_user_alloc && stream_captures(s)) {
+        set_error("%s: recorded into a graph, its scratch has to come from the caller's allocator (fx_set_allocator)", who);
+        return FX_EUNSUPPORTED;
+    }
+    return dev_alloc(p, bytes, s);
+}
+
 bool stream_captures(hipStream_t st) {
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
     return st && hipStreamIsCapturing(st, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone;

@@ -619,7 +619,7 @@ static fx_status launch_scan(ScanArgs& a, hipStream_t st) {
     if (tiles <= 1 && a.last && a.n_empty) launch_prepare(a, 0, st);
     if (tiles > 1) {
         const int64_t words = (int64_t)a.slabs * 64 * (a.tiles + a.groups);
-        FX_TRY(dev_alloc(&work, (size_t)words * 8 + 256, st));
+        FX_TRY(scratch_alloc("gated scan", &work, (size_t)words * 8 + 256, st));
         a.tile_runs = (uint64_t*)work;
         a.group_runs = a.tile_runs + (int64_t)a.slabs * 64 * a.tiles;
         a.ticket = (uint32_t*)(a.tile_runs + words);
