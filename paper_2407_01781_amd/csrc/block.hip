@@ -275,7 +275,7 @@ k_block_bwd(BlockArgs a) {
 #pragma unroll
             for (int e = 0; e < kPiece; ++e) {
                 y[e] *= ry;                      // yh
-                const float yk = kept(y[e], keep[e]), r = kept(yk * wp[e], keep[e]);
+                const float yk = kept(y[e], keep[e]), r = yk * wp[e];
                 acc_scale[e] += D[e] * (r * f[e]);
                 const float t = D[e] * ws[e], u = t * f[e];
                 df[e] *= t * r;
