@@ -524,7 +524,8 @@ def upsample2_bwd(kmap: KernelMap, grad_out: torch.Tensor) -> torch.Tensor:
 
 # ------------------------------------------------------------------------------------------ around the convolution
 class Sequences:
-    """Handle on the rows' division into sequences (fx_build_sequences)."""
+    """Handle on the rows' division into sequences (fx_build_sequences).  Calls on any stream may use it; let go of it when
+    those on other streams than the one it was built on have ended, and keep it for as long as a graph that uses it."""
 
     def __init__(self, handle: int, batch_size: int, rows: int):
         self._h = C.c_void_p(handle)

@@ -185,9 +185,10 @@ __device__ __forceinline__ void write_partial(float (&acc)[kPiece], int lanes, i
 //   J^T of n(v; w) on g:  (g w - vh mean_c(g w vh)) / rms(v)
 // The three sums over rows run in every lane's registers over the rows that its workgroup takes, are joined in the
 // workgroup and added over the workgroups, in index order, by k_block_sums: the same bits from every call.
-// 1,068,658 x 64 f16 with everything (1094 MB): 217 us, 5.0 TB/s, a copy's rate, at 183 registers and so eight waves a
-// compute unit (held to 168 or 128 registers it spills: 221, 687 us), which is also how many workgroups are launched:
-// 16 waves 230 us, the rows' sums of each being joined once.  The norm alone (77 registers) 194,497 x 256 bf16 54 us, best at 16
+// 1,068,658 x 64 f16 with everything (1094 MB): 222 us, 4.9 TB/s, near a copy's rate, at 184 registers and so eight waves a
+// compute unit, which is also how many workgroups are launched: 16 waves took 230 us where 8 took 217, the rows' sums of
+// each being joined once.  Selecting what is dropped costs 3 of the 222 us and 8 registers (one word of bits a lane in place
+// of eight masks: 7 us more); held to 168 or 128 registers the form without it spilled (221, 687 us).  The norm alone (77 registers) 194,497 x 256 bf16 54 us, best at 16
 // waves (8: 95 us for 76 at 986,880 x 64).  A row that is small is bound by latency: 20,011 x 45 fp32 16 us for 22 MB.
 template <int DT, int KIND, bool WIDE, int MODE>
 __global__ void __launch_bounds__(WIDE ? kWideThreads : kBlockThreads)

@@ -1,6 +1,7 @@
 """GPU parity of the gated linear recurrence: forward, gradients and single steps against the formulas in 64 bits, row
-by row, at lengths around a lane's rows (8), a tile (512 rows at 64 channels, 4096 at 8) and many tiles; sequences
-without rows; every type; column ranges of wider tensors; infinities and NaN; streams and graphs."""
+by row, at lengths around a lane's rows (8) and of up to some thirty tiles (the lengths named after a tile are from tiles
+of 512 rows; today one has 32 there, and test_gpu_scan_long.py tests the edges); sequences without rows; every type; column
+ranges of wider tensors; infinities and NaN; streams."""
 import numpy as np
 import pytest
 import torch

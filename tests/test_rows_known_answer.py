@@ -1,5 +1,5 @@
-"""Dropout's generator against the known answer that its authors publish: Philox4x32 with seven rounds at zero counter and key
-(Random123's kat_vectors)."""
+"""Dropout's generator against the known answer that its authors publish with it: Philox4x32 with seven rounds at zero counter and
+key."""
 import numpy as np
 
 import rows_reference as R

@@ -1,5 +1,5 @@
 """The oracle of the operators around the convolution against differences of its own forward formulas, and dropout's
-generator against its authors' known answers' structure (equal shares, no dependence on the rows' number)."""
+generator by its shares (equal, and no dependence on the rows' number)."""
 import numpy as np
 import pytest
 
