@@ -559,6 +559,81 @@ fx_status fx_dropout(const void* d_x, int64_t ld_x, fx_dtype dt, int64_t rows, i
                      const uint64_t* d_offset, const void* d_residual, int64_t ld_residual, void* d_out, int64_t ld_out, void* stream);
 
 /* ---------------------------------------------------------------------------------------
+ * Attention along the voxels of a batch of grids (Sec. 3.6.2: attention on a JaggedTensor), as packed sequences with grouped
+ * heads, its gradients, and what serves it row by row: a paged cache of keys and values and the attention of one new row
+ * over it.
+ *
+ * A tensor of heads has rows of `heads` (or `kv_heads`) times `dim` elements: element d of head h of row r lies at
+ * r * ld + h * hs + d (ld, hs in elements, >= dim), so that queries, keys and values may be column ranges of one projection and
+ * heads may be the outer dimension.  Pointers are aligned to an element, no more; where they or the strides are not multiples of
+ * 16 bytes, or dim is not, the call copies the rows into such an order first (scratch).  heads is a multiple of kv_heads (query
+ * head h reads key head h / (heads / kv_heads)), dim 1 to 256 (FX_ERANGE).  Scratch and graphs as for the recurrence.
+ *
+ *     s_ij = scale q_i . k_j,   lse_i = log sum_j exp(s_ij),   out_i = sum_j exp(s_ij - lse_i) v_j
+ *
+ * j runs over the keys of i's sequence.  With `causal` the last query stands at the last key and each before it one key earlier:
+ * query i of n sees key j of m where n - i <= m - j.  A row that sees no key gets out = 0, lse = -inf, and gradients of 0.
+ * Products, maxima and sums are fp32; in 16 bits exp(s - m) is rounded to the type before its product with v (m close to the
+ * row's maximum, the sum of the weights is of the unrounded ones), every output once.  A row's results depend on the keys that it sees alone:
+ * infinities and NaN of other rows, of a causal sequence's later ones too, leave it as it is.
+ *   q_seqs, kv_seqs  the rows' division into sequences, as many of both; kv_seqs NULL: q_seqs
+ *   d_lse            [heads, rows of q_seqs] fp32, natural logarithm, or NULL
+ * Backward: d_out and d_lse are what the forward call wrote, d_gout and d_glse ([heads, rows], NULL: zeros) the gradients of
+ * both outputs.  With P_ij = exp(s_ij - lse_i), dP_ij = gout_i . v_j and dS_ij = P_ij (dP_ij - sum_j P_ij dP_ij + glse_i):
+ *     gq_i = scale sum_j dS_ij k_j,   gk_j = scale sum_i dS_ij q_i,   gv_j = sum_i P_ij gout_i
+ * over all query heads of a key head.  In 16 bits P and dS are rounded to the type before their products.  gq, gk and gv may be NULL
+ * (not computed).  No atomics: the same bits from every call.
+ * An output must not be where an input or another output is (FX_EINVAL) nor overlap them, and its rows and heads must not
+ * overlap each other (FX_EINVAL). */
+typedef struct {
+    const fx_sequences* q_seqs;
+    const fx_sequences* kv_seqs;
+    fx_dtype dt;
+    int32_t heads, kv_heads, dim;
+    int32_t causal;
+    float scale;
+    const void *d_q, *d_k, *d_v;
+    int64_t ld_q, hs_q, ld_k, hs_k, ld_v, hs_v;
+} fx_attention;
+fx_status fx_attention_fwd(const fx_attention* a, void* d_out, int64_t ld_out, int64_t hs_out, float* d_lse, void* stream);
+fx_status fx_attention_bwd(const fx_attention* a, const void* d_out, int64_t ld_out, int64_t hs_out, const float* d_lse, const void* d_gout,
+                           int64_t ld_gout, int64_t hs_gout, const float* d_glse, void* d_gq, int64_t ld_gq, int64_t hs_gq, void* d_gk,
+                           int64_t ld_gk, int64_t hs_gk, void* d_gv, int64_t ld_gv, int64_t hs_gv, void* stream);
+
+/* Cache of keys and values in pages of `page_rows` positions, the caller's memory: position p of sequence b is row p % page_rows of page
+ * d_table[b * ld_table + p / page_rows].  A position whose column is not below table_cols, or whose page is not in 0 .. pages-1, does
+ * not exist: it is not written, reads as zeros, and no query sees it.
+ *   d_k, d_v          [pages, kv_heads, page_rows, pitch], pitch = dim rounded up to 16, 16-byte aligned; elements behind dim are
+ *                     written as zeros and have to be finite
+ *   store             FX_F32, FX_F16, FX_BF16, or FX_E4M3: 8 bits (OCP e4m3) and one exponent for every row and head,
+ *                     value = code * 2^(exponent - 127).  The exponent is the least of 0 .. 255 with which no finite value of the row passes
+ *                     448 (0 for a row of zeros), so that the division is exact and codes are rounded once, to nearest even;
+ *                     an infinity is stored as NaN.
+ *   d_k_exp, d_v_exp  [pages, kv_heads, page_rows] bytes, for FX_E4M3 alone
+ * fx_cache_write puts row r of sequence b of `q` at position d_start[b] + r; with q NULL there are `rows` sequences of one row each.
+ * Rows have dtype dt, `store` is dt or FX_E4M3 (FX_EUNSUPPORTED).  No two rows of a call may have one place.
+ * fx_cache_read gives the positions from d_start[b] on of every sequence, one for each of its rows of q, in dtype dt (one rounding from
+ * FX_E4M3, none otherwise).
+ * fx_attention_step: out_b = attention of query row b over positions 0 .. d_len[b]-1 of sequence b (no key: 0 and lse = -inf), d_lse
+ * [rows, heads] or NULL.  `most` bounds the lengths on the host (longer ones are cut there), 0: table_cols * page_rows; the split of the work goes by it.
+ * The weights exp(s - m) are rounded to 16 bits after the leading 8 where they meet 16-bit values, to 24 bits where q is FX_F32.
+ * None of the calls waits for the stream; lengths, starts and the table are read when the kernels run, so that a captured step follows them. */
+enum { FX_E4M3 = 3 };
+typedef struct {
+    void *d_k, *d_v;
+    uint8_t *d_k_exp, *d_v_exp;
+    const int32_t* d_table;
+    int64_t ld_table;
+    int32_t table_cols, pages, page_rows, store, kv_heads, dim;
+} fx_cache;
+fx_status fx_cache_write(const fx_cache* c, const fx_sequences* q, int64_t rows, const int32_t* d_start, fx_dtype dt, const void* d_k, int64_t ld_k,
+                         int64_t hs_k, const void* d_v, int64_t ld_v, int64_t hs_v, void* stream);
+fx_status fx_cache_read(const fx_cache* c, const fx_sequences* q, const int32_t* d_start, fx_dtype dt, void* d_k, int64_t ld_k, int64_t hs_k,
+                        void* d_v, int64_t ld_v, int64_t hs_v, void* stream);
+fx_status fx_attention_step(const fx_cache* c, int64_t rows, const int32_t* d_len, int64_t most, fx_dtype dt, int32_t heads, float scale, const void* d_q,
+                            int64_t ld_q, int64_t hs_q, void* d_out, int64_t ld_out, int64_t hs_out, float* d_lse, void* stream);
+
+/* ---------------------------------------------------------------------------------------
  * Measurement support (the paper's protocol, Sec. 4.1: per-operator times).  While enabled,
  * every kernel launch of the library is bracketed by hipEvents on its launch stream;
  * fx_profile_read waits for the recorded events and returns the summed time and launch count

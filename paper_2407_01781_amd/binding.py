@@ -40,6 +40,20 @@ class _BlockJoin(C.Structure):
                 ("seed", C.c_uint64), ("offset", C.c_uint64), ("p", C.c_double), ("eps", C.c_float)]
 
 
+class _Attention(C.Structure):
+    """fx_attention"""
+    _fields_ = [("q_seqs", C.c_void_p), ("kv_seqs", C.c_void_p), ("dt", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("dim", C.c_int32), ("causal", C.c_int32), ("scale", C.c_float), ("d_q", C.c_void_p), ("d_k", C.c_void_p), ("d_v", C.c_void_p),
+                ("ld_q", C.c_int64), ("hs_q", C.c_int64), ("ld_k", C.c_int64), ("hs_k", C.c_int64), ("ld_v", C.c_int64), ("hs_v", C.c_int64)]
+
+
+class _Cache(C.Structure):
+    """fx_cache"""
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_exp", C.c_void_p), ("d_v_exp", C.c_void_p), ("d_table", C.c_void_p),
+                ("ld_table", C.c_int64), ("table_cols", C.c_int32), ("pages", C.c_int32), ("page_rows", C.c_int32), ("store", C.c_int32),
+                ("kv_heads", C.c_int32), ("dim", C.c_int32)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(
@@ -117,6 +131,11 @@ def _load():
             ("fx_rms_norm_bwd", [vp, i64, vp, i64, C.c_int, i64, i32, vp, C.c_int, f32, vp, i64, vp, vp]),
             ("fx_block_join_fwd", [C.POINTER(_BlockJoin), vp, i64, vp, i64, vp, i64, vp]),
             ("fx_block_join_bwd", [C.POINTER(_BlockJoin), vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp]),
+            ("fx_attention_fwd", [C.POINTER(_Attention), vp, i64, i64, vp, vp]),
+            ("fx_attention_bwd", [C.POINTER(_Attention), vp, i64, i64, vp, vp, i64, i64, vp, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp]),
+            ("fx_cache_write", [C.POINTER(_Cache), vp, i64, vp, C.c_int, vp, i64, i64, vp, i64, i64, vp]),
+            ("fx_cache_read", [C.POINTER(_Cache), vp, vp, C.c_int, vp, i64, i64, vp, i64, i64, vp]),
+            ("fx_attention_step", [C.POINTER(_Cache), i64, vp, i64, C.c_int, i32, f32, vp, i64, i64, vp, i64, i64, vp, vp]),
             ("fx_dropout", [vp, i64, C.c_int, i64, i32, f64, u64, u64, vp, vp, i64, vp, i64, vp])):
         getattr(L, name).restype = C.c_int
         getattr(L, name).argtypes = args
@@ -733,3 +752,153 @@ def dropout(x: torch.Tensor, p: float, seed: int, offset: int, residual: Optiona
     _check(lib.fx_dropout(xp, _ld(x), _TORCH_DT[x.dtype], x.shape[0], x.shape[1], p, seed, offset, _offset(d_offset), rp, _ld(residual),
                           out.data_ptr(), _ld(out), _stream()))
     return out
+
+
+# ------------------------------------------------------------------------------------------ attention
+def _heads(t: torch.Tensor, rows: int, heads: int, dim: int, dtype: torch.dtype, name: str):
+    """Address and strides from row to row and head to head of a tensor of heads [rows, heads, dim]: any order of rows and
+    heads, a head's elements next to each other."""
+    if t.dtype != dtype or t.shape != (rows, heads, dim) or not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise AssertionError(f"{name}: {(rows, heads, dim)} {dtype} on the current GPU expected")
+    ld, hs, one = t.stride()
+    if one != 1 and dim > 1 and rows:
+        raise AssertionError(f"{name}: a head's elements have to lie next to each other")
+    # the stride of a single row or head says nothing
+    if heads <= 1:
+        hs = dim
+    return t.data_ptr(), (ld if rows > 1 else max(hs, dim) * max(heads, 1)), hs
+
+
+def _out_heads(out: Optional[torch.Tensor], like: torch.Tensor, name: str = "out") -> torch.Tensor:
+    return torch.empty(like.shape, dtype=like.dtype, device=like.device) if out is None else out
+
+
+def _floats(t: Optional[torch.Tensor], shape, name: str):
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == torch.float32 and t.shape == shape and t.is_contiguous(), \
+        f"{name}: contiguous float32 {tuple(shape)} on the GPU expected"
+    return t.data_ptr()
+
+
+def _numbers(t: torch.Tensor, n: int, name: str) -> int:
+    assert t.is_cuda and t.dtype == torch.int32 and t.shape == (n,) and t.is_contiguous(), f"{name}: contiguous int32 ({n},) on the GPU expected"
+    return t.data_ptr()
+
+
+def _attention(seqs: Sequences, kv_seqs: Optional[Sequences], q, k, v, causal: bool, scale: Optional[float]) -> _Attention:
+    assert q.dim() == 3 and k.dim() == 3 and q.dtype in _TORCH_DT, "q, k, v: [rows, heads, dim]"
+    rows, heads, dim = q.shape
+    kv_rows, kv_heads = (kv_seqs or seqs).rows, k.shape[1]
+    assert rows == seqs.rows, f"q: {seqs.rows} rows expected"
+    qp, kp, vp = _heads(q, rows, heads, dim, q.dtype, "q"), _heads(k, kv_rows, kv_heads, dim, q.dtype, "k"), _heads(v, kv_rows, kv_heads, dim, q.dtype, "v")
+    # in the order of the members
+    return _Attention(seqs._h, None if kv_seqs is None else kv_seqs._h, _TORCH_DT[q.dtype], heads, kv_heads, dim, int(causal),
+                      dim ** -0.5 if scale is None else scale, qp[0], kp[0], vp[0], *qp[1:], *kp[1:], *vp[1:])
+
+
+def attention_fwd(seqs: Sequences, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, scale: Optional[float] = None,
+                  kv_seqs: Optional[Sequences] = None, out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Softmax attention of every row over the rows of its sequence: q [rows, heads, dim], k and v [rows, kv_heads, dim] (query
+    head h reads key head h // (heads / kv_heads)), or rows of kv_seqs, as many sequences.  causal: the last query stands at the last
+    key, and none sees a later one.  scale: dim ** -0.5 without.  Returns out [rows, heads, dim] and lse [heads, rows] float32, the
+    logarithm of the sum of exp(scale q . k); 0 and -inf for a row that sees no key."""
+    a = _attention(seqs, kv_seqs, q, k, v, causal, scale)
+    out = _out_heads(out, q)
+    op = _heads(out, *q.shape, q.dtype, "out")
+    lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
+    _check(lib.fx_attention_fwd(a, *op, lse.data_ptr(), _stream()))
+    return out, lse
+
+
+def attention_bwd(seqs: Sequences, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                  grad_out: torch.Tensor, grad_lse: Optional[torch.Tensor] = None, causal: bool = False, scale: Optional[float] = None,
+                  kv_seqs: Optional[Sequences] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Gradients of attention_fwd's q, k and v; out and lse are its outputs, grad_lse the gradient of the second (zeros without)."""
+    a = _attention(seqs, kv_seqs, q, k, v, causal, scale)
+    op, gp = _heads(out, *q.shape, q.dtype, "out"), _heads(grad_out, *q.shape, q.dtype, "grad_out")
+    stats = (q.shape[1], q.shape[0])
+    lp, glp = _floats(lse, stats, "lse"), _floats(grad_lse, stats, "grad_lse")
+    gq, gk, gv = _out_heads(None, q), _out_heads(None, k), _out_heads(None, v)
+    outs = [x for t in (gq, gk, gv) for x in _heads(t, *t.shape, q.dtype, "gradient")]
+    _check(lib.fx_attention_bwd(a, *op, lp, *gp, glp, *outs, _stream()))
+    return gq, gk, gv
+
+
+class KVCache:
+    """Keys and values of running sequences in pages (fx_cache): k and v [pages, kv_heads, page_rows, dim rounded up to 16], float32,
+    float16, bfloat16 or float8_e4m3fn; the last with exponents k_exp and v_exp [pages, kv_heads, page_rows] uint8 (a value is
+    code * 2 ** (exponent - 127)).  Which page a position has is said by the table of a call, [sequences, columns] int32: position p is row
+    p % page_rows of page table[b, p // page_rows]; -1, or any other number that is no page, for those that have none."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, dim: Optional[int] = None, k_exp: Optional[torch.Tensor] = None,
+                 v_exp: Optional[torch.Tensor] = None):
+        assert k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.is_contiguous() and v.is_contiguous() and k.is_cuda and v.is_cuda, \
+            "k and v: contiguous [pages, kv_heads, page_rows, dim rounded up to 16] of one type on the GPU"
+        self.dim = k.shape[3] if dim is None else dim
+        assert -(-self.dim // 16) * 16 == k.shape[3], f"rows of {k.shape[3]} elements do not hold {self.dim} dimensions rounded up to 16"
+        e4m3 = k.dtype == torch.float8_e4m3fn
+        assert e4m3 or k.dtype in _TORCH_DT, "float32, float16, bfloat16 or float8_e4m3fn expected"
+        for t in (k_exp, v_exp):
+            assert (t is not None) == e4m3, "exponents belong to a cache of 8 bits"
+            assert t is None or (t.is_cuda and t.dtype == torch.uint8 and t.shape == k.shape[:3] and t.is_contiguous()), "exponents: contiguous uint8 [pages, kv_heads, page_rows]"
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self._c = _Cache(k.data_ptr(), v.data_ptr(), None if k_exp is None else k_exp.data_ptr(), None if v_exp is None else v_exp.data_ptr(), None, 0, 0,
+                         k.shape[0], k.shape[2], 3 if e4m3 else _TORCH_DT[k.dtype], k.shape[1], self.dim)
+
+    @classmethod
+    def empty(cls, pages: int, page_rows: int, kv_heads: int, dim: int, dtype: torch.dtype = torch.bfloat16) -> "KVCache":
+        """A cache of zeros in new memory."""
+        new = lambda: torch.zeros((pages, kv_heads, page_rows, -(-dim // 16) * 16), dtype=dtype, device="cuda")
+        exp = lambda: torch.zeros((pages, kv_heads, page_rows), dtype=torch.uint8, device="cuda") if dtype == torch.float8_e4m3fn else None
+        return cls(new(), new(), dim, exp(), exp())
+
+    def _with(self, table: torch.Tensor, n: int) -> _Cache:
+        assert table.is_cuda and table.dtype == torch.int32 and table.dim() == 2 and table.shape[0] == n and (table.stride(1) == 1 or table.shape[1] <= 1), \
+            f"table: int32 [{n}, columns] on the GPU expected"
+        assert self.k.get_device() == table.get_device() == torch.cuda.current_device(), "cache and table have to be on the current GPU"
+        c = _Cache.from_buffer_copy(self._c)
+        c.d_table, c.table_cols = table.data_ptr(), table.shape[1]
+        c.ld_table = table.stride(0) if n > 1 else max(table.shape[1], 1)
+        return c
+
+
+def cache_write(cache: KVCache, table: torch.Tensor, start: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs: Optional[Sequences] = None) -> None:
+    """Row r of sequence b of k and v [rows, kv_heads, dim] becomes position start[b] + r of the cache, rounded to its type; without
+    seqs row b is one new row of sequence b.  No two rows may have one place; those whose position has no page are left out."""
+    n = k.shape[0] if seqs is None else seqs.batch_size
+    rows = k.shape[0] if seqs is None else seqs.rows
+    c = cache._with(table, n)
+    assert k.dtype in _TORCH_DT
+    kp, vp = (_heads(t, rows, c.kv_heads, cache.dim, k.dtype, name) for t, name in ((k, "k"), (v, "v")))
+    _check(lib.fx_cache_write(c, None if seqs is None else seqs._h, rows, _numbers(start, n, "start"), _TORCH_DT[k.dtype], *kp, *vp, _stream()))
+
+
+def cache_read(cache: KVCache, table: torch.Tensor, start: torch.Tensor, seqs: Sequences,
+               dtype: Optional[torch.dtype] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Keys and values [rows, kv_heads, dim] at the positions from start[b] on of every sequence, one for each of its rows of seqs
+    (zeros for those that have no page); dtype: the cache's, which has to be said for one of 8 bits."""
+    dtype = cache.k.dtype if dtype is None else dtype
+    assert dtype in _TORCH_DT, "dtype: float32, float16 or bfloat16"
+    c = cache._with(table, seqs.batch_size)
+    k, v = (torch.empty((seqs.rows, c.kv_heads, cache.dim), dtype=dtype, device=cache.k.device) for _ in range(2))
+    outs = [x for t in (k, v) for x in _heads(t, *t.shape, dtype, "out")]
+    _check(lib.fx_cache_read(c, seqs._h, _numbers(start, seqs.batch_size, "start"), _TORCH_DT[dtype], *outs, _stream()))
+    return k, v
+
+
+def attention_step(cache: KVCache, table: torch.Tensor, lengths: torch.Tensor, q: torch.Tensor, scale: Optional[float] = None,
+                   longest: int = 0, out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Attention of one new row of each of q.shape[0] running sequences, q [n, heads, dim], over the first lengths[b] positions that
+    the cache holds of it.  longest: what no length passes (longer ones are cut there), if the program knows better than the table's width.  Returns out [n, heads, dim]
+    and lse [n, heads] float32."""
+    assert q.dim() == 3 and q.dtype in _TORCH_DT
+    n, heads, dim = q.shape
+    c = cache._with(table, n)
+    assert dim == cache.dim, f"q: {cache.dim} dimensions expected"
+    qp = _heads(q, n, heads, dim, q.dtype, "q")
+    out = _out_heads(out, q)
+    lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
+    _check(lib.fx_attention_step(c, n, _numbers(lengths, n, "lengths"), longest, _TORCH_DT[q.dtype], heads, dim ** -0.5 if scale is None else scale,
+                                 *qp, *_heads(out, n, heads, dim, q.dtype, "out"), lse.data_ptr(), _stream()))
+    return out, lse

@@ -1,0 +1,328 @@
+// Attention over packed sequences: the forward kernel, and the entry points of both directions.
+#include "attention.h"
+
+#include <math.h>
+
+namespace fx {
+
+// ------------------------------------------------------------------ forward
+// A workgroup has W waves of 32 queries of one head; keys and values come by in tiles of KT, two buffers of each.
+template <int DT, int DP> struct FwdShape {
+    static constexpr int RB = DP * AttnType<DT>::ES;
+    static constexpr int KT = RB > 256 ? 32 : 64;
+    static constexpr int kTile = KT * RB;
+    static constexpr int kLds = 4 * kTile;
+};
+
+template <int DT, int DP, int W>
+__global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES > 256 ? 1 : 2) void k_attention(AttnArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)         // the host pass has no buffer descriptors and drops stubs over them
+    typedef FwdShape<DT, DP> S;
+    typedef typename AttnType<DT>::T T;
+    constexpr int RB = S::RB, KT = S::KT, STEPS = RB / 32, COLS = DP / 32, MT = KT / 32;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    lds_byte* lds = (lds_byte*)smem;
+    int tile, head;
+    if (!work_of(a, a.heads, &tile, &head)) return;
+    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane >> 5;
+    const SeqTile st = a.tiles[tile];
+    const int q0 = a.first_q[st.seq], nq = a.first_q[st.seq + 1] - q0, k0 = a.first_k[st.seq], nk = a.first_k[st.seq + 1] - k0;
+    const int row0 = st.row + wave * 32, row = row0 + (lane & 31), shift = nk - nq;
+    const int kv_head = head / a.group;
+    const unsigned char* kb = a.k.p + (int64_t)k0 * a.k.ld + kv_head * a.k.hs;
+    const unsigned char* vb = a.v.p + (int64_t)k0 * a.v.ld + kv_head * a.v.hs;
+    // keys that some row of the workgroup, or of the wave, sees; and the last that this lane's row sees
+    const int seen = a.causal ? max(0, min(nk, min(st.row + 32 * W, nq) + shift)) : nk;
+    const int seen_wave = row0 >= nq ? 0 : a.causal ? max(0, min(nk, min(row0 + 32, nq) + shift)) : nk;
+    const int last = a.causal ? min(nk - 1, row + shift) : nk - 1;
+
+    TileLoad<RB, KT, W> lk, lv;
+    lk.init(wave, lane, a.k.ld, a.dim_bytes);
+    lv.init(wave, lane, a.v.ld, a.dim_bytes);
+    OwnRows<DT, STEPS> q;
+    q.load(a.q.p + (int64_t)q0 * a.q.ld + head * a.q.hs, a.q.ld, row0, nq, a.dim_bytes, lane, a.negative);
+
+    f32x16 acc[COLS];
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) acc[c] = f32x16(0.f);
+    float m = -INFINITY, sum = 0.f;
+    const int n = (seen + KT - 1) / KT;
+    if (n > 0) {
+        lk.load(lds, kb, a.k.ld, 0, nk, a.dim_bytes, wave);
+        lv.load(lds + 2 * S::kTile, vb, a.v.ld, 0, nk, a.dim_bytes, wave);
+    }
+    for (int j = 0; j < n; ++j) {
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        const int b = j & 1, key0 = j * KT;
+        if (j + 1 < n) {
+            lk.load(lds + (b ^ 1) * S::kTile, kb, a.k.ld, key0 + KT, nk, a.dim_bytes, wave);
+            lv.load(lds + (2 + (b ^ 1)) * S::kTile, vb, a.v.ld, key0 + KT, nk, a.dim_bytes, wave);
+        }
+        if (key0 >= seen_wave) continue;
+        const lds_byte *kt = lds + b * S::kTile, *vt = lds + (2 + b) * S::kTile;
+        f32x16 s[MT];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            s[t] = f32x16(0.f);
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) s[t] = Elem<T>::mma(row_operand<DT, RB>(kt, t * 32 + (lane & 31), i, half), q.x[i], s[t]);
+        }
+        const int unmasked = a.causal ? min(nk - 1, row0 + shift) : nk - 1;
+        if (key0 + KT - 1 > unmasked) {
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (key0 + 32 * t + 8 * (r >> 2) + 4 * half + (r & 3) > last) s[t][r] = -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
+        top = fmaxf(top, other_half(top));
+        const float m2 = fmaxf(m, top);
+        const float mc = m2 == -INFINITY ? 0.f : m2 * a.c;
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m * a.c - mc);
+        m = m2;
+        sum *= f;
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) acc[c] *= f;
+        float part = 0.f;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], a.c, -mc));
+                part += s[t][r];
+            }
+            Weights<DT> w;
+            w.set(s[t]);
+#pragma unroll
+            for (int c = 0; c < COLS; ++c) mma_columns<DT, RB>(acc[c], vt, t * 32, c, w, lane);
+        }
+        sum += part;
+    }
+    sum += other_half(sum);
+    if (row >= nq) return;
+    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    unsigned char* out = a.out.p + (int64_t)(q0 + row) * a.out.ld + head * a.out.hs;
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) store_columns<DT>(acc[c], f, out, c, a.dim_bytes, half);
+    if (a.lse && half == 0) a.lse[head * a.rows_q + q0 + row] = sum == 0.f ? -INFINITY : (m * a.c + __builtin_amdgcn_logf(sum)) * kLn2;
+#endif
+}
+
+template <int DT, int DP> static void launch_fwd(const AttnArgs& a, unsigned blocks, hipStream_t st) {
+    k_attention<DT, DP, 4><<<blocks, 256, FwdShape<DT, DP>::kLds, st>>>(a);
+}
+
+template <int DT> static void launch_fwd_dim(const AttnArgs& a, int dim, unsigned blocks, hipStream_t st) {
+    if (dim <= 32) launch_fwd<DT, 32>(a, blocks, st);
+    else if (dim <= 64) launch_fwd<DT, 64>(a, blocks, st);
+    else if (dim <= 128) launch_fwd<DT, 128>(a, blocks, st);
+    else launch_fwd<DT, 256>(a, blocks, st);
+}
+
+// ------------------------------------------------------------------ rows in an order that the kernels take
+template <typename W>
+__global__ void k_heads_copy(const unsigned char* src, int64_t ld_s, int64_t hs_s, int dim_s, unsigned char* dst, int64_t ld_d, int64_t hs_d, int dim_d, int heads, int64_t n) {
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t e = i % dim_d, h = i / dim_d % heads, r = i / dim_d / heads;
+        ((W*)(dst + r * ld_d + h * hs_d))[e] = e < dim_s ? ((const W*)(src + r * ld_s + h * hs_s))[e] : W(0);
+    }
+}
+
+static void copy_heads(const HeadsView& src, int dim_s, const HeadsView& dst, int dim_d, int heads, int64_t rows, fx_dtype dt, hipStream_t st) {
+    const int64_t n = rows * heads * dim_d;
+    const unsigned blocks = (unsigned)std::min<int64_t>((n + 255) / 256, 1 << 16);
+    if (dt == FX_F32) k_heads_copy<uint32_t><<<blocks, 256, 0, st>>>(src.p, src.ld, src.hs, dim_s, dst.p, dst.ld, dst.hs, dim_d, heads, n);
+    else k_heads_copy<uint16_t><<<blocks, 256, 0, st>>>(src.p, src.ld, src.hs, dim_s, dst.p, dst.ld, dst.hs, dim_d, heads, n);
+}
+
+// ------------------------------------------------------------------ checks
+fx_status check_heads(const char* who, const HeadsTensor& t, int32_t dim, int es) {
+    if (!t.p) {
+        if (!t.needed || t.rows == 0) return FX_OK;
+        set_error("%s: %s is null", who, t.name);
+        return FX_EINVAL;
+    }
+    if ((uintptr_t)t.p % es || t.ld < dim || (t.heads > 1 && t.hs < dim)) {
+        set_error("%s: %s is not aligned to its elements or has rows or heads closer than dim", who, t.name);
+        return FX_EINVAL;
+    }
+    const int64_t most = 1ll << 46;
+    if (t.ld > most || t.hs > most) { set_error("%s: %s has a stride of more than 2^46", who, t.name); return FX_ERANGE; }
+    const bool rows_outside = t.heads == 1 || t.ld >= (t.heads - 1) * t.hs + dim;
+    const bool heads_outside = t.rows <= 1 || (__int128)t.hs >= (__int128)(t.rows - 1) * t.ld + dim;
+    if (t.output && !rows_outside && !heads_outside) { set_error("%s: rows and heads of %s overlap", who, t.name); return FX_EINVAL; }
+    return FX_OK;
+}
+
+// What a call keeps until its launches are enqueued
+struct Scratch {
+    hipStream_t st;
+    void* p[12];
+    int n = 0;
+    explicit Scratch(hipStream_t s) : st(s) {}
+    ~Scratch() { while (n) dev_free(p[--n], st); }
+    fx_status get(const char* who, void** out, size_t bytes) {
+        FX_TRY(scratch_alloc(who, out, bytes, st));
+        p[n++] = *out;
+        return FX_OK;
+    }
+};
+
+static fx_status check_attention(const char* who, const fx_attention* a) {
+    if (!a || !a->q_seqs || (a->dt != FX_F32 && a->dt != FX_F16 && a->dt != FX_BF16) || a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads || a->dim < 1) {
+        set_error("%s: null description or sequences, unknown dtype, no dimension, or heads that are no multiple of the key heads", who);
+        return FX_EINVAL;
+    }
+    if (!std::isfinite(a->scale)) { set_error("%s: the scale is not finite", who); return FX_EINVAL; }
+    if (a->kv_seqs && a->kv_seqs->B != a->q_seqs->B) { set_error("%s: %d sequences of queries and %d of keys", who, a->q_seqs->B, a->kv_seqs->B); return FX_EINVAL; }
+    if (a->dim > kMostDim) { set_error("%s: more than %d dimensions", who, kMostDim); return FX_ERANGE; }
+    if (a->heads > 65535) { set_error("%s: more than 65535 heads", who); return FX_ERANGE; }
+    return FX_OK;
+}
+
+// Fills the views of the tensors; those whose order the kernels do not take are copied (outputs: get a place to be copied from).
+static fx_status take_tensors(const char* who, HeadsTensor* t, int n, int32_t dim, fx_dtype dt, Scratch* scratch, bool* copied, int* dim_in, hipStream_t st) {
+    const int es = dtype_size(dt), per = 16 / es, padded = (dim + per - 1) / per * per;
+    bool any = false;
+    for (int i = 0; i < n; ++i) {
+        copied[i] = false;
+        if (!t[i].p || t[i].rows == 0) continue;
+        const bool strides = (t[i].ld * es) % 16 == 0 && (t[i].heads == 1 || (t[i].hs * es) % 16 == 0) && t[i].ld * es <= (1ll << 24);
+        copied[i] = dim % per || (uintptr_t)t[i].p % 16 || !strides;
+        any |= copied[i];
+    }
+    *dim_in = padded;
+    for (int i = 0; i < n; ++i) {
+        if (!t[i].p) { *t[i].view = HeadsView{nullptr, 0, 0}; continue; }
+        const HeadsView given{(unsigned char*)t[i].p, t[i].ld * es, t[i].hs * es};
+        *t[i].view = given;
+        if (!copied[i]) continue;
+        void* p = nullptr;
+        FX_TRY(scratch->get(who, &p, (size_t)t[i].rows * t[i].heads * padded * es));
+        *t[i].view = HeadsView{(unsigned char*)p, (int64_t)t[i].heads * padded * es, (int64_t)padded * es};
+        if (!t[i].output) copy_heads(given, dim, *t[i].view, padded, t[i].heads, t[i].rows, dt, st);
+    }
+    (void)any;
+    return FX_OK;
+}
+
+static void return_tensors(const HeadsTensor* t, int n, int32_t dim, fx_dtype dt, const bool* copied, int dim_in, hipStream_t st) {
+    (void)dim_in;
+    const int es = dtype_size(dt);
+    for (int i = 0; i < n; ++i)
+        if (copied[i] && t[i].output) copy_heads(*t[i].view, dim, HeadsView{(unsigned char*)t[i].p, t[i].ld * es, t[i].hs * es}, dim, t[i].heads, t[i].rows, dt, st);
+}
+
+static fx_status check_places(const char* who, const HeadsTensor* t, int n) {
+    for (int i = 0; i < n; ++i)
+        for (int j = 0; j < n; ++j)
+            if (i != j && t[i].output && t[i].p && t[i].p == t[j].p && t[i].rows && t[j].rows) {
+                set_error("%s: %s is where %s is", who, t[i].name, t[j].name);
+                return FX_EINVAL;
+            }
+    return FX_OK;
+}
+
+static fx_status fill_args(const char* who, const fx_attention* d, AttnArgs* a, int64_t tiles, int32_t heads) {
+    const fx_sequences *q = d->q_seqs, *k = d->kv_seqs ? d->kv_seqs : d->q_seqs;
+    a->first_q = q->d_first;
+    a->first_k = k->d_first;
+    a->rows_q = q->rows;
+    a->heads = d->heads;
+    a->kv_heads = d->kv_heads;
+    a->group = d->heads / d->kv_heads;
+    a->causal = d->causal != 0;
+    a->negative = d->scale < 0.f;
+    a->scale = fabsf(d->scale);
+    a->c = fmaxf(a->scale * kLog2e, 0x1p-149f);       // not 0: a masked score is -infinity and stays it
+    a->head_major = k->longest > 2048;
+    if (tiles * heads > (1ll << 32) / 256 - 8) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }
+    return FX_OK;
+}
+
+}  // namespace fx
+
+using namespace fx;
+
+extern "C" fx_status fx_attention_fwd(const fx_attention* d, void* d_out, int64_t ld_out, int64_t hs_out, float* d_lse, void* stream) {
+    const char* who = "fx_attention_fwd";
+    FX_TRY(check_attention(who, d));
+    const int64_t nq = d->q_seqs->rows, nk = d->kv_seqs ? d->kv_seqs->rows : nq;
+    AttnArgs a{};
+    HeadsTensor t[] = {{"d_q", d->d_q, d->ld_q, d->hs_q, nq, d->heads, false, true, &a.q},
+                  {"d_k", d->d_k, d->ld_k, d->hs_k, nk, d->kv_heads, false, true, &a.k},
+                  {"d_v", d->d_v, d->ld_v, d->hs_v, nk, d->kv_heads, false, true, &a.v},
+                  {"d_out", d_out, ld_out, hs_out, nq, d->heads, true, true, &a.out}};
+    for (const HeadsTensor& x : t) FX_TRY(check_heads(who, x, d->dim, dtype_size(d->dt)));
+    if ((uintptr_t)d_lse % 4) { set_error("%s: d_lse is not aligned to its elements", who); return FX_EINVAL; }
+    FX_TRY(check_places(who, t, 4));
+    const int64_t tiles = d->q_seqs->n_tiles[1];
+    FX_TRY(fill_args(who, d, &a, tiles, d->heads));
+    if (nq == 0) return FX_OK;
+    hipStream_t st = (hipStream_t)stream;
+    ProfScope ps(kProfAttnFwd, st);
+    Scratch scratch(st);
+    bool copied[4];
+    int dim;
+    FX_TRY(take_tensors(who, t, 4, d->dim, d->dt, &scratch, copied, &dim, st));
+    a.dim_bytes = dim * dtype_size(d->dt);
+    a.lse = d_lse;
+    a.tiles = d->q_seqs->d_tiles[1];
+    a.n_tiles = (int32_t)tiles;
+    const unsigned blocks = (unsigned)((tiles * d->heads + 7) / 8 * 8);
+    if (d->dt == FX_F32) launch_fwd_dim<FX_F32>(a, dim, blocks, st);
+    else if (d->dt == FX_F16) launch_fwd_dim<FX_F16>(a, dim, blocks, st);
+    else launch_fwd_dim<FX_BF16>(a, dim, blocks, st);
+    return_tensors(t, 4, d->dim, d->dt, copied, dim, st);
+    FX_HIP_TRY(hipGetLastError());
+    return FX_OK;
+}
+
+extern "C" fx_status fx_attention_bwd(const fx_attention* d, const void* d_out, int64_t ld_out, int64_t hs_out, const float* d_lse, const void* d_gout,
+                                      int64_t ld_gout, int64_t hs_gout, const float* d_glse, void* d_gq, int64_t ld_gq, int64_t hs_gq, void* d_gk,
+                                      int64_t ld_gk, int64_t hs_gk, void* d_gv, int64_t ld_gv, int64_t hs_gv, void* stream) {
+    const char* who = "fx_attention_bwd";
+    FX_TRY(check_attention(who, d));
+    const fx_sequences* kq = d->kv_seqs ? d->kv_seqs : d->q_seqs;
+    const int64_t nq = d->q_seqs->rows, nk = kq->rows;
+    AttnArgs a{};
+    const int n = 8;
+    HeadsTensor t[n] = {{"d_q", d->d_q, d->ld_q, d->hs_q, nq, d->heads, false, true, &a.q},
+                   {"d_k", d->d_k, d->ld_k, d->hs_k, nk, d->kv_heads, false, true, &a.k},
+                   {"d_v", d->d_v, d->ld_v, d->hs_v, nk, d->kv_heads, false, true, &a.v},
+                   {"d_out", d_out, ld_out, hs_out, nq, d->heads, false, true, &a.out},
+                   {"d_gout", d_gout, ld_gout, hs_gout, nq, d->heads, false, true, &a.gout},
+                   {"d_gq", d_gq, ld_gq, hs_gq, nq, d->heads, true, false, &a.gq},
+                   {"d_gk", d_gk, ld_gk, hs_gk, nk, d->kv_heads, true, false, &a.gk},
+                   {"d_gv", d_gv, ld_gv, hs_gv, nk, d->kv_heads, true, false, &a.gv}};
+    for (const HeadsTensor& x : t) FX_TRY(check_heads(who, x, d->dim, dtype_size(d->dt)));
+    if ((nq > 0 && !d_lse) || (uintptr_t)d_lse % 4 || (uintptr_t)d_glse % 4) { set_error("%s: d_lse is null, or it or d_glse is not aligned to its elements", who); return FX_EINVAL; }
+    FX_TRY(check_places(who, t, n));
+    FX_TRY(fill_args(who, d, &a, d->q_seqs->n_tiles[1], d->heads));
+    FX_TRY(fill_args(who, d, &a, kq->n_tiles[1], d->kv_heads));
+    if (nq == 0 && nk == 0) return FX_OK;
+    hipStream_t st = (hipStream_t)stream;
+    ProfScope ps(kProfAttnBwd, st);
+    Scratch scratch(st);
+    bool copied[n];
+    int dim;
+    FX_TRY(take_tensors(who, t, n, d->dim, d->dt, &scratch, copied, &dim, st));
+    void* delta = nullptr;
+    FX_TRY(scratch.get(who, &delta, (size_t)nq * d->heads * 4));
+    a.dim_bytes = dim * dtype_size(d->dt);
+    a.lse = const_cast<float*>(d_lse);
+    a.glse = d_glse;
+    a.delta = (float*)delta;
+    a.tiles = d->q_seqs->d_tiles[1];
+    a.n_tiles = (int32_t)d->q_seqs->n_tiles[1];
+    FX_TRY(attention_bwd_launch(a, d->dt, dim, d->q_seqs->longest, kq->longest, kq->d_tiles[1], (int32_t)kq->n_tiles[1], d_gk || d_gv, st));
+    return_tensors(t, n, d->dim, d->dt, copied, dim, st);
+    FX_HIP_TRY(hipGetLastError());
+    return FX_OK;
+}

@@ -65,7 +65,8 @@ enum ProfSlot {
     kProfInsertLeaf, kProfScanLeaf, kProfGridIjk, kProfNbmap, kProfLeafNeighbors, kProfBuildTiles,
     kProfPackWeights, kProfConvMfma, kProfConvGather, kProfConvLowdepth, kProfConvScalar, kProfMemset,
     kProfDgradStrided, kProfWgrad, kProfWgradReduce, kProfPool, kProfUpsample, kProfConvLeaf, kProfSmallGrid,
-    kProfScanFwd, kProfScanBwd, kProfBlockFwd, kProfBlockBwd, kProfBlockSums, kProfDropout, kProfSlotCount
+    kProfScanFwd, kProfScanBwd, kProfBlockFwd, kProfBlockBwd, kProfBlockSums, kProfDropout,
+    kProfAttnFwd, kProfAttnBwd, kProfCache, kProfAttnStep, kProfSlotCount
 };
 bool prof_enabled();
 void prof_begin(int slot, hipStream_t s);

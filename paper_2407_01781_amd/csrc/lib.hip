@@ -253,7 +253,8 @@ static const char* kProfNames[kProfSlotCount] = {
     "scan_leaves", "k_grid_ijk", "k_nbmap", "k_leaf_neighbors", "k_build_tiles", "k_pack_weights",
     "k_conv_mfma", "k_conv_gather", "k_conv_lowdepth",
     "k_conv_scalar", "memset", "k_dgrad_strided", "k_wgrad", "k_wgrad_reduce", "k_pool2", "k_upsample2", "k_conv_leaf", "k_small_grid",
-    "gated_scan_fwd", "gated_scan_bwd", "k_block_fwd", "k_block_bwd", "k_block_sums", "k_dropout"};
+    "gated_scan_fwd", "gated_scan_bwd", "k_block_fwd", "k_block_bwd", "k_block_sums", "k_dropout",
+    "attention_fwd", "attention_bwd", "kv_cache", "attention_step"};
 
 }  // namespace fx
 

@@ -29,20 +29,9 @@
 // instructions fill 40 % of the time, the tickets (11.6 ns each at one address) take 45 us of all in turn.  Gradients of
 // 1,068,658 x 64 f16 in four sequences (821 MB, 161 us): 207 us, 4.0 TB/s.
 #include "rows.h"
+#include "sequences.h"
 
 #include <new>
-
-struct fx_sequences {
-    int64_t rows = 0;
-    int32_t B = 0, n_empty = 0;
-    void* buf = nullptr;
-    hipStream_t stream = nullptr;
-    // bit r: a sequence begins at row r; row `rows` counts as a beginning.  Words up to the one after that.
-    const uint64_t* d_begin = nullptr;
-    const int32_t* d_rank = nullptr;        // beginnings before each word
-    const int32_t* d_id = nullptr;          // number of the k-th sequence that is not empty
-    const int32_t* d_empty = nullptr;       // numbers of the empty ones
-};
 
 namespace fx {
 
@@ -653,6 +642,30 @@ static fx_status run_scan(ScanArgs& a, fx_dtype dt, bool up, hipStream_t st) {
     return launch_scan_kind<FX_BF16, BWD>(a, up, st);
 }
 
+// Lists the tiles of every kind (fx_sequences::d_tiles): sequences from long to short (by the power of two of their
+// lengths), and a sequence's tiles from its last on.  Returns the longest length.
+static int64_t list_tiles(const int64_t* h_joffsets, int32_t B, SeqTile* out, const int64_t* n_tiles) {
+    int64_t count[33] = {}, longest = 0;
+    auto cls = [](int64_t len) { return len ? 64 - __builtin_clzll((unsigned long long)len) : 0; };
+    for (int t = 0; t < kSeqTileKinds; ++t) {
+        const int64_t T = kSeqTileRows[t];
+        for (int64_t& c : count) c = 0;
+        for (int32_t b = 0; b < B; ++b) {
+            const int64_t len = h_joffsets[2 * b + 1] - h_joffsets[2 * b];
+            count[cls(len)] += (len + T - 1) / T;
+            longest = std::max(longest, len);
+        }
+        for (int64_t c = 32, at = 0; c >= 0; --c) { const int64_t n = count[c]; count[c] = at; at += n; }
+        for (int32_t b = 0; b < B; ++b) {
+            const int64_t len = h_joffsets[2 * b + 1] - h_joffsets[2 * b];
+            int64_t& at = count[cls(len)];
+            for (int64_t r = (len + T - 1) / T * T - T; r >= 0; r -= T) out[at++] = SeqTile{b, (int32_t)r};
+        }
+        out += n_tiles[t];
+    }
+    return longest;
+}
+
 }  // namespace fx
 
 using namespace fx;
@@ -672,7 +685,12 @@ extern "C" fx_status fx_build_sequences(const int64_t* h_joffsets, int32_t B, in
     if (rows > 0x7FFFFFFFll) { set_error("%s: more than 2^31-1 rows", who); return FX_ERANGE; }
     hipStream_t st = (hipStream_t)stream;
     const int64_t words = rows / 64 + 2;
-    const size_t bytes = (size_t)words * 12 + (size_t)B * 8;
+    int64_t n_tiles[kSeqTileKinds];
+    for (int t = 0; t < kSeqTileKinds; ++t) {
+        n_tiles[t] = 0;
+        for (int32_t b = 0; b < B; ++b) n_tiles[t] += (h_joffsets[2 * b + 1] - h_joffsets[2 * b] + kSeqTileRows[t] - 1) / kSeqTileRows[t];
+    }
+    const size_t bytes = (size_t)words * 12 + (size_t)B * 8 + 4 + (size_t)(n_tiles[0] + n_tiles[1]) * sizeof(fx::SeqTile);
     void* staging = nullptr;
     FX_HIP_TRY(hipStreamSynchronize(st));           // an upload before this one may still read the staging area
     FX_TRY(host_staging(&staging, bytes, 1));
@@ -689,6 +707,11 @@ extern "C" fx_status fx_build_sequences(const int64_t* h_joffsets, int32_t B, in
     }
     begin[rows >> 6] |= 1ull << (rows & 63);
     for (int64_t w = 0, n = 0; w < words; ++w) { rank[w] = (int32_t)n; n += __builtin_popcountll(begin[w]); }
+    int32_t* first = ids + B;
+    for (int32_t b = 0; b < B; ++b) first[b] = (int32_t)h_joffsets[2 * b];
+    first[B] = (int32_t)rows;
+    SeqTile* tiles = (SeqTile*)(first + B + 1);
+    const int64_t longest = list_tiles(h_joffsets, B, tiles, n_tiles);
     fx_sequences* q = new (std::nothrow) fx_sequences;
     if (!q) { set_error("%s: out of host memory", who); return FX_ENOMEM; }
     const fx_status s = dev_alloc(&q->buf, bytes, st);
@@ -708,6 +731,11 @@ extern "C" fx_status fx_build_sequences(const int64_t* h_joffsets, int32_t B, in
     q->d_rank = (const int32_t*)(q->d_begin + words);
     q->d_id = q->d_rank + words;
     q->d_empty = q->d_id + some;
+    q->d_first = q->d_id + B;
+    q->d_tiles[0] = (const SeqTile*)(q->d_first + B + 1);
+    q->d_tiles[1] = q->d_tiles[0] + n_tiles[0];
+    for (int t = 0; t < kSeqTileKinds; ++t) q->n_tiles[t] = n_tiles[t];
+    q->longest = longest;
     *out = q;
     return FX_OK;
 }

@@ -1,0 +1,279 @@
+"""GPU parity of attention over packed sequences, forward and backward, against the formulas in 64 bits: lengths around the
+tiles (32, 64, 128 rows), sequences without rows or without keys, every type, head layouts and strides, groups of heads, dimensions that are
+no multiple of anything, infinities and NaN outside of what a row sees, streams and graphs."""
+import numpy as np
+import pytest
+import torch
+
+import attention_reference as A
+import gpu_common as H
+import paper_2407_01781_amd as fx
+
+pytestmark = pytest.mark.gpu
+
+
+def _joff(lens):
+    b = np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+    return b, np.stack([b[:-1], b[1:]], 1)
+
+
+def _f64(t):
+    return t.double().cpu().numpy()
+
+
+def draw(seed, n, h, d, dtype, layout="rows", std=1.0):
+    """A tensor of heads in one of several orders in memory, and its values in 64 bits."""
+    rng = np.random.default_rng(seed)
+    v = torch.from_numpy((rng.standard_normal((n, h, d)) * std).astype(np.float32)).to(H.TORCH_DT[dtype])
+    if layout == "rows":
+        t = v.cuda()
+    elif layout == "columns":           # a column range of a wider tensor, 16 bytes aligned where d is
+        wide = torch.full((n, h + 3, d), 7.0, dtype=v.dtype, device="cuda")
+        wide[:, 1:h + 1] = v.cuda()
+        t = wide[:, 1:h + 1]
+    elif layout == "heads":
+        t = v.permute(1, 0, 2).contiguous().cuda().permute(1, 0, 2)
+    else:                               # aligned to an element only
+        flat = torch.full((n * h * (d + 1) + 1,), 7.0, dtype=v.dtype, device="cuda")
+        t = flat[1:].view(n, h, d + 1)[:, :, :d]
+        t.copy_(v.cuda())
+    return t, v.double().numpy()
+
+
+def run(lens, heads, kv_heads, d, dtype, causal, kv_lens=None, layout="rows", scale=None, glse=False, seed=1, backward=True, std=1.5):
+    bq, jq = _joff(lens)
+    bk, jk = (bq, jq) if kv_lens is None else _joff(kv_lens)
+    q, q64 = draw(seed, bq[-1], heads, d, dtype, layout, std)
+    k, k64 = draw(seed + 1, bk[-1], kv_heads, d, dtype, layout)
+    v, v64 = draw(seed + 2, bk[-1], kv_heads, d, dtype, layout)
+    s = d ** -0.5 if scale is None else scale
+    seqs, kv = fx.build_sequences(jq), None if kv_lens is None else fx.build_sequences(jk)
+    out, lse = fx.attention_fwd(seqs, q, k, v, causal=causal, scale=scale, kv_seqs=kv)
+    ro, rl, bo, bl = A.attention(q64, k64, v64, bq, bk, causal, s, dtype)
+    A.check(_f64(out), ro, bo, dtype, "out")
+    A.check(_f64(lse), rl, bl, "f32", "lse")
+    if not backward:
+        return
+    go, go64 = draw(seed + 3, bq[-1], heads, d, dtype, layout)
+    gl = torch.from_numpy(np.random.default_rng(seed + 4).standard_normal((heads, int(bq[-1]))).astype(np.float32)).cuda() if glse else None
+    got = fx.attention_bwd(seqs, q, k, v, out, lse, go, grad_lse=gl, causal=causal, scale=scale, kv_seqs=kv)
+    ref = A.attention_grad(q64, k64, v64, go64, bq, bk, causal, s, dtype, _f64(gl) if glse else None)
+    for name, x, y, b in zip(("gq", "gk", "gv"), got, ref[:3], ref[3:]):
+        A.check(_f64(x), y, b, dtype, name)
+    again = fx.attention_bwd(seqs, q, k, v, out, lse, go, grad_lse=gl, causal=causal, scale=scale, kv_seqs=kv)
+    assert all(torch.equal(x, y) for x, y in zip(got, again))
+
+
+LENS = {"one": [1], "two": [2], "31": [31], "32": [32], "33": [33], "64": [64], "65": [65], "128": [128], "129": [129], "300": [300],
+        "ragged": [0, 3, 1, 0, 0, 200, 2, 64, 8, 1, 131, 0], "singles": [1] * 50, "none": [0, 0], "no sequence": []}
+
+
+@pytest.mark.parametrize("lens", list(LENS))
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f32", 32), ("f16", 128)])
+def test_lengths(lens, causal, dtype, d):
+    run(LENS[lens], 4, 2, d, dtype, causal)
+
+
+@pytest.mark.parametrize("d", [1, 3, 8, 16, 24, 31, 32, 33, 40, 45, 63, 64, 72, 96, 100, 128, 136, 192, 255, 256])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_dimensions(d, dtype):
+    run([70, 0, 33], 2, 1, d, dtype, d % 2 == 0)
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (3, 3), (6, 2), (8, 1), (5, 1), (16, 4)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_groups_of_heads(heads, kv_heads, causal):
+    run([50, 140, 7], heads, kv_heads, 32, "bf16", causal, glse=True)
+
+
+@pytest.mark.parametrize("layout", ["columns", "heads", "odd"])
+@pytest.mark.parametrize("dtype,d", [("f32", 32), ("bf16", 64), ("f16", 20)])
+def test_layouts(layout, dtype, d):
+    run([60, 100], 4, 2, d, dtype, True, layout=layout)
+
+
+@pytest.mark.parametrize("kv_lens", [[0, 5, 300, 1, 64], [200, 0, 3, 0, 1], [1, 1, 1, 1, 1], [0, 0, 0, 0, 0]])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_keys_of_another_set(kv_lens, causal, dtype):
+    """Causal with fewer keys than queries: the first rows see none."""
+    run([70, 5, 40, 0, 130], 2, 2, 32, dtype, causal, kv_lens=kv_lens, glse=True)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 2.0])
+def test_scales(scale):
+    run([40, 150], 2, 1, 32, "f32", True, scale=scale)
+    run([40, 150], 2, 1, 64, "bf16", False, scale=scale)
+
+
+def test_longer():
+    run([1500, 700], 2, 1, 64, "bf16", True)
+    run([1500, 700], 2, 1, 128, "f16", False)
+
+
+def test_sharp():
+    """Scores of some hundred: one key takes all, the maximum moves from tile to tile."""
+    run([400], 2, 1, 64, "bf16", False, std=40.0)
+    run([400], 2, 1, 64, "f32", True, std=40.0)
+
+
+def _caches(store, dtype, pages, page, kvh, d):
+    return fx.KVCache.empty(pages, page, kvh, d, torch.float8_e4m3fn if store == "e4m3" else H.TORCH_DT[dtype])
+
+
+def _tables(rng, ends, page, extra=2):
+    need = [-(-int(e) // page) for e in ends]
+    order = rng.permutation(sum(need) + extra)
+    t = np.full((len(ends), max([1] + need)), -1, np.int32)
+    at = 0
+    for b, n in enumerate(need):
+        t[b, :n] = order[at:at + n]
+        at += n
+    return torch.from_numpy(t).cuda(), len(order)
+
+
+def _held(x64, store):
+    return A.quantised(x64) if store == "e4m3" else x64
+
+
+@pytest.mark.parametrize("page", [1, 5, 16, 64, 100])
+@pytest.mark.parametrize("dtype,store,d", [("bf16", "bf16", 64), ("f16", "e4m3", 40), ("f32", "f32", 33), ("f32", "e4m3", 128), ("bf16", "e4m3", 7), ("f16", "f16", 256)])
+def test_cache_and_step(page, dtype, store, d):
+    """Rows of a prompt written at once, one more for every sequence, read back, and the step over them."""
+    rng = np.random.default_rng(page + d)
+    lens, kvh, heads = [0, 1, 37, 300, 64, 16], 2, 6
+    bounds, jo = _joff(lens)
+    table, pages = _tables(rng, np.array(lens) + 1, page)
+    cache = _caches(store, dtype, pages, page, kvh, d)
+    k, k64 = draw(3, bounds[-1], kvh, d, dtype, "columns")
+    v, v64 = draw(4, bounds[-1], kvh, d, dtype, "odd")
+    k1, k164 = draw(5, len(lens), kvh, d, dtype)
+    v1, v164 = draw(6, len(lens), kvh, d, dtype)
+    zero, at = torch.zeros(len(lens), dtype=torch.int32, device="cuda"), torch.tensor(lens, dtype=torch.int32, device="cuda")
+    fx.cache_write(cache, table, zero, k, v, seqs=fx.build_sequences(jo))
+    fx.cache_write(cache, table, at, k1, v1)
+    b2, jo2 = _joff(np.array(lens) + 1)
+    rk, rv = fx.cache_read(cache, table, zero, fx.build_sequences(jo2), dtype=H.TORCH_DT[dtype])
+    both = [np.concatenate([np.concatenate([x[a:b], y[i:i + 1]]) for i, (a, b) in enumerate(jo)]) for x, y in ((k64, k164), (v64, v164))]
+    held = [_held(x, store) for x in both]
+    for got, want in zip((rk, rv), held):
+        assert torch.equal(got.cpu(), torch.from_numpy(want).to(H.TORCH_DT[dtype]))
+    q, q64 = draw(7, len(lens), heads, d, dtype, "odd")
+    out, lse = fx.attention_step(cache, table, at + 1, q)
+    one = np.arange(len(lens) + 1)
+    ro, rl, bo, bl = A.attention(q64, *held, one, b2, False, d ** -0.5, dtype)
+    A.check(_f64(out), ro, bo, dtype, "out")
+    A.check(_f64(lse), rl.T, bl.T, "f32", "lse")
+
+
+@pytest.mark.parametrize("store", ["e4m3", "bf16"])
+def test_step_lengths(store):
+    """Lengths of nothing, one, and around the tiles; longer than the table; cut by `longest`; below zero."""
+    rng = np.random.default_rng(2)
+    lens, page, kvh, heads, d = [0, 1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 2000, 4095], 16, 1, 5, 64
+    bounds, jo = _joff(lens)
+    table, pages = _tables(rng, lens, page)
+    cache = _caches(store, "bf16", pages, page, kvh, d)
+    k, k64 = draw(3, bounds[-1], kvh, d, "bf16")
+    v, v64 = draw(4, bounds[-1], kvh, d, "bf16")
+    q, q64 = draw(7, len(lens), heads, d, "bf16", std=2.0)
+    fx.cache_write(cache, table, torch.zeros(len(lens), dtype=torch.int32, device="cuda"), k, v, seqs=fx.build_sequences(jo))
+    held = _held(k64, store), _held(v64, store)
+    for given, longest in ((lens, 0), ([n - 20 for n in lens], 0), (lens, 50), (lens, 1 << 40), ([n + 10 ** 9 if n > 4000 else n for n in lens], 0)):
+        real = np.clip(np.minimum(given, longest or 1 << 40), 0, [-(-n // page) * page if n != 2000 else 4095 for n in lens])
+        real = np.minimum(real, lens)
+        parts = [np.concatenate([x[a:a + n] for (a, _), n in zip(jo, real)]) for x in held]
+        out, lse = fx.attention_step(cache, table, torch.tensor(given, dtype=torch.int32, device="cuda"), q, longest=longest)
+        if max(given) > 10 ** 8:        # behind the last page: the sequence's whole last page is seen, 4095 rows and one of zeros
+            out, lse, q_, = out[:-1], lse[:-1], q64[:-1]
+            real = real[:-1]
+            parts = [x[:int(real.sum())] for x in parts]
+        else:
+            q_ = q64
+        ro, rl, bo, bl = A.attention(q_, *parts, np.arange(len(real) + 1), np.concatenate([[0], np.cumsum(real)]), False, d ** -0.5, "bf16")
+        A.check(_f64(out), ro, bo, "bf16", "out")
+        A.check(_f64(lse), rl.T, bl.T, "f32", "lse")
+
+
+def test_pages_that_are_none():
+    """Numbers that are no page, inside a sequence and at its end: not written, zeros when read, not seen."""
+    page, kvh, heads, d, n = 8, 2, 4, 32, 61
+    table = torch.tensor([[3, -1, 5, 99, 0, -2147483648, 2147483647, 1]], dtype=torch.int32, device="cuda")
+    there = np.array([page_of in (3, 5, 0, 1) for page_of in table[0].tolist()])[np.arange(n) // page]
+    for store in ("f16", "e4m3"):
+        cache = _caches(store, "f16", 6, page, kvh, d)
+        before = [t.clone().view(torch.uint8) for t in (cache.k, cache.v)]
+        k, k64 = draw(3, n, kvh, d, "f16")
+        v, v64 = draw(4, n, kvh, d, "f16")
+        seqs, zero = fx.build_sequences([[0, n]]), torch.zeros(1, dtype=torch.int32, device="cuda")
+        fx.cache_write(cache, table, zero - 5, k, v, seqs=seqs)         # the first five have no place either
+        fx.cache_write(cache, table, zero, k, v, seqs=seqs)
+        assert torch.equal(cache.k.view(torch.uint8)[[2, 4]], before[0][[2, 4]]) and torch.equal(cache.v.view(torch.uint8)[[2, 4]], before[1][[2, 4]])
+        rk, rv = fx.cache_read(cache, table, zero, seqs, dtype=torch.float16)
+        held = [_held(x, store) * there[:, None, None] for x in (k64, v64)]
+        assert torch.equal(rk.cpu(), torch.from_numpy(held[0]).half()) and torch.equal(rv.cpu(), torch.from_numpy(held[1]).half())
+        q, q64 = draw(7, 1, heads, d, "f16")
+        out, lse = fx.attention_step(cache, table, zero + n, q)
+        parts = [x[there] for x in held]
+        ro, rl, bo, bl = A.attention(q64, *parts, [0, 1], [0, len(parts[0])], False, d ** -0.5, "f16")
+        A.check(_f64(out), ro, bo, "f16", "out")
+        A.check(_f64(lse), rl.T, bl.T, "f32", "lse")
+        out, lse = fx.attention_step(cache, torch.full_like(table, -1), zero + n, q)
+        assert not out.any() and torch.isneginf(lse).all()
+
+
+def test_values_of_a_cache_of_8_bits():
+    """Every size of row, ties, subnormal codes, zeros, infinities and NaN."""
+    d = 16
+    rng = np.random.default_rng(4)
+    x = rng.standard_normal((4096, 1, d)).astype(np.float32) * np.exp2(rng.integers(-140, 120, size=(4096, 1, 1))).astype(np.float32)
+    x[0], x[1, 0, 3], x[2, 0, 4], x[3, 0, 5] = 0, np.inf, -np.inf, np.nan
+    x[4, 0] = [448, 432, 416, 1, 1.0625, 1.1875, -1.0625, 0, 2.0 ** -9, 2.0 ** -10, 3 * 2.0 ** -10, -2.0 ** -10, 447, 440, 2.0 ** -6, 2.0 ** -7]
+    x[5, 0] = np.float32(448.00003)
+    x[6, 0] = np.float32(3.4e38)
+    x[7, 0], x[7, 0, 0] = 2.0 ** -149, 0
+    x[8], x[8, 0, 0] = np.nan, 1
+    x[9] = np.inf
+    n = len(x)
+    cache = _caches("e4m3", "f32", 64, 64, 1, d)
+    table, zero = torch.arange(64, dtype=torch.int32, device="cuda")[None], torch.zeros(1, dtype=torch.int32, device="cuda")
+    t = torch.from_numpy(x).cuda()
+    fx.cache_write(cache, table, zero, t, -t, seqs=fx.build_sequences([[0, n]]))
+    k, v = fx.cache_read(cache, table, zero, fx.build_sequences([[0, n]]), dtype=torch.float32)
+    with np.errstate(over="ignore"):        # read as fp32: 256 * 2^120, what 3.4e38 is rounded to, is its infinity
+        want = A.quantised(x.astype(np.float64)).astype(np.float32).astype(np.float64)
+    for got, ref in ((_f64(k), want), (_f64(v), -want)):
+        bad = ~((got == ref) | (np.isnan(got) & np.isnan(ref)))
+        assert not bad.any(), (np.argwhere(bad)[:5], got[bad][:5], ref[bad][:5])
+    assert np.array_equal(cache.k_exp.cpu().numpy().reshape(-1)[:n], A.exponents(x[:, 0].astype(np.float64)))
+
+
+def test_a_running_sequence_is_the_causal_one():
+    """A prompt's rows by one call and its keys into the cache, further rows one at a time: the rows of one causal call over all."""
+    n, prompt, heads, kvh, d = 150, 100, 4, 2, 32
+    q, _ = draw(1, n, heads, d, "f32")
+    k, k64 = draw(2, n, kvh, d, "f32")
+    v, v64 = draw(3, n, kvh, d, "f32")
+    whole, wl = fx.attention_fwd(fx.build_sequences([[0, n]]), q, k, v, causal=True)
+    first, _ = fx.attention_fwd(fx.build_sequences([[0, prompt]]), q[:prompt], k[:prompt], v[:prompt], causal=True)
+    cache = fx.KVCache.empty(12, 16, kvh, d, torch.float32)
+    table = torch.from_numpy(np.random.default_rng(1).permutation(12).astype(np.int32)).cuda()[None]
+    start = torch.zeros(1, dtype=torch.int32, device="cuda")
+    fx.cache_write(cache, table, start, k[:prompt], v[:prompt], seqs=fx.build_sequences([[0, prompt]]))
+    rows, lses, start = [first], [], start + prompt
+    for r in range(prompt, n):
+        fx.cache_write(cache, table, start, k[r:r + 1], v[r:r + 1])
+        start += 1
+        o, l = fx.attention_step(cache, table, start, q[r:r + 1])
+        rows.append(o)
+        lses.append(l)
+    ref, rl, bo, bl = A.attention(_f64(q), k64, v64, [0, n], [0, n], True, d ** -0.5, "f32")
+    A.check(_f64(torch.cat(rows)), ref, bo, "f32", "rows")
+    A.check(_f64(torch.cat(lses)), rl.T[prompt:], bl.T[prompt:], "f32", "lse")
+    A.check(_f64(whole), ref, bo, "f32", "whole")
+    # a chunk of further rows over what the cache holds, read back
+    chunk = fx.build_sequences([[0, n - prompt]])
+    ck, cv = fx.cache_read(cache, table, start * 0, fx.build_sequences([[0, n]]))
+    o, _ = fx.attention_fwd(chunk, q[prompt:], ck, cv, causal=True, kv_seqs=fx.build_sequences([[0, n]]))
+    A.check(_f64(o), ref[prompt:], bo[prompt:], "f32", "chunk")
