@@ -82,13 +82,16 @@ __global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES > 256 ? 1 : 2) void k
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
         top = fmaxf(top, other_half(top));
-        const float m2 = fmaxf(m, top);
-        const float mc = m2 == -INFINITY ? 0.f : m2 * a.c;
-        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m * a.c - mc);
-        m = m2;
-        sum *= f;
+        // The maximum that weights are relative to follows the row's own only when that has grown by a factor of 2^8: acc and
+        // sum are exact in whichever they are, a weight is at most 2^8, and few tiles have to scale what is there.
+        if (__any(top * a.c > m * a.c + 8.f)) {
+            const float m2 = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m2) * a.c);
+            m = m2;
+            sum *= f;
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) acc[c] *= f;
+            for (int c = 0; c < COLS; ++c) acc[c] *= f;
+        }
+        const float mc = m == -INFINITY ? 0.f : m * a.c;
         float part = 0.f;
 #pragma unroll
         for (int t = 0; t < MT; ++t) {

@@ -37,122 +37,476 @@ __host__ __device__ __forceinline__ int exponent_of(float top) {
     return e < 0 ? 0 : e;
 }
 
-template <int DT, bool E4M3>
-__global__ void k_cache_write(CacheArgs c, const int32_t* first, int32_t n_seqs, int64_t rows, HeadsView k, HeadsView v) {
+// Eight elements of a row and head are a lane's; the lanes of a row (a power of two) find its largest value by shuffles.  Bound
+// by HBM: sixteen bytes in and eight to sixteen out a lane, keys and values in one thread so that two loads are in flight.
+struct CacheRows {
+    const int32_t* first;           // sequences, or NULL: a row of each
+    int32_t n_seqs, lanes_log2;
+    int64_t rows;
+    HeadsView k, v;
+};
+
+// Row r's place in the cache (row over pages, heads and positions), or -1
+__device__ __forceinline__ int64_t place_of(const CacheArgs& c, const CacheRows& a, int64_t r, int head) {
+    int64_t seq = r, in = 0;
+    if (a.first) {
+        int lo = 0, hi = a.n_seqs;              // the last sequence that begins at r or before: the one that has row r
+        while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (a.first[mid] <= r) lo = mid; else hi = mid; }
+        seq = lo;
+        in = r - a.first[lo];
+    }
+    return cache_row(c, seq, (int64_t)c.start[seq] + in, head);
+}
+
+// N elements of type T, at once where VEC, else those below n one by one and zeros
+template <typename T, bool VEC> __device__ __forceinline__ void take8(T* x, const T* p, int n) {
+    if (VEC) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) ((u32x4*)x)[i] = n > 0 ? ((const u32x4*)p)[i] : u32x4(0u);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = e < n ? p[e] : T(0.f);
+    }
+}
+template <typename T, bool VEC> __device__ __forceinline__ void put8(T* p, const T* x, int n) {
+    if (VEC) {
+        if (n > 0)
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) ((u32x4*)p)[i] = ((const u32x4*)x)[i];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < n) p[e] = x[e];
+    }
+}
+
+template <int DT, bool E4M3, bool VEC>
+__global__ __launch_bounds__(256) void k_cache_write(CacheArgs c, CacheRows a) {
     typedef typename AttnType<DT>::T T;
-    const int lane = threadIdx.x & 63;
-    for (int64_t i = blockIdx.x * (int64_t)(blockDim.x / 64) + threadIdx.x / 64; i < rows * c.kv_heads; i += (int64_t)gridDim.x * (blockDim.x / 64)) {
-        const int64_t r = i / c.kv_heads;
-        const int head = (int)(i % c.kv_heads);
-        int64_t seq = r, in = 0;
-        if (first) {
-            int lo = 0, hi = n_seqs;            // the last sequence that begins at r or before, and has rows
-            while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (first[mid] <= r) lo = mid; else hi = mid; }
-            seq = lo;
-            in = r - first[lo];
+    const int lanes = 1 << a.lanes_log2, d = (threadIdx.x & (lanes - 1)) * 8;
+    const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> a.lanes_log2, all = a.rows * c.kv_heads;
+    const int64_t u = min(unit, all - 1), r = u / c.kv_heads;       // lanes without a row take part in the shuffles
+    const int head = (int)(u - r * c.kv_heads);
+    const int64_t at = place_of(c, a, r, head);
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        const HeadsView s = which ? a.v : a.k;
+        __attribute__((aligned(16))) T x[8];
+        take8<T, VEC>(x, (const T*)(s.p + r * s.ld + head * s.hs) + d, c.dim - d);
+        unsigned char* to = (which ? c.v : c.k) + (at * c.pitch + d) * (E4M3 ? 1 : AttnType<DT>::ES);
+        const bool write = unit < all && at >= 0 && d < c.pitch;
+        if (E4M3) {
+            float f[8], top = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                f[e] = (float)x[e];
+                top = isfinite(f[e]) ? fmaxf(top, fabsf(f[e])) : top;
+            }
+            for (int o = 1; o < lanes; o *= 2) top = fmaxf(top, __shfl_xor(top, o, 64));
+            const int ex = exponent_of(top);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = isfinite(f[e]) ? ldexpf(f[e], 127 - ex) : NAN;
+            if (write) {
+                *(u32x2*)to = u32x2{to_e4m3(f[0], f[1]) | to_e4m3(f[2], f[3]) << 16, to_e4m3(f[4], f[5]) | to_e4m3(f[6], f[7]) << 16};
+                if (d == 0) (which ? c.v_exp : c.k_exp)[at] = (uint8_t)ex;
+            }
+        } else if (write) {
+            put8<T, true>((T*)to, x, 8);
         }
-        const int64_t at = cache_row(c, seq, (int64_t)c.start[seq] + in, head);
-        if (at < 0) continue;
-        for (int which = 0; which < 2; ++which) {
-            const HeadsView& s = which ? v : k;
-            const T* src = (const T*)(s.p + r * s.ld + head * s.hs);
-            unsigned char* dst = (which ? c.v : c.k) + at * c.pitch * (E4M3 ? 1 : AttnType<DT>::ES);
-            float x[4], top = 0.f;
+    }
+}
+
+template <int DT, bool E4M3, bool VEC>
+__global__ __launch_bounds__(256) void k_cache_read(CacheArgs c, CacheRows a) {
+    typedef typename AttnType<DT>::T T;
+    const int lanes = 1 << a.lanes_log2, d = (threadIdx.x & (lanes - 1)) * 8;
+    const int64_t u = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> a.lanes_log2, r = u / c.kv_heads;
+    if (r >= a.rows || d >= c.dim) return;
+    const int head = (int)(u - r * c.kv_heads);
+    const int64_t at = place_of(c, a, r, head);
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        const HeadsView s = which ? a.v : a.k;
+        __attribute__((aligned(16))) T x[8];
+        const unsigned char* from = (which ? c.v : c.k) + (at * c.pitch + d) * (E4M3 ? 1 : AttnType<DT>::ES);
+        if (E4M3) {
+            u32x2 w = u32x2(0u);
+            int ex = 127;
+            if (at >= 0) { w = *(const u32x2*)from; ex = (which ? c.v_exp : c.k_exp)[at]; }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int d = lane * 4 + e;
-                x[e] = d < c.dim ? (float)src[d] : 0.f;
-                if (isfinite(x[e])) top = fmaxf(top, fabsf(x[e]));
+                const f32v2 f = e & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)w[e >> 1], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)w[e >> 1], false);
+                x[2 * e] = (T)ldexpf(f[0], ex - 127);
+                x[2 * e + 1] = (T)ldexpf(f[1], ex - 127);
             }
-            if (E4M3) {
-                for (int o = 1; o < 64; o *= 2) top = fmaxf(top, __shfl_xor(top, o, 64));
-                const int ex = exponent_of(top);
+        } else {
+            take8<T, true>(x, (const T*)from, at >= 0 ? 8 : 0);
+        }
+        put8<T, VEC>((T*)(s.p + r * s.ld + head * s.hs) + d, x, c.dim - d);
+    }
+}
+
+// ------------------------------------------------------------------ step
+// One new row of every sequence over its pages.  A workgroup takes one key head of one sequence, up to 16 of its query heads,
+// and a chunk of positions; each of its W waves takes every W-th tile of 32 positions and needs no other until the end.
+//   scores     two 16x16 results, keys as rows and query heads as columns: lane l holds keys 4 (l / 16) + r of head l % 16.  A lane loads
+//              16 bytes of the keys l % 16, the contracted dimensions in whatever order makes a load: the query's are in the same.
+//   out        dimensions as rows, heads as columns, over the 32 keys in the order in which the lanes hold their weights.  A lane loads
+//              VE neighbouring dimensions of each of its eight keys -- sixteen lanes a whole row -- and turns the 8 x VE block by byte
+//              permutes into VE operands, dimension VE (l % 16) + j for the j-th.  Nothing of keys or values passes through LDS.
+// Weights are split into a leading and a trailing part (three for fp32 queries over 8 bits), so that the product with 16-bit
+// values loses nothing that the output would show.
+constexpr int kStepTile = 32, kStepHeads = 16;
+
+struct StepArgs {
+    CacheArgs c;
+    HeadsView q, out;
+    float *lse, *part, *stats;          // part [row, head, split, dim], stats [row, head, split, 2]: maximum (base 2), sum
+    int64_t most;
+    int32_t heads, group, groups, splits, chunk;
+    float scale2;                       // scale log2(e)
+    uint32_t magic;                     // p / page_rows = p * magic >> shift for p below 2^31
+    int32_t shift;
+};
+
+template <int DT, bool E4M3, int DP> struct StepShape {
+    static constexpr bool kWide = DT == FX_F32 && !E4M3;           // fp32 keys and values
+    static constexpr int SB = E4M3 ? 1 : AttnType<DT>::ES;         // bytes of a stored element
+    static constexpr int VE = DP / 16;                             // dimensions of a value's row that a lane loads
+    static constexpr int KL = DP * SB / 64;                        // 16-byte loads of a key by a lane
+    static constexpr int QP = !E4M3 || DT == FX_BF16 ? 1 : DT == FX_F16 ? 2 : 3;    // parts of a query
+    static constexpr int PP = E4M3 && DT == FX_F32 ? 3 : 2;                        // parts of a weight
+    // waves of a workgroup that has a sequence to itself: as many as the registers hold without spills
+    static constexpr int kMany = DP > 128 ? 4 : DP > 64 || kWide || (E4M3 && DT != FX_BF16) ? 8 : 16;
+};
+
+template <bool F16> struct Mma16;
+template <> struct Mma16<true> {
+    typedef _Float16 T;
+    typedef f16x8 vec;
+    static __device__ __forceinline__ f32x4 mma(vec a, vec b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Mma16<false> {
+    typedef __bf16 T;
+    typedef bf16x8 vec;
+    static __device__ __forceinline__ f32x4 mma(vec a, vec b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+
+// pairs of codes, as bf16 times 2^(exponent of scale)
+__device__ __forceinline__ uint32_t codes_to_bf16(uint32_t codes, float scale, bool high) {
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    const bf16x2 h = high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false);
+    uint32_t u;
+    __builtin_memcpy(&u, &h, 4);
+    return u;
+}
+
+template <int DT, bool E4M3, int DP, int W>
+__global__ __launch_bounds__(64 * W) void k_attention_step(StepArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef StepShape<DT, E4M3, DP> S;
+    typedef typename AttnType<DT>::T T;
+    typedef Mma16<DT == FX_F16 && !E4M3> M;
+    constexpr int VE = S::VE, KL = S::KL, SB = S::SB, QP = S::QP, PP = S::PP;
+    constexpr int VW = VE * SB >= 4 ? VE * SB / 4 : 1;             // words of a value's piece
+    constexpr int KF = S::kWide ? KL : E4M3 ? 2 * KL : KL;         // operands of a key
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63, g = lane >> 4, m16 = lane & 15;
+    uint32_t item = blockIdx.x;
+    const int split = item % a.splits;
+    item /= a.splits;
+    const int part_of_group = item % a.groups;
+    item /= a.groups;
+    const int kv = item % a.c.kv_heads;
+    const int64_t b = item / a.c.kv_heads;
+    const int64_t len = min((int64_t)a.c.start[b], a.most);
+    const int64_t from = (int64_t)split * a.chunk;
+    if (a.splits > 1 && from >= len) return;           // the join knows as much
+    const int end = (int)max((int64_t)0, min(len, from + a.chunk));
+    const int first_head = kv * a.group + part_of_group * kStepHeads, n_heads = min(kStepHeads, a.group - part_of_group * kStepHeads);
+    const int row_bytes = a.c.pitch * SB;
+
+    // the queries, in the order of the keys' operands; zeros for heads and dimensions that are none
+    u32x4 qw[QP][KF];
+    {
+        const T* qr = (const T*)(a.q.p + b * a.q.ld + (first_head + min(m16, n_heads - 1)) * a.q.hs);
+        const bool some = m16 < n_heads;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = isfinite(x[e]) ? ldexpf(x[e], 127 - ex) : NAN;
-                if (lane * 4 < c.pitch) ((uint32_t*)dst)[lane] = to_e4m3(x[0], x[1]) | to_e4m3(x[2], x[3]) << 16;
-                if (lane == 0) (which ? c.v_exp : c.k_exp)[at] = (uint8_t)ex;
+        for (int f = 0; f < KF; ++f) {
+            constexpr int PER = S::kWide ? 4 : 8;
+            const int d0 = E4M3 ? (f >> 1) * 64 + g * 16 + (f & 1) * 8 : f * (4 * PER) + g * PER;
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < PER; ++e) x[e] = some && d0 + e < a.c.dim ? (float)qr[min(d0 + e, a.c.dim - 1)] : 0.f;
+            if constexpr (S::kWide) {
+                qw[0][f] = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (lane * 4 + e < c.pitch) ((T*)dst)[lane * 4 + e] = lane * 4 + e < c.dim ? src[lane * 4 + e] : T(0.f);
-            }
-        }
-    }
-}
-
-template <int DT, bool E4M3>
-__global__ void k_cache_read(CacheArgs c, const int32_t* first, int32_t n_seqs, int64_t rows, HeadsView k, HeadsView v) {
-    typedef typename AttnType<DT>::T T;
-    const int lane = threadIdx.x & 63;
-    for (int64_t i = blockIdx.x * (int64_t)(blockDim.x / 64) + threadIdx.x / 64; i < rows * c.kv_heads; i += (int64_t)gridDim.x * (blockDim.x / 64)) {
-        const int64_t r = i / c.kv_heads;
-        const int head = (int)(i % c.kv_heads);
-        int lo = 0, hi = n_seqs;
-        while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (first[mid] <= r) lo = mid; else hi = mid; }
-        const int64_t at = cache_row(c, lo, (int64_t)c.start[lo] + r - first[lo], head);
-        for (int which = 0; which < 2; ++which) {
-            const HeadsView& s = which ? v : k;
-            T* dst = (T*)(s.p + r * s.ld + head * s.hs);
-            const unsigned char* src = (which ? c.v : c.k) + at * c.pitch * (E4M3 ? 1 : AttnType<DT>::ES);
-            for (int d = lane; d < c.dim; d += 64) {
-                T x = T(0.f);
-                if (at >= 0) {
-                    if (E4M3) x = (T)ldexpf(__builtin_amdgcn_cvt_pk_f32_fp8((int)src[d], false)[0], (int)(which ? c.v_exp : c.k_exp)[at] - 127);
-                    else x = ((const T*)src)[d];
+                for (int p = 0; p < QP; ++p) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        qw[p][f][e] = Elem<typename M::T>::pack2(x[2 * e], x[2 * e + 1]);
+                        if (p + 1 < QP) {
+                            x[2 * e] -= Elem<typename M::T>::to_float((uint16_t)qw[p][f][e]);
+                            x[2 * e + 1] -= Elem<typename M::T>::to_float((uint16_t)(qw[p][f][e] >> 16));
+                        }
+                    }
                 }
-                dst[d] = x;
             }
         }
     }
+    f32x4 acc[VE];
+#pragma unroll
+    for (int j = 0; j < VE; ++j) acc[j] = f32x4(0.f);
+    float top = -INFINITY, sum = 0.f;
+
+    // row of the cache that position t + lane % 32 has, or -1; asked for one tile ahead
+    const int32_t* table = a.c.table + b * a.c.ld_table;
+    auto row_of = [&](int t) -> int64_t {
+        const uint32_t pos = (uint32_t)t + (lane & 31);
+        if ((int)pos >= end) return -1;
+        const uint32_t col = (uint32_t)(((uint64_t)pos * a.magic) >> a.shift);
+        const int32_t page = table[col];
+        if (page < 0 || page >= a.c.pages) return -1;
+        return ((int64_t)page * a.c.kv_heads + kv) * a.c.page_rows + (pos - col * a.c.page_rows);
+    };
+    int t = (int)from + wave * kStepTile;
+    int64_t row = t < end ? row_of(t) : -1;
+    for (; t < end; t += W * kStepTile) {
+        const uint64_t there = __ballot(row >= 0);          // both halves of the wave hold the same 32
+        const int64_t safe = max(row, (int64_t)0);
+        const int lo = (int)(uint32_t)safe, hi = (int)(safe >> 32);
+        auto row_at = [&](int key) { return ((int64_t)__shfl(hi, key, 64) << 32) | (uint32_t)__shfl(lo, key, 64); };
+        u32x4 kw[2][KL];
+        float k_scale[2], v_scale[8];
+        uint32_t vw[8][VW];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int64_t r = row_at(16 * s + m16);
+            const unsigned char* p = a.c.k + r * row_bytes;
+#pragma unroll
+            for (int i = 0; i < KL; ++i) kw[s][i] = i * 64 + g * 16 < row_bytes ? *(const u32x4*)(p + i * 64 + g * 16) : u32x4(0u);
+            if (E4M3) k_scale[s] = __uint_as_float((uint32_t)a.c.k_exp[r] << 23);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t r = row_at(16 * (i >> 2) + 4 * g + (i & 3));
+            const unsigned char* p = a.c.v + r * row_bytes + m16 * VE * SB;
+            if (E4M3) v_scale[i] = __uint_as_float((uint32_t)a.c.v_exp[r] << 23);
+            if (m16 * VE < a.c.pitch) {
+                if constexpr (VW >= 4) {
+#pragma unroll
+                    for (int w = 0; w < VW; w += 4) { const u32x4 x = *(const u32x4*)(p + 4 * w); vw[i][w] = x[0]; vw[i][w + 1] = x[1]; vw[i][w + 2] = x[2]; vw[i][w + 3] = x[3]; }
+                } else if constexpr (VW == 2) {
+                    const u32x2 x = *(const u32x2*)p;
+                    vw[i][0] = x[0];
+                    vw[i][1] = x[1];
+                } else {
+                    vw[i][0] = *(const uint32_t*)p;
+                }
+            } else {
+#pragma unroll
+                for (int w = 0; w < VW; ++w) vw[i][w] = 0;
+            }
+        }
+        const int next = t + W * kStepTile;
+        row = next < end ? row_of(next) : -1;
+
+        float s[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            f32x4 r = f32x4(0.f);
+            if constexpr (S::kWide) {
+#pragma unroll
+                for (int i = 0; i < KL; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) r = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kw[h][i][e]), __uint_as_float(qw[0][i][e]), r, 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int f = 0; f < KF; ++f) {
+                    u32x4 w;
+                    if constexpr (E4M3) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e] = codes_to_bf16(kw[h][f >> 1][(f & 1) * 2 + (e >> 1)], k_scale[h], e & 1);
+                    } else {
+                        w = kw[h][f];
+                    }
+                    typename M::vec x, y;
+                    __builtin_memcpy(&x, &w, 16);
+#pragma unroll
+                    for (int p = QP - 1; p >= 0; --p) { __builtin_memcpy(&y, &qw[p][f], 16); r = M::mma(x, y, r); }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[4 * h + e] = r[e] * a.scale2;
+        }
+        if (there != ~0ull) {           // keys that are none: no score, and zeros in the place of what lies there
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (!(there >> (16 * (i >> 2) + 4 * g + (i & 3)) & 1)) {
+                    s[i] = -INFINITY;
+#pragma unroll
+                    for (int w = 0; w < VW; ++w) vw[i][w] = 0;
+                }
+        }
+        float best = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+        best = fmaxf(best, __shfl_xor(best, 16, 64));
+        best = fmaxf(best, __shfl_xor(best, 32, 64));
+        if (__any(best > top)) {
+            const float next_top = fmaxf(top, best), f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - next_top);
+            top = next_top;
+            sum *= f;
+#pragma unroll
+            for (int j = 0; j < VE; ++j) acc[j] *= f;
+        }
+        const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            s[i] = __builtin_amdgcn_exp2f(s[i] - base);
+            sum += s[i];
+        }
+        if constexpr (S::kWide) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < VE; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vw[i][j]), s[i], acc[j], 0, 0, 0);
+        } else {
+            typename M::vec p[PP];
+#pragma unroll
+            for (int k = 0; k < PP; ++k) {
+                u32x4 w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    w[e] = Elem<typename M::T>::pack2(s[2 * e], s[2 * e + 1]);
+                    if (k + 1 < PP) {
+                        s[2 * e] -= Elem<typename M::T>::to_float((uint16_t)w[e]);
+                        s[2 * e + 1] -= Elem<typename M::T>::to_float((uint16_t)(w[e] >> 16));
+                    }
+                }
+                __builtin_memcpy(&p[k], &w, 16);
+            }
+#pragma unroll
+            for (int j = 0; j < VE; j += 2) {
+                uint32_t x[8];          // dimensions j and j + 1 of the eight keys
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = E4M3 ? codes_to_bf16(vw[i][j >> 2], v_scale[i], (j >> 1) & 1) : vw[i][j >> 1];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    u32x4 w;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], h ? 0x07060302 : 0x05040100);
+                    typename M::vec v;
+                    __builtin_memcpy(&v, &w, 16);
+#pragma unroll
+                    for (int k = PP - 1; k >= 0; --k) acc[j + h] = M::mma(v, p[k], acc[j + h]);
+                }
+            }
+        }
+    }
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    // the waves' results joined, half of them by the other half at a time
+    float* shared = (float*)smem;
+    constexpr int SLOT = DP * kStepHeads + 2 * kStepHeads;
+#pragma unroll
+    for (int n = W / 2; n >= 1; n /= 2) {
+        if (wave >= n && wave < 2 * n) {
+            float* to = shared + (wave - n) * SLOT;
+#pragma unroll
+            for (int j = 0; j < VE; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) to[(j * 4 + r) * 64 + lane] = acc[j][r];
+            if (g == 0) { to[DP * kStepHeads + m16] = top; to[DP * kStepHeads + kStepHeads + m16] = sum; }
+        }
+        __syncthreads();
+        if (wave < n) {
+            const float* in = shared + wave * SLOT;
+            const float top2 = in[DP * kStepHeads + m16], sum2 = in[DP * kStepHeads + kStepHeads + m16], both = fmaxf(top, top2);
+            const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - both), f2 = top2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top2 - both);
+            top = both;
+            sum = sum * f + sum2 * f2;
+#pragma unroll
+            for (int j = 0; j < VE; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[j][r] = acc[j][r] * f + in[(j * 4 + r) * 64 + lane] * f2;
+        }
+        __syncthreads();
+    }
+    if (wave != 0 || m16 >= n_heads) return;
+    const int head = first_head + m16;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    T* out = (T*)(a.out.p + b * a.out.ld + head * a.out.hs);
+    const int64_t slot = (b * a.heads + head) * a.splits + split;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < VE; ++j) {
+            const int d = (4 * g + r) * VE + j;
+            if (d >= a.c.dim) continue;
+            if (a.splits > 1) a.part[slot * a.c.dim + d] = acc[j][r];
+            else out[d] = (T)(acc[j][r] * inv);
+        }
+    if (g) return;
+    if (a.splits > 1) { a.stats[2 * slot] = top; a.stats[2 * slot + 1] = sum; }
+    else if (a.lse) a.lse[b * a.heads + head] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+#endif
 }
 
-// One wave a row and query head
-template <int DT, bool E4M3>
-__global__ void k_attention_step(CacheArgs c, int64_t rows, int64_t most, int heads, float scale, HeadsView q, HeadsView out, float* lse) {
+// The splits of a row and head joined: factors of the splits in LDS, then their sums, a thread a dimension and every n-th split
+constexpr int kJoinThreads = 512, kMostSplits = 1024;
+template <int DT>
+__global__ __launch_bounds__(kJoinThreads) void k_attention_join(StepArgs a) {
     typedef typename AttnType<DT>::T T;
-    const int lane = threadIdx.x & 63, group = heads / c.kv_heads;
-    const int64_t i = blockIdx.x;
-    const int64_t b = i / heads;
-    const int head = (int)(i % heads), kv = head / group;
-    const T* qr = (const T*)(q.p + b * q.ld + head * q.hs);
-    const int64_t n = c.start[b] < most ? c.start[b] : most;
-    float m = -INFINITY, sum = 0.f, acc[4] = {};
-    for (int64_t p0 = 0; p0 < n; p0 += 64) {
-        const int64_t pos = p0 + lane, at = pos < n ? cache_row(c, b, pos, kv) : -1;
-        float s = -INFINITY;
-        if (at >= 0) {
-            float d = 0.f;
-            const unsigned char* src = c.k + at * c.pitch * (E4M3 ? 1 : AttnType<DT>::ES);
-            for (int e = 0; e < c.dim; ++e) d = fmaf((float)qr[e], E4M3 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)src[e], false)[0] : (float)((const T*)src)[e], d);
-            if (E4M3) d = ldexpf(d, (int)c.k_exp[at] - 127);
-            s = d * scale;
-        }
-        float top = s;
-        for (int o = 1; o < 64; o *= 2) top = fmaxf(top, __shfl_xor(top, o, 64));
-        const float m2 = fmaxf(m, top), mu = m2 == -INFINITY ? 0.f : m2, f = m == -INFINITY ? 0.f : expf(m - mu);
-        m = m2;
-        const float p = at >= 0 ? expf(s - mu) : 0.f;
-        float part = p;
-        for (int o = 1; o < 64; o *= 2) part += __shfl_xor(part, o, 64);
-        sum = sum * f + part;
-        for (int e = 0; e < 4; ++e) acc[e] *= f;
-        for (int j = 0; j < 64; ++j) {
-            const int64_t a2 = __shfl(at, j, 64);
-            const float pj = __shfl(p, j, 64);
-            if (a2 < 0) continue;
-            const unsigned char* src = c.v + a2 * c.pitch * (E4M3 ? 1 : AttnType<DT>::ES);
-            for (int e = 0; e < 4; ++e) {
-                const int d = lane + 64 * e;
-                if (d >= c.dim) continue;
-                float x = E4M3 ? ldexpf(__builtin_amdgcn_cvt_pk_f32_fp8((int)src[d], false)[0], (int)c.v_exp[a2] - 127) : (float)((const T*)src)[d];
-                acc[e] = fmaf(pj, x, acc[e]);
-            }
-        }
+    __shared__ float f[kMostSplits], red[kJoinThreads / 64], sums[kJoinThreads];
+    const int64_t item = blockIdx.x, b = item / a.heads;
+    const int head = (int)(item % a.heads), tid = threadIdx.x;
+    const int64_t len = max((int64_t)0, min((int64_t)a.c.start[b], a.most));
+    const int n = (int)((len + a.chunk - 1) / a.chunk);
+    const float* stats = a.stats + 2 * item * a.splits;
+    float top = -INFINITY;
+    for (int i = tid; i < n; i += kJoinThreads) top = fmaxf(top, stats[2 * i]);
+    for (int o = 1; o < 64; o *= 2) top = fmaxf(top, __shfl_xor(top, o, 64));
+    if ((tid & 63) == 0) red[tid / 64] = top;
+    __syncthreads();
+    for (int i = 0; i < kJoinThreads / 64; ++i) top = fmaxf(top, red[i]);
+    __syncthreads();
+    float sum = 0.f;
+    for (int i = tid; i < n; i += kJoinThreads) {
+        f[i] = stats[2 * i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stats[2 * i] - top);
+        sum += f[i] * stats[2 * i + 1];
     }
-    T* o = (T*)(out.p + b * out.ld + head * out.hs);
-    for (int e = 0; e < 4; ++e)
-        if (lane + 64 * e < c.dim) o[lane + 64 * e] = (T)(sum == 0.f ? 0.f : acc[e] / sum);
-    if (lse && lane == 0) lse[b * heads + head] = sum == 0.f ? -INFINITY : m + logf(sum);
+    for (int o = 1; o < 64; o *= 2) sum += __shfl_xor(sum, o, 64);
+    if ((tid & 63) == 0) red[tid / 64] = sum;
+    __syncthreads();
+    sum = 0.f;
+    for (int i = 0; i < kJoinThreads / 64; ++i) sum += red[i];
+    // as many splits side by side as there are threads for; their sums are added in order
+    const int dim = a.c.dim, lanes = dim <= 32 ? 32 : dim <= 64 ? 64 : dim <= 128 ? 128 : 256, rows = kJoinThreads / lanes, d = tid % lanes;
+    float acc = 0.f;
+    if (d < dim)
+#pragma unroll 8
+        for (int i = tid / lanes; i < n; i += rows) acc = fmaf(f[i], a.part[(item * a.splits + i) * dim + d], acc);
+    sums[tid] = acc;
+    __syncthreads();
+    if (tid >= dim) return;
+    acc = 0.f;
+    for (int r = 0; r < rows; ++r) acc += sums[r * lanes + tid];
+    ((T*)(a.out.p + b * a.out.ld + head * a.out.hs))[tid] = (T)(sum == 0.f ? 0.f : acc / sum);
+    if (a.lse && tid == 0) a.lse[item] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+template <int DT, bool E4M3, int DP> static void launch_step(const StepArgs& a, int64_t blocks, hipStream_t st) {
+    constexpr int SLOT = (DP * kStepHeads + 2 * kStepHeads) * 4;
+    constexpr int MANY = StepShape<DT, E4M3, DP>::kMany;
+    if (MANY == 4 || a.splits > 1) k_attention_step<DT, E4M3, DP, 4><<<(unsigned)blocks, 256, 2 * SLOT, st>>>(a);
+    else k_attention_step<DT, E4M3, DP, MANY><<<(unsigned)blocks, 64 * MANY, MANY / 2 * SLOT, st>>>(a);
+}
+
+template <int DT, bool E4M3> static void launch_step_dim(const StepArgs& a, int64_t blocks, int64_t rows, hipStream_t st) {
+    if (a.c.dim <= 64) launch_step<DT, E4M3, 64>(a, blocks, st);
+    else if (a.c.dim <= 128) launch_step<DT, E4M3, 128>(a, blocks, st);
+    else launch_step<DT, E4M3, 256>(a, blocks, st);
+    if (a.splits > 1) k_attention_join<DT><<<(unsigned)(rows * a.heads), kJoinThreads, 0, st>>>(a);
 }
 
 // ------------------------------------------------------------------ host
@@ -180,6 +534,22 @@ static fx_status check_cache(const char* who, const fx_cache* c, fx_dtype dt, Ca
     return FX_OK;
 }
 
+// Keys and values of a call: their views, whether they can be moved 16 bytes at a time, and the launch
+static fx_status take_rows(const char* who, const HeadsTensor* t, const CacheArgs& c, fx_dtype dt, CacheRows* x, unsigned* blocks, bool* vec) {
+    const int es = dtype_size(dt);
+    HeadsView* view[2] = {&x->k, &x->v};
+    *vec = c.dim % 8 == 0;
+    for (int i = 0; i < 2; ++i) {
+        *view[i] = HeadsView{(unsigned char*)t[i].p, t[i].ld * es, t[i].hs * es};
+        *vec = *vec && (uintptr_t)t[i].p % 16 == 0 && view[i]->ld % 16 == 0 && (t[i].heads == 1 || view[i]->hs % 16 == 0);
+    }
+    while ((8 << x->lanes_log2) < c.pitch) ++x->lanes_log2;
+    const int64_t threads = (x->rows * c.kv_heads) << x->lanes_log2;
+    if (threads > (1ll << 32) - 256) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }
+    *blocks = (unsigned)((threads + 255) / 256);
+    return FX_OK;
+}
+
 }  // namespace fx
 
 using namespace fx;
@@ -198,12 +568,11 @@ extern "C" fx_status fx_cache_write(const fx_cache* c, const fx_sequences* q, in
     a.start = d_start;
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps(kProfCache, st);
-    const int es = dtype_size(dt);
-    const HeadsView k{(unsigned char*)d_k, ld_k * es, hs_k * es}, v{(unsigned char*)d_v, ld_v * es, hs_v * es};
-    const unsigned blocks = (unsigned)std::min<int64_t>((rows * c->kv_heads + 3) / 4, 1 << 16);
-    const int32_t* first = q ? q->d_first : nullptr;
-    const int32_t n = q ? q->B : 0;
-#define FX_RUN(DT, E) k_cache_write<DT, E><<<blocks, 256, 0, st>>>(a, first, n, rows, k, v)
+    CacheRows x{q ? q->d_first : nullptr, q ? q->B : 0, 0, rows, {}, {}};
+    unsigned blocks;
+    bool vec;
+    FX_TRY(take_rows(who, t, a, dt, &x, &blocks, &vec));
+#define FX_RUN(DT, E) do { if (vec) k_cache_write<DT, E, true><<<blocks, 256, 0, st>>>(a, x); else k_cache_write<DT, E, false><<<blocks, 256, 0, st>>>(a, x); } while (0)
 #define FX_RUN_TYPES() do { const bool e = c->store == FX_E4M3; \
         if (dt == FX_F32) { if (e) FX_RUN(FX_F32, true); else FX_RUN(FX_F32, false); } \
         else if (dt == FX_F16) { if (e) FX_RUN(FX_F16, true); else FX_RUN(FX_F16, false); } \
@@ -229,12 +598,11 @@ extern "C" fx_status fx_cache_read(const fx_cache* c, const fx_sequences* q, con
     a.start = d_start;
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps(kProfCache, st);
-    const int es = dtype_size(dt);
-    const HeadsView k{(unsigned char*)d_k, ld_k * es, hs_k * es}, v{(unsigned char*)d_v, ld_v * es, hs_v * es};
-    const unsigned blocks = (unsigned)std::min<int64_t>((rows * c->kv_heads + 3) / 4, 1 << 16);
-    const int32_t* first = q->d_first;
-    const int32_t n = q->B;
-#define FX_RUN(DT, E) k_cache_read<DT, E><<<blocks, 256, 0, st>>>(a, first, n, rows, k, v)
+    CacheRows x{q->d_first, q->B, 0, rows, {}, {}};
+    unsigned blocks;
+    bool vec;
+    FX_TRY(take_rows(who, t, a, dt, &x, &blocks, &vec));
+#define FX_RUN(DT, E) do { if (vec) k_cache_read<DT, E, true><<<blocks, 256, 0, st>>>(a, x); else k_cache_read<DT, E, false><<<blocks, 256, 0, st>>>(a, x); } while (0)
     FX_RUN_TYPES();
 #undef FX_RUN
     FX_HIP_TRY(hipGetLastError());
@@ -255,18 +623,54 @@ extern "C" fx_status fx_attention_step(const fx_cache* c, int64_t rows, const in
     for (const HeadsTensor& x : t) FX_TRY(check_heads(who, x, c->dim, dtype_size(dt)));
     if (rows > 0 && (!d_len || (uintptr_t)d_len % 4 || (uintptr_t)d_lse % 4)) { set_error("%s: d_len is null, or it or d_lse is not aligned to its elements", who); return FX_EINVAL; }
     if (rows > 0 && d_q == d_out) { set_error("%s: d_out is where d_q is", who); return FX_EINVAL; }
-    if (rows * heads > 0x7FFFFFFFll / 64 || rows > 0x7FFFFFFFll) { set_error("%s: too many rows", who); return FX_ERANGE; }
+    if (rows > 0x7FFFFFFFll / 64 / heads) { set_error("%s: too many rows", who); return FX_ERANGE; }
+    const int64_t all = (int64_t)a.cols * a.page_rows;
+    if (all > 0x7FFFFFFFll) { set_error("%s: a table of more than 2^31-1 positions", who); return FX_ERANGE; }
     if (rows == 0) return FX_OK;
     a.start = d_len;
-    const int64_t all = (int64_t)a.cols * a.page_rows;
-    most = most == 0 ? all : std::min(most, all);
+    StepArgs s{};
+    s.c = a;
+    s.most = a.pages == 0 ? 0 : most == 0 ? all : std::min(most, all);
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps(kProfAttnStep, st);
     const int es = dtype_size(dt);
-    const HeadsView q{(unsigned char*)d_q, ld_q * es, hs_q * es}, out{(unsigned char*)d_out, ld_out * es, hs_out * es};
-#define FX_RUN(DT, E) k_attention_step<DT, E><<<(unsigned)(rows * heads), 64, 0, st>>>(a, rows, most, heads, scale, q, out, d_lse)
-    FX_RUN_TYPES();
-#undef FX_RUN
-    FX_HIP_TRY(hipGetLastError());
+    s.q = HeadsView{(unsigned char*)d_q, ld_q * es, hs_q * es};
+    s.out = HeadsView{(unsigned char*)d_out, ld_out * es, hs_out * es};
+    s.lse = d_lse;
+    s.heads = heads;
+    s.group = heads / c->kv_heads;
+    s.groups = (s.group + kStepHeads - 1) / kStepHeads;
+    s.scale2 = scale * kLog2e;
+    while ((1ll << s.shift) < a.page_rows) ++s.shift;
+    s.magic = (uint32_t)((1ull << (31 + s.shift)) / (uint32_t)a.page_rows + 1);
+    s.shift += 31;
+    // Up to 1024 positions a workgroup of 8 or 16 waves takes them all and there is no second launch; beyond, chunks of equal
+    // length, such that there are about eight workgroups for a compute unit where that leaves them 256 positions at least.
+    const int64_t items = rows * c->kv_heads * s.groups;
+    int64_t chunk = std::max<int64_t>(s.most, 1);
+    if (s.most > 1024) {
+        chunk = std::max<int64_t>(256, (s.most * items / (8 * compute_units()) + 127) / 128 * 128);
+        chunk = std::max(chunk, ((s.most + kMostSplits - 1) / kMostSplits + 127) / 128 * 128);
+        chunk = std::min(chunk, s.most);
+    }
+    s.chunk = (int32_t)chunk;
+    s.splits = (int32_t)std::max<int64_t>(1, (s.most + chunk - 1) / chunk);
+    if (items * s.splits > 0x7FFFFFFFll / 64) { set_error("%s: too many rows", who); return FX_ERANGE; }
+    void* part = nullptr;
+    if (s.splits > 1) {
+        FX_TRY(scratch_alloc(who, &part, ((size_t)rows * heads * s.splits) * (a.dim + 2) * 4, st));
+        s.part = (float*)part;
+        s.stats = s.part + (size_t)rows * heads * s.splits * a.dim;
+    }
+    if (c->store == FX_E4M3) {
+        if (dt == FX_F32) launch_step_dim<FX_F32, true>(s, items * s.splits, rows, st);
+        else if (dt == FX_F16) launch_step_dim<FX_F16, true>(s, items * s.splits, rows, st);
+        else launch_step_dim<FX_BF16, true>(s, items * s.splits, rows, st);
+    } else if (dt == FX_F32) launch_step_dim<FX_F32, false>(s, items * s.splits, rows, st);
+    else if (dt == FX_F16) launch_step_dim<FX_F16, false>(s, items * s.splits, rows, st);
+    else launch_step_dim<FX_BF16, false>(s, items * s.splits, rows, st);
+    const hipError_t e = hipGetLastError();
+    dev_free(part, st);
+    if (e != hipSuccess) { set_error("%s: launch failed: %s", who, hipGetErrorString(e)); return FX_EDEVICE; }
     return FX_OK;
 }
