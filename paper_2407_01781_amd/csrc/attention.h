@@ -40,49 +40,65 @@ struct AttnArgs {
 };
 
 // ------------------------------------------------------------------ tiles in LDS
-// ROWS rows of DP elements in pieces of 16 bytes, filled by loads that write LDS directly: lane l of a load writes 16 bytes
-// at 16 l, so the pieces of a row are put in another order by the address that a lane loads from.  Piece c of row r stands
-// at place c ^ mix(r): eight rows' pieces of one column, which a matrix operand's lanes fetch together, lie in different banks.
-template <int RB> __device__ __forceinline__ int mix(int row) {
-    constexpr int CR = RB / 16;
-    if (CR >= 16) return (row & 7) << 1;
-    if (CR == 8) return row & 7;
-    return (row >> 1) & (CR - 1);
-}
-template <int RB> __device__ __forceinline__ int lds_piece(int row, int piece) { return row * RB + ((piece ^ mix<RB>(row)) << 4); }
+// A tile has rows of RB bytes in pieces of 16, filled by loads that write LDS directly: a load writes 1024 bytes in the order of
+// its lanes, R = 1024 / RB rows, so the order of the pieces is a matter of the addresses that the lanes load from.  Segments of four
+// neighbouring pieces stay together (a quad of lanes loads 64 bytes of a row); segment by segment the R rows follow each other,
+// and a row's four pieces are exchanged by x -> x ^ (row / 4).  Then the operands of a matrix instruction, whose
+// lanes take one piece of 32 rows, or by transposing reads 32 bytes of four, meet each bank once, and a lane's addresses
+// are one of two registers plus a constant.
+template <int RB> struct LdsRows {
+    static constexpr int R = 1024 / RB;
+    static constexpr int kPad = R == 2 ? 128 : R == 1 ? 64 : 0;         // fewer than four rows a load: those that follow lie in other banks
+    static constexpr int kLoad = 1024 + kPad;
+    static constexpr int kSegment = R * 64;
+    static_assert(R >= 1 && R * RB == 1024, "rows fill a load");
+    // row part (additive over rows that have no bit in common) and the whole place of a piece
+    static __host__ __device__ constexpr int row_at(int row) { return row / R * kLoad + row % R * 64; }
+    static __device__ __forceinline__ int place(int row, int piece) { return row_at(row) + (piece >> 2) * kSegment + (((piece & 3) ^ (row >> 2 & 3)) << 4); }
+    static constexpr int bytes(int rows) { return rows / R * kLoad; }
+};
 
-// Offsets in the rows of global memory for the loads of a tile by WAVES waves; a piece behind the row's end (dim_bytes) has an
-// offset that no buffer holds and loads as zeros.
+// The loads of a tile of ROWS rows by WAVES waves; a piece behind the row's end (dim_bytes) has an offset that no buffer holds
+// and comes as zeros, and so do rows that do not exist.
 constexpr uint32_t kNowhere = 0x80000000u;
 template <int RB, int ROWS, int WAVES> struct TileLoad {
-    static constexpr int N = ROWS * RB / 1024 / WAVES > 0 ? ROWS * RB / 1024 / WAVES : 1;
-    static constexpr bool kAll = ROWS * RB / 1024 >= WAVES;         // every wave loads
-    static_assert(ROWS * RB % 1024 == 0 && (!kAll || ROWS * RB / 1024 % WAVES == 0), "whole loads");
+    typedef LdsRows<RB> L;
+    static constexpr int kLoads = ROWS / L::R;
+    static constexpr int N = kLoads / WAVES > 0 ? kLoads / WAVES : 1;
+    static_assert(kLoads % WAVES == 0 || kLoads < WAVES, "the waves load equally");
     uint32_t off[N];
     __device__ __forceinline__ void init(int wave, int lane, int64_t ld, int dim_bytes) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int at = (wave * N + i) * 1024 + lane * 16, row = at / RB, piece = ((at % RB) >> 4) ^ mix<RB>(row);
-            off[i] = piece * 16 < dim_bytes ? (uint32_t)(row * (uint32_t)ld + piece * 16) : kNowhere;
+            const int row = (wave * N + i) * L::R + (lane >> 2) % L::R, piece = (lane / (4 * L::R)) * 4 + ((lane & 3) ^ (row >> 2 & 3));
+            off[i] = piece * 16 < dim_bytes ? (uint32_t)row * (uint32_t)ld + piece * 16 : kNowhere;
         }
     }
-    // rows [row0, row0 + ROWS) of `n` behind `base`; those from n on come as zeros
+    // rows [row0, row0 + ROWS) of the n behind `base`
     __device__ __forceinline__ void load(lds_byte* lds, const unsigned char* base, int64_t ld, int row0, int n, int dim_bytes, int wave) const {
-        if (!kAll && wave >= ROWS * RB / 1024) return;
+        if (kLoads < WAVES && wave >= kLoads) return;
         const int rows = min(n - row0, ROWS);
         const uint32_t bytes = rows > 0 ? (uint32_t)(rows - 1) * (uint32_t)ld + (uint32_t)dim_bytes : 0u;
         __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(base + row0 * ld), 0, (int)bytes, 0x27000);
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (wave * N + i) * 1024), 16, off[i], 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (wave * N + i) * L::kLoad), 16, off[i], 0, 0, 0);
     }
 };
 
-// Left or right operand whose contracted index runs along a row: lane l takes pieces 2 step + l / 32 of row l % 32
-template <int DT, int RB> __device__ __forceinline__ typename Elem<typename AttnType<DT>::T>::vec8 row_operand(const lds_byte* tile, int row, int step, int half) {
+// Operand whose contracted index runs along a row: lane l takes pieces 2 step + l / 32 of row l % 32 of the 32 rows from row0 on
+template <int DT, int RB> struct RowReader {
+    typedef LdsRows<RB> L;
     typedef typename Elem<typename AttnType<DT>::T>::vec8 vec;
-    return *(const __attribute__((address_space(3))) vec*)(tile + lds_piece<RB>(row, 2 * step + half));
-}
+    int a[2];
+    __device__ __forceinline__ void init(int lane) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) a[s] = L::place(lane & 31, 2 * s + (lane >> 5));
+    }
+    __device__ __forceinline__ vec operator()(const lds_byte* tile, int row0, int step) const {
+        return *(const __attribute__((address_space(3))) vec*)(tile + a[step & 1] + (step >> 1) * L::kSegment + L::row_at(row0));
+    }
+};
 
 // The same straight from global memory, for the rows that a wave keeps: zeros behind the sequence and behind the row
 template <int DT, int STEPS> struct OwnRows {
@@ -102,9 +118,8 @@ template <int DT, int STEPS> struct OwnRows {
     }
 };
 
-// result += left^T right for 32 rows of a tile: left = columns 32 col .. 32 col + 31 of rows row0 .. row0 + 31, right = the 32x32
-// result p in its registers (row as the contracted index), result row = column of left.
-template <int DT> struct Weights;       // the right operand, packed
+// A 32x32 result in its registers as the right operand of a product over its rows
+template <int DT> struct Weights;
 template <> struct Weights<FX_F32> {
     f32x16 p;
     __device__ __forceinline__ void set(const f32x16& x) { p = x; }
@@ -125,34 +140,42 @@ template <int DT> struct Weights16 {
 template <> struct Weights<FX_F16> : Weights16<FX_F16> {};
 template <> struct Weights<FX_BF16> : Weights16<FX_BF16> {};
 
-template <int DT, int RB> __device__ __forceinline__ void mma_columns(f32x16& acc, const lds_byte* tile, int row0, int col, const Weights<DT>& w, int lane) {
-    const int half = lane >> 5;
-    if constexpr (DT == FX_F32) {
-        const int at = col * 128 + (lane & 31) * 4;
+// acc += (columns 32 col .. 32 col + 31 of the 32 rows from row0 on)^T w, the result's rows the tile's columns
+template <int DT, int RB> struct ColumnProduct {
+    typedef LdsRows<RB> L;
+    int a[2];
+    __device__ __forceinline__ void init(int lane) {
+        const int half = lane >> 5, i = lane & 15;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int row = row0 + 8 * (r >> 2) + 4 * half + (r & 3);
-            const float a = *(const __attribute__((address_space(3))) float*)(tile + lds_piece<RB>(row, at >> 4) + (at & 15));
-            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.p[r], acc, 0, 0, 0);
-        }
-    } else {
-        // a transposing read takes 8 bytes from each of 16 lanes, four rows of 16 columns, and gives lane i its column's four
-        const int i = lane & 15, piece = col * 4 + ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            s16x4 h[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int row = row0 + 16 * t + 8 * e + 4 * half + (i >> 2);
-                h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(tile + lds_piece<RB>(row, piece) + (i & 1) * 8));
-            }
-            const s16x8 a = __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
-            typename Elem<typename AttnType<DT>::T>::vec8 f;
-            __builtin_memcpy(&f, &a, 16);
-            acc = Elem<typename AttnType<DT>::T>::mma(f, w.p[t], acc);
+        for (int e = 0; e < 2; ++e) {
+            // fp32: the lane's column is a word of piece (l % 32) / 4, its rows 4 half + .. of every second group of eight.
+            // 16 bits: a transposing read takes 8 bytes from each of 16 lanes, four rows of 16 columns, and gives each its column's four
+            if (DT == FX_F32) a[e] = L::place(8 * e + 4 * half, (lane & 31) >> 2) + (lane & 3) * 4;
+            else a[e] = L::place(8 * e + 4 * half + (i >> 2), (lane >> 4 & 1) * 2 + ((i & 3) >> 1)) + (i & 1) * 8;
         }
     }
-}
+    __device__ __forceinline__ void operator()(f32x16& acc, const lds_byte* tile, int row0, int col, const Weights<DT>& w) const {
+        if constexpr (DT == FX_F32) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float x = *(const __attribute__((address_space(3))) float*)(tile + a[r >> 2 & 1] + L::row_at(row0 + 16 * (r >> 3) + (r & 3)) + col * 2 * L::kSegment);
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w.p[r], acc, 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                s16x4 h[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(tile + a[e] + L::row_at(row0 + 16 * t) + col * L::kSegment));
+                const s16x8 x = __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                typename Elem<typename AttnType<DT>::T>::vec8 f;
+                __builtin_memcpy(&f, &x, 16);
+                acc = Elem<typename AttnType<DT>::T>::mma(f, w.p[t], acc);
+            }
+        }
+    }
+};
 
 // Writes a 32x32 result whose rows are a row's elements 32 col .. and whose columns are rows, times f
 template <int DT> __device__ __forceinline__ void store_columns(const f32x16& acc, float f, unsigned char* row, int col, int dim_bytes, int half) {
@@ -174,12 +197,12 @@ __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 
 
 // The piece of work of this workgroup: workgroups are dealt to the eight XCDs in turn, and each XCD gets a range of neighbours
 // -- the tiles of few heads, whose keys its L2 then holds, or, where sequences are short, all heads of neighbouring rows.
-__device__ __forceinline__ bool work_of(const AttnArgs& a, int heads, int* tile, int* head) {
+struct Work { int tile, head; };            // head < 0: none
+__device__ __forceinline__ Work work_of(const AttnArgs& a, int heads) {
     const uint32_t total = (uint32_t)a.n_tiles * heads, per = gridDim.x / 8, item = (blockIdx.x % 8) * per + blockIdx.x / 8;
-    if (item >= total) return false;
-    if (a.head_major) { *head = item / a.n_tiles; *tile = item % a.n_tiles; }
-    else { *tile = item / heads; *head = item % heads; }
-    return true;
+    if (item >= total) return Work{0, -1};
+    const uint32_t by = a.head_major ? a.n_tiles : heads, high = item / by, low = item - high * by;
+    return a.head_major ? Work{(int)low, (int)high} : Work{(int)high, (int)low};
 }
 
 // ------------------------------------------------------------------ host

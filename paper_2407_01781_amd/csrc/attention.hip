@@ -10,7 +10,7 @@ namespace fx {
 template <int DT, int DP> struct FwdShape {
     static constexpr int RB = DP * AttnType<DT>::ES;
     static constexpr int KT = RB > 256 ? 32 : 64;
-    static constexpr int kTile = KT * RB;
+    static constexpr int kTile = LdsRows<RB>::bytes(KT);
     static constexpr int kLds = 4 * kTile;
 };
 
@@ -22,10 +22,11 @@ __global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES > 256 ? 1 : 2) void k
     constexpr int RB = S::RB, KT = S::KT, STEPS = RB / 32, COLS = DP / 32, MT = KT / 32;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     lds_byte* lds = (lds_byte*)smem;
-    int tile, head;
-    if (!work_of(a, a.heads, &tile, &head)) return;
+    const Work work = work_of(a, a.heads);
+    if (work.head < 0) return;
+    const int head = work.head;
     const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane >> 5;
-    const SeqTile st = a.tiles[tile];
+    const SeqTile st = a.tiles[work.tile];
     const int q0 = a.first_q[st.seq], nq = a.first_q[st.seq + 1] - q0, k0 = a.first_k[st.seq], nk = a.first_k[st.seq + 1] - k0;
     const int row0 = st.row + wave * 32, row = row0 + (lane & 31), shift = nk - nq;
     const int kv_head = head / a.group;
@@ -39,6 +40,10 @@ __global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES > 256 ? 1 : 2) void k
     TileLoad<RB, KT, W> lk, lv;
     lk.init(wave, lane, a.k.ld, a.dim_bytes);
     lv.init(wave, lane, a.v.ld, a.dim_bytes);
+    RowReader<DT, RB> rows_of;
+    rows_of.init(lane);
+    ColumnProduct<DT, RB> columns;
+    columns.init(lane);
     OwnRows<DT, STEPS> q;
     q.load(a.q.p + (int64_t)q0 * a.q.ld + head * a.q.hs, a.q.ld, row0, nq, a.dim_bytes, lane, a.negative);
 
@@ -66,7 +71,7 @@ __global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES > 256 ? 1 : 2) void k
         for (int t = 0; t < MT; ++t) {
             s[t] = f32x16(0.f);
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) s[t] = Elem<T>::mma(row_operand<DT, RB>(kt, t * 32 + (lane & 31), i, half), q.x[i], s[t]);
+            for (int i = 0; i < STEPS; ++i) s[t] = Elem<T>::mma(rows_of(kt, t * 32, i), q.x[i], s[t]);
         }
         const int unmasked = a.causal ? min(nk - 1, row0 + shift) : nk - 1;
         if (key0 + KT - 1 > unmasked) {
@@ -103,7 +108,7 @@ __global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES > 256 ? 1 : 2) void k
             Weights<DT> w;
             w.set(s[t]);
 #pragma unroll
-            for (int c = 0; c < COLS; ++c) mma_columns<DT, RB>(acc[c], vt, t * 32, c, w, lane);
+            for (int c = 0; c < COLS; ++c) columns(acc[c], vt, t * 32, c, w);
         }
         sum += part;
     }
@@ -245,7 +250,7 @@ static fx_status fill_args(const char* who, const fx_attention* d, AttnArgs* a, 
     a->scale = fabsf(d->scale);
     a->c = fmaxf(a->scale * kLog2e, 0x1p-149f);       // not 0: a masked score is -infinity and stays it
     a->head_major = k->longest > 2048;
-    if (tiles * heads > (1ll << 32) / 256 - 8) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }
+    if (tiles * heads * (d->dim > 128 ? 2 : 1) > (1ll << 32) / 256 - 8) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }
     return FX_OK;
 }
 

@@ -13,8 +13,13 @@ namespace fx {
 template <int DT, int DP> struct BwdShape {
     static constexpr int RB = DP * AttnType<DT>::ES;
     static constexpr int T = 32;                // rows of a tile that streams by
-    static constexpr int kTile = T * RB;
+    static constexpr int kTile = LdsRows<RB>::bytes(T);
     static constexpr int kLds = 4 * kTile + 4 * T * 4;
+    // Parts that the output's columns are dealt out in, as heads of their own: above 128 dimensions a lane's results, its own rows and
+    // their products would not fit 512 registers.
+    static constexpr int kParts = DP > 128 ? 2 : 1;
+    static constexpr int kCols = DP / 32 / kParts;
+    static constexpr int kPart = kCols * (DT == FX_F32 ? 2 : 1) * LdsRows<RB>::kSegment;        // from part to part in a tile
 };
 
 // ------------------------------------------------------------------ gradients of the queries
@@ -23,13 +28,14 @@ __global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES > 256 ? 1 : 2) void k
 #if defined(__HIP_DEVICE_COMPILE__)         // the host pass has no buffer descriptors and drops stubs over them
     typedef BwdShape<DT, DP> S;
     typedef typename AttnType<DT>::T T;
-    constexpr int RB = S::RB, KT = S::T, STEPS = RB / 32, COLS = DP / 32;
+    constexpr int RB = S::RB, KT = S::T, STEPS = RB / 32, COLS = S::kCols;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     lds_byte* lds = (lds_byte*)smem;
-    int tile, head;
-    if (!work_of(a, a.heads, &tile, &head)) return;
+    const Work work = work_of(a, a.heads * S::kParts);
+    if (work.head < 0) return;
+    const int head = work.head / S::kParts, part = work.head % S::kParts;
     const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane >> 5;
-    const SeqTile st = a.tiles[tile];
+    const SeqTile st = a.tiles[work.tile];
     const int q0 = a.first_q[st.seq], nq = a.first_q[st.seq + 1] - q0, k0 = a.first_k[st.seq], nk = a.first_k[st.seq + 1] - k0;
     const int row0 = st.row + wave * 32, row = row0 + (lane & 31), shift = nk - nq;
     const int kv_head = head / a.group;
@@ -42,6 +48,10 @@ __global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES > 256 ? 1 : 2) void k
     TileLoad<RB, KT, W> lk, lv;
     lk.init(wave, lane, a.k.ld, a.dim_bytes);
     lv.init(wave, lane, a.v.ld, a.dim_bytes);
+    RowReader<DT, RB> rows_of;
+    rows_of.init(lane);
+    ColumnProduct<DT, RB> columns;
+    columns.init(lane);
     OwnRows<DT, STEPS> q, go;
     go.load(a.gout.p + (int64_t)q0 * a.gout.ld + head * a.gout.hs, a.gout.ld, row0, nq, a.dim_bytes, lane);
     float delta = 0.f;
@@ -82,9 +92,9 @@ __global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES > 256 ? 1 : 2) void k
         const lds_byte *kt = lds + b * S::kTile, *vt = lds + (2 + b) * S::kTile;
         f32x16 p = f32x16(0.f), dp = f32x16(0.f);
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) p = Elem<T>::mma(row_operand<DT, RB>(kt, lane & 31, i, half), q.x[i], p);
+        for (int i = 0; i < STEPS; ++i) p = Elem<T>::mma(rows_of(kt, 0, i), q.x[i], p);
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) dp = Elem<T>::mma(row_operand<DT, RB>(vt, lane & 31, i, half), go.x[i], dp);
+        for (int i = 0; i < STEPS; ++i) dp = Elem<T>::mma(rows_of(vt, 0, i), go.x[i], dp);
         if (one_key) dp = f32x16(0.f);
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], a.c, -lse2));
@@ -111,34 +121,37 @@ __global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES > 256 ? 1 : 2) void k
         }
         w.set(ds);
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) mma_columns<DT, RB>(acc[c], kt, 0, c, w, lane);
+        for (int c = 0; c < COLS; ++c) columns(acc[c], kt + part * S::kPart, 0, c, w);
     }
     if (row >= nq) return;
-    if (half == 0) a.delta[at] = delta - glse;
+    if (half == 0 && part == 0) a.delta[at] = delta - glse;
     if (!a.gq.p) return;
     unsigned char* out = a.gq.p + (int64_t)(q0 + row) * a.gq.ld + head * a.gq.hs;
     const float f = a.negative ? -a.scale : a.scale;
 #pragma unroll
-    for (int c = 0; c < COLS; ++c) store_columns<DT>(acc[c], f, out, c, a.dim_bytes, half);
+    for (int c = 0; c < COLS; ++c) store_columns<DT>(acc[c], f, out, part * COLS + c, a.dim_bytes, half);
 #endif
 }
 
 // ------------------------------------------------------------------ gradients of keys and values
 template <int DT, int DP, int W>
-__global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES >= 256 ? 1 : 2) void k_attention_gkv(AttnArgs a) {
+__global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES > 256 ? 1 : 2) void k_attention_gkv(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)         // the host pass has no buffer descriptors and drops stubs over them
     typedef BwdShape<DT, DP> S;
     typedef typename AttnType<DT>::T T;
-    constexpr int RB = S::RB, QT = S::T, STEPS = RB / 32, COLS = DP / 32;
+    constexpr int RB = S::RB, QT = S::T, STEPS = RB / 32, COLS = S::kCols;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     lds_byte* lds = (lds_byte*)smem;
     float* stats = (float*)(smem + 4 * S::kTile);           // per buffer: lse, then delta
-    int tile, kv_head;
-    if (!work_of(a, a.kv_heads, &tile, &kv_head)) return;
+    const Work work = work_of(a, a.kv_heads * S::kParts);
+    if (work.head < 0) return;
+    const int kv_head = work.head / S::kParts, part = work.head % S::kParts;
     const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane >> 5;
-    const SeqTile st = a.tiles[tile];
+    const SeqTile st = a.tiles[work.tile];
     const int q0 = a.first_q[st.seq], nq = a.first_q[st.seq + 1] - q0, k0 = a.first_k[st.seq], nk = a.first_k[st.seq + 1] - k0;
-    const int key0 = st.row + wave * 32, key = key0 + (lane & 31), shift = nk - nq;
+    // the tile that most queries see is a causal sequence's first: it is begun first
+    const int tile0 = a.causal ? (nk - 1) / (32 * W) * (32 * W) - st.row : st.row;
+    const int key0 = tile0 + wave * 32, key = key0 + (lane & 31), shift = nk - nq;
     const bool one_key = nk == 1;
 
     OwnRows<DT, STEPS> k, v;
@@ -147,77 +160,87 @@ __global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES >= 256 ? 1 : 2) void 
     TileLoad<RB, QT, W> lq, lo;
     lq.init(wave, lane, a.q.ld, a.dim_bytes);
     lo.init(wave, lane, a.gout.ld, a.dim_bytes);
+    RowReader<DT, RB> rows_of;
+    rows_of.init(lane);
+    ColumnProduct<DT, RB> columns;
+    columns.init(lane);
     f32x16 gk[COLS], gv[COLS];
 #pragma unroll
     for (int c = 0; c < COLS; ++c) gk[c] = gv[c] = f32x16(0.f);
-    // the first tile in which a query sees the workgroup's first key; all heads of the group, tile after tile
-    const int t0 = a.causal ? max(0, st.row - shift) / QT : 0, per_head = max(0, (nq + QT - 1) / QT - t0), n = per_head * a.group;
-    auto load = [&](int j, int b) {
-        const int head = kv_head * a.group + j / per_head, r0 = (t0 + j % per_head) * QT;
-        lq.load(lds + b * S::kTile, a.q.p + (int64_t)q0 * a.q.ld + head * a.q.hs, a.q.ld, r0, nq, a.dim_bytes, wave);
-        lo.load(lds + (2 + b) * S::kTile, a.gout.p + (int64_t)q0 * a.gout.ld + head * a.gout.hs, a.gout.ld, r0, nq, a.dim_bytes, wave);
+    // all heads of the group in turn; of each the tiles from the first on in which a query sees the workgroup's first key
+    const int begin = a.causal ? max(0, tile0 - shift) / QT * QT : 0, n = begin < nq ? (nq - begin + QT - 1) / QT * a.group : 0;
+    int next_head = kv_head * a.group, next = begin;
+    auto load = [&](int b) {
+        lq.load(lds + b * S::kTile, a.q.p + (int64_t)q0 * a.q.ld + next_head * a.q.hs, a.q.ld, next, nq, a.dim_bytes, wave);
+        lo.load(lds + (2 + b) * S::kTile, a.gout.p + (int64_t)q0 * a.gout.ld + next_head * a.gout.hs, a.gout.ld, next, nq, a.dim_bytes, wave);
         if (threadIdx.x < 2 * QT) {
-            const int r = r0 + threadIdx.x % QT;
-            const int64_t at = head * a.rows_q + q0 + r;
+            const int r = next + threadIdx.x % QT;
+            const int64_t at = next_head * a.rows_q + q0 + r;
             stats[b * 2 * QT + threadIdx.x] = threadIdx.x < QT ? (r < nq ? a.lse[at] * kLog2e : INFINITY) : r < nq ? a.delta[at] : 0.f;
         }
+        next += QT;
+        if (next >= nq) { next = begin; ++next_head; }
     };
-    if (n > 0) load(0, 0);
+    if (n > 0) load(0);
+    int r0 = begin - QT;
     for (int j = 0; j < n; ++j) {
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
-        const int b = j & 1, r0 = (t0 + j % per_head) * QT;
-        if (j + 1 < n) load(j + 1, b ^ 1);
+        const int b = j & 1;
+        r0 += QT;
+        if (r0 >= nq) r0 = begin;
+        if (j + 1 < n) load(b ^ 1);
         if (key0 >= nk || (a.causal && r0 + QT - 1 + shift < key0)) continue;
         const lds_byte *qt = lds + b * S::kTile, *ot = lds + (2 + b) * S::kTile;
         f32x16 p = f32x16(0.f), dp = f32x16(0.f);
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) p = Elem<T>::mma(row_operand<DT, RB>(qt, lane & 31, i, half), k.x[i], p);
+        for (int i = 0; i < STEPS; ++i) p = Elem<T>::mma(rows_of(qt, 0, i), k.x[i], p);
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) dp = Elem<T>::mma(row_operand<DT, RB>(ot, lane & 31, i, half), v.x[i], dp);
+        for (int i = 0; i < STEPS; ++i) dp = Elem<T>::mma(rows_of(ot, 0, i), v.x[i], dp);
         if (one_key) dp = f32x16(0.f);
-        f32x4 lse[4], delta[4];
+        f32x16 ds;
+        const float* stat = stats + b * 2 * QT + 4 * half;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            lse[g] = *(const f32x4*)(stats + b * 2 * QT + 8 * g + 4 * half);
-            delta[g] = *(const f32x4*)(stats + b * 2 * QT + QT + 8 * g + 4 * half);
+            const f32x4 lse = *(const f32x4*)(stat + 8 * g), delta = *(const f32x4*)(stat + QT + 8 * g);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = 4 * g + e;
+                p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], a.c, -lse[e]));
+                ds[r] = p[r] * (dp[r] - delta[e]);
+            }
         }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], a.c, -lse[r >> 2][r & 3]));
-        f32x16 ds;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) ds[r] = p[r] * (dp[r] - delta[r >> 2][r & 3]);
         if (a.causal && r0 + shift < key0 + 31) {
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 if (r0 + 8 * (r >> 2) + 4 * half + (r & 3) + shift < key) p[r] = ds[r] = 0.f;
         }
-        Weights<DT> w;
-        w.set(p);
+        Weights<DT> wp, wd;
+        wp.set(p);
+        wd.set(ds);
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) mma_columns<DT, RB>(gv[c], ot, 0, c, w, lane);
-        w.set(ds);
+        for (int c = 0; c < COLS; ++c) columns(gv[c], ot + part * S::kPart, 0, c, wp);
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) mma_columns<DT, RB>(gk[c], qt, 0, c, w, lane);
+        for (int c = 0; c < COLS; ++c) columns(gk[c], qt + part * S::kPart, 0, c, wd);
     }
     if (key >= nk) return;
     if (a.gk.p) {
         unsigned char* out = a.gk.p + (int64_t)(k0 + key) * a.gk.ld + kv_head * a.gk.hs;
         const float f = a.negative ? -a.scale : a.scale;
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) store_columns<DT>(gk[c], f, out, c, a.dim_bytes, half);
+        for (int c = 0; c < COLS; ++c) store_columns<DT>(gk[c], f, out, part * COLS + c, a.dim_bytes, half);
     }
     if (a.gv.p) {
         unsigned char* out = a.gv.p + (int64_t)(k0 + key) * a.gv.ld + kv_head * a.gv.hs;
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) store_columns<DT>(gv[c], 1.f, out, c, a.dim_bytes, half);
+        for (int c = 0; c < COLS; ++c) store_columns<DT>(gv[c], 1.f, out, part * COLS + c, a.dim_bytes, half);
     }
 #endif
 }
 
 template <int DT, int DP> static void launch_bwd(const AttnArgs& a, const AttnArgs& b, bool keys, hipStream_t st) {
     typedef BwdShape<DT, DP> S;
-    const unsigned nq = (unsigned)(((int64_t)a.n_tiles * a.heads + 7) / 8 * 8), nk = (unsigned)(((int64_t)b.n_tiles * b.kv_heads + 7) / 8 * 8);
+    const unsigned nq = (unsigned)(((int64_t)a.n_tiles * a.heads * S::kParts + 7) / 8 * 8), nk = (unsigned)(((int64_t)b.n_tiles * b.kv_heads * S::kParts + 7) / 8 * 8);
     if (nq) k_attention_gq<DT, DP, 4><<<nq, 256, S::kLds, st>>>(a);
     if (keys && nk) k_attention_gkv<DT, DP, 4><<<nk, 256, S::kLds, st>>>(b);
 }
