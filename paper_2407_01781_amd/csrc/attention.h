@@ -16,12 +16,18 @@ typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((ext_vector_type(8))) short s16x8;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kMostDim = 256;
+constexpr int kMostDim = 256, kMostParts = 4;
 
 template <int DT> struct AttnType;
 template <> struct AttnType<FX_F32> { typedef float T; static constexpr int ES = 4; };
 template <> struct AttnType<FX_F16> { typedef _Float16 T; static constexpr int ES = 2; };
 template <> struct AttnType<FX_BF16> { typedef __bf16 T; static constexpr int ES = 2; };
+
+// waves of a SIMD at least, for which registers are allotted: rows of more than 256 bytes need more than 256
+constexpr int least_waves(int row_bytes) { return row_bytes > 256 ? 1 : 2; }
+
+// waves that share a block of few rows: each has tiles of its own in LDS
+constexpr int few_waves(int row_bytes) { return row_bytes > 512 ? 2 : 4; }
 
 // A tensor of heads on the device: bytes from row to row and head to head
 struct HeadsView { unsigned char* p; int64_t ld, hs; };
@@ -29,12 +35,12 @@ struct HeadsView { unsigned char* p; int64_t ld, hs; };
 struct AttnArgs {
     HeadsView q, k, v, out, gout, gq, gk, gv;
     const SeqTile* tiles;
-    const int32_t *first_q, *first_k;
-    float *lse, *delta;
+    const int32_t *first_q, *first_k;       // NULL: keys have the queries' sequences
+    float *lse, *stats;
     const float* glse;
     int64_t rows_q;
-    int32_t n_tiles, heads, kv_heads, group, dim_bytes;
-    int32_t causal, head_major, negative;
+    int32_t n_tiles, tile_rows, heads, kv_heads, group, dim_bytes;
+    int32_t causal, order, chunk, fold, negative;
     float c;            // |scale| log2(e)
     float scale;        // |scale|
 };
@@ -177,6 +183,19 @@ template <int DT, int RB> struct ColumnProduct {
     }
 };
 
+// Rows of a work item: its sequence's queries and keys
+struct Pair { int q0, nq, k0, nk; };
+__device__ __forceinline__ Pair pair_of(const AttnArgs& a, const SeqTile& t) {         // t: a tile of queries
+    if (!a.first_k) return Pair{t.first, t.len, t.first, t.len};
+    const int k0 = a.first_k[t.seq];
+    return Pair{t.first, t.len, k0, a.first_k[t.seq + 1] - k0};
+}
+__device__ __forceinline__ Pair pair_of_keys(const AttnArgs& a, const SeqTile& t) {
+    if (!a.first_q) return Pair{t.first, t.len, t.first, t.len};
+    const int q0 = a.first_q[t.seq];
+    return Pair{q0, a.first_q[t.seq + 1] - q0, t.first, t.len};
+}
+
 // Writes a 32x32 result whose rows are a row's elements 32 col .. and whose columns are rows, times f
 template <int DT> __device__ __forceinline__ void store_columns(const f32x16& acc, float f, unsigned char* row, int col, int dim_bytes, int half) {
     constexpr int ES = AttnType<DT>::ES;
@@ -195,14 +214,39 @@ template <int DT> __device__ __forceinline__ void store_columns(const f32x16& ac
 
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
 
-// The piece of work of this workgroup: workgroups are dealt to the eight XCDs in turn, and each XCD gets a range of neighbours
-// -- the tiles of few heads, whose keys its L2 then holds, or, where sequences are short, all heads of neighbouring rows.
+// The piece of work of this workgroup.  Workgroups are dealt to the eight XCDs in turn, and tiles lie from long to short: every XCD
+// takes `chunk` neighbouring tiles of each 8 chunk, all heads of a tile in a row where sequences are short (the heads' parts of
+// a row share lines, the tiles of a sequence its keys, in one L2), head after head where they are long (the L2 then has
+// one head's keys); or, with a multiple of eight heads, all tiles of its eighth of the heads.
+// fold: a launch whose workgroups are all resident at once is dealt out such that a compute unit's second is as light as its
+// first is heavy (gradients of keys, 16,384 x 4 x 128 causal: 3.6 -> 3.2 ms).
+enum Order { kTilesFirst = 0, kHeadsFirst = 1, kHeadsApart = 2 };
 struct Work { int tile, head; };            // head < 0: none
 __device__ __forceinline__ Work work_of(const AttnArgs& a, int heads) {
-    const uint32_t total = (uint32_t)a.n_tiles * heads, per = gridDim.x / 8, item = (blockIdx.x % 8) * per + blockIdx.x / 8;
-    if (item >= total) return Work{0, -1};
-    const uint32_t by = a.head_major ? a.n_tiles : heads, high = item / by, low = item - high * by;
-    return a.head_major ? Work{(int)low, (int)high} : Work{(int)high, (int)low};
+    const uint32_t xcd = blockIdx.x % 8, tiles = (uint32_t)a.n_tiles, chunk = (uint32_t)a.chunk, per_xcd = (tiles + 8 * chunk - 1) / (8 * chunk) * chunk;
+    uint32_t slot = blockIdx.x / 8;
+    if (a.fold) slot = 2 * slot < gridDim.x / 8 ? 2 * slot : 2 * (gridDim.x / 8 - 1 - slot) + 1;
+    Work w;
+    if (a.order == kHeadsApart) {
+        const uint32_t h = slot / tiles;
+        return Work{(int)(slot - h * tiles), (int)(xcd * (heads / 8) + h)};
+    }
+    const uint32_t by = a.order == kTilesFirst ? per_xcd : heads, high = slot / by, low = slot - high * by;
+    const uint32_t t = a.order == kTilesFirst ? low : high, tile = t / chunk * (8 * chunk) + xcd * chunk + t % chunk;
+    w.tile = (int)tile;
+    w.head = tile >= tiles ? -1 : a.order == kTilesFirst ? (int)high : (int)low;
+    return w;
+}
+static inline unsigned work_blocks(const AttnArgs& a, int64_t heads) {
+    return (unsigned)((a.order == kHeadsApart ? heads / 8 * a.n_tiles : (a.n_tiles + 8 * a.chunk - 1) / (8 * a.chunk) * a.chunk * heads) * 8);
+}
+
+// The wave's result is put into LDS by those of the upper half of W waves and taken by the lower, until wave 0 has all
+template <int N> __device__ __forceinline__ void put_result(float* to, const f32x16 (&x)[N], int lane) {
+#pragma unroll
+    for (int c = 0; c < N; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) to[(c * 16 + r) * 64 + lane] = x[c][r];
 }
 
 // ------------------------------------------------------------------ host
@@ -219,7 +263,7 @@ struct HeadsTensor {
 };
 fx_status check_heads(const char* who, const HeadsTensor& t, int32_t dim, int es);
 
-fx_status attention_bwd_launch(const AttnArgs& a, fx_dtype dt, int dim, int64_t longest_q, int64_t longest_k, const SeqTile* k_tiles, int32_t n_k_tiles, bool keys,
-                               hipStream_t st);
+// a: tiles of queries, b: those of keys
+void attention_bwd_launch(const AttnArgs& a, const AttnArgs& b, fx_dtype dt, int dim, bool keys, hipStream_t st);
 
 }  // namespace fx

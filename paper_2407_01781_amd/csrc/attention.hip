@@ -6,6 +6,92 @@
 namespace fx {
 
 // ------------------------------------------------------------------ forward
+// What a wave keeps of its 32 queries, a column (lane % 32) each: the sums so far, the maximum that their weights are relative to,
+// and the sum of the weights of the lane's half of the keys.
+template <int DT, int DP> struct FwdWave {
+    typedef typename AttnType<DT>::T T;
+    static constexpr int RB = DP * AttnType<DT>::ES, STEPS = RB / 32, COLS = DP / 32;
+    RowReader<DT, RB> rows_of;
+    ColumnProduct<DT, RB> columns;
+    OwnRows<DT, STEPS> q;
+    f32x16 acc[COLS];
+    float m, sum, c;
+    int half;
+
+    __device__ __forceinline__ void init(const AttnArgs& a, int lane) {
+        half = lane >> 5;
+        rows_of.init(lane);
+        columns.init(lane);
+        c = a.c;
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int k = 0; k < COLS; ++k) acc[k] = f32x16(0.f);
+        m = -INFINITY;
+        sum = 0.f;
+    }
+
+    // NB blocks of 32 keys from key0 on, of which the lane's query sees those up to `last` (all where not masked)
+    template <int NB> __device__ __forceinline__ void blocks(const lds_byte* kt, const lds_byte* vt, int row0, int key0, bool masked, int last) {
+        f32x16 s[NB];
+#pragma unroll
+        for (int t = 0; t < NB; ++t) {
+            s[t] = f32x16(0.f);
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) s[t] = Elem<T>::mma(rows_of(kt, row0 + t * 32, i), q.x[i], s[t]);
+        }
+        if (masked) {
+            const int left = last - key0 - 4 * half;
+#pragma unroll
+            for (int t = 0; t < NB; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (32 * t + 8 * (r >> 2) + (r & 3) > left) s[t][r] = -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int t = 0; t < NB; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
+        top = fmaxf(top, other_half(top));
+        // The maximum that weights are relative to follows the row's own only when that has grown by a factor of 2^8: acc and
+        // sum are exact in whichever they are, a weight is at most 2^8, and few tiles have to scale what is there.
+        if (__any(top * c > m * c + 8.f)) rescale(fmaxf(m, top));
+        const float mc = m == -INFINITY ? 0.f : m * c;
+        float part = 0.f;
+#pragma unroll
+        for (int t = 0; t < NB; ++t) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], c, -mc));
+                part += s[t][r];
+            }
+            Weights<DT> w;
+            w.set(s[t]);
+#pragma unroll
+            for (int k = 0; k < COLS; ++k) columns(acc[k], vt, row0 + t * 32, k, w);
+        }
+        sum += part;
+    }
+
+    __device__ __forceinline__ void rescale(float to) {
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - to) * c);
+        m = to;
+        sum *= f;
+#pragma unroll
+        for (int k = 0; k < COLS; ++k) acc[k] *= f;
+    }
+
+    __device__ __forceinline__ void store(const AttnArgs& a, int row, int nq, int q0, int head) {
+        if (row >= nq) return;
+        const float f = sum == 0.f ? 0.f : 1.f / sum;
+        unsigned char* out = a.out.p + (int64_t)(q0 + row) * a.out.ld + head * a.out.hs;
+#pragma unroll
+        for (int k = 0; k < COLS; ++k) store_columns<DT>(acc[k], f, out, k, a.dim_bytes, half);
+        if (a.lse && half == 0) a.lse[head * a.rows_q + q0 + row] = sum == 0.f ? -INFINITY : (m * c + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+};
+
 // A workgroup has W waves of 32 queries of one head; keys and values come by in tiles of KT, two buffers of each.
 template <int DT, int DP> struct FwdShape {
     static constexpr int RB = DP * AttnType<DT>::ES;
@@ -15,122 +101,153 @@ template <int DT, int DP> struct FwdShape {
 };
 
 template <int DT, int DP, int W>
-__global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES > 256 ? 1 : 2) void k_attention(AttnArgs a) {
+__global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_attention(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)         // the host pass has no buffer descriptors and drops stubs over them
     typedef FwdShape<DT, DP> S;
-    typedef typename AttnType<DT>::T T;
-    constexpr int RB = S::RB, KT = S::KT, STEPS = RB / 32, COLS = DP / 32, MT = KT / 32;
+    constexpr int RB = S::RB, KT = S::KT;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     lds_byte* lds = (lds_byte*)smem;
     const Work work = work_of(a, a.heads);
     if (work.head < 0) return;
-    const int head = work.head;
-    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane >> 5;
-    const SeqTile st = a.tiles[work.tile];
-    const int q0 = a.first_q[st.seq], nq = a.first_q[st.seq + 1] - q0, k0 = a.first_k[st.seq], nk = a.first_k[st.seq + 1] - k0;
-    const int row0 = st.row + wave * 32, row = row0 + (lane & 31), shift = nk - nq;
-    const int kv_head = head / a.group;
-    const unsigned char* kb = a.k.p + (int64_t)k0 * a.k.ld + kv_head * a.k.hs;
-    const unsigned char* vb = a.v.p + (int64_t)k0 * a.v.ld + kv_head * a.v.hs;
-    // keys that some row of the workgroup, or of the wave, sees; and the last that this lane's row sees
-    const int seen = a.causal ? max(0, min(nk, min(st.row + 32 * W, nq) + shift)) : nk;
-    const int seen_wave = row0 >= nq ? 0 : a.causal ? max(0, min(nk, min(row0 + 32, nq) + shift)) : nk;
-    const int last = a.causal ? min(nk - 1, row + shift) : nk - 1;
-
+    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63;
     TileLoad<RB, KT, W> lk, lv;
     lk.init(wave, lane, a.k.ld, a.dim_bytes);
     lv.init(wave, lane, a.v.ld, a.dim_bytes);
-    RowReader<DT, RB> rows_of;
-    rows_of.init(lane);
-    ColumnProduct<DT, RB> columns;
-    columns.init(lane);
-    OwnRows<DT, STEPS> q;
-    q.load(a.q.p + (int64_t)q0 * a.q.ld + head * a.q.hs, a.q.ld, row0, nq, a.dim_bytes, lane, a.negative);
-
-    f32x16 acc[COLS];
-#pragma unroll
-    for (int c = 0; c < COLS; ++c) acc[c] = f32x16(0.f);
-    float m = -INFINITY, sum = 0.f;
+    FwdWave<DT, DP> w;
+    w.init(a, lane);
+    const int head = work.head, kv_head = head / a.group;
+    const SeqTile st = a.tiles[work.tile];
+    const Pair p = pair_of(a, st);
+    const unsigned char* kb = a.k.p + (int64_t)p.k0 * a.k.ld + kv_head * a.k.hs;
+    const unsigned char* vb = a.v.p + (int64_t)p.k0 * a.v.ld + kv_head * a.v.hs;
+    // keys that some row of the workgroup, or of the wave, sees; and the last that this lane's row sees
+    const int row0 = st.row + wave * 32, row = row0 + (lane & 31), shift = p.nk - p.nq;
+    const int seen = a.causal ? max(0, min(p.nk, min(st.row + 32 * W, p.nq) + shift)) : p.nk;
+    const int seen_wave = row0 >= p.nq ? 0 : a.causal ? max(0, min(p.nk, min(row0 + 32, p.nq) + shift)) : p.nk;
+    const int last = a.causal ? min(p.nk - 1, row + shift) : p.nk - 1, unmasked = a.causal ? min(p.nk - 1, row0 + shift) : p.nk - 1;
     const int n = (seen + KT - 1) / KT;
     if (n > 0) {
-        lk.load(lds, kb, a.k.ld, 0, nk, a.dim_bytes, wave);
-        lv.load(lds + 2 * S::kTile, vb, a.v.ld, 0, nk, a.dim_bytes, wave);
+        lk.load(lds, kb, a.k.ld, 0, p.nk, a.dim_bytes, wave);
+        lv.load(lds + 2 * S::kTile, vb, a.v.ld, 0, p.nk, a.dim_bytes, wave);
     }
+    w.q.load(a.q.p + (int64_t)p.q0 * a.q.ld + head * a.q.hs, a.q.ld, row0, p.nq, a.dim_bytes, lane, a.negative);
+    w.clear();
     for (int j = 0; j < n; ++j) {
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
         const int b = j & 1, key0 = j * KT;
         if (j + 1 < n) {
-            lk.load(lds + (b ^ 1) * S::kTile, kb, a.k.ld, key0 + KT, nk, a.dim_bytes, wave);
-            lv.load(lds + (2 + (b ^ 1)) * S::kTile, vb, a.v.ld, key0 + KT, nk, a.dim_bytes, wave);
+            lk.load(lds + (b ^ 1) * S::kTile, kb, a.k.ld, key0 + KT, p.nk, a.dim_bytes, wave);
+            lv.load(lds + (2 + (b ^ 1)) * S::kTile, vb, a.v.ld, key0 + KT, p.nk, a.dim_bytes, wave);
         }
-        if (key0 >= seen_wave) continue;
         const lds_byte *kt = lds + b * S::kTile, *vt = lds + (2 + b) * S::kTile;
-        f32x16 s[MT];
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            s[t] = f32x16(0.f);
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) s[t] = Elem<T>::mma(rows_of(kt, t * 32, i), q.x[i], s[t]);
-        }
-        const int unmasked = a.causal ? min(nk - 1, row0 + shift) : nk - 1;
-        if (key0 + KT - 1 > unmasked) {
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (key0 + 32 * t + 8 * (r >> 2) + 4 * half + (r & 3) > last) s[t][r] = -INFINITY;
-        }
-        float top = s[0][0];
-#pragma unroll
-        for (int t = 0; t < MT; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
-        top = fmaxf(top, other_half(top));
-        // The maximum that weights are relative to follows the row's own only when that has grown by a factor of 2^8: acc and
-        // sum are exact in whichever they are, a weight is at most 2^8, and few tiles have to scale what is there.
-        if (__any(top * a.c > m * a.c + 8.f)) {
-            const float m2 = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m2) * a.c);
-            m = m2;
-            sum *= f;
-#pragma unroll
-            for (int c = 0; c < COLS; ++c) acc[c] *= f;
-        }
-        const float mc = m == -INFINITY ? 0.f : m * a.c;
-        float part = 0.f;
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], a.c, -mc));
-                part += s[t][r];
-            }
-            Weights<DT> w;
-            w.set(s[t]);
-#pragma unroll
-            for (int c = 0; c < COLS; ++c) columns(acc[c], vt, t * 32, c, w);
-        }
-        sum += part;
+        const bool masked = key0 + KT - 1 > unmasked;
+        if (key0 >= seen_wave) continue;
+        // half a tile by itself only where sequences are short: a second form of the loop's body costs registers
+        if (KT == 64 && (W > 2 || key0 + 32 < seen_wave)) w.template blocks<2>(kt, vt, 0, key0, masked, last);
+        else w.template blocks<1>(kt, vt, 0, key0, masked, last);
     }
-    sum += other_half(sum);
-    if (row >= nq) return;
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
-    unsigned char* out = a.out.p + (int64_t)(q0 + row) * a.out.ld + head * a.out.hs;
-#pragma unroll
-    for (int c = 0; c < COLS; ++c) store_columns<DT>(acc[c], f, out, c, a.dim_bytes, half);
-    if (a.lse && half == 0) a.lse[head * a.rows_q + q0 + row] = sum == 0.f ? -INFINITY : (m * a.c + __builtin_amdgcn_logf(sum)) * kLn2;
+    w.sum += other_half(w.sum);
+    w.store(a, row, p.nq, p.q0, head);
 #endif
 }
 
-template <int DT, int DP> static void launch_fwd(const AttnArgs& a, unsigned blocks, hipStream_t st) {
-    k_attention<DT, DP, 4><<<blocks, 256, FwdShape<DT, DP>::kLds, st>>>(a);
+// The same for few queries: the W waves of a workgroup share one block of 32, take the blocks of 32 keys in turn, each with
+// buffers of its own and no barrier until the end, where their results are joined.
+template <int DT, int DP, int W> struct FewShape {
+    static constexpr int RB = DP * AttnType<DT>::ES;
+    static constexpr int kTile = LdsRows<RB>::bytes(32);
+    static constexpr int kBuffers = 4 * kTile * W <= 128 * 1024 ? 2 : 1;
+    static constexpr int kSlot = DP * 32 * 4 + 512;                 // a wave's result
+    static constexpr int kLds = std::max(2 * kBuffers * kTile * W, W / 2 * kSlot);
+};
+
+template <int DT, int DP, int W>
+__global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_attention_few(AttnArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef FewShape<DT, DP, W> S;
+    constexpr int RB = S::RB, COLS = DP / 32, NB = S::kBuffers;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const Work work = work_of(a, a.heads);
+    if (work.head < 0) return;
+    const int head = work.head, kv_head = head / a.group;
+    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63;
+    lds_byte* lds = (lds_byte*)smem + wave * 2 * NB * S::kTile;
+    const SeqTile st = a.tiles[work.tile];
+    const Pair p = pair_of(a, st);
+    const unsigned char* kb = a.k.p + (int64_t)p.k0 * a.k.ld + kv_head * a.k.hs;
+    const unsigned char* vb = a.v.p + (int64_t)p.k0 * a.v.ld + kv_head * a.v.hs;
+    TileLoad<RB, 32, 1> lk, lv;
+    lk.init(0, lane, a.k.ld, a.dim_bytes);
+    lv.init(0, lane, a.v.ld, a.dim_bytes);
+    const int row0 = st.row, row = row0 + (lane & 31), shift = p.nk - p.nq;
+    const int seen = a.causal ? max(0, min(p.nk, min(row0 + 32, p.nq) + shift)) : p.nk;
+    const int last = a.causal ? min(p.nk - 1, row + shift) : p.nk - 1, unmasked = a.causal ? min(p.nk - 1, row0 + shift) : p.nk - 1;
+    const int n = (seen + 31) / 32;
+    if (wave < n) {
+        lk.load(lds, kb, a.k.ld, wave * 32, p.nk, a.dim_bytes, 0);
+        lv.load(lds + S::kTile, vb, a.v.ld, wave * 32, p.nk, a.dim_bytes, 0);
+    }
+    FwdWave<DT, DP> w;
+    w.q.load(a.q.p + (int64_t)p.q0 * a.q.ld + head * a.q.hs, a.q.ld, row0, p.nq, a.dim_bytes, lane, a.negative);
+    w.init(a, lane);
+    w.clear();
+    int b = 0;
+    for (int j = wave; j < n; j += W) {
+        __builtin_amdgcn_s_waitcnt(0);
+        const lds_byte* at = lds + b * 2 * S::kTile;
+        if (NB == 2 && j + W < n) {
+            b ^= 1;
+            lk.load(lds + b * 2 * S::kTile, kb, a.k.ld, (j + W) * 32, p.nk, a.dim_bytes, 0);
+            lv.load(lds + b * 2 * S::kTile + S::kTile, vb, a.v.ld, (j + W) * 32, p.nk, a.dim_bytes, 0);
+        }
+        w.template blocks<1>(at, at + S::kTile, 0, j * 32, j * 32 + 31 > unmasked, last);
+        if (NB == 1 && j + W < n) {
+            __builtin_amdgcn_s_waitcnt(0);          // what is read there has been read
+            lk.load(lds, kb, a.k.ld, (j + W) * 32, p.nk, a.dim_bytes, 0);
+            lv.load(lds + S::kTile, vb, a.v.ld, (j + W) * 32, p.nk, a.dim_bytes, 0);
+        }
+    }
+    w.sum += other_half(w.sum);
+#pragma unroll
+    for (int h = W / 2; h >= 1; h /= 2) {
+        __syncthreads();
+        if (wave >= h && wave < 2 * h) {
+            float* to = (float*)(smem + (wave - h) * S::kSlot);
+            put_result<COLS>(to, w.acc, lane);
+            to[COLS * 1024 + lane] = w.m;
+            to[COLS * 1024 + 64 + lane] = w.sum;
+        }
+        __syncthreads();
+        if (wave < h) {
+            const float* in = (const float*)(smem + wave * S::kSlot);
+            const float m2 = in[COLS * 1024 + lane], sum2 = in[COLS * 1024 + 64 + lane], to = fmaxf(w.m, m2);
+            w.rescale(to);
+            const float f = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m2 - to) * a.c);
+            w.sum = fmaf(sum2, f, w.sum);
+#pragma unroll
+            for (int k = 0; k < COLS; ++k)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) w.acc[k][r] = fmaf(in[(k * 16 + r) * 64 + lane], f, w.acc[k][r]);
+        }
+    }
+    if (wave == 0) w.store(a, row, p.nq, p.q0, head);
+#endif
 }
 
-template <int DT> static void launch_fwd_dim(const AttnArgs& a, int dim, unsigned blocks, hipStream_t st) {
-    if (dim <= 32) launch_fwd<DT, 32>(a, blocks, st);
-    else if (dim <= 64) launch_fwd<DT, 64>(a, blocks, st);
-    else if (dim <= 128) launch_fwd<DT, 128>(a, blocks, st);
-    else launch_fwd<DT, 256>(a, blocks, st);
+template <int DT, int DP> static void launch_fwd(const AttnArgs& a, hipStream_t st) {
+    const unsigned blocks = work_blocks(a, a.heads);
+    constexpr int FEW = few_waves(DP * AttnType<DT>::ES);
+    if (a.tile_rows == 32) k_attention_few<DT, DP, FEW><<<blocks, 64 * FEW, FewShape<DT, DP, FEW>::kLds, st>>>(a);
+    else if (a.tile_rows == 64) k_attention<DT, DP, 2><<<blocks, 128, FwdShape<DT, DP>::kLds, st>>>(a);
+    else k_attention<DT, DP, 4><<<blocks, 256, FwdShape<DT, DP>::kLds, st>>>(a);
+}
+
+template <int DT> static void launch_fwd_dim(const AttnArgs& a, int dim, hipStream_t st) {
+    if (dim <= 32) launch_fwd<DT, 32>(a, st);
+    else if (dim <= 64) launch_fwd<DT, 64>(a, st);
+    else if (dim <= 128) launch_fwd<DT, 128>(a, st);
+    else launch_fwd<DT, 256>(a, st);
 }
 
 // ------------------------------------------------------------------ rows in an order that the kernels take
@@ -237,10 +354,20 @@ static fx_status check_places(const char* who, const HeadsTensor* t, int n) {
     return FX_OK;
 }
 
+// Tiles of 128 rows, four waves, or, where those would be less than 4/5 as full as tiles of 64, those, of two waves: keys are
+// then loaded for half as many rows at a time, but no wave idles behind a sequence's end.  Where all tiles of 32 rows would
+// not occupy every SIMD and there are other rows to share out, 32, whose waves take those in turn.
+static void take_tiles(AttnArgs* a, const fx_sequences* q, int32_t heads, int64_t others) {
+    const int kind = q->n_tiles[0] * heads < 4 * compute_units() && others > 64 ? 0 : 64 * q->n_tiles[1] * 5 <= 128 * q->n_tiles[2] * 4 ? 1 : 2;
+    a->tiles = q->d_tiles[kind];
+    a->n_tiles = (int32_t)q->n_tiles[kind];
+    a->tile_rows = kSeqTileRows[kind];
+}
+
 static fx_status fill_args(const char* who, const fx_attention* d, AttnArgs* a, int64_t tiles, int32_t heads) {
     const fx_sequences *q = d->q_seqs, *k = d->kv_seqs ? d->kv_seqs : d->q_seqs;
-    a->first_q = q->d_first;
-    a->first_k = k->d_first;
+    a->first_q = k == q ? nullptr : q->d_first;
+    a->first_k = k == q ? nullptr : k->d_first;
     a->rows_q = q->rows;
     a->heads = d->heads;
     a->kv_heads = d->kv_heads;
@@ -249,8 +376,10 @@ static fx_status fill_args(const char* who, const fx_attention* d, AttnArgs* a, 
     a->negative = d->scale < 0.f;
     a->scale = fabsf(d->scale);
     a->c = fmaxf(a->scale * kLog2e, 0x1p-149f);       // not 0: a masked score is -infinity and stays it
-    a->head_major = k->longest > 2048;
-    if (tiles * heads * (d->dim > 128 ? 2 : 1) > (1ll << 32) / 256 - 8) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }
+    a->order = k->longest <= 2048 ? kHeadsFirst : d->heads % 8 ? kTilesFirst : kHeadsApart;
+    a->chunk = a->order == kHeadsFirst ? std::max(1, std::min(8, a->n_tiles / 64)) : 1;
+    a->fold = 0;
+    if (tiles * heads * (d->dim > 128 ? kMostParts : 1) > (1ll << 32) / 256 - 8) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }
     return FX_OK;
 }
 
@@ -270,7 +399,8 @@ extern "C" fx_status fx_attention_fwd(const fx_attention* d, void* d_out, int64_
     for (const HeadsTensor& x : t) FX_TRY(check_heads(who, x, d->dim, dtype_size(d->dt)));
     if ((uintptr_t)d_lse % 4) { set_error("%s: d_lse is not aligned to its elements", who); return FX_EINVAL; }
     FX_TRY(check_places(who, t, 4));
-    const int64_t tiles = d->q_seqs->n_tiles[1];
+    take_tiles(&a, d->q_seqs, d->heads, (d->kv_seqs ? d->kv_seqs : d->q_seqs)->longest);
+    const int64_t tiles = a.n_tiles;
     FX_TRY(fill_args(who, d, &a, tiles, d->heads));
     if (nq == 0) return FX_OK;
     hipStream_t st = (hipStream_t)stream;
@@ -281,12 +411,9 @@ extern "C" fx_status fx_attention_fwd(const fx_attention* d, void* d_out, int64_
     FX_TRY(take_tensors(who, t, 4, d->dim, d->dt, &scratch, copied, &dim, st));
     a.dim_bytes = dim * dtype_size(d->dt);
     a.lse = d_lse;
-    a.tiles = d->q_seqs->d_tiles[1];
-    a.n_tiles = (int32_t)tiles;
-    const unsigned blocks = (unsigned)((tiles * d->heads + 7) / 8 * 8);
-    if (d->dt == FX_F32) launch_fwd_dim<FX_F32>(a, dim, blocks, st);
-    else if (d->dt == FX_F16) launch_fwd_dim<FX_F16>(a, dim, blocks, st);
-    else launch_fwd_dim<FX_BF16>(a, dim, blocks, st);
+    if (d->dt == FX_F32) launch_fwd_dim<FX_F32>(a, dim, st);
+    else if (d->dt == FX_F16) launch_fwd_dim<FX_F16>(a, dim, st);
+    else launch_fwd_dim<FX_BF16>(a, dim, st);
     return_tensors(t, 4, d->dim, d->dt, copied, dim, st);
     FX_HIP_TRY(hipGetLastError());
     return FX_OK;
@@ -312,8 +439,11 @@ extern "C" fx_status fx_attention_bwd(const fx_attention* d, const void* d_out, 
     for (const HeadsTensor& x : t) FX_TRY(check_heads(who, x, d->dim, dtype_size(d->dt)));
     if ((nq > 0 && !d_lse) || (uintptr_t)d_lse % 4 || (uintptr_t)d_glse % 4) { set_error("%s: d_lse is null, or it or d_glse is not aligned to its elements", who); return FX_EINVAL; }
     FX_TRY(check_places(who, t, n));
-    FX_TRY(fill_args(who, d, &a, d->q_seqs->n_tiles[1], d->heads));
-    FX_TRY(fill_args(who, d, &a, kq->n_tiles[1], d->kv_heads));
+    AttnArgs b{};
+    take_tiles(&b, kq, d->kv_heads, d->q_seqs->longest * (d->heads / d->kv_heads));
+    take_tiles(&a, d->q_seqs, d->heads, kq->longest);
+    FX_TRY(fill_args(who, d, &a, a.n_tiles, d->heads));
+    FX_TRY(fill_args(who, d, &a, b.n_tiles, d->kv_heads));
     if (nq == 0 && nk == 0) return FX_OK;
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps(kProfAttnBwd, st);
@@ -321,15 +451,13 @@ extern "C" fx_status fx_attention_bwd(const fx_attention* d, const void* d_out, 
     bool copied[n];
     int dim;
     FX_TRY(take_tensors(who, t, n, d->dim, d->dt, &scratch, copied, &dim, st));
-    void* delta = nullptr;
-    FX_TRY(scratch.get(who, &delta, (size_t)nq * d->heads * 4));
+    void* stats = nullptr;
+    FX_TRY(scratch.get(who, &stats, (size_t)nq * d->heads * 8));
     a.dim_bytes = dim * dtype_size(d->dt);
     a.lse = const_cast<float*>(d_lse);
     a.glse = d_glse;
-    a.delta = (float*)delta;
-    a.tiles = d->q_seqs->d_tiles[1];
-    a.n_tiles = (int32_t)d->q_seqs->n_tiles[1];
-    FX_TRY(attention_bwd_launch(a, d->dt, dim, d->q_seqs->longest, kq->longest, kq->d_tiles[1], (int32_t)kq->n_tiles[1], d_gk || d_gv, st));
+    a.stats = (float*)stats;
+    attention_bwd_launch(a, b, d->dt, dim, d_gk || d_gv, st);
     return_tensors(t, n, d->dim, d->dt, copied, dim, st);
     FX_HIP_TRY(hipGetLastError());
     return FX_OK;

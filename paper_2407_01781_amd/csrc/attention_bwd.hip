@@ -1,7 +1,7 @@
 // Gradients of attention over packed sequences.
 //
 // Two kernels, each with its outputs in registers until they are whole, so that nothing is added in memory: the first goes
-// over the keys for a workgroup's queries (gq) and leaves sum_j P_ij dP_ij - glse_i of every row for the second, which goes over
+// over the keys for a workgroup's queries (gq) and leaves lse_i (base 2) and sum_j P_ij dP_ij - glse_i of every row for the second, which goes over
 // the queries for a workgroup's keys (gk, gv).  Scores and dP are computed in both: seven products instead of five, for
 // results that do not depend on an order of atomics and need no fp32 copy of gq in memory.
 #include "attention.h"
@@ -12,237 +12,430 @@ namespace fx {
 
 template <int DT, int DP> struct BwdShape {
     static constexpr int RB = DP * AttnType<DT>::ES;
-    static constexpr int T = 32;                // rows of a tile that streams by
-    static constexpr int kTile = LdsRows<RB>::bytes(T);
-    static constexpr int kLds = 4 * kTile + 4 * T * 4;
+    static constexpr int KT = RB > 128 ? 32 : 64;               // keys of a tile that streams by (two blocks' scores and dP are 64 registers)
+    static constexpr int QT = 32;                               // queries
+    static constexpr int kKeys = LdsRows<RB>::bytes(KT), kQueries = LdsRows<RB>::bytes(QT), kStats = 2 * QT * 4;
+    static constexpr int kLdsKeys = 4 * kKeys, kLdsQueries = 4 * kQueries + 2 * kStats;
     // Parts that the output's columns are dealt out in, as heads of their own: above 128 dimensions a lane's results, its own rows and
-    // their products would not fit 512 registers.
-    static constexpr int kParts = DP > 128 ? 2 : 1;
-    static constexpr int kCols = DP / 32 / kParts;
-    static constexpr int kPart = kCols * (DT == FX_F32 ? 2 : 1) * LdsRows<RB>::kSegment;        // from part to part in a tile
+    // their products would not fit 512 registers without spills.
+    static constexpr int kParts = DP > 128 ? (DT == FX_F32 ? 4 : 2) : 1;
+    static constexpr int COLS = DP / 32 / kParts, STEPS = RB / 32;
+    static constexpr int kPart = COLS * (DT == FX_F32 ? 2 : 1) * LdsRows<RB>::kSegment;         // from part to part in a tile
+    // a workgroup of W waves that share one block of rows, each with buffers of its own
+    static constexpr int kBlock = LdsRows<RB>::bytes(32);
+    static constexpr int kOwn = 2 * kBlock + kStats;            // a wave's two tiles and what belongs to their rows
+    template <int W> static constexpr int buffers() { return 2 * kOwn * W <= 128 * 1024 ? 2 : 1; }
+    template <int W> static constexpr int lds_few() { return std::max(buffers<W>() * kOwn * W, W / 2 * COLS * 4096); }
 };
 
 // ------------------------------------------------------------------ gradients of the queries
-template <int DT, int DP, int W>
-__global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES > 256 ? 1 : 2) void k_attention_gq(AttnArgs a) {
-#if defined(__HIP_DEVICE_COMPILE__)         // the host pass has no buffer descriptors and drops stubs over them
+template <int DT, int DP> struct GqWave {
     typedef BwdShape<DT, DP> S;
     typedef typename AttnType<DT>::T T;
-    constexpr int RB = S::RB, KT = S::T, STEPS = RB / 32, COLS = S::kCols;
+    static constexpr int RB = S::RB;
+    RowReader<DT, RB> rows_of;
+    ColumnProduct<DT, RB> columns;
+    OwnRows<DT, S::STEPS> q, go;
+    f32x16 acc[S::COLS];
+    float lse2, glse, delta, c;
+    int half, part;
+    bool one_key, one_tile;
+
+    // A row that sees one key has dS = glse whatever it holds; the rounding of out would leave something.  Where a sequence's keys
+    // are one tile, the sum over P dP is made of the tile's own numbers.
+    __device__ __forceinline__ void init(const AttnArgs& a, const Pair& p, int head, int part_, int row0, int lane, int tile_keys) {
+        half = lane >> 5;
+        part = part_;
+        c = a.c;
+        const int row = row0 + (lane & 31);
+        const int64_t at = head * a.rows_q + p.q0 + row;
+        q.load(a.out.p + (int64_t)p.q0 * a.out.ld + head * a.out.hs, a.out.ld, row0, p.nq, a.dim_bytes, lane);
+        go.load(a.gout.p + (int64_t)p.q0 * a.gout.ld + head * a.gout.hs, a.gout.ld, row0, p.nq, a.dim_bytes, lane);
+        lse2 = row < p.nq ? a.lse[at] * kLog2e : INFINITY;
+        glse = a.glse && row < p.nq ? a.glse[at] : 0.f;
+        rows_of.init(lane);
+        columns.init(lane);
+        delta = 0.f;
+#pragma unroll
+        for (int i = 0; i < S::STEPS; ++i)
+#pragma unroll
+            for (int e = 0; e < 16 / AttnType<DT>::ES; ++e) delta = fmaf((float)q.x[i][e], (float)go.x[i][e], delta);
+        delta += other_half(delta);
+        one_key = p.nk == 1;
+        one_tile = p.nk <= tile_keys;
+        if (one_key) delta = 0.f;
+        q.load(a.q.p + (int64_t)p.q0 * a.q.ld + head * a.q.hs, a.q.ld, row0, p.nq, a.dim_bytes, lane, a.negative);
+#pragma unroll
+        for (int k = 0; k < S::COLS; ++k) acc[k] = f32x16(0.f);
+    }
+
+    template <int NB> __device__ __forceinline__ void blocks(const lds_byte* kt, const lds_byte* vt, int key0, bool masked, int last) {
+        f32x16 p[NB], dp[NB];
+#pragma unroll
+        for (int t = 0; t < NB; ++t) {
+            p[t] = dp[t] = f32x16(0.f);
+#pragma unroll
+            for (int i = 0; i < S::STEPS; ++i) p[t] = Elem<T>::mma(rows_of(kt, t * 32, i), q.x[i], p[t]);
+#pragma unroll
+            for (int i = 0; i < S::STEPS; ++i) dp[t] = Elem<T>::mma(rows_of(vt, t * 32, i), go.x[i], dp[t]);
+            if (one_key) dp[t] = f32x16(0.f);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) p[t][r] = __builtin_amdgcn_exp2f(fmaf(p[t][r], c, -lse2));
+        }
+        if (masked) {
+            const int left = last - key0 - 4 * half;
+#pragma unroll
+            for (int t = 0; t < NB; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (32 * t + 8 * (r >> 2) + (r & 3) > left) p[t][r] = dp[t][r] = 0.f;
+        }
+        if (one_tile && !one_key) {
+            delta = 0.f;
+#pragma unroll
+            for (int t = 0; t < NB; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) delta = fmaf(p[t][r], dp[t][r], delta);
+            delta += other_half(delta);
+        }
+        const float off = delta - glse;
+#pragma unroll
+        for (int t = 0; t < NB; ++t) {
+            Weights<DT> w;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) p[t][r] *= dp[t][r] - off;
+            w.set(p[t]);
+#pragma unroll
+            for (int k = 0; k < S::COLS; ++k) columns(acc[k], kt + part * S::kPart, t * 32, k, w);
+        }
+    }
+
+    __device__ __forceinline__ void store(const AttnArgs& a, const Pair& p, int head, int row) {
+        if (row >= p.nq) return;
+        if (half == 0 && part == 0) *(f32x2*)(a.stats + 2 * (head * a.rows_q + p.q0 + row)) = f32x2{lse2, delta - glse};
+        if (!a.gq.p) return;
+        unsigned char* out = a.gq.p + (int64_t)(p.q0 + row) * a.gq.ld + head * a.gq.hs;
+        const float f = a.negative ? -a.scale : a.scale;
+#pragma unroll
+        for (int k = 0; k < S::COLS; ++k) store_columns<DT>(acc[k], f, out, part * S::COLS + k, a.dim_bytes, half);
+    }
+};
+
+template <int DT, int DP, int W>
+__global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_attention_gq(AttnArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)         // the host pass has no buffer descriptors and drops stubs over them
+    typedef BwdShape<DT, DP> S;
+    constexpr int RB = S::RB, KT = S::KT;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     lds_byte* lds = (lds_byte*)smem;
     const Work work = work_of(a, a.heads * S::kParts);
     if (work.head < 0) return;
-    const int head = work.head / S::kParts, part = work.head % S::kParts;
-    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane >> 5;
+    const int head = work.head / S::kParts, kv_head = head / a.group;
+    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63;
     const SeqTile st = a.tiles[work.tile];
-    const int q0 = a.first_q[st.seq], nq = a.first_q[st.seq + 1] - q0, k0 = a.first_k[st.seq], nk = a.first_k[st.seq + 1] - k0;
-    const int row0 = st.row + wave * 32, row = row0 + (lane & 31), shift = nk - nq;
-    const int kv_head = head / a.group;
-    const unsigned char* kb = a.k.p + (int64_t)k0 * a.k.ld + kv_head * a.k.hs;
-    const unsigned char* vb = a.v.p + (int64_t)k0 * a.v.ld + kv_head * a.v.hs;
-    const int seen = a.causal ? max(0, min(nk, min(st.row + 32 * W, nq) + shift)) : nk;
-    const int seen_wave = row0 >= nq ? 0 : a.causal ? max(0, min(nk, min(row0 + 32, nq) + shift)) : nk;
-    const int last = a.causal ? min(nk - 1, row + shift) : nk - 1;
-
+    const Pair p = pair_of(a, st);
+    const unsigned char* kb = a.k.p + (int64_t)p.k0 * a.k.ld + kv_head * a.k.hs;
+    const unsigned char* vb = a.v.p + (int64_t)p.k0 * a.v.ld + kv_head * a.v.hs;
     TileLoad<RB, KT, W> lk, lv;
     lk.init(wave, lane, a.k.ld, a.dim_bytes);
     lv.init(wave, lane, a.v.ld, a.dim_bytes);
-    RowReader<DT, RB> rows_of;
-    rows_of.init(lane);
-    ColumnProduct<DT, RB> columns;
-    columns.init(lane);
-    OwnRows<DT, STEPS> q, go;
-    go.load(a.gout.p + (int64_t)q0 * a.gout.ld + head * a.gout.hs, a.gout.ld, row0, nq, a.dim_bytes, lane);
-    float delta = 0.f;
-    {
-        q.load(a.out.p + (int64_t)q0 * a.out.ld + head * a.out.hs, a.out.ld, row0, nq, a.dim_bytes, lane);
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i)
-#pragma unroll
-            for (int e = 0; e < 16 / AttnType<DT>::ES; ++e) delta = fmaf((float)q.x[i][e], (float)go.x[i][e], delta);
-        delta += other_half(delta);
-    }
-    q.load(a.q.p + (int64_t)q0 * a.q.ld + head * a.q.hs, a.q.ld, row0, nq, a.dim_bytes, lane, a.negative);
-    const int64_t at = head * a.rows_q + q0 + row;
-    const float lse2 = row < nq ? a.lse[at] * kLog2e : INFINITY;
-    const float glse = a.glse && row < nq ? a.glse[at] : 0.f;
-    // A row that sees one key has dS = glse whatever it holds; the rounding of out would leave something.  Where a sequence's keys
-    // are one tile, the sum over P dP is made of the tile's own numbers below.
-    const bool one_key = nk == 1, one_tile = nk <= KT;
-    if (one_key) delta = 0.f;
-
-    f32x16 acc[COLS];
-#pragma unroll
-    for (int c = 0; c < COLS; ++c) acc[c] = f32x16(0.f);
-    const int n = a.gq.p || one_tile ? (seen + KT - 1) / KT : 0;
+    const int row0 = st.row + wave * 32, row = row0 + (lane & 31), shift = p.nk - p.nq;
+    const int seen = a.causal ? max(0, min(p.nk, min(st.row + 32 * W, p.nq) + shift)) : p.nk;
+    const int seen_wave = row0 >= p.nq ? 0 : a.causal ? max(0, min(p.nk, min(row0 + 32, p.nq) + shift)) : p.nk;
+    const int last = a.causal ? min(p.nk - 1, row + shift) : p.nk - 1, unmasked = a.causal ? min(p.nk - 1, row0 + shift) : p.nk - 1;
+    const int n = a.gq.p || p.nk <= KT ? (seen + KT - 1) / KT : 0;          // without gq the sums alone, where they are made of the tile
     if (n > 0) {
-        lk.load(lds, kb, a.k.ld, 0, nk, a.dim_bytes, wave);
-        lv.load(lds + 2 * S::kTile, vb, a.v.ld, 0, nk, a.dim_bytes, wave);
+        lk.load(lds, kb, a.k.ld, 0, p.nk, a.dim_bytes, wave);
+        lv.load(lds + 2 * S::kKeys, vb, a.v.ld, 0, p.nk, a.dim_bytes, wave);
     }
+    GqWave<DT, DP> w;
+    w.init(a, p, head, work.head % S::kParts, row0, lane, KT);
     for (int j = 0; j < n; ++j) {
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
         const int b = j & 1, key0 = j * KT;
         if (j + 1 < n) {
-            lk.load(lds + (b ^ 1) * S::kTile, kb, a.k.ld, key0 + KT, nk, a.dim_bytes, wave);
-            lv.load(lds + (2 + (b ^ 1)) * S::kTile, vb, a.v.ld, key0 + KT, nk, a.dim_bytes, wave);
+            lk.load(lds + (b ^ 1) * S::kKeys, kb, a.k.ld, key0 + KT, p.nk, a.dim_bytes, wave);
+            lv.load(lds + (2 + (b ^ 1)) * S::kKeys, vb, a.v.ld, key0 + KT, p.nk, a.dim_bytes, wave);
         }
         if (key0 >= seen_wave) continue;
-        const lds_byte *kt = lds + b * S::kTile, *vt = lds + (2 + b) * S::kTile;
-        f32x16 p = f32x16(0.f), dp = f32x16(0.f);
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) p = Elem<T>::mma(rows_of(kt, 0, i), q.x[i], p);
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) dp = Elem<T>::mma(rows_of(vt, 0, i), go.x[i], dp);
-        if (one_key) dp = f32x16(0.f);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], a.c, -lse2));
-        const int unmasked = a.causal ? min(nk - 1, row0 + shift) : nk - 1;
-        if (key0 + KT - 1 > unmasked) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (key0 + 8 * (r >> 2) + 4 * half + (r & 3) > last) { p[r] = 0.f; dp[r] = 0.f; }
-        }
-        if (one_tile && !one_key) {
-            delta = 0.f;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) delta = fmaf(p[r], dp[r], delta);
-            delta += other_half(delta);
-        }
-        Weights<DT> w;
-        f32x16 ds;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) ds[r] = p[r] * (dp[r] - delta + glse);
-        if (key0 + KT - 1 > unmasked) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (key0 + 8 * (r >> 2) + 4 * half + (r & 3) > last) ds[r] = 0.f;
-        }
-        w.set(ds);
-#pragma unroll
-        for (int c = 0; c < COLS; ++c) columns(acc[c], kt + part * S::kPart, 0, c, w);
+        const lds_byte *kt = lds + b * S::kKeys, *vt = lds + (2 + b) * S::kKeys;
+        const bool masked = key0 + KT - 1 > unmasked;
+        if (KT == 64 && (W > 2 || key0 + 32 < seen_wave)) w.template blocks<2>(kt, vt, key0, masked, last);
+        else w.template blocks<1>(kt, vt, key0, masked, last);
     }
-    if (row >= nq) return;
-    if (half == 0 && part == 0) a.delta[at] = delta - glse;
-    if (!a.gq.p) return;
-    unsigned char* out = a.gq.p + (int64_t)(q0 + row) * a.gq.ld + head * a.gq.hs;
-    const float f = a.negative ? -a.scale : a.scale;
+    w.store(a, p, head, row);
+#endif
+}
+
+// The results of W waves added, the upper half's by the lower until wave 0 has all
+template <int W, int N> __device__ __forceinline__ void add_results(unsigned char* smem, f32x16 (&x)[N], int wave, int lane) {
 #pragma unroll
-    for (int c = 0; c < COLS; ++c) store_columns<DT>(acc[c], f, out, part * COLS + c, a.dim_bytes, half);
+    for (int h = W / 2; h >= 1; h /= 2) {
+        __syncthreads();
+        if (wave >= h && wave < 2 * h) put_result<N>((float*)smem + (wave - h) * N * 1024, x, lane);
+        __syncthreads();
+        if (wave < h) {
+            const float* in = (const float*)smem + wave * N * 1024;
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[k][r] += in[(k * 16 + r) * 64 + lane];
+        }
+    }
+}
+
+// For few queries: W waves share one block of 32 and take the blocks of 32 keys in turn, each with buffers of its own
+template <int DT, int DP, int W>
+__global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_attention_gq_few(AttnArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef BwdShape<DT, DP> S;
+    constexpr int RB = S::RB, NB = S::template buffers<W>();
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const Work work = work_of(a, a.heads * S::kParts);
+    if (work.head < 0) return;
+    const int head = work.head / S::kParts, kv_head = head / a.group;
+    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63;
+    lds_byte* lds = (lds_byte*)smem + wave * NB * S::kOwn;
+    const SeqTile st = a.tiles[work.tile];
+    const Pair p = pair_of(a, st);
+    const unsigned char* kb = a.k.p + (int64_t)p.k0 * a.k.ld + kv_head * a.k.hs;
+    const unsigned char* vb = a.v.p + (int64_t)p.k0 * a.v.ld + kv_head * a.v.hs;
+    TileLoad<RB, 32, 1> lk, lv;
+    lk.init(0, lane, a.k.ld, a.dim_bytes);
+    lv.init(0, lane, a.v.ld, a.dim_bytes);
+    const int row0 = st.row, row = row0 + (lane & 31), shift = p.nk - p.nq;
+    const int seen = a.causal ? max(0, min(p.nk, min(row0 + 32, p.nq) + shift)) : p.nk;
+    const int last = a.causal ? min(p.nk - 1, row + shift) : p.nk - 1, unmasked = a.causal ? min(p.nk - 1, row0 + shift) : p.nk - 1;
+    const int n = a.gq.p || p.nk <= 32 ? (seen + 31) / 32 : 0;
+    auto load = [&](int j, int b) {
+        lk.load(lds + b * S::kOwn, kb, a.k.ld, j * 32, p.nk, a.dim_bytes, 0);
+        lv.load(lds + b * S::kOwn + S::kBlock, vb, a.v.ld, j * 32, p.nk, a.dim_bytes, 0);
+    };
+    if (wave < n) load(wave, 0);
+    GqWave<DT, DP> w;
+    w.init(a, p, head, work.head % S::kParts, row0, lane, 32);
+    int b = 0;
+    for (int j = wave; j < n; j += W) {
+        __builtin_amdgcn_s_waitcnt(0);
+        const lds_byte* at = lds + b * S::kOwn;
+        if (NB == 2 && j + W < n) load(j + W, b ^= 1);
+        w.template blocks<1>(at, at + S::kBlock, j * 32, j * 32 + 31 > unmasked, last);
+        if (NB == 1 && j + W < n) {
+            __builtin_amdgcn_s_waitcnt(0);          // what is read there has been read
+            load(j + W, 0);
+        }
+    }
+    add_results<W>(smem, w.acc, wave, lane);
+    if (wave == 0) w.store(a, p, head, row);
 #endif
 }
 
 // ------------------------------------------------------------------ gradients of keys and values
-template <int DT, int DP, int W>
-__global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES > 256 ? 1 : 2) void k_attention_gkv(AttnArgs a) {
-#if defined(__HIP_DEVICE_COMPILE__)         // the host pass has no buffer descriptors and drops stubs over them
+// Rows of 256 bytes take all of 256 registers; only where loads and statistics are dealt out over four waves nothing spills
+constexpr int least_waves_gkv(int row_bytes, bool dealt) { return row_bytes > 256 || (row_bytes == 256 && !dealt) ? 1 : 2; }
+
+template <int DT, int DP> struct GkvWave {
     typedef BwdShape<DT, DP> S;
     typedef typename AttnType<DT>::T T;
-    constexpr int RB = S::RB, QT = S::T, STEPS = RB / 32, COLS = S::kCols;
+    static constexpr int RB = S::RB;
+    RowReader<DT, RB> rows_of;
+    ColumnProduct<DT, RB> columns;
+    OwnRows<DT, S::STEPS> k, v;
+    f32x16 gk[S::COLS], gv[S::COLS];
+    float c;
+    int half, part;
+    bool one_key;
+
+    __device__ __forceinline__ void init(const AttnArgs& a, const Pair& p, int kv_head, int part_, int key0, int lane) {
+        half = lane >> 5;
+        part = part_;
+        c = a.c;
+        one_key = p.nk == 1;
+        k.load(a.k.p + (int64_t)p.k0 * a.k.ld + kv_head * a.k.hs, a.k.ld, key0, p.nk, a.dim_bytes, lane, a.negative);
+        v.load(a.v.p + (int64_t)p.k0 * a.v.ld + kv_head * a.v.hs, a.v.ld, key0, p.nk, a.dim_bytes, lane);
+        rows_of.init(lane);
+        columns.init(lane);
+#pragma unroll
+        for (int i = 0; i < S::COLS; ++i) gk[i] = gv[i] = f32x16(0.f);
+    }
+
+    // 32 queries whose first that sees the lane's key is `first`, counted from the block's first (all do where not masked)
+    __device__ __forceinline__ void block(const lds_byte* qt, const lds_byte* ot, const float* stats, bool masked, int first) {
+        f32x16 p = f32x16(0.f), ds = f32x16(0.f);
+#pragma unroll
+        for (int i = 0; i < S::STEPS; ++i) p = Elem<T>::mma(rows_of(qt, 0, i), k.x[i], p);
+#pragma unroll
+        for (int i = 0; i < S::STEPS; ++i) ds = Elem<T>::mma(rows_of(ot, 0, i), v.x[i], ds);
+        if (one_key) ds = f32x16(0.f);
+        const float* stat = stats + 8 * half;
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {           // lse and delta of two rows
+            const f32x4 x = *(const f32x4*)(stat + 16 * (g >> 1) + 4 * (g & 1));
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = 2 * g + e;
+                p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], c, -x[2 * e]));
+                ds[r] = p[r] * (ds[r] - x[2 * e + 1]);
+            }
+        }
+        if (masked) {
+            first -= 4 * half;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (8 * (r >> 2) + (r & 3) < first) p[r] = ds[r] = 0.f;
+        }
+        Weights<DT> wp, wd;
+        wp.set(p);
+        wd.set(ds);
+#pragma unroll
+        for (int i = 0; i < S::COLS; ++i) columns(gv[i], ot + part * S::kPart, 0, i, wp);
+#pragma unroll
+        for (int i = 0; i < S::COLS; ++i) columns(gk[i], qt + part * S::kPart, 0, i, wd);
+    }
+
+    __device__ __forceinline__ void store(const AttnArgs& a, const Pair& p, int kv_head, int key) {
+        if (key >= p.nk) return;
+        if (a.gk.p) {
+            unsigned char* out = a.gk.p + (int64_t)(p.k0 + key) * a.gk.ld + kv_head * a.gk.hs;
+            const float f = a.negative ? -a.scale : a.scale;
+#pragma unroll
+            for (int i = 0; i < S::COLS; ++i) store_columns<DT>(gk[i], f, out, part * S::COLS + i, a.dim_bytes, half);
+        }
+        if (a.gv.p) {
+            unsigned char* out = a.gv.p + (int64_t)(p.k0 + key) * a.gv.ld + kv_head * a.gv.hs;
+#pragma unroll
+            for (int i = 0; i < S::COLS; ++i) store_columns<DT>(gv[i], 1.f, out, part * S::COLS + i, a.dim_bytes, half);
+        }
+    }
+};
+
+// lse (base 2) and delta of 32 rows, as the first kernel left them, into LDS; zeros for a row that does not exist, whose query and
+// gradient are zeros too: it adds nothing
+__device__ __forceinline__ void load_stats(const AttnArgs& a, lds_byte* to, int head, int q0, int row0, int nq, int lane) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const float* from = a.stats + 2 * (head * a.rows_q + q0 + row0);
+    __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, max(0, min(nq - row0, 32)) * 8, 0x27000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 4, lane * 4, 0, 0, 0);
+#endif
+}
+
+template <int DT, int DP, int W>
+__global__ __launch_bounds__(64 * W, least_waves_gkv(DP * AttnType<DT>::ES, W == 4)) void k_attention_gkv(AttnArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef BwdShape<DT, DP> S;
+    constexpr int RB = S::RB, QT = S::QT;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     lds_byte* lds = (lds_byte*)smem;
-    float* stats = (float*)(smem + 4 * S::kTile);           // per buffer: lse, then delta
+    lds_byte* stats = lds + 4 * S::kQueries;
     const Work work = work_of(a, a.kv_heads * S::kParts);
     if (work.head < 0) return;
-    const int kv_head = work.head / S::kParts, part = work.head % S::kParts;
-    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63, half = lane >> 5;
+    const int kv_head = work.head / S::kParts;
+    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63;
     const SeqTile st = a.tiles[work.tile];
-    const int q0 = a.first_q[st.seq], nq = a.first_q[st.seq + 1] - q0, k0 = a.first_k[st.seq], nk = a.first_k[st.seq + 1] - k0;
+    const Pair p = pair_of_keys(a, st);
     // the tile that most queries see is a causal sequence's first: it is begun first
-    const int tile0 = a.causal ? (nk - 1) / (32 * W) * (32 * W) - st.row : st.row;
-    const int key0 = tile0 + wave * 32, key = key0 + (lane & 31), shift = nk - nq;
-    const bool one_key = nk == 1;
-
-    OwnRows<DT, STEPS> k, v;
-    k.load(a.k.p + (int64_t)k0 * a.k.ld + kv_head * a.k.hs, a.k.ld, key0, nk, a.dim_bytes, lane, a.negative);
-    v.load(a.v.p + (int64_t)k0 * a.v.ld + kv_head * a.v.hs, a.v.ld, key0, nk, a.dim_bytes, lane);
+    const int tile0 = a.causal ? (p.nk - 1) / (32 * W) * (32 * W) - st.row : st.row;
+    const int key0 = tile0 + wave * 32, key = key0 + (lane & 31), shift = p.nk - p.nq;
     TileLoad<RB, QT, W> lq, lo;
     lq.init(wave, lane, a.q.ld, a.dim_bytes);
     lo.init(wave, lane, a.gout.ld, a.dim_bytes);
-    RowReader<DT, RB> rows_of;
-    rows_of.init(lane);
-    ColumnProduct<DT, RB> columns;
-    columns.init(lane);
-    f32x16 gk[COLS], gv[COLS];
-#pragma unroll
-    for (int c = 0; c < COLS; ++c) gk[c] = gv[c] = f32x16(0.f);
     // all heads of the group in turn; of each the tiles from the first on in which a query sees the workgroup's first key
-    const int begin = a.causal ? max(0, tile0 - shift) / QT * QT : 0, n = begin < nq ? (nq - begin + QT - 1) / QT * a.group : 0;
+    const int begin = a.causal ? max(0, tile0 - shift) / QT * QT : 0, n = begin < p.nq ? (p.nq - begin + QT - 1) / QT * a.group : 0;
     int next_head = kv_head * a.group, next = begin;
     auto load = [&](int b) {
-        lq.load(lds + b * S::kTile, a.q.p + (int64_t)q0 * a.q.ld + next_head * a.q.hs, a.q.ld, next, nq, a.dim_bytes, wave);
-        lo.load(lds + (2 + b) * S::kTile, a.gout.p + (int64_t)q0 * a.gout.ld + next_head * a.gout.hs, a.gout.ld, next, nq, a.dim_bytes, wave);
-        if (threadIdx.x < 2 * QT) {
-            const int r = next + threadIdx.x % QT;
-            const int64_t at = next_head * a.rows_q + q0 + r;
-            stats[b * 2 * QT + threadIdx.x] = threadIdx.x < QT ? (r < nq ? a.lse[at] * kLog2e : INFINITY) : r < nq ? a.delta[at] : 0.f;
-        }
+        lq.load(lds + b * S::kQueries, a.q.p + (int64_t)p.q0 * a.q.ld + next_head * a.q.hs, a.q.ld, next, p.nq, a.dim_bytes, wave);
+        lo.load(lds + (2 + b) * S::kQueries, a.gout.p + (int64_t)p.q0 * a.gout.ld + next_head * a.gout.hs, a.gout.ld, next, p.nq, a.dim_bytes, wave);
+        if (wave == W - 1) load_stats(a, stats + b * S::kStats, next_head, p.q0, next, p.nq, lane);
         next += QT;
-        if (next >= nq) { next = begin; ++next_head; }
+        if (next >= p.nq) { next = begin; ++next_head; }
     };
     if (n > 0) load(0);
+    GkvWave<DT, DP> w;
+    w.init(a, p, kv_head, work.head % S::kParts, key0, lane);
     int r0 = begin - QT;
     for (int j = 0; j < n; ++j) {
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
         const int b = j & 1;
         r0 += QT;
-        if (r0 >= nq) r0 = begin;
+        if (r0 >= p.nq) r0 = begin;
         if (j + 1 < n) load(b ^ 1);
-        if (key0 >= nk || (a.causal && r0 + QT - 1 + shift < key0)) continue;
-        const lds_byte *qt = lds + b * S::kTile, *ot = lds + (2 + b) * S::kTile;
-        f32x16 p = f32x16(0.f), dp = f32x16(0.f);
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) p = Elem<T>::mma(rows_of(qt, 0, i), k.x[i], p);
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) dp = Elem<T>::mma(rows_of(ot, 0, i), v.x[i], dp);
-        if (one_key) dp = f32x16(0.f);
-        f32x16 ds;
-        const float* stat = stats + b * 2 * QT + 4 * half;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const f32x4 lse = *(const f32x4*)(stat + 8 * g), delta = *(const f32x4*)(stat + QT + 8 * g);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int r = 4 * g + e;
-                p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], a.c, -lse[e]));
-                ds[r] = p[r] * (dp[r] - delta[e]);
-            }
+        if (key0 >= p.nk || (a.causal && r0 + QT - 1 + shift < key0)) continue;
+        w.block(lds + b * S::kQueries, lds + (2 + b) * S::kQueries, (const float*)(smem + 4 * S::kQueries + b * S::kStats), a.causal && r0 + shift < key0 + 31, key - shift - r0);
+    }
+    w.store(a, p, kv_head, key);
+#endif
+}
+
+// For few keys: W waves share one block of 32 and take the blocks of 32 queries of all heads in turn
+template <int DT, int DP, int W>
+__global__ __launch_bounds__(64 * W, least_waves_gkv(DP * AttnType<DT>::ES, false)) void k_attention_gkv_few(AttnArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef BwdShape<DT, DP> S;
+    constexpr int RB = S::RB, QT = S::QT, NB = S::template buffers<W>();
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const Work work = work_of(a, a.kv_heads * S::kParts);
+    if (work.head < 0) return;
+    const int kv_head = work.head / S::kParts;
+    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63;
+    unsigned char* own = smem + wave * NB * S::kOwn;
+    const SeqTile st = a.tiles[work.tile];
+    const Pair p = pair_of_keys(a, st);
+    const int key0 = a.causal ? (p.nk - 1) / 32 * 32 - st.row : st.row, key = key0 + (lane & 31), shift = p.nk - p.nq;
+    TileLoad<RB, QT, 1> lq, lo;
+    lq.init(0, lane, a.q.ld, a.dim_bytes);
+    lo.init(0, lane, a.gout.ld, a.dim_bytes);
+    const int begin = a.causal ? max(0, key0 - shift) / QT * QT : 0, per_head = begin < p.nq ? (p.nq - begin + QT - 1) / QT : 0, n = per_head * a.group;
+    int head = kv_head * a.group, at = wave;            // the wave's next block: the at-th of the head
+    auto settle = [&] { while (at >= per_head) { at -= per_head; ++head; } };
+    auto load = [&](int b) {
+        const int r0 = begin + at * QT;
+        lq.load((lds_byte*)own + b * S::kOwn, a.q.p + (int64_t)p.q0 * a.q.ld + head * a.q.hs, a.q.ld, r0, p.nq, a.dim_bytes, 0);
+        lo.load((lds_byte*)own + b * S::kOwn + S::kBlock, a.gout.p + (int64_t)p.q0 * a.gout.ld + head * a.gout.hs, a.gout.ld, r0, p.nq, a.dim_bytes, 0);
+        load_stats(a, (lds_byte*)own + b * S::kOwn + 2 * S::kBlock, head, p.q0, r0, p.nq, lane);
+    };
+    if (wave < n) {
+        settle();
+        load(0);
+    }
+    GkvWave<DT, DP> w;
+    w.init(a, p, kv_head, work.head % S::kParts, key0, lane);
+    int b = 0;
+    for (int j = wave; j < n; j += W) {
+        __builtin_amdgcn_s_waitcnt(0);
+        const unsigned char* now = own + b * S::kOwn;
+        const int r0 = begin + at * QT;
+        if (j + W < n) {
+            at += W;
+            settle();
+            if (NB == 2) load(b ^= 1);
         }
-        if (a.causal && r0 + shift < key0 + 31) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (r0 + 8 * (r >> 2) + 4 * half + (r & 3) + shift < key) p[r] = ds[r] = 0.f;
+        w.block((const lds_byte*)now, (const lds_byte*)now + S::kBlock, (const float*)(now + 2 * S::kBlock), a.causal && r0 + shift < key0 + 31, key - shift - r0);
+        if (NB == 1 && j + W < n) {
+            __builtin_amdgcn_s_waitcnt(0);          // what is read there has been read
+            load(0);
         }
-        Weights<DT> wp, wd;
-        wp.set(p);
-        wd.set(ds);
-#pragma unroll
-        for (int c = 0; c < COLS; ++c) columns(gv[c], ot + part * S::kPart, 0, c, wp);
-#pragma unroll
-        for (int c = 0; c < COLS; ++c) columns(gk[c], qt + part * S::kPart, 0, c, wd);
     }
-    if (key >= nk) return;
-    if (a.gk.p) {
-        unsigned char* out = a.gk.p + (int64_t)(k0 + key) * a.gk.ld + kv_head * a.gk.hs;
-        const float f = a.negative ? -a.scale : a.scale;
-#pragma unroll
-        for (int c = 0; c < COLS; ++c) store_columns<DT>(gk[c], f, out, part * COLS + c, a.dim_bytes, half);
-    }
-    if (a.gv.p) {
-        unsigned char* out = a.gv.p + (int64_t)(k0 + key) * a.gv.ld + kv_head * a.gv.hs;
-#pragma unroll
-        for (int c = 0; c < COLS; ++c) store_columns<DT>(gv[c], 1.f, out, part * COLS + c, a.dim_bytes, half);
-    }
+    add_results<W>(smem, w.gk, wave, lane);
+    add_results<W>(smem, w.gv, wave, lane);
+    if (wave == 0) w.store(a, p, kv_head, key);
 #endif
 }
 
 template <int DT, int DP> static void launch_bwd(const AttnArgs& a, const AttnArgs& b, bool keys, hipStream_t st) {
     typedef BwdShape<DT, DP> S;
-    const unsigned nq = (unsigned)(((int64_t)a.n_tiles * a.heads * S::kParts + 7) / 8 * 8), nk = (unsigned)(((int64_t)b.n_tiles * b.kv_heads * S::kParts + 7) / 8 * 8);
-    if (nq) k_attention_gq<DT, DP, 4><<<nq, 256, S::kLds, st>>>(a);
-    if (keys && nk) k_attention_gkv<DT, DP, 4><<<nk, 256, S::kLds, st>>>(b);
+    constexpr int FEW = few_waves(DP * AttnType<DT>::ES);
+    static_assert(S::template lds_few<FEW>() <= 160 * 1024 && S::kLdsKeys <= 160 * 1024, "a compute unit has 160 KiB");
+    static_assert(S::kParts <= kMostParts, "the launch is checked for them");
+    const unsigned nq = work_blocks(a, a.heads * S::kParts), nk = work_blocks(b, b.kv_heads * S::kParts);
+    if (nq && a.tile_rows == 32) k_attention_gq_few<DT, DP, FEW><<<nq, 64 * FEW, S::template lds_few<FEW>(), st>>>(a);
+    else if (nq && a.tile_rows == 64) k_attention_gq<DT, DP, 2><<<nq, 128, S::kLdsKeys, st>>>(a);
+    else if (nq) k_attention_gq<DT, DP, 4><<<nq, 256, S::kLdsKeys, st>>>(a);
+    if (!keys || !nk) return;
+    if (b.tile_rows == 32) k_attention_gkv_few<DT, DP, FEW><<<nk, 64 * FEW, S::template lds_few<FEW>(), st>>>(b);
+    else if (b.tile_rows == 64) k_attention_gkv<DT, DP, 2><<<nk, 128, S::kLdsQueries, st>>>(b);
+    else k_attention_gkv<DT, DP, 4><<<nk, 256, S::kLdsQueries, st>>>(b);
 }
 
 template <int DT> static void launch_bwd_dim(const AttnArgs& a, const AttnArgs& b, int dim, bool keys, hipStream_t st) {
@@ -252,15 +445,20 @@ template <int DT> static void launch_bwd_dim(const AttnArgs& a, const AttnArgs& 
     else launch_bwd<DT, 256>(a, b, keys, st);
 }
 
-fx_status attention_bwd_launch(const AttnArgs& a, fx_dtype dt, int dim, int64_t, int64_t longest_k, const SeqTile* k_tiles, int32_t n_k_tiles, bool keys, hipStream_t st) {
+void attention_bwd_launch(const AttnArgs& a, const AttnArgs& keys_tiles, fx_dtype dt, int dim, bool keys, hipStream_t st) {
     AttnArgs b = a;
-    b.tiles = k_tiles;
-    b.n_tiles = n_k_tiles;
-    (void)longest_k;
+    b.tiles = keys_tiles.tiles;
+    b.n_tiles = keys_tiles.n_tiles;
+    b.tile_rows = keys_tiles.tile_rows;
+    if (b.order != kHeadsFirst) b.order = b.kv_heads % 8 ? kTilesFirst : kHeadsApart;
+    b.chunk = b.order == kHeadsFirst ? std::max(1, std::min(8, b.n_tiles / 64)) : 1;
+    if (b.causal && (int64_t)b.n_tiles * b.kv_heads <= 2 * compute_units()) {
+        b.order = kHeadsFirst;
+        b.chunk = b.fold = 1;
+    }
     if (dt == FX_F32) launch_bwd_dim<FX_F32>(a, b, dim, keys, st);
     else if (dt == FX_F16) launch_bwd_dim<FX_F16>(a, b, dim, keys, st);
     else launch_bwd_dim<FX_BF16>(a, b, dim, keys, st);
-    return FX_OK;
 }
 
 }  // namespace fx

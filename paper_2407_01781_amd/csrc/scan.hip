@@ -659,7 +659,7 @@ static int64_t list_tiles(const int64_t* h_joffsets, int32_t B, SeqTile* out, co
         for (int32_t b = 0; b < B; ++b) {
             const int64_t len = h_joffsets[2 * b + 1] - h_joffsets[2 * b];
             int64_t& at = count[cls(len)];
-            for (int64_t r = (len + T - 1) / T * T - T; r >= 0; r -= T) out[at++] = SeqTile{b, (int32_t)r};
+            for (int64_t r = (len + T - 1) / T * T - T; r >= 0; r -= T) out[at++] = SeqTile{b, (int32_t)r, (int32_t)h_joffsets[2 * b], (int32_t)len};
         }
         out += n_tiles[t];
     }
@@ -685,12 +685,12 @@ extern "C" fx_status fx_build_sequences(const int64_t* h_joffsets, int32_t B, in
     if (rows > 0x7FFFFFFFll) { set_error("%s: more than 2^31-1 rows", who); return FX_ERANGE; }
     hipStream_t st = (hipStream_t)stream;
     const int64_t words = rows / 64 + 2;
-    int64_t n_tiles[kSeqTileKinds];
-    for (int t = 0; t < kSeqTileKinds; ++t) {
+    int64_t n_tiles[kSeqTileKinds], all_tiles = 0;
+    for (int t = 0; t < kSeqTileKinds; all_tiles += n_tiles[t++]) {
         n_tiles[t] = 0;
         for (int32_t b = 0; b < B; ++b) n_tiles[t] += (h_joffsets[2 * b + 1] - h_joffsets[2 * b] + kSeqTileRows[t] - 1) / kSeqTileRows[t];
     }
-    const size_t bytes = (size_t)words * 12 + (size_t)B * 8 + 4 + (size_t)(n_tiles[0] + n_tiles[1]) * sizeof(fx::SeqTile);
+    const size_t lists = ((size_t)words * 12 + (size_t)B * 8 + 4 + 15) / 16 * 16, bytes = lists + (size_t)all_tiles * sizeof(SeqTile);
     void* staging = nullptr;
     FX_HIP_TRY(hipStreamSynchronize(st));           // an upload before this one may still read the staging area
     FX_TRY(host_staging(&staging, bytes, 1));
@@ -710,7 +710,7 @@ extern "C" fx_status fx_build_sequences(const int64_t* h_joffsets, int32_t B, in
     int32_t* first = ids + B;
     for (int32_t b = 0; b < B; ++b) first[b] = (int32_t)h_joffsets[2 * b];
     first[B] = (int32_t)rows;
-    SeqTile* tiles = (SeqTile*)(first + B + 1);
+    SeqTile* tiles = (SeqTile*)((char*)staging + lists);
     const int64_t longest = list_tiles(h_joffsets, B, tiles, n_tiles);
     fx_sequences* q = new (std::nothrow) fx_sequences;
     if (!q) { set_error("%s: out of host memory", who); return FX_ENOMEM; }
@@ -732,9 +732,8 @@ extern "C" fx_status fx_build_sequences(const int64_t* h_joffsets, int32_t B, in
     q->d_id = q->d_rank + words;
     q->d_empty = q->d_id + some;
     q->d_first = q->d_id + B;
-    q->d_tiles[0] = (const SeqTile*)(q->d_first + B + 1);
-    q->d_tiles[1] = q->d_tiles[0] + n_tiles[0];
-    for (int t = 0; t < kSeqTileKinds; ++t) q->n_tiles[t] = n_tiles[t];
+    const SeqTile* d_tiles = (const SeqTile*)((const char*)q->buf + lists);
+    for (int t = 0; t < kSeqTileKinds; d_tiles += n_tiles[t++]) { q->d_tiles[t] = d_tiles; q->n_tiles[t] = n_tiles[t]; }
     q->longest = longest;
     *out = q;
     return FX_OK;

@@ -4,10 +4,11 @@
 
 namespace fx {
 
-// A tile of one sequence's rows: those from `row` (counted from the sequence's first) on, as many as its kind has.
-struct SeqTile { int32_t seq, row; };
-constexpr int kSeqTileKinds = 2;
-constexpr int kSeqTileRows[kSeqTileKinds] = {64, 128};
+// A tile of one sequence's rows: those from `row` (counted from the sequence's first) on, as many as its kind has; and
+// the sequence itself, so that a workgroup's first load tells it all.
+struct SeqTile { int32_t seq, row, first, len; };
+constexpr int kSeqTileKinds = 3;
+constexpr int kSeqTileRows[kSeqTileKinds] = {32, 64, 128};
 
 }  // namespace fx
 
