@@ -755,12 +755,13 @@ def dropout(x: torch.Tensor, p: float, seed: int, offset: int, residual: Optiona
 
 
 # ------------------------------------------------------------------------------------------ attention
-def _heads(t: torch.Tensor, rows: int, heads: int, dim: int, dtype: torch.dtype, name: str):
+def _heads(t: torch.Tensor, shape, dtype: torch.dtype, device: int, name: str):
     """Address and strides from row to row and head to head of a tensor of heads [rows, heads, dim]: any order of rows and
     heads, a head's elements next to each other."""
-    if t.dtype != dtype or t.shape != (rows, heads, dim) or not t.is_cuda or t.get_device() != torch.cuda.current_device():
-        raise AssertionError(f"{name}: {(rows, heads, dim)} {dtype} on the current GPU expected")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        raise AssertionError(f"{name}: {tuple(shape)} {dtype} on the current GPU expected")
     ld, hs, one = t.stride()
+    rows, heads, dim = shape
     if one != 1 and dim > 1 and rows:
         raise AssertionError(f"{name}: a head's elements have to lie next to each other")
     # the stride of a single row or head says nothing
@@ -776,25 +777,26 @@ def _out_heads(out: Optional[torch.Tensor], like: torch.Tensor, name: str = "out
 def _floats(t: Optional[torch.Tensor], shape, name: str):
     if t is None:
         return None
-    assert t.is_cuda and t.dtype == torch.float32 and t.shape == shape and t.is_contiguous(), \
+    assert t.is_cuda and t.dtype is torch.float32 and t.shape == shape and t.is_contiguous(), \
         f"{name}: contiguous float32 {tuple(shape)} on the GPU expected"
     return t.data_ptr()
 
 
 def _numbers(t: torch.Tensor, n: int, name: str) -> int:
-    assert t.is_cuda and t.dtype == torch.int32 and t.shape == (n,) and t.is_contiguous(), f"{name}: contiguous int32 ({n},) on the GPU expected"
+    assert t.is_cuda and t.dtype is torch.int32 and t.shape == (n,) and t.is_contiguous(), f"{name}: contiguous int32 ({n},) on the GPU expected"
     return t.data_ptr()
 
 
-def _attention(seqs: Sequences, kv_seqs: Optional[Sequences], q, k, v, causal: bool, scale: Optional[float]) -> _Attention:
+def _attention(seqs: Sequences, kv_seqs: Optional[Sequences], q, k, v, causal: bool, scale: Optional[float], device: int) -> _Attention:
     assert q.dim() == 3 and k.dim() == 3 and q.dtype in _TORCH_DT, "q, k, v: [rows, heads, dim]"
-    rows, heads, dim = q.shape
-    kv_rows, kv_heads = (kv_seqs or seqs).rows, k.shape[1]
+    rows, heads, dim = shape = q.shape
+    dtype = q.dtype
     assert rows == seqs.rows, f"q: {seqs.rows} rows expected"
-    qp, kp, vp = _heads(q, rows, heads, dim, q.dtype, "q"), _heads(k, kv_rows, kv_heads, dim, q.dtype, "k"), _heads(v, kv_rows, kv_heads, dim, q.dtype, "v")
+    kv = (seqs if kv_seqs is None else kv_seqs).rows, k.shape[1], dim
     # in the order of the members
-    return _Attention(seqs._h, None if kv_seqs is None else kv_seqs._h, _TORCH_DT[q.dtype], heads, kv_heads, dim, int(causal),
-                      dim ** -0.5 if scale is None else scale, qp[0], kp[0], vp[0], *qp[1:], *kp[1:], *vp[1:])
+    (qp, lq, hq), (kp, lk, hk), (vp, lv, hv) = _heads(q, shape, dtype, device, "q"), _heads(k, kv, dtype, device, "k"), _heads(v, kv, dtype, device, "v")
+    return _Attention(seqs._h, None if kv_seqs is None else kv_seqs._h, _TORCH_DT[dtype], heads, kv[1], dim, causal,
+                      dim ** -0.5 if scale is None else scale, qp, kp, vp, lq, hq, lk, hk, lv, hv)
 
 
 def attention_fwd(seqs: Sequences, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, scale: Optional[float] = None,
@@ -803,9 +805,10 @@ def attention_fwd(seqs: Sequences, q: torch.Tensor, k: torch.Tensor, v: torch.Te
     head h reads key head h // (heads / kv_heads)), or rows of kv_seqs, as many sequences.  causal: the last query stands at the last
     key, and none sees a later one.  scale: dim ** -0.5 without.  Returns out [rows, heads, dim] and lse [heads, rows] float32, the
     logarithm of the sum of exp(scale q . k); 0 and -inf for a row that sees no key."""
-    a = _attention(seqs, kv_seqs, q, k, v, causal, scale)
+    device = torch.cuda.current_device()
+    a = _attention(seqs, kv_seqs, q, k, v, causal, scale, device)
     out = _out_heads(out, q)
-    op = _heads(out, *q.shape, q.dtype, "out")
+    op = _heads(out, q.shape, q.dtype, device, "out")
     lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
     _check(lib.fx_attention_fwd(a, *op, lse.data_ptr(), _stream()))
     return out, lse
@@ -815,13 +818,14 @@ def attention_bwd(seqs: Sequences, q: torch.Tensor, k: torch.Tensor, v: torch.Te
                   grad_out: torch.Tensor, grad_lse: Optional[torch.Tensor] = None, causal: bool = False, scale: Optional[float] = None,
                   kv_seqs: Optional[Sequences] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """Gradients of attention_fwd's q, k and v; out and lse are its outputs, grad_lse the gradient of the second (zeros without)."""
-    a = _attention(seqs, kv_seqs, q, k, v, causal, scale)
-    op, gp = _heads(out, *q.shape, q.dtype, "out"), _heads(grad_out, *q.shape, q.dtype, "grad_out")
+    device = torch.cuda.current_device()
+    a = _attention(seqs, kv_seqs, q, k, v, causal, scale, device)
+    op, gp = _heads(out, q.shape, q.dtype, device, "out"), _heads(grad_out, q.shape, q.dtype, device, "grad_out")
     stats = (q.shape[1], q.shape[0])
     lp, glp = _floats(lse, stats, "lse"), _floats(grad_lse, stats, "grad_lse")
     gq, gk, gv = _out_heads(None, q), _out_heads(None, k), _out_heads(None, v)
-    outs = [x for t in (gq, gk, gv) for x in _heads(t, *t.shape, q.dtype, "gradient")]
-    _check(lib.fx_attention_bwd(a, *op, lp, *gp, glp, *outs, _stream()))
+    grads = [_heads(t, t.shape, q.dtype, device, "gradient") for t in (gq, gk, gv)]
+    _check(lib.fx_attention_bwd(a, *op, lp, *gp, glp, *grads[0], *grads[1], *grads[2], _stream()))
     return gq, gk, gv
 
 
@@ -843,6 +847,7 @@ class KVCache:
             assert (t is not None) == e4m3, "exponents belong to a cache of 8 bits"
             assert t is None or (t.is_cuda and t.dtype == torch.uint8 and t.shape == k.shape[:3] and t.is_contiguous()), "exponents: contiguous uint8 [pages, kv_heads, page_rows]"
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.kv_heads, self._device = k.shape[1], k.get_device()
         self._c = _Cache(k.data_ptr(), v.data_ptr(), None if k_exp is None else k_exp.data_ptr(), None if v_exp is None else v_exp.data_ptr(), None, 0, 0,
                          k.shape[0], k.shape[2], 3 if e4m3 else _TORCH_DT[k.dtype], k.shape[1], self.dim)
 
@@ -853,13 +858,12 @@ class KVCache:
         exp = lambda: torch.zeros((pages, kv_heads, page_rows), dtype=torch.uint8, device="cuda") if dtype == torch.float8_e4m3fn else None
         return cls(new(), new(), dim, exp(), exp())
 
-    def _with(self, table: torch.Tensor, n: int) -> _Cache:
-        assert table.is_cuda and table.dtype == torch.int32 and table.dim() == 2 and table.shape[0] == n and (table.stride(1) == 1 or table.shape[1] <= 1), \
-            f"table: int32 [{n}, columns] on the GPU expected"
-        assert self.k.get_device() == table.get_device() == torch.cuda.current_device(), "cache and table have to be on the current GPU"
-        c = _Cache.from_buffer_copy(self._c)
-        c.d_table, c.table_cols = table.data_ptr(), table.shape[1]
-        c.ld_table = table.stride(0) if n > 1 else max(table.shape[1], 1)
+    def _with(self, table: torch.Tensor, n: int, device: int) -> _Cache:
+        assert table.dtype is torch.int32 and table.dim() == 2 and table.shape[0] == n and (table.stride(1) == 1 or table.shape[1] <= 1), \
+            f"table: int32 [{n}, columns] expected"
+        assert self._device == device and table.get_device() == device, "cache and table have to be on the current GPU"
+        c, cols = _Cache.from_buffer_copy(self._c), table.shape[1]
+        c.d_table, c.table_cols, c.ld_table = table.data_ptr(), cols, table.stride(0) if n > 1 else max(cols, 1)
         return c
 
 
@@ -868,10 +872,12 @@ def cache_write(cache: KVCache, table: torch.Tensor, start: torch.Tensor, k: tor
     seqs row b is one new row of sequence b.  No two rows may have one place; those whose position has no page are left out."""
     n = k.shape[0] if seqs is None else seqs.batch_size
     rows = k.shape[0] if seqs is None else seqs.rows
-    c = cache._with(table, n)
-    assert k.dtype in _TORCH_DT
-    kp, vp = (_heads(t, rows, c.kv_heads, cache.dim, k.dtype, name) for t, name in ((k, "k"), (v, "v")))
-    _check(lib.fx_cache_write(c, None if seqs is None else seqs._h, rows, _numbers(start, n, "start"), _TORCH_DT[k.dtype], *kp, *vp, _stream()))
+    device = torch.cuda.current_device()
+    c = cache._with(table, n, device)
+    assert k.dtype in _TORCH_DT, "k and v: float32, float16 or bfloat16"
+    shape = rows, cache.kv_heads, cache.dim
+    _check(lib.fx_cache_write(c, None if seqs is None else seqs._h, rows, _numbers(start, n, "start"), _TORCH_DT[k.dtype],
+                              *_heads(k, shape, k.dtype, device, "k"), *_heads(v, shape, k.dtype, device, "v"), _stream()))
 
 
 def cache_read(cache: KVCache, table: torch.Tensor, start: torch.Tensor, seqs: Sequences,
@@ -880,10 +886,12 @@ def cache_read(cache: KVCache, table: torch.Tensor, start: torch.Tensor, seqs: S
     (zeros for those that have no page); dtype: the cache's, which has to be said for one of 8 bits."""
     dtype = cache.k.dtype if dtype is None else dtype
     assert dtype in _TORCH_DT, "dtype: float32, float16 or bfloat16"
-    c = cache._with(table, seqs.batch_size)
-    k, v = (torch.empty((seqs.rows, c.kv_heads, cache.dim), dtype=dtype, device=cache.k.device) for _ in range(2))
-    outs = [x for t in (k, v) for x in _heads(t, *t.shape, dtype, "out")]
-    _check(lib.fx_cache_read(c, seqs._h, _numbers(start, seqs.batch_size, "start"), _TORCH_DT[dtype], *outs, _stream()))
+    device = torch.cuda.current_device()
+    c = cache._with(table, seqs.batch_size, device)
+    shape = seqs.rows, cache.kv_heads, cache.dim
+    k, v = (torch.empty(shape, dtype=dtype, device=cache.k.device) for _ in range(2))
+    _check(lib.fx_cache_read(c, seqs._h, _numbers(start, seqs.batch_size, "start"), _TORCH_DT[dtype], *_heads(k, shape, dtype, device, "k"),
+                             *_heads(v, shape, dtype, device, "v"), _stream()))
     return k, v
 
 
@@ -893,12 +901,13 @@ def attention_step(cache: KVCache, table: torch.Tensor, lengths: torch.Tensor, q
     the cache holds of it.  longest: what no length passes (longer ones are cut there), if the program knows better than the table's width.  Returns out [n, heads, dim]
     and lse [n, heads] float32."""
     assert q.dim() == 3 and q.dtype in _TORCH_DT
-    n, heads, dim = q.shape
-    c = cache._with(table, n)
+    n, heads, dim = shape = q.shape
+    device = torch.cuda.current_device()
+    c = cache._with(table, n, device)
     assert dim == cache.dim, f"q: {cache.dim} dimensions expected"
-    qp = _heads(q, n, heads, dim, q.dtype, "q")
+    qp = _heads(q, shape, q.dtype, device, "q")
     out = _out_heads(out, q)
     lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
     _check(lib.fx_attention_step(c, n, _numbers(lengths, n, "lengths"), longest, _TORCH_DT[q.dtype], heads, dim ** -0.5 if scale is None else scale,
-                                 *qp, *_heads(out, n, heads, dim, q.dtype, "out"), lse.data_ptr(), _stream()))
+                                 *qp, *_heads(out, shape, q.dtype, device, "out"), lse.data_ptr(), _stream()))
     return out, lse

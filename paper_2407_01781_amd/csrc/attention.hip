@@ -251,20 +251,51 @@ template <int DT> static void launch_fwd_dim(const AttnArgs& a, int dim, hipStre
 }
 
 // ------------------------------------------------------------------ rows in an order that the kernels take
+// Copies of a call, all in one launch: rows of dim_s elements a head, 16 bytes of the destination a thread (dim_d is whole pieces
+// of 16 bytes, or dim_s where the destination is the caller's), zeros behind dim_s.
+struct Copy { HeadsView src, dst; uint32_t heads, pieces, first_block; int64_t n; };
+struct Copies { Copy c[8]; int32_t count, dim_s, dim_d; };
+
 template <typename W>
-__global__ void k_heads_copy(const unsigned char* src, int64_t ld_s, int64_t hs_s, int dim_s, unsigned char* dst, int64_t ld_d, int64_t hs_d, int dim_d, int heads, int64_t n) {
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
-        const int64_t e = i % dim_d, h = i / dim_d % heads, r = i / dim_d / heads;
-        ((W*)(dst + r * ld_d + h * hs_d))[e] = e < dim_s ? ((const W*)(src + r * ld_s + h * hs_s))[e] : W(0);
-    }
+__global__ __launch_bounds__(256) void k_heads_copy(Copies a) {
+    constexpr int PER = 16 / sizeof(W);
+    int which = 0;
+    while (which + 1 < a.count && blockIdx.x >= a.c[which + 1].first_block) ++which;
+    const Copy& c = a.c[which];
+    const int64_t i = (int64_t)(blockIdx.x - c.first_block) * 256 + threadIdx.x;
+    if (i >= c.n) return;
+    const int64_t unit = i / c.pieces, r = unit / c.heads;
+    const int e0 = (int)(i - unit * c.pieces) * PER;
+    const int64_t h = unit - r * c.heads;
+    const W* src = (const W*)(c.src.p + r * c.src.ld + h * c.src.hs) + e0;
+    W* dst = (W*)(c.dst.p + r * c.dst.ld + h * c.dst.hs) + e0;
+    W x[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) x[e] = e0 + e < a.dim_s ? src[e] : W(0);
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+        if (e0 + e < a.dim_d) dst[e] = x[e];
 }
 
-static void copy_heads(const HeadsView& src, int dim_s, const HeadsView& dst, int dim_d, int heads, int64_t rows, fx_dtype dt, hipStream_t st) {
-    const int64_t n = rows * heads * dim_d;
-    const unsigned blocks = (unsigned)std::min<int64_t>((n + 255) / 256, 1 << 16);
-    if (dt == FX_F32) k_heads_copy<uint32_t><<<blocks, 256, 0, st>>>(src.p, src.ld, src.hs, dim_s, dst.p, dst.ld, dst.hs, dim_d, heads, n);
-    else k_heads_copy<uint16_t><<<blocks, 256, 0, st>>>(src.p, src.ld, src.hs, dim_s, dst.p, dst.ld, dst.hs, dim_d, heads, n);
-}
+struct CopyList {
+    Copies a{};
+    int64_t blocks = 0;
+    void add(const HeadsView& src, const HeadsView& dst, int dim_d, int32_t heads, int64_t rows, int es) {
+        const uint32_t pieces = (uint32_t)((dim_d * es + 15) / 16);
+        const int64_t n = rows * heads * pieces;
+        a.c[a.count++] = Copy{src, dst, (uint32_t)heads, pieces, (uint32_t)blocks, n};
+        blocks += (n + 255) / 256;
+    }
+    fx_status run(const char* who, int dim_s, int dim_d, int es, hipStream_t st) {
+        if (!a.count) return FX_OK;
+        if (blocks > (1ll << 32) / 256 - 1) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }
+        a.dim_s = dim_s;
+        a.dim_d = dim_d;
+        if (es == 4) k_heads_copy<uint32_t><<<(unsigned)blocks, 256, 0, st>>>(a);
+        else k_heads_copy<uint16_t><<<(unsigned)blocks, 256, 0, st>>>(a);
+        return FX_OK;
+    }
+};
 
 // ------------------------------------------------------------------ checks
 fx_status check_heads(const char* who, const HeadsTensor& t, int32_t dim, int es) {
@@ -311,37 +342,25 @@ static fx_status check_attention(const char* who, const fx_attention* a) {
     return FX_OK;
 }
 
-// Fills the views of the tensors; those whose order the kernels do not take are copied (outputs: get a place to be copied from).
-static fx_status take_tensors(const char* who, HeadsTensor* t, int n, int32_t dim, fx_dtype dt, Scratch* scratch, bool* copied, int* dim_in, hipStream_t st) {
+// Fills the views of the tensors; those whose order the kernels do not take are copied, and outputs get a place to be copied from
+// (back).
+static fx_status take_tensors(const char* who, HeadsTensor* t, int n, int32_t dim, fx_dtype dt, Scratch* scratch, CopyList* back, int* dim_in, hipStream_t st) {
     const int es = dtype_size(dt), per = 16 / es, padded = (dim + per - 1) / per * per;
-    bool any = false;
-    for (int i = 0; i < n; ++i) {
-        copied[i] = false;
-        if (!t[i].p || t[i].rows == 0) continue;
-        const bool strides = (t[i].ld * es) % 16 == 0 && (t[i].heads == 1 || (t[i].hs * es) % 16 == 0) && t[i].ld * es <= (1ll << 24);
-        copied[i] = dim % per || (uintptr_t)t[i].p % 16 || !strides;
-        any |= copied[i];
-    }
+    CopyList in;
     *dim_in = padded;
     for (int i = 0; i < n; ++i) {
-        if (!t[i].p) { *t[i].view = HeadsView{nullptr, 0, 0}; continue; }
         const HeadsView given{(unsigned char*)t[i].p, t[i].ld * es, t[i].hs * es};
         *t[i].view = given;
-        if (!copied[i]) continue;
+        if (!t[i].p || t[i].rows == 0) continue;
+        const bool strides = given.ld % 16 == 0 && (t[i].heads == 1 || given.hs % 16 == 0) && given.ld <= (1ll << 24);
+        if (dim % per == 0 && (uintptr_t)t[i].p % 16 == 0 && strides) continue;
         void* p = nullptr;
         FX_TRY(scratch->get(who, &p, (size_t)t[i].rows * t[i].heads * padded * es));
         *t[i].view = HeadsView{(unsigned char*)p, (int64_t)t[i].heads * padded * es, (int64_t)padded * es};
-        if (!t[i].output) copy_heads(given, dim, *t[i].view, padded, t[i].heads, t[i].rows, dt, st);
+        if (t[i].output) back->add(*t[i].view, given, dim, t[i].heads, t[i].rows, es);
+        else in.add(given, *t[i].view, padded, t[i].heads, t[i].rows, es);
     }
-    (void)any;
-    return FX_OK;
-}
-
-static void return_tensors(const HeadsTensor* t, int n, int32_t dim, fx_dtype dt, const bool* copied, int dim_in, hipStream_t st) {
-    (void)dim_in;
-    const int es = dtype_size(dt);
-    for (int i = 0; i < n; ++i)
-        if (copied[i] && t[i].output) copy_heads(*t[i].view, dim, HeadsView{(unsigned char*)t[i].p, t[i].ld * es, t[i].hs * es}, dim, t[i].heads, t[i].rows, dt, st);
+    return in.run(who, dim, padded, es, st);
 }
 
 static fx_status check_places(const char* who, const HeadsTensor* t, int n) {
@@ -406,15 +425,15 @@ extern "C" fx_status fx_attention_fwd(const fx_attention* d, void* d_out, int64_
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps(kProfAttnFwd, st);
     Scratch scratch(st);
-    bool copied[4];
+    CopyList back;
     int dim;
-    FX_TRY(take_tensors(who, t, 4, d->dim, d->dt, &scratch, copied, &dim, st));
+    FX_TRY(take_tensors(who, t, 4, d->dim, d->dt, &scratch, &back, &dim, st));
     a.dim_bytes = dim * dtype_size(d->dt);
     a.lse = d_lse;
     if (d->dt == FX_F32) launch_fwd_dim<FX_F32>(a, dim, st);
     else if (d->dt == FX_F16) launch_fwd_dim<FX_F16>(a, dim, st);
     else launch_fwd_dim<FX_BF16>(a, dim, st);
-    return_tensors(t, 4, d->dim, d->dt, copied, dim, st);
+    FX_TRY(back.run(who, d->dim, d->dim, dtype_size(d->dt), st));
     FX_HIP_TRY(hipGetLastError());
     return FX_OK;
 }
@@ -448,9 +467,9 @@ extern "C" fx_status fx_attention_bwd(const fx_attention* d, const void* d_out, 
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps(kProfAttnBwd, st);
     Scratch scratch(st);
-    bool copied[n];
+    CopyList back;
     int dim;
-    FX_TRY(take_tensors(who, t, n, d->dim, d->dt, &scratch, copied, &dim, st));
+    FX_TRY(take_tensors(who, t, n, d->dim, d->dt, &scratch, &back, &dim, st));
     void* stats = nullptr;
     FX_TRY(scratch.get(who, &stats, (size_t)nq * d->heads * 8));
     a.dim_bytes = dim * dtype_size(d->dt);
@@ -458,7 +477,7 @@ extern "C" fx_status fx_attention_bwd(const fx_attention* d, const void* d_out, 
     a.glse = d_glse;
     a.stats = (float*)stats;
     attention_bwd_launch(a, b, d->dt, dim, d_gk || d_gv, st);
-    return_tensors(t, n, d->dim, d->dt, copied, dim, st);
+    FX_TRY(back.run(who, d->dim, d->dim, dtype_size(d->dt), st));
     FX_HIP_TRY(hipGetLastError());
     return FX_OK;
 }

@@ -87,12 +87,13 @@ __global__ __launch_bounds__(256) void k_cache_write(CacheArgs c, CacheRows a) {
     const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> a.lanes_log2, all = a.rows * c.kv_heads;
     const int64_t u = min(unit, all - 1), r = u / c.kv_heads;       // lanes without a row take part in the shuffles
     const int head = (int)(u - r * c.kv_heads);
+    __attribute__((aligned(16))) T both[2][8];
+    take8<T, VEC>(both[0], (const T*)(a.k.p + r * a.k.ld + head * a.k.hs) + d, c.dim - d);
+    take8<T, VEC>(both[1], (const T*)(a.v.p + r * a.v.ld + head * a.v.hs) + d, c.dim - d);
     const int64_t at = place_of(c, a, r, head);
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        const HeadsView s = which ? a.v : a.k;
-        __attribute__((aligned(16))) T x[8];
-        take8<T, VEC>(x, (const T*)(s.p + r * s.ld + head * s.hs) + d, c.dim - d);
+        const T* x = both[which];
         unsigned char* to = (which ? c.v : c.k) + (at * c.pitch + d) * (E4M3 ? 1 : AttnType<DT>::ES);
         const bool write = unit < all && at >= 0 && d < c.pitch;
         if (E4M3) {
@@ -161,13 +162,20 @@ constexpr int kStepTile = 32, kStepHeads = 16;
 struct StepArgs {
     CacheArgs c;
     HeadsView q, out;
-    float *lse, *part, *stats;          // part [row, head, split, dim], stats [row, head, split, 2]: maximum (base 2), sum
+    float *lse, *part, *stats;          // part [row, head, split, pitch], stats [row, head, split, 2]: maximum (base 2), sum
     int64_t most;
-    int32_t heads, group, groups, splits, chunk;
+    int32_t heads, group, groups, splits;
+    int32_t whole;                      // queries may be loaded 16 bytes at a time
     float scale2;                       // scale log2(e)
     uint32_t magic;                     // p / page_rows = p * magic >> shift for p below 2^31
     int32_t shift;
 };
+
+// Workgroups of four waves that share a compute unit, a wave on each SIMD: registers are allotted for them
+constexpr int step_resident(int dt, bool e4m3, int dp) {
+    const bool wide = dt == FX_F32 && !e4m3;
+    return dp > 128 ? (e4m3 && dt == FX_BF16 ? 2 : 1) : dp > 64 ? (dt == FX_F32 ? 2 : 3) : wide ? 3 : 4;
+}
 
 template <int DT, bool E4M3, int DP> struct StepShape {
     static constexpr bool kWide = DT == FX_F32 && !E4M3;           // fp32 keys and values
@@ -176,9 +184,11 @@ template <int DT, bool E4M3, int DP> struct StepShape {
     static constexpr int KL = DP * SB / 64;                        // 16-byte loads of a key by a lane
     static constexpr int QP = !E4M3 || DT == FX_BF16 ? 1 : DT == FX_F16 ? 2 : 3;    // parts of a query
     static constexpr int PP = E4M3 && DT == FX_F32 ? 3 : 2;                        // parts of a weight
+    static constexpr int kResident = step_resident(DT, E4M3, DP);
     // waves of a workgroup that has a sequence to itself: as many as the registers hold without spills
     static constexpr int kMany = DP > 128 ? 4 : DP > 64 || kWide || (E4M3 && DT != FX_BF16) ? 8 : 16;
 };
+
 
 template <bool F16> struct Mma16;
 template <> struct Mma16<true> {
@@ -201,8 +211,14 @@ __device__ __forceinline__ uint32_t codes_to_bf16(uint32_t codes, float scale, b
     return u;
 }
 
-template <int DT, bool E4M3, int DP, int W>
-__global__ __launch_bounds__(64 * W) void k_attention_step(StepArgs a) {
+// Positions of a split: the sequence's own share, whole rounds of a workgroup's waves, and enough to be worth its beginning and end
+constexpr int kLeastChunk = 256;
+__device__ __forceinline__ int chunk_of(const StepArgs& a, int len) {
+    return a.splits == 1 ? max(len, 1) : max(kLeastChunk, ((len - 1) / a.splits + 128) / 128 * 128);
+}
+
+template <int DT, bool E4M3, int DP, int W, int RESIDENT>
+__global__ __launch_bounds__(64 * W, RESIDENT) void k_attention_step(StepArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef StepShape<DT, E4M3, DP> S;
     typedef typename AttnType<DT>::T T;
@@ -219,10 +235,15 @@ __global__ __launch_bounds__(64 * W) void k_attention_step(StepArgs a) {
     item /= a.groups;
     const int kv = item % a.c.kv_heads;
     const int64_t b = item / a.c.kv_heads;
-    const int64_t len = min((int64_t)a.c.start[b], a.most);
-    const int64_t from = (int64_t)split * a.chunk;
+    // row of the cache that position t + lane % 32 has, or -1; asked for one tile ahead
+    const int32_t* table = a.c.table + b * a.c.ld_table;
+    auto row_in = [&](int page, uint32_t pos, uint32_t col) {
+        return page < 0 || page >= a.c.pages ? -1 : (page * a.c.kv_heads + kv) * a.c.page_rows + (int)(pos - col * a.c.page_rows);
+    };
+    const int len = (int)max((int64_t)0, min((int64_t)a.c.start[b], a.most)), chunk = chunk_of(a, len);
+    const int64_t from = (int64_t)split * chunk;
     if (a.splits > 1 && from >= len) return;           // the join knows as much
-    const int end = (int)max((int64_t)0, min(len, from + a.chunk));
+    const int end = (int)min((int64_t)len, from + chunk);
     const int first_head = kv * a.group + part_of_group * kStepHeads, n_heads = min(kStepHeads, a.group - part_of_group * kStepHeads);
     const int row_bytes = a.c.pitch * SB;
 
@@ -236,8 +257,17 @@ __global__ __launch_bounds__(64 * W) void k_attention_step(StepArgs a) {
             constexpr int PER = S::kWide ? 4 : 8;
             const int d0 = E4M3 ? (f >> 1) * 64 + g * 16 + (f & 1) * 8 : f * (4 * PER) + g * PER;
             float x[8];
+            if (a.whole) {
+                __attribute__((aligned(16))) T y[8];
+                const bool there = some && d0 < a.c.dim;
 #pragma unroll
-            for (int e = 0; e < PER; ++e) x[e] = some && d0 + e < a.c.dim ? (float)qr[min(d0 + e, a.c.dim - 1)] : 0.f;
+                for (int i = 0; i < PER * (int)sizeof(T) / 16; ++i) ((u32x4*)y)[i] = there ? ((const u32x4*)(qr + d0))[i] : u32x4(0u);
+#pragma unroll
+                for (int e = 0; e < PER; ++e) x[e] = (float)y[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < PER; ++e) x[e] = some && d0 + e < a.c.dim ? (float)qr[min(d0 + e, a.c.dim - 1)] : 0.f;
+            }
             if constexpr (S::kWide) {
                 qw[0][f] = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
             } else {
@@ -260,23 +290,17 @@ __global__ __launch_bounds__(64 * W) void k_attention_step(StepArgs a) {
     for (int j = 0; j < VE; ++j) acc[j] = f32x4(0.f);
     float top = -INFINITY, sum = 0.f;
 
-    // row of the cache that position t + lane % 32 has, or -1; asked for one tile ahead
-    const int32_t* table = a.c.table + b * a.c.ld_table;
-    auto row_of = [&](int t) -> int64_t {
-        const uint32_t pos = (uint32_t)t + (lane & 31);
-        if ((int)pos >= end) return -1;
-        const uint32_t col = (uint32_t)(((uint64_t)pos * a.magic) >> a.shift);
-        const int32_t page = table[col];
-        if (page < 0 || page >= a.c.pages) return -1;
-        return ((int64_t)page * a.c.kv_heads + kv) * a.c.page_rows + (pos - col * a.c.page_rows);
+    auto row_of = [&](int t) {
+        const uint32_t pos = (uint32_t)t + (lane & 31), col = (uint32_t)(((uint64_t)pos * a.magic) >> a.shift);
+        const int page = col < (uint32_t)a.c.cols ? table[col] : -1;        // does not wait for the length
+        return (int)pos < end ? row_in(page, pos, col) : -1;
     };
     int t = (int)from + wave * kStepTile;
-    int64_t row = t < end ? row_of(t) : -1;
+    int row = row_of(t);
     for (; t < end; t += W * kStepTile) {
         const uint64_t there = __ballot(row >= 0);          // both halves of the wave hold the same 32
-        const int64_t safe = max(row, (int64_t)0);
-        const int lo = (int)(uint32_t)safe, hi = (int)(safe >> 32);
-        auto row_at = [&](int key) { return ((int64_t)__shfl(hi, key, 64) << 32) | (uint32_t)__shfl(lo, key, 64); };
+        const int safe = max(row, 0);
+        auto row_at = [&](int key) { return (int64_t)__shfl(safe, key, 64); };
         u32x4 kw[2][KL];
         float k_scale[2], v_scale[8];
         uint32_t vw[8][VW];
@@ -405,12 +429,13 @@ __global__ __launch_bounds__(64 * W) void k_attention_step(StepArgs a) {
     }
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
-    // the waves' results joined, half of them by the other half at a time
+    // the waves' results joined: three quarters of them put theirs into LDS, the others take three each
     float* shared = (float*)smem;
     constexpr int SLOT = DP * kStepHeads + 2 * kStepHeads;
 #pragma unroll
-    for (int n = W / 2; n >= 1; n /= 2) {
-        if (wave >= n && wave < 2 * n) {
+    for (int left = W; left > 1;) {
+        const int n = left >= 4 ? left / 4 : 1;
+        if (wave >= n && wave < left) {
             float* to = shared + (wave - n) * SLOT;
 #pragma unroll
             for (int j = 0; j < VE; ++j)
@@ -419,18 +444,20 @@ __global__ __launch_bounds__(64 * W) void k_attention_step(StepArgs a) {
             if (g == 0) { to[DP * kStepHeads + m16] = top; to[DP * kStepHeads + kStepHeads + m16] = sum; }
         }
         __syncthreads();
-        if (wave < n) {
-            const float* in = shared + wave * SLOT;
-            const float top2 = in[DP * kStepHeads + m16], sum2 = in[DP * kStepHeads + kStepHeads + m16], both = fmaxf(top, top2);
-            const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - both), f2 = top2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top2 - both);
-            top = both;
-            sum = sum * f + sum2 * f2;
+        if (wave < n)
+            for (int other = wave; other < left - n; other += n) {
+                const float* in = shared + other * SLOT;
+                const float top2 = in[DP * kStepHeads + m16], sum2 = in[DP * kStepHeads + kStepHeads + m16], both = fmaxf(top, top2);
+                const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - both), f2 = top2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top2 - both);
+                top = both;
+                sum = sum * f + sum2 * f2;
 #pragma unroll
-            for (int j = 0; j < VE; ++j)
+                for (int j = 0; j < VE; ++j)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[j][r] = acc[j][r] * f + in[(j * 4 + r) * 64 + lane] * f2;
-        }
-        __syncthreads();
+                    for (int r = 0; r < 4; ++r) acc[j][r] = acc[j][r] * f + in[(j * 4 + r) * 64 + lane] * f2;
+            }
+        left = n;
+        if (left > 1) __syncthreads();
     }
     if (wave != 0 || m16 >= n_heads) return;
     const int head = first_head + m16;
@@ -443,7 +470,7 @@ __global__ __launch_bounds__(64 * W) void k_attention_step(StepArgs a) {
         for (int j = 0; j < VE; ++j) {
             const int d = (4 * g + r) * VE + j;
             if (d >= a.c.dim) continue;
-            if (a.splits > 1) a.part[slot * a.c.dim + d] = acc[j][r];
+            if (a.splits > 1) a.part[slot * a.c.pitch + d] = acc[j][r];
             else out[d] = (T)(acc[j][r] * inv);
         }
     if (g) return;
@@ -452,16 +479,16 @@ __global__ __launch_bounds__(64 * W) void k_attention_step(StepArgs a) {
 #endif
 }
 
-// The splits of a row and head joined: factors of the splits in LDS, then their sums, a thread a dimension and every n-th split
+// The splits of a row and head joined: their factors in LDS, then the sums, a thread four dimensions of every n-th split
 constexpr int kJoinThreads = 512, kMostSplits = 1024;
 template <int DT>
 __global__ __launch_bounds__(kJoinThreads) void k_attention_join(StepArgs a) {
     typedef typename AttnType<DT>::T T;
-    __shared__ float f[kMostSplits], red[kJoinThreads / 64], sums[kJoinThreads];
+    __shared__ float f[kMostSplits], red[kJoinThreads / 64];
+    __shared__ f32x4 sums[kJoinThreads];
     const int64_t item = blockIdx.x, b = item / a.heads;
     const int head = (int)(item % a.heads), tid = threadIdx.x;
-    const int64_t len = max((int64_t)0, min((int64_t)a.c.start[b], a.most));
-    const int n = (int)((len + a.chunk - 1) / a.chunk);
+    const int len = (int)max((int64_t)0, min((int64_t)a.c.start[b], a.most)), chunk = chunk_of(a, len), n = (len + chunk - 1) / chunk;
     const float* stats = a.stats + 2 * item * a.splits;
     float top = -INFINITY;
     for (int i = tid; i < n; i += kJoinThreads) top = fmaxf(top, stats[2 * i]);
@@ -481,25 +508,31 @@ __global__ __launch_bounds__(kJoinThreads) void k_attention_join(StepArgs a) {
     sum = 0.f;
     for (int i = 0; i < kJoinThreads / 64; ++i) sum += red[i];
     // as many splits side by side as there are threads for; their sums are added in order
-    const int dim = a.c.dim, lanes = dim <= 32 ? 32 : dim <= 64 ? 64 : dim <= 128 ? 128 : 256, rows = kJoinThreads / lanes, d = tid % lanes;
-    float acc = 0.f;
-    if (d < dim)
+    const int fours = a.c.pitch / 4, rows = kJoinThreads / fours, at = tid % fours, first = tid / fours;
+    f32x4 acc = f32x4(0.f);
+    if (first < rows) {
+        const f32x4* part = (const f32x4*)(a.part + item * a.splits * a.c.pitch) + at;
 #pragma unroll 8
-        for (int i = tid / lanes; i < n; i += rows) acc = fmaf(f[i], a.part[(item * a.splits + i) * dim + d], acc);
+        for (int i = first; i < n; i += rows) acc += f[i] * part[(int64_t)i * fours];
+    }
     sums[tid] = acc;
     __syncthreads();
-    if (tid >= dim) return;
-    acc = 0.f;
-    for (int r = 0; r < rows; ++r) acc += sums[r * lanes + tid];
-    ((T*)(a.out.p + b * a.out.ld + head * a.out.hs))[tid] = (T)(sum == 0.f ? 0.f : acc / sum);
+    if (tid >= fours) return;
+    for (int r = 1; r < rows; ++r) acc += sums[r * fours + tid];
+    T* out = (T*)(a.out.p + b * a.out.ld + head * a.out.hs) + 4 * tid;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (4 * tid + e < a.c.dim) out[e] = (T)(sum == 0.f ? 0.f : acc[e] / sum);
     if (a.lse && tid == 0) a.lse[item] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 template <int DT, bool E4M3, int DP> static void launch_step(const StepArgs& a, int64_t blocks, hipStream_t st) {
     constexpr int SLOT = (DP * kStepHeads + 2 * kStepHeads) * 4;
-    constexpr int MANY = StepShape<DT, E4M3, DP>::kMany;
-    if (MANY == 4 || a.splits > 1) k_attention_step<DT, E4M3, DP, 4><<<(unsigned)blocks, 256, 2 * SLOT, st>>>(a);
-    else k_attention_step<DT, E4M3, DP, MANY><<<(unsigned)blocks, 64 * MANY, MANY / 2 * SLOT, st>>>(a);
+    typedef StepShape<DT, E4M3, DP> S;
+    constexpr int MANY = S::kMany;
+    static_assert((MANY - MANY / 4) * SLOT <= 160 * 1024, "a compute unit has 160 KiB");
+    if (MANY == 4 || a.splits > 1) k_attention_step<DT, E4M3, DP, 4, S::kResident><<<(unsigned)blocks, 256, 3 * SLOT, st>>>(a);
+    else k_attention_step<DT, E4M3, DP, MANY, 1><<<(unsigned)blocks, 64 * MANY, (MANY - MANY / 4) * SLOT, st>>>(a);
 }
 
 template <int DT, bool E4M3> static void launch_step_dim(const StepArgs& a, int64_t blocks, int64_t rows, hipStream_t st) {
@@ -520,6 +553,7 @@ static fx_status check_cache(const char* who, const fx_cache* c, fx_dtype dt, Ca
     if (c->store != FX_E4M3 && c->store != (int32_t)dt) { set_error("%s: rows of one type and a cache of another", who); return FX_EUNSUPPORTED; }
     if (c->dim > kMostDim) { set_error("%s: more than %d dimensions", who, kMostDim); return FX_ERANGE; }
     if (c->kv_heads > 65535) { set_error("%s: more than 65535 heads", who); return FX_ERANGE; }
+    if ((int64_t)c->pages * c->page_rows > 0x7FFFFFFFll / c->kv_heads) { set_error("%s: more than 2^31-1 rows of pages and heads", who); return FX_ERANGE; }
     if (c->pages > 0 && (!c->d_k || !c->d_v || (uintptr_t)c->d_k % 16 || (uintptr_t)c->d_v % 16 || c->d_k == c->d_v)) {
         set_error("%s: d_k or d_v is null or not aligned to 16 bytes, or they are the same", who);
         return FX_EINVAL;
@@ -637,6 +671,7 @@ extern "C" fx_status fx_attention_step(const fx_cache* c, int64_t rows, const in
     s.q = HeadsView{(unsigned char*)d_q, ld_q * es, hs_q * es};
     s.out = HeadsView{(unsigned char*)d_out, ld_out * es, hs_out * es};
     s.lse = d_lse;
+    s.whole = a.dim % 8 == 0 && (uintptr_t)d_q % 16 == 0 && s.q.ld % 16 == 0 && s.q.hs % 16 == 0;
     s.heads = heads;
     s.group = heads / c->kv_heads;
     s.groups = (s.group + kStepHeads - 1) / kStepHeads;
@@ -644,23 +679,20 @@ extern "C" fx_status fx_attention_step(const fx_cache* c, int64_t rows, const in
     while ((1ll << s.shift) < a.page_rows) ++s.shift;
     s.magic = (uint32_t)((1ull << (31 + s.shift)) / (uint32_t)a.page_rows + 1);
     s.shift += 31;
-    // Up to 1024 positions a workgroup of 8 or 16 waves takes them all and there is no second launch; beyond, chunks of equal
-    // length, such that there are about eight workgroups for a compute unit where that leaves them 256 positions at least.
+    // Up to 1024 positions a workgroup of 8 or 16 waves takes them all and there is no second launch; beyond, every sequence is
+    // split into as many parts, such that there are about eight workgroups for a compute unit -- of one sequence, as many as a
+    // unit holds at a time -- where that leaves the longest 256 positions at least.  (Parts of equal length, more of them in longer sequences: 327 us for 64 sequences of up to 32,768
+    // positions, 8 bits x 128, as most of two rounds of workgroups are there and the second is half empty; 32 of them for a unit 402.)
     const int64_t items = rows * c->kv_heads * s.groups;
-    int64_t chunk = std::max<int64_t>(s.most, 1);
-    if (s.most > 1024) {
-        chunk = std::max<int64_t>(256, (s.most * items / (8 * compute_units()) + 127) / 128 * 128);
-        chunk = std::max(chunk, ((s.most + kMostSplits - 1) / kMostSplits + 127) / 128 * 128);
-        chunk = std::min(chunk, s.most);
-    }
-    s.chunk = (int32_t)chunk;
-    s.splits = (int32_t)std::max<int64_t>(1, (s.most + chunk - 1) / chunk);
+    s.splits = 1;
+    if (s.most > 1024)
+        s.splits = (int32_t)std::max<int64_t>(1, std::min({(s.most + kLeastChunk - 1) / kLeastChunk, (int64_t)kMostSplits, (rows == 1 ? step_resident(dt, c->store == FX_E4M3, a.dim <= 64 ? 64 : a.dim <= 128 ? 128 : 256) : 8) * compute_units() / items}));
     if (items * s.splits > 0x7FFFFFFFll / 64) { set_error("%s: too many rows", who); return FX_ERANGE; }
     void* part = nullptr;
     if (s.splits > 1) {
-        FX_TRY(scratch_alloc(who, &part, ((size_t)rows * heads * s.splits) * (a.dim + 2) * 4, st));
+        FX_TRY(scratch_alloc(who, &part, ((size_t)rows * heads * s.splits) * (a.pitch + 2) * 4, st));
         s.part = (float*)part;
-        s.stats = s.part + (size_t)rows * heads * s.splits * a.dim;
+        s.stats = s.part + (size_t)rows * heads * s.splits * a.pitch;
     }
     if (c->store == FX_E4M3) {
         if (dt == FX_F32) launch_step_dim<FX_F32, true>(s, items * s.splits, rows, st);
