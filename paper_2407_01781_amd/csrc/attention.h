@@ -26,6 +26,9 @@ template <> struct AttnType<FX_BF16> { typedef __bf16 T; static constexpr int ES
 // waves of a SIMD at least, for which registers are allotted: rows of more than 256 bytes need more than 256
 constexpr int least_waves(int row_bytes) { return row_bytes > 256 ? 1 : 2; }
 
+// The same where rows of 256 bytes take all of 256 registers, and only where the loads are dealt out over four waves nothing spills
+constexpr int least_waves_of(int row_bytes, bool dealt) { return row_bytes > 256 || (row_bytes == 256 && !dealt) ? 1 : 2; }
+
 // waves that share a block of few rows: each has tiles of its own in LDS
 constexpr int few_waves(int row_bytes) { return row_bytes > 512 ? 2 : 4; }
 
@@ -195,6 +198,74 @@ __device__ __forceinline__ Pair pair_of_keys(const AttnArgs& a, const SeqTile& t
     const int q0 = a.first_q[t.seq];
     return Pair{q0, a.first_q[t.seq + 1] - q0, t.first, t.len};
 }
+
+// ------------------------------------------------------------------ infinities and NaN in rows that are not seen
+// A causal sequence's diagonal blocks multiply weights of 0 with rows that are not seen, and 0 times an infinity is NaN.  A wave looks
+// into such blocks before it multiplies; where one holds a value that is not finite, the wave computes its 32 rows again
+// behind its loop, one after the other over what each sees alone (the registers of the loop are free there: products with
+// guarded values in the loop itself cost up to 80 of them).
+template <int DT> __device__ __forceinline__ uint32_t not_finite(uint32_t w) {       // the sign bit of every value that is not
+    if (DT == FX_F32) return ((w & 0x7F800000u) + 0x00800000u) & 0x80000000u;
+    if (DT == FX_F16) return ((w & 0x7C007C00u) + 0x04000400u) & 0x80008000u;
+    return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+}
+// The lane's number, made where it is used: what hangs on it is not kept in registers through the loop
+__device__ __forceinline__ int lane_here() {
+    int lane = threadIdx.x & 63;
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("" : "+v"(lane));
+#endif
+    return lane;
+}
+// The kernel's arguments, read again from where the launch left them: a path that is hardly ever taken would else keep them
+// in scalar registers through the loop
+__device__ __forceinline__ const AttnArgs& args_here() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    uint64_t p = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const AttnArgs*)p;
+#else
+    __builtin_unreachable();
+#endif
+}
+// has one of the tile's 32 rows from row0 on a value that is not finite?
+template <int DT, int RB> __device__ __forceinline__ bool block_not_finite(const lds_byte* tile, int row0) {
+    uint32_t any = 0;
+    const int lane = lane_here();
+    const lds_byte* at = tile + LdsRows<RB>::row_at(row0) + LdsRows<RB>::row_at(lane & 31) + (lane >> 5) * 16;
+#pragma unroll 1
+    for (int i = 0; i < RB / 32; ++i) {          // in whatever order a row's pieces lie
+        const u32x4 w = *(const __attribute__((address_space(3))) u32x4*)(at + (i >> 1) * LdsRows<RB>::kSegment + (i & 1) * 32);
+        any |= not_finite<DT>(w[0]) | not_finite<DT>(w[1]) | not_finite<DT>(w[2]) | not_finite<DT>(w[3]);
+    }
+    return __any(any != 0);
+}
+
+// A row in a wave's registers, elements lane + 64 e
+template <int DT> struct LaneRow {
+    float x[kMostDim / 64];
+    __device__ __forceinline__ void load(const unsigned char* p, int dim, int lane, float f = 1.f) {
+#pragma unroll
+        for (int e = 0; e < kMostDim / 64; ++e) x[e] = lane + 64 * e < dim ? (float)((const typename AttnType<DT>::T*)p)[lane + 64 * e] * f : 0.f;
+    }
+    __device__ __forceinline__ void store(unsigned char* p, int dim, int lane, float f) const {
+#pragma unroll
+        for (int e = 0; e < kMostDim / 64; ++e)
+            if (lane + 64 * e < dim) ((typename AttnType<DT>::T*)p)[lane + 64 * e] = (typename AttnType<DT>::T)(x[e] * f);
+    }
+    __device__ __forceinline__ void add(float f, const LaneRow& o) {
+#pragma unroll
+        for (int e = 0; e < kMostDim / 64; ++e) x[e] = fmaf(f, o.x[e], x[e]);
+    }
+    __device__ __forceinline__ float dot(const LaneRow& o) const {
+        float s = 0.f;
+#pragma unroll
+        for (int e = 0; e < kMostDim / 64; ++e) s = fmaf(x[e], o.x[e], s);
+        for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d, 64);
+        return s;
+    }
+};
+__device__ __forceinline__ unsigned char* row_of_head(const HeadsView& v, int64_t row, int head) { return v.p + row * v.ld + head * v.hs; }
 
 // Writes a 32x32 result whose rows are a row's elements 32 col .. and whose columns are rows, times f
 template <int DT> __device__ __forceinline__ void store_columns(const f32x16& acc, float f, unsigned char* row, int col, int dim_bytes, int half) {

@@ -92,6 +92,31 @@ template <int DT, int DP> struct FwdWave {
     }
 };
 
+// The wave's rows again, each over the keys that it sees and no others
+template <int DT> __device__ void again(const AttnArgs& a, const Pair& p, int head, int row0, int lane) {
+    const int dim = a.dim_bytes / AttnType<DT>::ES, kv_head = head / a.group;
+    for (int row = row0; row < min(row0 + 32, p.nq); ++row) {
+        LaneRow<DT> q, x, acc;
+        q.load(row_of_head(a.q, p.q0 + row, head), dim, lane, a.negative ? -a.c : a.c);
+        float m = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < kMostDim / 64; ++e) acc.x[e] = 0.f;
+        const int n = min(p.nk, row + 1 + p.nk - p.nq);
+        for (int j = 0; j < n; ++j) {
+            x.load(row_of_head(a.k, p.k0 + j, kv_head), dim, lane);
+            const float s = q.dot(x), top = fmaxf(m, s), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top), w = __builtin_amdgcn_exp2f(s - (top == -INFINITY ? 0.f : top));
+            m = top;
+            sum = fmaf(sum, f, w);
+#pragma unroll
+            for (int e = 0; e < kMostDim / 64; ++e) acc.x[e] *= f;
+            x.load(row_of_head(a.v, p.k0 + j, kv_head), dim, lane);
+            acc.add(w, x);
+        }
+        acc.store(row_of_head(a.out, p.q0 + row, head), dim, lane, sum == 0.f ? 0.f : 1.f / sum);
+        if (a.lse && lane == 0) a.lse[head * a.rows_q + p.q0 + row] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+}
+
 // A workgroup has W waves of 32 queries of one head; keys and values come by in tiles of KT, two buffers of each.
 template <int DT, int DP> struct FwdShape {
     static constexpr int RB = DP * AttnType<DT>::ES;
@@ -101,7 +126,7 @@ template <int DT, int DP> struct FwdShape {
 };
 
 template <int DT, int DP, int W>
-__global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_attention(AttnArgs a) {
+__global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 4)) void k_attention(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)         // the host pass has no buffer descriptors and drops stubs over them
     typedef FwdShape<DT, DP> S;
     constexpr int RB = S::RB, KT = S::KT;
@@ -132,6 +157,7 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
     }
     w.q.load(a.q.p + (int64_t)p.q0 * a.q.ld + head * a.q.hs, a.q.ld, row0, p.nq, a.dim_bytes, lane, a.negative);
     w.clear();
+    bool odd = false;
     for (int j = 0; j < n; ++j) {
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
@@ -143,12 +169,14 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
         const lds_byte *kt = lds + b * S::kTile, *vt = lds + (2 + b) * S::kTile;
         const bool masked = key0 + KT - 1 > unmasked;
         if (key0 >= seen_wave) continue;
+        if (a.causal && masked) odd |= block_not_finite<DT, RB>(vt, 0) || (KT == 64 && block_not_finite<DT, RB>(vt, KT - 32));
         // half a tile by itself only where sequences are short: a second form of the loop's body costs registers
         if (KT == 64 && (W > 2 || key0 + 32 < seen_wave)) w.template blocks<2>(kt, vt, 0, key0, masked, last);
         else w.template blocks<1>(kt, vt, 0, key0, masked, last);
     }
     w.sum += other_half(w.sum);
     w.store(a, row, p.nq, p.q0, head);
+    if (odd) again<DT>(args_here(), p, head, row0, lane_here());
 #endif
 }
 
@@ -193,6 +221,7 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
     w.init(a, lane);
     w.clear();
     int b = 0;
+    bool odd = false;
     for (int j = wave; j < n; j += W) {
         __builtin_amdgcn_s_waitcnt(0);
         const lds_byte* at = lds + b * 2 * S::kTile;
@@ -201,7 +230,9 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
             lk.load(lds + b * 2 * S::kTile, kb, a.k.ld, (j + W) * 32, p.nk, a.dim_bytes, 0);
             lv.load(lds + b * 2 * S::kTile + S::kTile, vb, a.v.ld, (j + W) * 32, p.nk, a.dim_bytes, 0);
         }
-        w.template blocks<1>(at, at + S::kTile, 0, j * 32, j * 32 + 31 > unmasked, last);
+        const bool masked = j * 32 + 31 > unmasked;
+        if (a.causal && masked) odd |= block_not_finite<DT, RB>(at + S::kTile, 0);
+        w.template blocks<1>(at, at + S::kTile, 0, j * 32, masked, last);
         if (NB == 1 && j + W < n) {
             __builtin_amdgcn_s_waitcnt(0);          // what is read there has been read
             lk.load(lds, kb, a.k.ld, (j + W) * 32, p.nk, a.dim_bytes, 0);
@@ -231,7 +262,11 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
                 for (int r = 0; r < 16; ++r) w.acc[k][r] = fmaf(in[(k * 16 + r) * 64 + lane], f, w.acc[k][r]);
         }
     }
-    if (wave == 0) w.store(a, row, p.nq, p.q0, head);
+    odd = __syncthreads_or(odd);
+    if (wave == 0) {
+        w.store(a, row, p.nq, p.q0, head);
+        if (odd) again<DT>(args_here(), p, head, row0, lane_here());
+    }
 #endif
 }
 

@@ -121,6 +121,29 @@ template <int DT, int DP> struct GqWave {
     }
 };
 
+// The wave's rows again, each over the keys that it sees and no others
+template <int DT> __device__ void gq_again(const AttnArgs& a, const Pair& p, int head, int row0, int lane) {
+    const int dim = a.dim_bytes / AttnType<DT>::ES, kv_head = head / a.group;
+    for (int row = row0; row < min(row0 + 32, p.nq); ++row) {
+        LaneRow<DT> q, go, x, y, acc;
+        go.load(row_of_head(a.gout, p.q0 + row, head), dim, lane);
+        x.load(row_of_head(a.out, p.q0 + row, head), dim, lane);
+        const int64_t at = head * a.rows_q + p.q0 + row;
+        const float delta = (p.nk == 1 ? 0.f : go.dot(x)) - (a.glse ? a.glse[at] : 0.f), lse2 = a.lse[at] * kLog2e;
+        q.load(row_of_head(a.q, p.q0 + row, head), dim, lane, a.negative ? -a.c : a.c);
+#pragma unroll
+        for (int e = 0; e < kMostDim / 64; ++e) acc.x[e] = 0.f;
+        const int n = min(p.nk, row + 1 + p.nk - p.nq);
+        for (int j = 0; j < n; ++j) {
+            x.load(row_of_head(a.k, p.k0 + j, kv_head), dim, lane);
+            y.load(row_of_head(a.v, p.k0 + j, kv_head), dim, lane);
+            acc.add(__builtin_amdgcn_exp2f(q.dot(x) - lse2) * ((p.nk == 1 ? 0.f : go.dot(y)) - delta), x);
+        }
+        if (lane == 0) *(f32x2*)(a.stats + 2 * at) = f32x2{lse2, delta};
+        if (a.gq.p) acc.store(row_of_head(a.gq, p.q0 + row, head), dim, lane, a.negative ? -a.scale : a.scale);
+    }
+}
+
 template <int DT, int DP, int W>
 __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_attention_gq(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)         // the host pass has no buffer descriptors and drops stubs over them
@@ -150,6 +173,7 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
     }
     GqWave<DT, DP> w;
     w.init(a, p, head, work.head % S::kParts, row0, lane, KT);
+    bool odd = false;
     for (int j = 0; j < n; ++j) {
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
@@ -161,10 +185,12 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
         if (key0 >= seen_wave) continue;
         const lds_byte *kt = lds + b * S::kKeys, *vt = lds + (2 + b) * S::kKeys;
         const bool masked = key0 + KT - 1 > unmasked;
+        if (a.causal && masked) odd |= block_not_finite<DT, RB>(kt, 0) || (KT == 64 && block_not_finite<DT, RB>(kt, KT - 32));
         if (KT == 64 && (W > 2 || key0 + 32 < seen_wave)) w.template blocks<2>(kt, vt, key0, masked, last);
         else w.template blocks<1>(kt, vt, key0, masked, last);
     }
     w.store(a, p, head, row);
+    if (odd && w.part == 0) gq_again<DT>(args_here(), p, head, row0, lane_here());
 #endif
 }
 
@@ -216,25 +242,29 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
     GqWave<DT, DP> w;
     w.init(a, p, head, work.head % S::kParts, row0, lane, 32);
     int b = 0;
+    bool odd = false;
     for (int j = wave; j < n; j += W) {
         __builtin_amdgcn_s_waitcnt(0);
         const lds_byte* at = lds + b * S::kOwn;
         if (NB == 2 && j + W < n) load(j + W, b ^= 1);
-        w.template blocks<1>(at, at + S::kBlock, j * 32, j * 32 + 31 > unmasked, last);
+        const bool masked = j * 32 + 31 > unmasked;
+        if (a.causal && masked) odd |= block_not_finite<DT, RB>(at, 0);
+        w.template blocks<1>(at, at + S::kBlock, j * 32, masked, last);
         if (NB == 1 && j + W < n) {
             __builtin_amdgcn_s_waitcnt(0);          // what is read there has been read
             load(j + W, 0);
         }
     }
     add_results<W>(smem, w.acc, wave, lane);
-    if (wave == 0) w.store(a, p, head, row);
+    odd = __syncthreads_or(odd);
+    if (wave == 0) {
+        w.store(a, p, head, row);
+        if (odd && w.part == 0) gq_again<DT>(args_here(), p, head, row0, lane_here());
+    }
 #endif
 }
 
 // ------------------------------------------------------------------ gradients of keys and values
-// Rows of 256 bytes take all of 256 registers; only where loads and statistics are dealt out over four waves nothing spills
-constexpr int least_waves_gkv(int row_bytes, bool dealt) { return row_bytes > 256 || (row_bytes == 256 && !dealt) ? 1 : 2; }
-
 template <int DT, int DP> struct GkvWave {
     typedef BwdShape<DT, DP> S;
     typedef typename AttnType<DT>::T T;
@@ -280,7 +310,7 @@ template <int DT, int DP> struct GkvWave {
             }
         }
         if (masked) {
-            first -= 4 * half;
+            first -= 4 * (lane_here() >> 5);
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 if (8 * (r >> 2) + (r & 3) < first) p[r] = ds[r] = 0.f;
@@ -310,18 +340,42 @@ template <int DT, int DP> struct GkvWave {
     }
 };
 
+// The wave's keys again, each over the queries that see it and no others
+template <int DT> __device__ void gkv_again(const AttnArgs& a, const Pair& p, int kv_head, int key0, int lane) {
+    const int dim = a.dim_bytes / AttnType<DT>::ES;
+    for (int key = key0; key < min(key0 + 32, p.nk); ++key) {
+        LaneRow<DT> k, v, x, y, gk, gv;
+        k.load(row_of_head(a.k, p.k0 + key, kv_head), dim, lane, a.negative ? -a.c : a.c);
+        v.load(row_of_head(a.v, p.k0 + key, kv_head), dim, lane);
+#pragma unroll
+        for (int e = 0; e < kMostDim / 64; ++e) gk.x[e] = gv.x[e] = 0.f;
+        for (int head = kv_head * a.group; head < (kv_head + 1) * a.group; ++head)
+            for (int row = max(0, key - (p.nk - p.nq)); row < p.nq; ++row) {
+                x.load(row_of_head(a.q, p.q0 + row, head), dim, lane);
+                y.load(row_of_head(a.gout, p.q0 + row, head), dim, lane);
+                const f32x2 stat = *(const f32x2*)(a.stats + 2 * (head * a.rows_q + p.q0 + row));
+                const float w = __builtin_amdgcn_exp2f(k.dot(x) - stat[0]);
+                gv.add(w, y);
+                gk.add(w * ((p.nk == 1 ? 0.f : v.dot(y)) - stat[1]), x);
+            }
+        if (a.gk.p) gk.store(row_of_head(a.gk, p.k0 + key, kv_head), dim, lane, a.negative ? -a.scale : a.scale);
+        if (a.gv.p) gv.store(row_of_head(a.gv, p.k0 + key, kv_head), dim, lane, 1.f);
+    }
+}
+
 // lse (base 2) and delta of 32 rows, as the first kernel left them, into LDS; zeros for a row that does not exist, whose query and
 // gradient are zeros too: it adds nothing
 __device__ __forceinline__ void load_stats(const AttnArgs& a, lds_byte* to, int head, int q0, int row0, int nq, int lane) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    const float* from = a.stats + 2 * (head * a.rows_q + q0 + row0);
-    __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, max(0, min(nq - row0, 32)) * 8, 0x27000);
+    const uint64_t from = (uint64_t)(a.stats + 2 * (head * a.rows_q + q0 + row0));
+    const uint64_t base = (uint32_t)uni((int)(uint32_t)from) | (uint64_t)(uint32_t)uni((int)(from >> 32)) << 32;        // one for the wave, the compiler does not see it
+    __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, uni(max(0, min(nq - row0, 32)) * 8), 0x27000);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 4, lane * 4, 0, 0, 0);
 #endif
 }
 
 template <int DT, int DP, int W>
-__global__ __launch_bounds__(64 * W, least_waves_gkv(DP * AttnType<DT>::ES, W == 4)) void k_attention_gkv(AttnArgs a) {
+__global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 4)) void k_attention_gkv(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef BwdShape<DT, DP> S;
     constexpr int RB = S::RB, QT = S::QT;
@@ -354,6 +408,7 @@ __global__ __launch_bounds__(64 * W, least_waves_gkv(DP * AttnType<DT>::ES, W ==
     GkvWave<DT, DP> w;
     w.init(a, p, kv_head, work.head % S::kParts, key0, lane);
     int r0 = begin - QT;
+    bool odd = false;
     for (int j = 0; j < n; ++j) {
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
@@ -362,15 +417,19 @@ __global__ __launch_bounds__(64 * W, least_waves_gkv(DP * AttnType<DT>::ES, W ==
         if (r0 >= p.nq) r0 = begin;
         if (j + 1 < n) load(b ^ 1);
         if (key0 >= p.nk || (a.causal && r0 + QT - 1 + shift < key0)) continue;
-        w.block(lds + b * S::kQueries, lds + (2 + b) * S::kQueries, (const float*)(smem + 4 * S::kQueries + b * S::kStats), a.causal && r0 + shift < key0 + 31, key - shift - r0);
+        const lds_byte *qt = lds + b * S::kQueries, *ot = lds + (2 + b) * S::kQueries;
+        const bool masked = a.causal && r0 + shift < key0 + 31;
+        if (masked) odd |= block_not_finite<DT, RB>(qt, 0) || block_not_finite<DT, RB>(ot, 0);
+        w.block(qt, ot, (const float*)(smem + 4 * S::kQueries + b * S::kStats), masked, key - shift - r0);
     }
     w.store(a, p, kv_head, key);
+    if (odd && w.part == 0) gkv_again<DT>(args_here(), p, kv_head, key0, lane_here());
 #endif
 }
 
 // For few keys: W waves share one block of 32 and take the blocks of 32 queries of all heads in turn
 template <int DT, int DP, int W>
-__global__ __launch_bounds__(64 * W, least_waves_gkv(DP * AttnType<DT>::ES, false)) void k_attention_gkv_few(AttnArgs a) {
+__global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, false)) void k_attention_gkv_few(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef BwdShape<DT, DP> S;
     constexpr int RB = S::RB, QT = S::QT, NB = S::template buffers<W>();
@@ -402,6 +461,7 @@ __global__ __launch_bounds__(64 * W, least_waves_gkv(DP * AttnType<DT>::ES, fals
     GkvWave<DT, DP> w;
     w.init(a, p, kv_head, work.head % S::kParts, key0, lane);
     int b = 0;
+    bool odd = false;
     for (int j = wave; j < n; j += W) {
         __builtin_amdgcn_s_waitcnt(0);
         const unsigned char* now = own + b * S::kOwn;
@@ -411,7 +471,9 @@ __global__ __launch_bounds__(64 * W, least_waves_gkv(DP * AttnType<DT>::ES, fals
             settle();
             if (NB == 2) load(b ^= 1);
         }
-        w.block((const lds_byte*)now, (const lds_byte*)now + S::kBlock, (const float*)(now + 2 * S::kBlock), a.causal && r0 + shift < key0 + 31, key - shift - r0);
+        const bool masked = a.causal && r0 + shift < key0 + 31;
+        if (masked) odd |= block_not_finite<DT, RB>((const lds_byte*)now, 0) || block_not_finite<DT, RB>((const lds_byte*)now + S::kBlock, 0);
+        w.block((const lds_byte*)now, (const lds_byte*)now + S::kBlock, (const float*)(now + 2 * S::kBlock), masked, key - shift - r0);
         if (NB == 1 && j + W < n) {
             __builtin_amdgcn_s_waitcnt(0);          // what is read there has been read
             load(0);
@@ -419,7 +481,11 @@ __global__ __launch_bounds__(64 * W, least_waves_gkv(DP * AttnType<DT>::ES, fals
     }
     add_results<W>(smem, w.gk, wave, lane);
     add_results<W>(smem, w.gv, wave, lane);
-    if (wave == 0) w.store(a, p, kv_head, key);
+    odd = __syncthreads_or(odd);
+    if (wave == 0) {
+        w.store(a, p, kv_head, key);
+        if (odd && w.part == 0) gkv_again<DT>(args_here(), p, kv_head, key0, lane_here());
+    }
 #endif
 }
 

@@ -277,3 +277,81 @@ def test_a_running_sequence_is_the_causal_one():
     ck, cv = fx.cache_read(cache, table, start * 0, fx.build_sequences([[0, n]]))
     o, _ = fx.attention_fwd(chunk, q[prompt:], ck, cv, causal=True, kv_seqs=fx.build_sequences([[0, n]]))
     A.check(_f64(o), ref[prompt:], bo[prompt:], "f32", "chunk")
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f32", 20), ("f16", 128)])
+@pytest.mark.parametrize("lens", [[40, 150, 33], [700]])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_rows_do_not_see_what_comes_later(dtype, d, lens, bad):
+    """An infinity or NaN in a key, a value, a query or an output's gradient of a causal sequence: the rows (or keys) that do not see it
+    have the bits that they have without it; those that see it in values have it there."""
+    heads, kv_heads = 4, 2
+    b, jo = _joff(lens)
+    n = int(b[-1])
+    seqs = fx.build_sequences(jo)
+    make = lambda: [draw(s, n, h, d, dtype)[0] for s, h in ((1, heads), (2, kv_heads), (3, kv_heads), (4, heads))]
+    q, k, v, go = make()
+    ref = fx.attention_fwd(seqs, q, k, v, causal=True)
+    gref = fx.attention_bwd(seqs, q, k, v, *ref, go, causal=True)
+    for which in range(4):
+        t = make()
+        rows = [int(b[s + 1]) - 1 - back for s in range(len(lens)) for back in (0, 5, 17)]       # near the ends of the sequences
+        for r in rows:
+            t[which][r, -1, r % d] = bad
+        first = np.array([min([x for x in rows if b[s] <= x < b[s + 1]]) for s in range(len(lens))])
+        before = np.concatenate([np.arange(b[s], first[s]) for s in range(len(lens))])
+        out, lse = fx.attention_fwd(seqs, *t[:3], causal=True)
+        # a few rows are computed in another order when their block has such a value: fp32 sums of the same weights, one rounding
+        ro, rl, bo, bl = A.attention(*(_f64(x) for x in (q, k, v)), b, b, True, d ** -0.5, dtype)
+        A.check(_f64(out)[before], ro[before], bo[before], dtype, f"out before {bad} in {which}")
+        A.check(_f64(lse)[:, before], rl[:, before], bl[:, before], "f32", "lse")
+        if which == 2:
+            with np.errstate(invalid="ignore"):
+                want, wl, bw, _ = A.attention(*(_f64(x) for x in t[:3]), b, b, True, d ** -0.5, dtype)
+            clean = np.isfinite(want)           # numpy's own products of zeros and infinities are NaN below the diagonal: those rows are checked above
+            seen = np.concatenate([np.arange(first[s], b[s + 1]) for s in range(len(lens))])
+            got = _f64(out)[seen]
+            assert (np.isfinite(got) | ~clean[seen]).all()
+            assert (~np.isfinite(got))[..., -1, [r % d for r in rows]].any()
+        g = fx.attention_bwd(seqs, *t[:3], *ref, t[3], causal=True)
+        rg = A.attention_grad(*(_f64(x) for x in (q, k, v, go)), b, b, True, d ** -0.5, dtype)
+        if which in (1, 2):         # rows before do not see the key
+            A.check(_f64(g[0])[before], rg[0][before], rg[3][before], dtype, f"gq before {bad} in {which}")
+        else:                       # keys behind the last such row of their sequence are not seen by it
+            last = np.array([max([x for x in rows if b[s] <= x < b[s + 1]]) for s in range(len(lens))])
+            assert (last == b[1:] - 1).all()
+            others = [h for h in range(heads - 2)]              # heads of the other key head
+            A.check(_f64(g[0])[:, others], rg[0][:, others], rg[3][:, others], dtype, f"gq of other heads, {bad} in {which}")
+            A.check(_f64(g[1])[:, :1], rg[1][:, :1], rg[4][:, :1], dtype, "gk of the other head")
+    # queries that keys behind them do not see: in the middle of a block
+    for which in (0, 3):
+        t = make()
+        row = int(b[-1]) - 20
+        t[which][row, 0, 3] = bad
+        g = fx.attention_bwd(seqs, *t[:3], *ref, t[3], causal=True)
+        after = np.arange(row + 1, n)
+        for i in (1, 2):
+            A.check(_f64(g[i])[after], rg[i][after], rg[3 + i][after], dtype, f"gradient {i} of keys behind {bad} in {which}")
+    assert all(torch.equal(x, y) for x, y in zip(fx.attention_fwd(seqs, q, k, v, causal=True), ref))
+    assert all(torch.equal(x, y) for x, y in zip(fx.attention_bwd(seqs, q, k, v, *ref, go, causal=True), gref))
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_sequences_do_not_see_each_other(bad):
+    """All rows of one sequence not finite: the others, whose tiles they lie in, have the same bits."""
+    lens = [50, 3, 200, 31, 64]
+    b, jo = _joff(lens)
+    seqs = fx.build_sequences(jo)
+    for causal in (False, True):
+        t = [draw(s, int(b[-1]), 2, 48, "bf16")[0] for s in range(4)]
+        ref = fx.attention_fwd(seqs, *t[:3], causal=causal)
+        gref = fx.attention_bwd(seqs, *t[:3], *ref, t[3], causal=causal)
+        for s in (1, 3):
+            u = [x.clone() for x in t]
+            for x in u:
+                x[b[s]:b[s + 1]] = bad
+            out, lse = fx.attention_fwd(seqs, *u[:3], causal=causal)
+            g = fx.attention_bwd(seqs, *u[:3], out, lse, u[3], causal=causal)
+            keep = np.concatenate([np.arange(b[i], b[i + 1]) for i in range(len(lens)) if i != s])
+            assert torch.equal(out[keep], ref[0][keep]) and torch.equal(lse[:, keep], ref[1][:, keep])
+            assert all(torch.equal(x[keep], y[keep]) for x, y in zip(g, gref))
