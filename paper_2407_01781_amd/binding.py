@@ -770,8 +770,11 @@ def _heads(t: torch.Tensor, shape, dtype: torch.dtype, device: int, name: str):
     return t.data_ptr(), (ld if rows > 1 else max(hs, dim) * max(heads, 1)), hs
 
 
-def _out_heads(out: Optional[torch.Tensor], like: torch.Tensor, name: str = "out") -> torch.Tensor:
-    return torch.empty(like.shape, dtype=like.dtype, device=like.device) if out is None else out
+def _new_heads(like: torch.Tensor):
+    """A tensor of heads in new memory, and its address and strides."""
+    t = torch.empty_like(like, memory_format=torch.contiguous_format)
+    _, heads, dim = like.shape
+    return t, t.data_ptr(), max(heads, 1) * dim, dim
 
 
 def _floats(t: Optional[torch.Tensor], shape, name: str):
@@ -807,9 +810,8 @@ def attention_fwd(seqs: Sequences, q: torch.Tensor, k: torch.Tensor, v: torch.Te
     logarithm of the sum of exp(scale q . k); 0 and -inf for a row that sees no key."""
     device = torch.cuda.current_device()
     a = _attention(seqs, kv_seqs, q, k, v, causal, scale, device)
-    out = _out_heads(out, q)
-    op = _heads(out, q.shape, q.dtype, device, "out")
-    lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
+    out, *op = _new_heads(q) if out is None else (out, *_heads(out, q.shape, q.dtype, device, "out"))
+    lse = torch.empty((a.heads, seqs.rows), dtype=torch.float32, device=q.device)
     _check(lib.fx_attention_fwd(a, *op, lse.data_ptr(), _stream()))
     return out, lse
 
@@ -823,9 +825,8 @@ def attention_bwd(seqs: Sequences, q: torch.Tensor, k: torch.Tensor, v: torch.Te
     op, gp = _heads(out, q.shape, q.dtype, device, "out"), _heads(grad_out, q.shape, q.dtype, device, "grad_out")
     stats = (q.shape[1], q.shape[0])
     lp, glp = _floats(lse, stats, "lse"), _floats(grad_lse, stats, "grad_lse")
-    gq, gk, gv = _out_heads(None, q), _out_heads(None, k), _out_heads(None, v)
-    grads = [_heads(t, t.shape, q.dtype, device, "gradient") for t in (gq, gk, gv)]
-    _check(lib.fx_attention_bwd(a, *op, lp, *gp, glp, *grads[0], *grads[1], *grads[2], _stream()))
+    (gq, *gqp), (gk, *gkp), (gv, *gvp) = _new_heads(q), _new_heads(k), _new_heads(v)
+    _check(lib.fx_attention_bwd(a, *op, lp, *gp, glp, *gqp, *gkp, *gvp, _stream()))
     return gq, gk, gv
 
 
@@ -889,9 +890,10 @@ def cache_read(cache: KVCache, table: torch.Tensor, start: torch.Tensor, seqs: S
     device = torch.cuda.current_device()
     c = cache._with(table, seqs.batch_size, device)
     shape = seqs.rows, cache.kv_heads, cache.dim
-    k, v = (torch.empty(shape, dtype=dtype, device=cache.k.device) for _ in range(2))
-    _check(lib.fx_cache_read(c, seqs._h, _numbers(start, seqs.batch_size, "start"), _TORCH_DT[dtype], *_heads(k, shape, dtype, device, "k"),
-                             *_heads(v, shape, dtype, device, "v"), _stream()))
+    k = torch.empty(shape, dtype=dtype, device=cache.k.device)
+    v = torch.empty_like(k)
+    ld, hs = max(shape[1] * shape[2], 1), shape[2]
+    _check(lib.fx_cache_read(c, seqs._h, _numbers(start, seqs.batch_size, "start"), _TORCH_DT[dtype], k.data_ptr(), ld, hs, v.data_ptr(), ld, hs, _stream()))
     return k, v
 
 
@@ -906,8 +908,8 @@ def attention_step(cache: KVCache, table: torch.Tensor, lengths: torch.Tensor, q
     c = cache._with(table, n, device)
     assert dim == cache.dim, f"q: {cache.dim} dimensions expected"
     qp = _heads(q, shape, q.dtype, device, "q")
-    out = _out_heads(out, q)
+    out, *op = _new_heads(q) if out is None else (out, *_heads(out, shape, q.dtype, device, "out"))
     lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
     _check(lib.fx_attention_step(c, n, _numbers(lengths, n, "lengths"), longest, _TORCH_DT[q.dtype], heads, dim ** -0.5 if scale is None else scale,
-                                 *qp, *_heads(out, shape, q.dtype, device, "out"), lse.data_ptr(), _stream()))
+                                 *qp, *op, lse.data_ptr(), _stream()))
     return out, lse

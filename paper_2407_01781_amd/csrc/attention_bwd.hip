@@ -13,7 +13,7 @@ namespace fx {
 template <int DT, int DP> struct BwdShape {
     static constexpr int RB = DP * AttnType<DT>::ES;
     static constexpr int KT = RB > 128 ? 32 : 64;               // keys of a tile that streams by (two blocks' scores and dP are 64 registers)
-    static constexpr int QT = 32;                               // queries
+    static constexpr int QT = RB > 128 ? 32 : 64;               // queries, a block of 32 after the other
     static constexpr int kKeys = LdsRows<RB>::bytes(KT), kQueries = LdsRows<RB>::bytes(QT), kStats = 2 * QT * 4;
     static constexpr int kLdsKeys = 4 * kKeys, kLdsQueries = 4 * kQueries + 2 * kStats;
     // Parts that the output's columns are dealt out in, as heads of their own: above 128 dimensions a lane's results, its own rows and
@@ -22,8 +22,8 @@ template <int DT, int DP> struct BwdShape {
     static constexpr int COLS = DP / 32 / kParts, STEPS = RB / 32;
     static constexpr int kPart = COLS * (DT == FX_F32 ? 2 : 1) * LdsRows<RB>::kSegment;         // from part to part in a tile
     // a workgroup of W waves that share one block of rows, each with buffers of its own
-    static constexpr int kBlock = LdsRows<RB>::bytes(32);
-    static constexpr int kOwn = 2 * kBlock + kStats;            // a wave's two tiles and what belongs to their rows
+    static constexpr int kBlock = LdsRows<RB>::bytes(32), kBlockStats = 32 * 8;
+    static constexpr int kOwn = 2 * kBlock + kBlockStats;            // a wave's two tiles and what belongs to their rows
     template <int W> static constexpr int buffers() { return 2 * kOwn * W <= 128 * 1024 ? 2 : 1; }
     template <int W> static constexpr int lds_few() { return std::max(buffers<W>() * kOwn * W, W / 2 * COLS * 4096); }
 };
@@ -363,14 +363,16 @@ template <int DT> __device__ void gkv_again(const AttnArgs& a, const Pair& p, in
     }
 }
 
-// lse (base 2) and delta of 32 rows, as the first kernel left them, into LDS; zeros for a row that does not exist, whose query and
+// lse (base 2) and delta of ROWS rows, as the first kernel left them, into LDS; zeros for a row that does not exist, whose query and
 // gradient are zeros too: it adds nothing
-__device__ __forceinline__ void load_stats(const AttnArgs& a, lds_byte* to, int head, int q0, int row0, int nq, int lane) {
+template <int ROWS> __device__ __forceinline__ void load_stats(const AttnArgs& a, lds_byte* to, int head, int q0, int row0, int nq, int lane) {
 #if defined(__HIP_DEVICE_COMPILE__)
     const uint64_t from = (uint64_t)(a.stats + 2 * (head * a.rows_q + q0 + row0));
     const uint64_t base = (uint32_t)uni((int)(uint32_t)from) | (uint64_t)(uint32_t)uni((int)(from >> 32)) << 32;        // one for the wave, the compiler does not see it
-    __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, uni(max(0, min(nq - row0, 32)) * 8), 0x27000);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)to, 4, lane * 4, 0, 0, 0);
+    __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, uni(max(0, min(nq - row0, ROWS)) * 8), 0x27000);
+#pragma unroll
+    for (int i = 0; i < ROWS / 32; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(to + 256 * i), 4, lane * 4 + 256 * i, 0, 0, 0);
 #endif
 }
 
@@ -400,7 +402,7 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
     auto load = [&](int b) {
         lq.load(lds + b * S::kQueries, a.q.p + (int64_t)p.q0 * a.q.ld + next_head * a.q.hs, a.q.ld, next, p.nq, a.dim_bytes, wave);
         lo.load(lds + (2 + b) * S::kQueries, a.gout.p + (int64_t)p.q0 * a.gout.ld + next_head * a.gout.hs, a.gout.ld, next, p.nq, a.dim_bytes, wave);
-        if (wave == W - 1) load_stats(a, stats + b * S::kStats, next_head, p.q0, next, p.nq, lane);
+        if (wave == W - 1) load_stats<QT>(a, stats + b * S::kStats, next_head, p.q0, next, p.nq, lane);
         next += QT;
         if (next >= p.nq) { next = begin; ++next_head; }
     };
@@ -416,11 +418,16 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
         r0 += QT;
         if (r0 >= p.nq) r0 = begin;
         if (j + 1 < n) load(b ^ 1);
-        if (key0 >= p.nk || (a.causal && r0 + QT - 1 + shift < key0)) continue;
         const lds_byte *qt = lds + b * S::kQueries, *ot = lds + (2 + b) * S::kQueries;
-        const bool masked = a.causal && r0 + shift < key0 + 31;
-        if (masked) odd |= block_not_finite<DT, RB>(qt, 0) || block_not_finite<DT, RB>(ot, 0);
-        w.block(qt, ot, (const float*)(smem + 4 * S::kQueries + b * S::kStats), masked, key - shift - r0);
+        const float* st = (const float*)(smem + 4 * S::kQueries + b * S::kStats);
+#pragma unroll
+        for (int t = 0; t < QT; t += 32) {
+            const int r = r0 + t;
+            if (key0 >= p.nk || r >= p.nq || (a.causal && r + 31 + shift < key0)) continue;
+            const bool masked = a.causal && r + shift < key0 + 31;
+            if (masked) odd |= block_not_finite<DT, RB>(qt, t) || block_not_finite<DT, RB>(ot, t);
+            w.block(qt + LdsRows<RB>::row_at(t), ot + LdsRows<RB>::row_at(t), st + 2 * t, masked, key - shift - r);
+        }
     }
     w.store(a, p, kv_head, key);
     if (odd && w.part == 0) gkv_again<DT>(args_here(), p, kv_head, key0, lane_here());
@@ -432,7 +439,7 @@ template <int DT, int DP, int W>
 __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, false)) void k_attention_gkv_few(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef BwdShape<DT, DP> S;
-    constexpr int RB = S::RB, QT = S::QT, NB = S::template buffers<W>();
+    constexpr int RB = S::RB, QT = 32, NB = S::template buffers<W>();
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const Work work = work_of(a, a.kv_heads * S::kParts);
     if (work.head < 0) return;
@@ -452,7 +459,7 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, false
         const int r0 = begin + at * QT;
         lq.load((lds_byte*)own + b * S::kOwn, a.q.p + (int64_t)p.q0 * a.q.ld + head * a.q.hs, a.q.ld, r0, p.nq, a.dim_bytes, 0);
         lo.load((lds_byte*)own + b * S::kOwn + S::kBlock, a.gout.p + (int64_t)p.q0 * a.gout.ld + head * a.gout.hs, a.gout.ld, r0, p.nq, a.dim_bytes, 0);
-        load_stats(a, (lds_byte*)own + b * S::kOwn + 2 * S::kBlock, head, p.q0, r0, p.nq, lane);
+        load_stats<QT>(a, (lds_byte*)own + b * S::kOwn + 2 * S::kBlock, head, p.q0, r0, p.nq, lane);
     };
     if (wave < n) {
         settle();
