@@ -29,8 +29,9 @@ constexpr int least_waves(int row_bytes) { return row_bytes > 256 ? 1 : 2; }
 // The same where rows of 256 bytes take all of 256 registers, and only where the loads are dealt out over four waves nothing spills
 constexpr int least_waves_of(int row_bytes, bool dealt) { return row_bytes > 256 || (row_bytes == 256 && !dealt) ? 1 : 2; }
 
-// waves that share a block of few rows: each has tiles of its own in LDS
-constexpr int few_waves(int row_bytes) { return row_bytes > 512 ? 2 : 4; }
+// whether two blocks of few rows share tiles of the others: rows of 16 bits from this many bytes on; of fp32, whose products take
+// longer than their loads, only the widest
+constexpr bool share_tiles(int dt, int row_bytes, bool gradients) { return dt == FX_F32 ? row_bytes > 256 : row_bytes > (gradients ? 128 : 64); }
 
 // A tensor of heads on the device: bytes from row to row and head to head
 struct HeadsView { unsigned char* p; int64_t ld, hs; };
@@ -42,7 +43,7 @@ struct AttnArgs {
     float *lse, *stats;
     const float* glse;
     int64_t rows_q;
-    int32_t n_tiles, tile_rows, heads, kv_heads, group, dim_bytes;
+    int32_t n_tiles, tile_rows, few, heads, kv_heads, group, dim_bytes;
     int32_t causal, order, chunk, fold, negative;
     float c;            // |scale| log2(e)
     float scale;        // |scale|
@@ -132,6 +133,7 @@ template <int DT> struct Weights;
 template <> struct Weights<FX_F32> {
     f32x16 p;
     __device__ __forceinline__ void set(const f32x16& x) { p = x; }
+    __device__ __forceinline__ f32x16 rest(const f32x16&) const { return f32x16(0.f); }
 };
 template <int DT> struct Weights16 {
     typedef typename Elem<typename AttnType<DT>::T>::vec8 vec;
@@ -145,9 +147,20 @@ template <int DT> struct Weights16 {
             __builtin_memcpy(&p[t], &w, 16);
         }
     }
+    // what the rounding of x left
+    __device__ __forceinline__ f32x16 rest(const f32x16& x) const {
+        f32x16 y;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) y[r] = x[r] - (float)p[r >> 3][r & 7];
+        return y;
+    }
 };
 template <> struct Weights<FX_F16> : Weights16<FX_F16> {};
 template <> struct Weights<FX_BF16> : Weights16<FX_BF16> {};
+
+// A sum over up to so many rows takes along what the rounding of its weights left: over more their errors cancel as good as ever, in
+// a product with one or two they are the result's own, beside its rounding.
+constexpr int kTinyRows = 16;
 
 // acc += (columns 32 col .. 32 col + 31 of the 32 rows from row0 on)^T w, the result's rows the tile's columns
 template <int DT, int RB> struct ColumnProduct {

@@ -8,7 +8,7 @@ namespace fx {
 // ------------------------------------------------------------------ forward
 // What a wave keeps of its 32 queries, a column (lane % 32) each: the sums so far, the maximum that their weights are relative to,
 // and the sum of the weights of the lane's half of the keys.
-template <int DT, int DP> struct FwdWave {
+template <int DT, int DP, bool TINY = false> struct FwdWave {
     typedef typename AttnType<DT>::T T;
     static constexpr int RB = DP * AttnType<DT>::ES, STEPS = RB / 32, COLS = DP / 32;
     RowReader<DT, RB> rows_of;
@@ -17,6 +17,7 @@ template <int DT, int DP> struct FwdWave {
     f32x16 acc[COLS];
     float m, sum, c;
     int half;
+    bool tiny = false;              // few keys in all
 
     __device__ __forceinline__ void init(const AttnArgs& a, int lane) {
         half = lane >> 5;
@@ -70,6 +71,11 @@ template <int DT, int DP> struct FwdWave {
             w.set(s[t]);
 #pragma unroll
             for (int k = 0; k < COLS; ++k) columns(acc[k], vt, row0 + t * 32, k, w);
+            if (TINY && DT != FX_F32 && tiny) {
+                w.set(w.rest(s[t]));
+#pragma unroll
+                for (int k = 0; k < COLS; ++k) columns(acc[k], vt, row0 + t * 32, k, w);
+            }
         }
         sum += part;
     }
@@ -138,7 +144,7 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
     TileLoad<RB, KT, W> lk, lv;
     lk.init(wave, lane, a.k.ld, a.dim_bytes);
     lv.init(wave, lane, a.v.ld, a.dim_bytes);
-    FwdWave<DT, DP> w;
+    FwdWave<DT, DP, W == 2> w;
     w.init(a, lane);
     const int head = work.head, kv_head = head / a.group;
     const SeqTile st = a.tiles[work.tile];
@@ -157,6 +163,7 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
     }
     w.q.load(a.q.p + (int64_t)p.q0 * a.q.ld + head * a.q.hs, a.q.ld, row0, p.nq, a.dim_bytes, lane, a.negative);
     w.clear();
+    w.tiny = p.nk <= kTinyRows;
     bool odd = false;
     for (int j = 0; j < n; ++j) {
         __builtin_amdgcn_s_waitcnt(0);
@@ -180,78 +187,79 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
 #endif
 }
 
-// The same for few queries: the W waves of a workgroup share one block of 32, take the blocks of 32 keys in turn, each with
-// buffers of its own and no barrier until the end, where their results are joined.
-template <int DT, int DP, int W> struct FewShape {
+// The same for few queries: RG blocks of 32 queries, for each of which KS waves take the blocks of 32 keys in turn.  The RG waves of a
+// turn share its tiles; at the end the KS results of a block of queries are joined.
+template <int DT, int DP, int RG, int KS> struct FewShape {
     static constexpr int RB = DP * AttnType<DT>::ES;
     static constexpr int kTile = LdsRows<RB>::bytes(32);
-    static constexpr int kBuffers = 4 * kTile * W <= 128 * 1024 ? 2 : 1;
+    static constexpr int kBuffers = 4 * kTile * KS <= 128 * 1024 ? 2 : 1;
     static constexpr int kSlot = DP * 32 * 4 + 512;                 // a wave's result
-    static constexpr int kLds = std::max(2 * kBuffers * kTile * W, W / 2 * kSlot);
+    static constexpr int kLds = std::max(2 * kBuffers * kTile * KS, KS / 2 * RG * kSlot);
 };
 
-template <int DT, int DP, int W>
-__global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_attention_few(AttnArgs a) {
+template <int DT, int DP, int RG, int KS>
+__global__ __launch_bounds__(64 * RG * KS, least_waves(DP * AttnType<DT>::ES)) void k_attention_few(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    typedef FewShape<DT, DP, W> S;
+    typedef FewShape<DT, DP, RG, KS> S;
     constexpr int RB = S::RB, COLS = DP / 32, NB = S::kBuffers;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const Work work = work_of(a, a.heads);
     if (work.head < 0) return;
     const int head = work.head, kv_head = head / a.group;
-    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63;
-    lds_byte* lds = (lds_byte*)smem + wave * 2 * NB * S::kTile;
+    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63, rg = wave % RG, turn = wave / RG;
+    lds_byte* lds = (lds_byte*)smem + turn * 2 * NB * S::kTile;
     const SeqTile st = a.tiles[work.tile];
     const Pair p = pair_of(a, st);
     const unsigned char* kb = a.k.p + (int64_t)p.k0 * a.k.ld + kv_head * a.k.hs;
     const unsigned char* vb = a.v.p + (int64_t)p.k0 * a.v.ld + kv_head * a.v.hs;
-    TileLoad<RB, 32, 1> lk, lv;
-    lk.init(0, lane, a.k.ld, a.dim_bytes);
-    lv.init(0, lane, a.v.ld, a.dim_bytes);
-    const int row0 = st.row, row = row0 + (lane & 31), shift = p.nk - p.nq;
-    const int seen = a.causal ? max(0, min(p.nk, min(row0 + 32, p.nq) + shift)) : p.nk;
+    TileLoad<RB, 32, RG> lk, lv;
+    lk.init(rg, lane, a.k.ld, a.dim_bytes);
+    lv.init(rg, lane, a.v.ld, a.dim_bytes);
+    const int row0 = st.row + rg * 32, row = row0 + (lane & 31), shift = p.nk - p.nq;
+    const int seen = a.causal ? max(0, min(p.nk, min(st.row + 32 * RG, p.nq) + shift)) : p.nk;
+    const int seen_wave = row0 >= p.nq ? 0 : a.causal ? max(0, min(p.nk, min(row0 + 32, p.nq) + shift)) : p.nk;
     const int last = a.causal ? min(p.nk - 1, row + shift) : p.nk - 1, unmasked = a.causal ? min(p.nk - 1, row0 + shift) : p.nk - 1;
-    const int n = (seen + 31) / 32;
-    if (wave < n) {
-        lk.load(lds, kb, a.k.ld, wave * 32, p.nk, a.dim_bytes, 0);
-        lv.load(lds + S::kTile, vb, a.v.ld, wave * 32, p.nk, a.dim_bytes, 0);
-    }
+    const int n = (seen + 31) / 32, rounds = (n + KS - 1) / KS;         // a wave without a block in the last round waits with the others
+    auto load = [&](int j, int b) {
+        lk.load(lds + b * 2 * S::kTile, kb, a.k.ld, j * 32, p.nk, a.dim_bytes, rg);
+        lv.load(lds + b * 2 * S::kTile + S::kTile, vb, a.v.ld, j * 32, p.nk, a.dim_bytes, rg);
+    };
+    if (turn < n) load(turn, 0);
     FwdWave<DT, DP> w;
     w.q.load(a.q.p + (int64_t)p.q0 * a.q.ld + head * a.q.hs, a.q.ld, row0, p.nq, a.dim_bytes, lane, a.negative);
     w.init(a, lane);
     w.clear();
-    int b = 0;
     bool odd = false;
-    for (int j = wave; j < n; j += W) {
+    for (int i = 0; i < rounds; ++i) {
+        const int j = i * KS + turn, b = NB == 2 ? i & 1 : 0;
         __builtin_amdgcn_s_waitcnt(0);
+        if (RG > 1) __syncthreads();
         const lds_byte* at = lds + b * 2 * S::kTile;
-        if (NB == 2 && j + W < n) {
-            b ^= 1;
-            lk.load(lds + b * 2 * S::kTile, kb, a.k.ld, (j + W) * 32, p.nk, a.dim_bytes, 0);
-            lv.load(lds + b * 2 * S::kTile + S::kTile, vb, a.v.ld, (j + W) * 32, p.nk, a.dim_bytes, 0);
+        if (NB == 2 && j + KS < n) load(j + KS, b ^ 1);
+        if (j * 32 < seen_wave) {
+            const bool masked = j * 32 + 31 > unmasked;
+            if (a.causal && masked) odd |= block_not_finite<DT, RB>(at + S::kTile, 0);
+            w.template blocks<1>(at, at + S::kTile, 0, j * 32, masked, last);
         }
-        const bool masked = j * 32 + 31 > unmasked;
-        if (a.causal && masked) odd |= block_not_finite<DT, RB>(at + S::kTile, 0);
-        w.template blocks<1>(at, at + S::kTile, 0, j * 32, masked, last);
-        if (NB == 1 && j + W < n) {
+        if (NB == 1) {
             __builtin_amdgcn_s_waitcnt(0);          // what is read there has been read
-            lk.load(lds, kb, a.k.ld, (j + W) * 32, p.nk, a.dim_bytes, 0);
-            lv.load(lds + S::kTile, vb, a.v.ld, (j + W) * 32, p.nk, a.dim_bytes, 0);
+            if (RG > 1) __syncthreads();
+            if (j + KS < n) load(j + KS, 0);
         }
     }
     w.sum += other_half(w.sum);
 #pragma unroll
-    for (int h = W / 2; h >= 1; h /= 2) {
+    for (int h = KS / 2; h >= 1; h /= 2) {
         __syncthreads();
-        if (wave >= h && wave < 2 * h) {
-            float* to = (float*)(smem + (wave - h) * S::kSlot);
+        if (turn >= h && turn < 2 * h) {
+            float* to = (float*)(smem + ((turn - h) * RG + rg) * S::kSlot);
             put_result<COLS>(to, w.acc, lane);
             to[COLS * 1024 + lane] = w.m;
             to[COLS * 1024 + 64 + lane] = w.sum;
         }
         __syncthreads();
-        if (wave < h) {
-            const float* in = (const float*)(smem + wave * S::kSlot);
+        if (turn < h) {
+            const float* in = (const float*)(smem + (turn * RG + rg) * S::kSlot);
             const float m2 = in[COLS * 1024 + lane], sum2 = in[COLS * 1024 + 64 + lane], to = fmaxf(w.m, m2);
             w.rescale(to);
             const float f = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m2 - to) * a.c);
@@ -263,7 +271,7 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
         }
     }
     odd = __syncthreads_or(odd);
-    if (wave == 0) {
+    if (turn == 0) {
         w.store(a, row, p.nq, p.q0, head);
         if (odd) again<DT>(args_here(), p, head, row0, lane_here());
     }
@@ -272,8 +280,10 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
 
 template <int DT, int DP> static void launch_fwd(const AttnArgs& a, hipStream_t st) {
     const unsigned blocks = work_blocks(a, a.heads);
-    constexpr int FEW = few_waves(DP * AttnType<DT>::ES);
-    if (a.tile_rows == 32) k_attention_few<DT, DP, FEW><<<blocks, 64 * FEW, FewShape<DT, DP, FEW>::kLds, st>>>(a);
+    // one block of 32 and eight waves, where those have registers enough, or four; or two that share tiles, and four waves for each
+    constexpr int RB = DP * AttnType<DT>::ES, RG = share_tiles(DT, RB, false) ? 2 : 1, KS = RB > 512 ? 2 : 4, KS1 = RB > 128 ? KS : 8;
+    if (a.few == 1) k_attention_few<DT, DP, 1, KS1><<<blocks, 64 * KS1, FewShape<DT, DP, 1, KS1>::kLds, st>>>(a);
+    else if (a.few) k_attention_few<DT, DP, RG, KS><<<blocks, 64 * RG * KS, FewShape<DT, DP, RG, KS>::kLds, st>>>(a);
     else if (a.tile_rows == 64) k_attention<DT, DP, 2><<<blocks, 128, FwdShape<DT, DP>::kLds, st>>>(a);
     else k_attention<DT, DP, 4><<<blocks, 256, FwdShape<DT, DP>::kLds, st>>>(a);
 }
@@ -409,14 +419,20 @@ static fx_status check_places(const char* who, const HeadsTensor* t, int n) {
 }
 
 // Tiles of 128 rows, four waves, or, where those would be less than 4/5 as full as tiles of 64, those, of two waves: keys are
-// then loaded for half as many rows at a time, but no wave idles behind a sequence's end.  Where all tiles of 32 rows would
-// not occupy every SIMD and there are other rows to share out, 32, whose waves take those in turn.
-static void take_tiles(AttnArgs* a, const fx_sequences* q, int32_t heads, int64_t others) {
-    const int kind = q->n_tiles[0] * heads < 4 * compute_units() && others > 64 ? 0 : 64 * q->n_tiles[1] * 5 <= 128 * q->n_tiles[2] * 4 ? 1 : 2;
+// then loaded for half as many rows at a time, but no wave idles behind a sequence's end.  Where all blocks of 32 rows would
+// not occupy every SIMD and there are other rows to share out, several waves take those in turn for one block (few = 1: fewer blocks
+// than compute units; 2: more, and two blocks share tiles if rows are wide enough: 6,820 x 3 x 96 bf16 causal 111 -> 80 us, but
+// gradients of 8,772 x 2 x 64 149 -> 168).
+static void take_tiles(AttnArgs* a, const fx_sequences* q, int32_t heads, int64_t others, bool wide) {
+    const int64_t waves = q->n_tiles[0] * heads;
+    a->few = waves >= 4 * compute_units() || others <= 64 ? 0 : waves <= compute_units() || (wide && 64 * q->n_tiles[1] * 4 > 32 * q->n_tiles[0] * 5) ? 1 : 2;
+    const int kind = a->few ? (a->few == 2 && wide ? 1 : 0) : 64 * q->n_tiles[1] * 5 <= 128 * q->n_tiles[2] * 4 ? 1 : 2;
     a->tiles = q->d_tiles[kind];
     a->n_tiles = (int32_t)q->n_tiles[kind];
     a->tile_rows = kSeqTileRows[kind];
 }
+// bytes of a row of a head in the kernel that takes it
+static int kernel_row_bytes(int dim, fx_dtype dt) { return (dim <= 32 ? 32 : dim <= 64 ? 64 : dim <= 128 ? 128 : 256) * dtype_size(dt); }
 
 static fx_status fill_args(const char* who, const fx_attention* d, AttnArgs* a, int64_t tiles, int32_t heads) {
     const fx_sequences *q = d->q_seqs, *k = d->kv_seqs ? d->kv_seqs : d->q_seqs;
@@ -453,7 +469,7 @@ extern "C" fx_status fx_attention_fwd(const fx_attention* d, void* d_out, int64_
     for (const HeadsTensor& x : t) FX_TRY(check_heads(who, x, d->dim, dtype_size(d->dt)));
     if ((uintptr_t)d_lse % 4) { set_error("%s: d_lse is not aligned to its elements", who); return FX_EINVAL; }
     FX_TRY(check_places(who, t, 4));
-    take_tiles(&a, d->q_seqs, d->heads, (d->kv_seqs ? d->kv_seqs : d->q_seqs)->longest);
+    take_tiles(&a, d->q_seqs, d->heads, (d->kv_seqs ? d->kv_seqs : d->q_seqs)->longest, share_tiles(d->dt, kernel_row_bytes(d->dim, d->dt), false));
     const int64_t tiles = a.n_tiles;
     FX_TRY(fill_args(who, d, &a, tiles, d->heads));
     if (nq == 0) return FX_OK;
@@ -494,8 +510,8 @@ extern "C" fx_status fx_attention_bwd(const fx_attention* d, const void* d_out, 
     if ((nq > 0 && !d_lse) || (uintptr_t)d_lse % 4 || (uintptr_t)d_glse % 4) { set_error("%s: d_lse is null, or it or d_glse is not aligned to its elements", who); return FX_EINVAL; }
     FX_TRY(check_places(who, t, n));
     AttnArgs b{};
-    take_tiles(&b, kq, d->kv_heads, d->q_seqs->longest * (d->heads / d->kv_heads));
-    take_tiles(&a, d->q_seqs, d->heads, kq->longest);
+    take_tiles(&b, kq, d->kv_heads, d->q_seqs->longest * (d->heads / d->kv_heads), share_tiles(d->dt, kernel_row_bytes(d->dim, d->dt), true));
+    take_tiles(&a, d->q_seqs, d->heads, kq->longest, share_tiles(d->dt, kernel_row_bytes(d->dim, d->dt), true));
     FX_TRY(fill_args(who, d, &a, a.n_tiles, d->heads));
     FX_TRY(fill_args(who, d, &a, b.n_tiles, d->kv_heads));
     if (nq == 0 && nk == 0) return FX_OK;

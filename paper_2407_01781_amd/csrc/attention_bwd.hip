@@ -21,15 +21,15 @@ template <int DT, int DP> struct BwdShape {
     static constexpr int kParts = DP > 128 ? (DT == FX_F32 ? 4 : 2) : 1;
     static constexpr int COLS = DP / 32 / kParts, STEPS = RB / 32;
     static constexpr int kPart = COLS * (DT == FX_F32 ? 2 : 1) * LdsRows<RB>::kSegment;         // from part to part in a tile
-    // a workgroup of W waves that share one block of rows, each with buffers of its own
+    // workgroups of RG blocks of rows, for each of which KS waves take the others' blocks in turn
     static constexpr int kBlock = LdsRows<RB>::bytes(32), kBlockStats = 32 * 8;
     static constexpr int kOwn = 2 * kBlock + kBlockStats;            // a wave's two tiles and what belongs to their rows
-    template <int W> static constexpr int buffers() { return 2 * kOwn * W <= 128 * 1024 ? 2 : 1; }
-    template <int W> static constexpr int lds_few() { return std::max(buffers<W>() * kOwn * W, W / 2 * COLS * 4096); }
+    template <int KS> static constexpr int buffers() { return 2 * kOwn * KS <= 128 * 1024 ? 2 : 1; }
+    template <int RG, int KS> static constexpr int lds_few() { return std::max(buffers<KS>() * kOwn * KS, KS / 2 * RG * COLS * 4096); }
 };
 
 // ------------------------------------------------------------------ gradients of the queries
-template <int DT, int DP> struct GqWave {
+template <int DT, int DP, bool TINY = false> struct GqWave {
     typedef BwdShape<DT, DP> S;
     typedef typename AttnType<DT>::T T;
     static constexpr int RB = S::RB;
@@ -39,7 +39,7 @@ template <int DT, int DP> struct GqWave {
     f32x16 acc[S::COLS];
     float lse2, glse, delta, c;
     int half, part;
-    bool one_key, one_tile;
+    bool one_key, one_tile, tiny;
 
     // A row that sees one key has dS = glse whatever it holds; the rounding of out would leave something.  Where a sequence's keys
     // are one tile, the sum over P dP is made of the tile's own numbers.
@@ -63,6 +63,7 @@ template <int DT, int DP> struct GqWave {
         delta += other_half(delta);
         one_key = p.nk == 1;
         one_tile = p.nk <= tile_keys;
+        tiny = p.nk <= kTinyRows;
         if (one_key) delta = 0.f;
         q.load(a.q.p + (int64_t)p.q0 * a.q.ld + head * a.q.hs, a.q.ld, row0, p.nq, a.dim_bytes, lane, a.negative);
 #pragma unroll
@@ -107,6 +108,11 @@ template <int DT, int DP> struct GqWave {
             w.set(p[t]);
 #pragma unroll
             for (int k = 0; k < S::COLS; ++k) columns(acc[k], kt + part * S::kPart, t * 32, k, w);
+            if (TINY && DT != FX_F32 && tiny) {
+                w.set(w.rest(p[t]));
+#pragma unroll
+                for (int k = 0; k < S::COLS; ++k) columns(acc[k], kt + part * S::kPart, t * 32, k, w);
+            }
         }
     }
 
@@ -171,7 +177,7 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
         lk.load(lds, kb, a.k.ld, 0, p.nk, a.dim_bytes, wave);
         lv.load(lds + 2 * S::kKeys, vb, a.v.ld, 0, p.nk, a.dim_bytes, wave);
     }
-    GqWave<DT, DP> w;
+    GqWave<DT, DP, W == 2> w;
     w.init(a, p, head, work.head % S::kParts, row0, lane, KT);
     bool odd = false;
     for (int j = 0; j < n; ++j) {
@@ -194,15 +200,15 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
 #endif
 }
 
-// The results of W waves added, the upper half's by the lower until wave 0 has all
-template <int W, int N> __device__ __forceinline__ void add_results(unsigned char* smem, f32x16 (&x)[N], int wave, int lane) {
+// The results of a block's KS waves added, the upper half's by the lower until the first has all
+template <int RG, int KS, int N> __device__ __forceinline__ void add_results(unsigned char* smem, f32x16 (&x)[N], int rg, int turn, int lane) {
 #pragma unroll
-    for (int h = W / 2; h >= 1; h /= 2) {
+    for (int h = KS / 2; h >= 1; h /= 2) {
         __syncthreads();
-        if (wave >= h && wave < 2 * h) put_result<N>((float*)smem + (wave - h) * N * 1024, x, lane);
+        if (turn >= h && turn < 2 * h) put_result<N>((float*)smem + ((turn - h) * RG + rg) * N * 1024, x, lane);
         __syncthreads();
-        if (wave < h) {
-            const float* in = (const float*)smem + wave * N * 1024;
+        if (turn < h) {
+            const float* in = (const float*)smem + (turn * RG + rg) * N * 1024;
 #pragma unroll
             for (int k = 0; k < N; ++k)
 #pragma unroll
@@ -211,53 +217,58 @@ template <int W, int N> __device__ __forceinline__ void add_results(unsigned cha
     }
 }
 
-// For few queries: W waves share one block of 32 and take the blocks of 32 keys in turn, each with buffers of its own
-template <int DT, int DP, int W>
-__global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_attention_gq_few(AttnArgs a) {
+// For few queries: RG blocks of 32, for each of which KS waves take the blocks of 32 keys in turn
+template <int DT, int DP, int RG, int KS>
+__global__ __launch_bounds__(64 * RG * KS, least_waves(DP * AttnType<DT>::ES)) void k_attention_gq_few(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef BwdShape<DT, DP> S;
-    constexpr int RB = S::RB, NB = S::template buffers<W>();
+    constexpr int RB = S::RB, NB = S::template buffers<KS>();
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const Work work = work_of(a, a.heads * S::kParts);
     if (work.head < 0) return;
     const int head = work.head / S::kParts, kv_head = head / a.group;
-    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63;
-    lds_byte* lds = (lds_byte*)smem + wave * NB * S::kOwn;
+    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63, rg = wave % RG, turn = wave / RG;
+    lds_byte* lds = (lds_byte*)smem + turn * NB * S::kOwn;
     const SeqTile st = a.tiles[work.tile];
     const Pair p = pair_of(a, st);
     const unsigned char* kb = a.k.p + (int64_t)p.k0 * a.k.ld + kv_head * a.k.hs;
     const unsigned char* vb = a.v.p + (int64_t)p.k0 * a.v.ld + kv_head * a.v.hs;
-    TileLoad<RB, 32, 1> lk, lv;
-    lk.init(0, lane, a.k.ld, a.dim_bytes);
-    lv.init(0, lane, a.v.ld, a.dim_bytes);
-    const int row0 = st.row, row = row0 + (lane & 31), shift = p.nk - p.nq;
-    const int seen = a.causal ? max(0, min(p.nk, min(row0 + 32, p.nq) + shift)) : p.nk;
+    TileLoad<RB, 32, RG> lk, lv;
+    lk.init(rg, lane, a.k.ld, a.dim_bytes);
+    lv.init(rg, lane, a.v.ld, a.dim_bytes);
+    const int row0 = st.row + rg * 32, row = row0 + (lane & 31), shift = p.nk - p.nq;
+    const int seen = a.causal ? max(0, min(p.nk, min(st.row + 32 * RG, p.nq) + shift)) : p.nk;
+    const int seen_wave = row0 >= p.nq ? 0 : a.causal ? max(0, min(p.nk, min(row0 + 32, p.nq) + shift)) : p.nk;
     const int last = a.causal ? min(p.nk - 1, row + shift) : p.nk - 1, unmasked = a.causal ? min(p.nk - 1, row0 + shift) : p.nk - 1;
-    const int n = a.gq.p || p.nk <= 32 ? (seen + 31) / 32 : 0;
+    const int n = a.gq.p || p.nk <= 32 ? (seen + 31) / 32 : 0, rounds = (n + KS - 1) / KS;
     auto load = [&](int j, int b) {
-        lk.load(lds + b * S::kOwn, kb, a.k.ld, j * 32, p.nk, a.dim_bytes, 0);
-        lv.load(lds + b * S::kOwn + S::kBlock, vb, a.v.ld, j * 32, p.nk, a.dim_bytes, 0);
+        lk.load(lds + b * S::kOwn, kb, a.k.ld, j * 32, p.nk, a.dim_bytes, rg);
+        lv.load(lds + b * S::kOwn + S::kBlock, vb, a.v.ld, j * 32, p.nk, a.dim_bytes, rg);
     };
-    if (wave < n) load(wave, 0);
+    if (turn < n) load(turn, 0);
     GqWave<DT, DP> w;
     w.init(a, p, head, work.head % S::kParts, row0, lane, 32);
-    int b = 0;
     bool odd = false;
-    for (int j = wave; j < n; j += W) {
+    for (int i = 0; i < rounds; ++i) {
+        const int j = i * KS + turn, b = NB == 2 ? i & 1 : 0;
         __builtin_amdgcn_s_waitcnt(0);
+        if (RG > 1) __syncthreads();
         const lds_byte* at = lds + b * S::kOwn;
-        if (NB == 2 && j + W < n) load(j + W, b ^= 1);
-        const bool masked = j * 32 + 31 > unmasked;
-        if (a.causal && masked) odd |= block_not_finite<DT, RB>(at, 0);
-        w.template blocks<1>(at, at + S::kBlock, j * 32, masked, last);
-        if (NB == 1 && j + W < n) {
+        if (NB == 2 && j + KS < n) load(j + KS, b ^ 1);
+        if (j * 32 < seen_wave) {
+            const bool masked = j * 32 + 31 > unmasked;
+            if (a.causal && masked) odd |= block_not_finite<DT, RB>(at, 0);
+            w.template blocks<1>(at, at + S::kBlock, j * 32, masked, last);
+        }
+        if (NB == 1) {
             __builtin_amdgcn_s_waitcnt(0);          // what is read there has been read
-            load(j + W, 0);
+            if (RG > 1) __syncthreads();
+            if (j + KS < n) load(j + KS, 0);
         }
     }
-    add_results<W>(smem, w.acc, wave, lane);
+    add_results<RG, KS>(smem, w.acc, rg, turn, lane);
     odd = __syncthreads_or(odd);
-    if (wave == 0) {
+    if (turn == 0) {
         w.store(a, p, head, row);
         if (odd && w.part == 0) gq_again<DT>(args_here(), p, head, row0, lane_here());
     }
@@ -265,7 +276,7 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
 }
 
 // ------------------------------------------------------------------ gradients of keys and values
-template <int DT, int DP> struct GkvWave {
+template <int DT, int DP, bool TINY = false> struct GkvWave {
     typedef BwdShape<DT, DP> S;
     typedef typename AttnType<DT>::T T;
     static constexpr int RB = S::RB;
@@ -275,13 +286,14 @@ template <int DT, int DP> struct GkvWave {
     f32x16 gk[S::COLS], gv[S::COLS];
     float c;
     int half, part;
-    bool one_key;
+    bool one_key, tiny;
 
     __device__ __forceinline__ void init(const AttnArgs& a, const Pair& p, int kv_head, int part_, int key0, int lane) {
         half = lane >> 5;
         part = part_;
         c = a.c;
         one_key = p.nk == 1;
+        tiny = p.nq * a.group <= kTinyRows;
         k.load(a.k.p + (int64_t)p.k0 * a.k.ld + kv_head * a.k.hs, a.k.ld, key0, p.nk, a.dim_bytes, lane, a.negative);
         v.load(a.v.p + (int64_t)p.k0 * a.v.ld + kv_head * a.v.hs, a.v.ld, key0, p.nk, a.dim_bytes, lane);
         rows_of.init(lane);
@@ -322,6 +334,14 @@ template <int DT, int DP> struct GkvWave {
         for (int i = 0; i < S::COLS; ++i) columns(gv[i], ot + part * S::kPart, 0, i, wp);
 #pragma unroll
         for (int i = 0; i < S::COLS; ++i) columns(gk[i], qt + part * S::kPart, 0, i, wd);
+        if (TINY && DT != FX_F32 && tiny) {
+            wp.set(wp.rest(p));
+            wd.set(wd.rest(ds));
+#pragma unroll
+            for (int i = 0; i < S::COLS; ++i) columns(gv[i], ot + part * S::kPart, 0, i, wp);
+#pragma unroll
+            for (int i = 0; i < S::COLS; ++i) columns(gk[i], qt + part * S::kPart, 0, i, wd);
+        }
     }
 
     __device__ __forceinline__ void store(const AttnArgs& a, const Pair& p, int kv_head, int key) {
@@ -407,7 +427,7 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
         if (next >= p.nq) { next = begin; ++next_head; }
     };
     if (n > 0) load(0);
-    GkvWave<DT, DP> w;
+    GkvWave<DT, DP, W == 2> w;
     w.init(a, p, kv_head, work.head % S::kParts, key0, lane);
     int r0 = begin - QT;
     bool odd = false;
@@ -434,62 +454,65 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
 #endif
 }
 
-// For few keys: W waves share one block of 32 and take the blocks of 32 queries of all heads in turn
-template <int DT, int DP, int W>
-__global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, false)) void k_attention_gkv_few(AttnArgs a) {
+// For few keys: RG blocks of 32, for each of which KS waves take the blocks of 32 queries of all heads in turn
+template <int DT, int DP, int RG, int KS>
+__global__ __launch_bounds__(64 * RG * KS, least_waves_of(DP * AttnType<DT>::ES, false)) void k_attention_gkv_few(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef BwdShape<DT, DP> S;
-    constexpr int RB = S::RB, QT = 32, NB = S::template buffers<W>();
+    constexpr int RB = S::RB, QT = 32, NB = S::template buffers<KS>();
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const Work work = work_of(a, a.kv_heads * S::kParts);
     if (work.head < 0) return;
     const int kv_head = work.head / S::kParts;
-    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63;
-    unsigned char* own = smem + wave * NB * S::kOwn;
+    const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63, rg = wave % RG, turn = wave / RG;
+    unsigned char* own = smem + turn * NB * S::kOwn;
     const SeqTile st = a.tiles[work.tile];
     const Pair p = pair_of_keys(a, st);
-    const int key0 = a.causal ? (p.nk - 1) / 32 * 32 - st.row : st.row, key = key0 + (lane & 31), shift = p.nk - p.nq;
-    TileLoad<RB, QT, 1> lq, lo;
-    lq.init(0, lane, a.q.ld, a.dim_bytes);
-    lo.init(0, lane, a.gout.ld, a.dim_bytes);
-    const int begin = a.causal ? max(0, key0 - shift) / QT * QT : 0, per_head = begin < p.nq ? (p.nq - begin + QT - 1) / QT : 0, n = per_head * a.group;
-    int head = kv_head * a.group, at = wave;            // the wave's next block: the at-th of the head
-    auto settle = [&] { while (at >= per_head) { at -= per_head; ++head; } };
+    const int tile0 = a.causal ? (p.nk - 1) / (32 * RG) * (32 * RG) - st.row : st.row;
+    const int key0 = tile0 + rg * 32, key = key0 + (lane & 31), shift = p.nk - p.nq;
+    TileLoad<RB, QT, RG> lq, lo;
+    lq.init(rg, lane, a.q.ld, a.dim_bytes);
+    lo.init(rg, lane, a.gout.ld, a.dim_bytes);
+    const int begin = a.causal ? max(0, tile0 - shift) / QT * QT : 0, per_head = begin < p.nq ? (p.nq - begin + QT - 1) / QT : 0;
+    const int n = per_head * a.group, rounds = (n + KS - 1) / KS;
+    int head = kv_head * a.group, at = turn;            // the next block of the wave's turn: the at-th of the head
     auto load = [&](int b) {
+        while (at >= per_head) { at -= per_head; ++head; }
         const int r0 = begin + at * QT;
-        lq.load((lds_byte*)own + b * S::kOwn, a.q.p + (int64_t)p.q0 * a.q.ld + head * a.q.hs, a.q.ld, r0, p.nq, a.dim_bytes, 0);
-        lo.load((lds_byte*)own + b * S::kOwn + S::kBlock, a.gout.p + (int64_t)p.q0 * a.gout.ld + head * a.gout.hs, a.gout.ld, r0, p.nq, a.dim_bytes, 0);
-        load_stats<QT>(a, (lds_byte*)own + b * S::kOwn + 2 * S::kBlock, head, p.q0, r0, p.nq, lane);
+        lds_byte* to = (lds_byte*)own + b * S::kOwn;
+        lq.load(to, a.q.p + (int64_t)p.q0 * a.q.ld + head * a.q.hs, a.q.ld, r0, p.nq, a.dim_bytes, rg);
+        lo.load(to + S::kBlock, a.gout.p + (int64_t)p.q0 * a.gout.ld + head * a.gout.hs, a.gout.ld, r0, p.nq, a.dim_bytes, rg);
+        if (rg == RG - 1) load_stats<QT>(a, to + 2 * S::kBlock, head, p.q0, r0, p.nq, lane);
+        at += KS;
+        return r0;
     };
-    if (wave < n) {
-        settle();
-        load(0);
-    }
+    int r0 = 0, next = 0;
+    if (turn < n) next = load(0);
     GkvWave<DT, DP> w;
     w.init(a, p, kv_head, work.head % S::kParts, key0, lane);
-    int b = 0;
     bool odd = false;
-    for (int j = wave; j < n; j += W) {
+    for (int i = 0; i < rounds; ++i) {
+        const int j = i * KS + turn, b = NB == 2 ? i & 1 : 0;
         __builtin_amdgcn_s_waitcnt(0);
-        const unsigned char* now = own + b * S::kOwn;
-        const int r0 = begin + at * QT;
-        if (j + W < n) {
-            at += W;
-            settle();
-            if (NB == 2) load(b ^= 1);
+        if (RG > 1) __syncthreads();
+        r0 = next;
+        if (NB == 2 && j + KS < n) next = load(b ^ 1);
+        if (j < n && key0 < p.nk && !(a.causal && r0 + 31 + shift < key0)) {
+            const unsigned char* now = own + b * S::kOwn;
+            const bool masked = a.causal && r0 + shift < key0 + 31;
+            if (masked) odd |= block_not_finite<DT, RB>((const lds_byte*)now, 0) || block_not_finite<DT, RB>((const lds_byte*)now + S::kBlock, 0);
+            w.block((const lds_byte*)now, (const lds_byte*)now + S::kBlock, (const float*)(now + 2 * S::kBlock), masked, key - shift - r0);
         }
-        const bool masked = a.causal && r0 + shift < key0 + 31;
-        if (masked) odd |= block_not_finite<DT, RB>((const lds_byte*)now, 0) || block_not_finite<DT, RB>((const lds_byte*)now + S::kBlock, 0);
-        w.block((const lds_byte*)now, (const lds_byte*)now + S::kBlock, (const float*)(now + 2 * S::kBlock), masked, key - shift - r0);
-        if (NB == 1 && j + W < n) {
+        if (NB == 1) {
             __builtin_amdgcn_s_waitcnt(0);          // what is read there has been read
-            load(0);
+            if (RG > 1) __syncthreads();
+            if (j + KS < n) next = load(0);
         }
     }
-    add_results<W>(smem, w.gk, wave, lane);
-    add_results<W>(smem, w.gv, wave, lane);
+    add_results<RG, KS>(smem, w.gk, rg, turn, lane);
+    add_results<RG, KS>(smem, w.gv, rg, turn, lane);
     odd = __syncthreads_or(odd);
-    if (wave == 0) {
+    if (turn == 0) {
         w.store(a, p, kv_head, key);
         if (odd && w.part == 0) gkv_again<DT>(args_here(), p, kv_head, key0, lane_here());
     }
@@ -498,15 +521,19 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, false
 
 template <int DT, int DP> static void launch_bwd(const AttnArgs& a, const AttnArgs& b, bool keys, hipStream_t st) {
     typedef BwdShape<DT, DP> S;
-    constexpr int FEW = few_waves(DP * AttnType<DT>::ES);
-    static_assert(S::template lds_few<FEW>() <= 160 * 1024 && S::kLdsKeys <= 160 * 1024, "a compute unit has 160 KiB");
+    // as forward; eight waves have 256 registers each, which the gradients of wider rows do not do with
+    constexpr int RG = share_tiles(DT, S::RB, true) ? 2 : 1, KS = RG == 1 ? (S::RB > 512 ? 2 : 4) : S::RB > 256 ? 2 : 4, KSK = RG == 1 ? KS : S::RB > 128 ? 2 : 4, KS1 = S::RB > 512 ? 2 : S::RB > 128 ? 4 : 8;
+    constexpr int LDS = S::template lds_few<RG, KS>(), LDSK = S::template lds_few<RG, KSK>(), LDS1 = S::template lds_few<1, KS1>();
+    static_assert(LDS + 1024 <= 160 * 1024 && LDSK + 1024 <= 160 * 1024 && LDS1 + 1024 <= 160 * 1024 && S::kLdsKeys <= 160 * 1024, "a compute unit has 160 KiB");
     static_assert(S::kParts <= kMostParts, "the launch is checked for them");
     const unsigned nq = work_blocks(a, a.heads * S::kParts), nk = work_blocks(b, b.kv_heads * S::kParts);
-    if (nq && a.tile_rows == 32) k_attention_gq_few<DT, DP, FEW><<<nq, 64 * FEW, S::template lds_few<FEW>(), st>>>(a);
+    if (nq && a.few == 1) k_attention_gq_few<DT, DP, 1, KS1><<<nq, 64 * KS1, LDS1, st>>>(a);
+    else if (nq && a.few) k_attention_gq_few<DT, DP, RG, KS><<<nq, 64 * RG * KS, LDS, st>>>(a);
     else if (nq && a.tile_rows == 64) k_attention_gq<DT, DP, 2><<<nq, 128, S::kLdsKeys, st>>>(a);
     else if (nq) k_attention_gq<DT, DP, 4><<<nq, 256, S::kLdsKeys, st>>>(a);
     if (!keys || !nk) return;
-    if (b.tile_rows == 32) k_attention_gkv_few<DT, DP, FEW><<<nk, 64 * FEW, S::template lds_few<FEW>(), st>>>(b);
+    if (b.few == 1) k_attention_gkv_few<DT, DP, 1, KS1><<<nk, 64 * KS1, LDS1, st>>>(b);
+    else if (b.few) k_attention_gkv_few<DT, DP, RG, KSK><<<nk, 64 * RG * KSK, LDSK, st>>>(b);
     else if (b.tile_rows == 64) k_attention_gkv<DT, DP, 2><<<nk, 128, S::kLdsQueries, st>>>(b);
     else k_attention_gkv<DT, DP, 4><<<nk, 256, S::kLdsQueries, st>>>(b);
 }
@@ -523,6 +550,7 @@ void attention_bwd_launch(const AttnArgs& a, const AttnArgs& keys_tiles, fx_dtyp
     b.tiles = keys_tiles.tiles;
     b.n_tiles = keys_tiles.n_tiles;
     b.tile_rows = keys_tiles.tile_rows;
+    b.few = keys_tiles.few;
     if (b.order != kHeadsFirst) b.order = b.kv_heads % 8 ? kTilesFirst : kHeadsApart;
     b.chunk = b.order == kHeadsFirst ? std::max(1, std::min(8, b.n_tiles / 64)) : 1;
     if (b.causal && (int64_t)b.n_tiles * b.kv_heads <= 2 * compute_units()) {
