@@ -1,5 +1,6 @@
 // The paged cache of keys and values, and attention of one new row of each of many running sequences over it.
 #include "attention.h"
+#include "cache_rows.h"
 
 #include <math.h>
 
@@ -10,32 +11,13 @@ typedef __attribute__((ext_vector_type(2))) float f32v2;
 struct CacheArgs {
     unsigned char *k, *v;
     uint8_t *k_exp, *v_exp;
-    const int32_t *table, *start;       // start: of the rows written or read, or the lengths of a step
-    int64_t ld_table;
-    int32_t cols, pages, page_rows, kv_heads, dim, pitch;
+    const int32_t* start;               // of the rows written or read, or the lengths of a step
+    PageTable t;
+    int32_t dim, pitch;
 };
-
-// Row of the cache (over pages, heads, positions) that a position has, or -1
-__host__ __device__ __forceinline__ int64_t cache_row(const CacheArgs& c, int64_t seq, int64_t pos, int head) {
-    if (pos < 0) return -1;
-    const int64_t col = pos / c.page_rows;
-    if (col >= c.cols) return -1;
-    const int32_t page = c.table[seq * c.ld_table + col];
-    if (page < 0 || page >= c.pages) return -1;
-    return ((int64_t)page * c.kv_heads + head) * c.page_rows + pos % c.page_rows;
-}
 
 // e4m3 code of x, which is at most 448 in size or NaN
 __device__ __forceinline__ uint32_t to_e4m3(float a, float b) { return __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false) & 0xFFFF; }
-
-// the least e + 127 in 0 .. 255 with top <= 448 2^e = 1.75 2^(e + 8)
-__host__ __device__ __forceinline__ int exponent_of(float top) {
-    uint32_t u;
-    memcpy(&u, &top, 4);
-    if (u < 0x00800000u) return 0;                      // below 2^-126 all is left to e = -127
-    const int e = (int)(u >> 23) - 8 + ((u & 0x7FFFFF) > 0x600000u ? 1 : 0);
-    return e < 0 ? 0 : e;
-}
 
 // Eight elements of a row and head are a lane's; the lanes of a row (a power of two) find its largest value by shuffles.  Bound
 // by HBM: sixteen bytes in and eight to sixteen out a lane, keys and values in one thread so that two loads are in flight.
@@ -55,7 +37,7 @@ __device__ __forceinline__ int64_t place_of(const CacheArgs& c, const CacheRows&
         seq = lo;
         in = r - a.first[lo];
     }
-    return cache_row(c, seq, (int64_t)c.start[seq] + in, head);
+    return cache_row(c.t, seq, (int64_t)c.start[seq] + in, head);
 }
 
 // N elements of type T, at once where VEC, else those below n one by one and zeros
@@ -84,9 +66,9 @@ template <int DT, bool E4M3, bool VEC>
 __global__ __launch_bounds__(256) void k_cache_write(CacheArgs c, CacheRows a) {
     typedef typename AttnType<DT>::T T;
     const int lanes = 1 << a.lanes_log2, d = (threadIdx.x & (lanes - 1)) * 8;
-    const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> a.lanes_log2, all = a.rows * c.kv_heads;
-    const int64_t u = min(unit, all - 1), r = u / c.kv_heads;       // lanes without a row take part in the shuffles
-    const int head = (int)(u - r * c.kv_heads);
+    const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> a.lanes_log2, all = a.rows * c.t.kv_heads;
+    const int64_t u = min(unit, all - 1), r = u / c.t.kv_heads;       // lanes without a row take part in the shuffles
+    const int head = (int)(u - r * c.t.kv_heads);
     __attribute__((aligned(16))) T both[2][8];
     take8<T, VEC>(both[0], (const T*)(a.k.p + r * a.k.ld + head * a.k.hs) + d, c.dim - d);
     take8<T, VEC>(both[1], (const T*)(a.v.p + r * a.v.ld + head * a.v.hs) + d, c.dim - d);
@@ -121,9 +103,9 @@ template <int DT, bool E4M3, bool VEC>
 __global__ __launch_bounds__(256) void k_cache_read(CacheArgs c, CacheRows a) {
     typedef typename AttnType<DT>::T T;
     const int lanes = 1 << a.lanes_log2, d = (threadIdx.x & (lanes - 1)) * 8;
-    const int64_t u = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> a.lanes_log2, r = u / c.kv_heads;
+    const int64_t u = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> a.lanes_log2, r = u / c.t.kv_heads;
     if (r >= a.rows || d >= c.dim) return;
-    const int head = (int)(u - r * c.kv_heads);
+    const int head = (int)(u - r * c.t.kv_heads);
     const int64_t at = place_of(c, a, r, head);
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
@@ -167,8 +149,6 @@ struct StepArgs {
     int32_t heads, group, groups, splits;
     int32_t whole;                      // queries may be loaded 16 bytes at a time
     float scale2;                       // scale log2(e)
-    uint32_t magic;                     // p / page_rows = p * magic >> shift for p below 2^31
-    int32_t shift;
 };
 
 // Workgroups of four waves that share a compute unit, a wave on each SIMD: registers are allotted for them
@@ -233,13 +213,10 @@ __global__ __launch_bounds__(64 * W, RESIDENT) void k_attention_step(StepArgs a)
     item /= a.splits;
     const int part_of_group = item % a.groups;
     item /= a.groups;
-    const int kv = item % a.c.kv_heads;
-    const int64_t b = item / a.c.kv_heads;
+    const int kv = item % a.c.t.kv_heads;
+    const int64_t b = item / a.c.t.kv_heads;
     // row of the cache that position t + lane % 32 has, or -1; asked for one tile ahead
-    const int32_t* table = a.c.table + b * a.c.ld_table;
-    auto row_in = [&](int page, uint32_t pos, uint32_t col) {
-        return page < 0 || page >= a.c.pages ? -1 : (page * a.c.kv_heads + kv) * a.c.page_rows + (int)(pos - col * a.c.page_rows);
-    };
+    const int32_t* table = a.c.t.table + b * a.c.t.ld;
     const int len = (int)max((int64_t)0, min((int64_t)a.c.start[b], a.most)), chunk = chunk_of(a, len);
     const int64_t from = (int64_t)split * chunk;
     if (a.splits > 1 && from >= len) return;           // the join knows as much
@@ -291,9 +268,9 @@ __global__ __launch_bounds__(64 * W, RESIDENT) void k_attention_step(StepArgs a)
     float top = -INFINITY, sum = 0.f;
 
     auto row_of = [&](int t) {
-        const uint32_t pos = (uint32_t)t + (lane & 31), col = (uint32_t)(((uint64_t)pos * a.magic) >> a.shift);
-        const int page = col < (uint32_t)a.c.cols ? table[col] : -1;        // does not wait for the length
-        return (int)pos < end ? row_in(page, pos, col) : -1;
+        const uint32_t pos = (uint32_t)t + (lane & 31), col = page_column(pos, a.c.t.division);
+        const int page = col < (uint32_t)a.c.t.cols ? table[col] : -1;        // does not wait for the length
+        return (int)pos < end ? row_in_page(a.c.t, page, pos, col, kv) : -1;
     };
     int t = (int)from + wave * kStepTile;
     int row = row_of(t);
@@ -563,8 +540,9 @@ static fx_status check_cache(const char* who, const fx_cache* c, fx_dtype dt, Ca
         return FX_EINVAL;
     }
     if ((c->table_cols > 0 && !c->d_table) || (uintptr_t)c->d_table % 4) { set_error("%s: d_table is null or not aligned to its elements", who); return FX_EINVAL; }
-    *a = CacheArgs{(unsigned char*)c->d_k, (unsigned char*)c->d_v, c->d_k_exp, c->d_v_exp, c->d_table, nullptr, c->ld_table, c->table_cols, c->pages, c->page_rows,
-                   c->kv_heads, c->dim, (c->dim + 15) / 16 * 16};
+    *a = CacheArgs{(unsigned char*)c->d_k, (unsigned char*)c->d_v, c->d_k_exp, c->d_v_exp, nullptr,
+                   PageTable{c->d_table, c->ld_table, c->table_cols, c->pages, c->page_rows, c->kv_heads, page_division(c->page_rows)}, c->dim,
+                   (c->dim + 15) / 16 * 16};
     return FX_OK;
 }
 
@@ -578,7 +556,7 @@ static fx_status take_rows(const char* who, const HeadsTensor* t, const CacheArg
         *vec = *vec && (uintptr_t)t[i].p % 16 == 0 && view[i]->ld % 16 == 0 && (t[i].heads == 1 || view[i]->hs % 16 == 0);
     }
     while ((8 << x->lanes_log2) < c.pitch) ++x->lanes_log2;
-    const int64_t threads = (x->rows * c.kv_heads) << x->lanes_log2;
+    const int64_t threads = (x->rows * c.t.kv_heads) << x->lanes_log2;
     if (threads > (1ll << 32) - 256) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }
     *blocks = (unsigned)((threads + 255) / 256);
     return FX_OK;
@@ -598,7 +576,7 @@ extern "C" fx_status fx_cache_write(const fx_cache* c, const fx_sequences* q, in
     for (const HeadsTensor& x : t) FX_TRY(check_heads(who, x, c->dim, dtype_size(dt)));
     if (rows > 0 && (!d_start || (uintptr_t)d_start % 4)) { set_error("%s: d_start is null or not aligned to its elements", who); return FX_EINVAL; }
     if (rows > 0x7FFFFFFFll) { set_error("%s: more than 2^31-1 rows", who); return FX_ERANGE; }
-    if (rows == 0 || a.pages == 0) return FX_OK;
+    if (rows == 0 || a.t.pages == 0) return FX_OK;
     a.start = d_start;
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps(kProfCache, st);
@@ -658,13 +636,13 @@ extern "C" fx_status fx_attention_step(const fx_cache* c, int64_t rows, const in
     if (rows > 0 && (!d_len || (uintptr_t)d_len % 4 || (uintptr_t)d_lse % 4)) { set_error("%s: d_len is null, or it or d_lse is not aligned to its elements", who); return FX_EINVAL; }
     if (rows > 0 && d_q == d_out) { set_error("%s: d_out is where d_q is", who); return FX_EINVAL; }
     if (rows > 0x7FFFFFFFll / 64 / heads) { set_error("%s: too many rows", who); return FX_ERANGE; }
-    const int64_t all = (int64_t)a.cols * a.page_rows;
+    const int64_t all = (int64_t)a.t.cols * a.t.page_rows;
     if (all > 0x7FFFFFFFll) { set_error("%s: a table of more than 2^31-1 positions", who); return FX_ERANGE; }
     if (rows == 0) return FX_OK;
     a.start = d_len;
     StepArgs s{};
     s.c = a;
-    s.most = a.pages == 0 ? 0 : most == 0 ? all : std::min(most, all);
+    s.most = a.t.pages == 0 ? 0 : most == 0 ? all : std::min(most, all);
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps(kProfAttnStep, st);
     const int es = dtype_size(dt);
@@ -676,9 +654,6 @@ extern "C" fx_status fx_attention_step(const fx_cache* c, int64_t rows, const in
     s.group = heads / c->kv_heads;
     s.groups = (s.group + kStepHeads - 1) / kStepHeads;
     s.scale2 = scale * kLog2e;
-    while ((1ll << s.shift) < a.page_rows) ++s.shift;
-    s.magic = (uint32_t)((1ull << (31 + s.shift)) / (uint32_t)a.page_rows + 1);
-    s.shift += 31;
     // Up to 1024 positions a workgroup of 8 or 16 waves takes them all and there is no second launch; beyond, every sequence is
     // split into as many parts, such that there are about eight workgroups for a compute unit -- of one sequence, as many as a
     // unit holds at a time -- where that leaves the longest 256 positions at least.  (Parts of equal length, more of them in longer sequences: 327 us for 64 sequences of up to 32,768
