@@ -105,9 +105,8 @@ def exponents(x):
     """Exponents (plus 127) of rows in a cache of 8 bits: the least e >= -127 with no finite value over 448 2^e."""
     top = np.abs(np.where(np.isfinite(x), x, 0)).max(-1)
     out = np.zeros(top.shape, np.int64)
-    for i, t in np.ndenumerate(top):
-        while t > 448.0 * 2.0 ** (int(out[i]) - 127):
-            out[i] += 1
+    while (more := top > 448.0 * np.exp2(out - 127.0)).any():
+        out[more] += 1
     return out
 
 
