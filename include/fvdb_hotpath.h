@@ -567,22 +567,25 @@ fx_status fx_dropout(const void* d_x, int64_t ld_x, fx_dtype dt, int64_t rows, i
  * r * ld + h * hs + d (ld, hs in elements, >= dim), so that queries, keys and values may be column ranges of one projection and
  * heads may be the outer dimension.  Pointers are aligned to an element, no more; where they or the strides are not multiples of
  * 16 bytes, or dim is not, the call copies the rows into such an order first (scratch).  heads is a multiple of kv_heads (query
- * head h reads key head h / (heads / kv_heads)), dim 1 to 256 (FX_ERANGE).  Scratch and graphs as for the recurrence.
+ * head h reads key head h / (heads / kv_heads)).  FX_ERANGE beyond dim 256, 65535 heads, strides of 2^46 elements, 2^31-1025 rows of a sequence, or where a launch's
+ * threads pass 2^32 (128 rows of a head take 256).  Scratch (those copies, two floats for every row and head of the gradients, the
+ * splits of a step) and graphs as for the recurrence.
  *
  *     s_ij = scale q_i . k_j,   lse_i = log sum_j exp(s_ij),   out_i = sum_j exp(s_ij - lse_i) v_j
  *
  * j runs over the keys of i's sequence.  With `causal` the last query stands at the last key and each before it one key earlier:
  * query i of n sees key j of m where n - i <= m - j.  A row that sees no key gets out = 0, lse = -inf, and gradients of 0.
  * Products, maxima and sums are fp32; in 16 bits exp(s - m) is rounded to the type before its product with v (m close to the
- * row's maximum, the sum of the weights is of the unrounded ones), every output once.  A row's results depend on the keys that it sees alone:
- * infinities and NaN of other rows, of a causal sequence's later ones too, leave it as it is.
+ * row's maximum, the sum of the weights is of the unrounded ones), every output once.  A row's results depend on the keys that it sees alone,
+ * a key's gradients on the queries that see it: infinities and NaN of others, of a causal sequence's later rows too, add nothing.
+ * (Where a causal sequence holds such a value, the elements that it would spoil of the rows around it are summed one by one.)
  *   q_seqs, kv_seqs  the rows' division into sequences, as many of both; kv_seqs NULL: q_seqs
  *   d_lse            [heads, rows of q_seqs] fp32, natural logarithm, or NULL
  * Backward: d_out and d_lse are what the forward call wrote, d_gout and d_glse ([heads, rows], NULL: zeros) the gradients of
  * both outputs.  With P_ij = exp(s_ij - lse_i), dP_ij = gout_i . v_j and dS_ij = P_ij (dP_ij - sum_j P_ij dP_ij + glse_i):
  *     gq_i = scale sum_j dS_ij k_j,   gk_j = scale sum_i dS_ij q_i,   gv_j = sum_i P_ij gout_i
- * over all query heads of a key head.  In 16 bits P and dS are rounded to the type before their products.  gq, gk and gv may be NULL
- * (not computed).  No atomics: the same bits from every call.
+ * over all query heads of a key head.  In 16 bits P and dS are rounded to the type before their products (not in sums over up to
+ * 16 rows).  The sum over P dP is taken as gout . out, of a sequence's few keys as it stands.  gq, gk and gv may be NULL (not computed).  No atomics: the same bits from every call.
  * An output must not be where an input or another output is (FX_EINVAL) nor overlap them, and its rows and heads must not
  * overlap each other (FX_EINVAL). */
 typedef struct {
@@ -616,7 +619,8 @@ fx_status fx_attention_bwd(const fx_attention* a, const void* d_out, int64_t ld_
  * FX_E4M3, none otherwise).
  * fx_attention_step: out_b = attention of query row b over positions 0 .. d_len[b]-1 of sequence b (no key: 0 and lse = -inf), d_lse
  * [rows, heads] or NULL.  `most` bounds the lengths on the host (longer ones are cut there), 0: table_cols * page_rows; the split of the work goes by it.
- * The weights exp(s - m) are rounded to 16 bits after the leading 8 where they meet 16-bit values, to 24 bits where q is FX_F32.
+ * The weights exp(s - m) have 16 bits at least where they meet values (22 in FX_F16, 24 where q is FX_F32).
+ * FX_ERANGE beyond 2^31-1 rows of pages and heads, 2^31-1 rows of a call, 2^31-8193 positions of a step's table, 65535 heads.
  * None of the calls waits for the stream; lengths, starts and the table are read when the kernels run, so that a captured step follows them. */
 enum { FX_E4M3 = 3 };
 typedef struct {

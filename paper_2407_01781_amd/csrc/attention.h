@@ -214,9 +214,10 @@ __device__ __forceinline__ Pair pair_of_keys(const AttnArgs& a, const SeqTile& t
 
 // ------------------------------------------------------------------ infinities and NaN in rows that are not seen
 // A causal sequence's diagonal blocks multiply weights of 0 with rows that are not seen, and 0 times an infinity is NaN.  A wave looks
-// into such blocks before it multiplies; where one holds a value that is not finite, the wave computes its 32 rows again
-// behind its loop, one after the other over what each sees alone (the registers of the loop are free there: products with
-// guarded values in the loop itself cost up to 80 of them).
+// into such blocks before it multiplies.  Where one holds a value that is not finite, the wave goes over its 32 rows again behind
+// its loop (the registers of the loop are free there: products with guarded values in the loop itself cost up to 80 of them): the
+// elements of a result that an unseen row has spoilt are summed anew over what is seen, from the diagonal on, until they
+// are not finite by themselves -- at once where everything is NaN, and no further than the next such value in any case.
 template <int DT> __device__ __forceinline__ uint32_t not_finite(uint32_t w) {       // the sign bit of every value that is not
     if (DT == FX_F32) return ((w & 0x7F800000u) + 0x00800000u) & 0x80000000u;
     if (DT == FX_F16) return ((w & 0x7C007C00u) + 0x04000400u) & 0x80008000u;
@@ -255,27 +256,58 @@ template <int DT, int RB> __device__ __forceinline__ bool block_not_finite(const
 }
 
 // A row in a wave's registers, elements lane + 64 e
+constexpr int kLaneParts = kMostDim / 64;
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
 template <int DT> struct LaneRow {
-    float x[kMostDim / 64];
+    typedef typename AttnType<DT>::T T;
+    float x[kLaneParts];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int e = 0; e < kLaneParts; ++e) x[e] = 0.f;
+    }
     __device__ __forceinline__ void load(const unsigned char* p, int dim, int lane, float f = 1.f) {
 #pragma unroll
-        for (int e = 0; e < kMostDim / 64; ++e) x[e] = lane + 64 * e < dim ? (float)((const typename AttnType<DT>::T*)p)[lane + 64 * e] * f : 0.f;
-    }
-    __device__ __forceinline__ void store(unsigned char* p, int dim, int lane, float f) const {
-#pragma unroll
-        for (int e = 0; e < kMostDim / 64; ++e)
-            if (lane + 64 * e < dim) ((typename AttnType<DT>::T*)p)[lane + 64 * e] = (typename AttnType<DT>::T)(x[e] * f);
+        for (int e = 0; e < kLaneParts; ++e) x[e] = lane + 64 * e < dim ? (float)((const T*)p)[lane + 64 * e] * f : 0.f;
     }
     __device__ __forceinline__ void add(float f, const LaneRow& o) {
 #pragma unroll
-        for (int e = 0; e < kMostDim / 64; ++e) x[e] = fmaf(f, o.x[e], x[e]);
+        for (int e = 0; e < kLaneParts; ++e) x[e] = fmaf(f, o.x[e], x[e]);
     }
     __device__ __forceinline__ float dot(const LaneRow& o) const {
         float s = 0.f;
 #pragma unroll
-        for (int e = 0; e < kMostDim / 64; ++e) s = fmaf(x[e], o.x[e], s);
+        for (int e = 0; e < kLaneParts; ++e) s = fmaf(x[e], o.x[e], s);
         for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d, 64);
         return s;
+    }
+};
+// The elements of a result that unseen rows have spoilt, of those from `from` to `to` - 1
+struct Spoilt {
+    bool is[kLaneParts];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int e = 0; e < kLaneParts; ++e) is[e] = false;
+    }
+    template <int DT> __device__ __forceinline__ void by(const LaneRow<DT>& r, int from, int to, int lane) {
+#pragma unroll
+        for (int e = 0; e < kLaneParts; ++e) is[e] |= lane + 64 * e >= from && lane + 64 * e < to && !finite(r.x[e]);
+    }
+    __device__ __forceinline__ bool any() const {
+        bool a = false;
+#pragma unroll
+        for (int e = 0; e < kLaneParts; ++e) a |= is[e];
+        return __any(a);
+    }
+    template <int DT> __device__ __forceinline__ bool settled(const LaneRow<DT>& r) const {      // none of them can become finite again
+        bool open = false;
+#pragma unroll
+        for (int e = 0; e < kLaneParts; ++e) open |= is[e] && finite(r.x[e]);
+        return !__any(open);
+    }
+    template <int DT> __device__ __forceinline__ void store(const LaneRow<DT>& r, unsigned char* p, int lane, float f) const {
+#pragma unroll
+        for (int e = 0; e < kLaneParts; ++e)
+            if (is[e]) ((typename AttnType<DT>::T*)p)[lane + 64 * e] = (typename AttnType<DT>::T)(r.x[e] * f);
     }
 };
 __device__ __forceinline__ unsigned char* row_of_head(const HeadsView& v, int64_t row, int head) { return v.p + row * v.ld + head * v.hs; }

@@ -98,28 +98,30 @@ template <int DT, int DP, bool TINY = false> struct FwdWave {
     }
 };
 
-// The wave's rows again, each over the keys that it sees and no others
-template <int DT> __device__ void again(const AttnArgs& a, const Pair& p, int head, int row0, int lane) {
+// The wave's rows again where values that they do not see, up to key `end`, are not finite.  lse2: of row0 + lane % 32, base 2
+template <int DT> __device__ void again(const AttnArgs& a, const Pair& p, int head, int row0, int end, float lse2, int lane) {
     const int dim = a.dim_bytes / AttnType<DT>::ES, kv_head = head / a.group;
-    for (int row = row0; row < min(row0 + 32, p.nq); ++row) {
+    int unseen = min(end, p.nk);
+    Spoilt spoilt;
+    spoilt.clear();
+    for (int row = min(row0 + 32, p.nq) - 1; row >= row0; --row) {          // each row's unseen keys are those of the row behind it and one more
         LaneRow<DT> q, x, acc;
+        const int n = max(0, row + 1 + p.nk - p.nq);
+        while (unseen > n) {
+            x.load(row_of_head(a.v, p.k0 + --unseen, kv_head), dim, lane);
+            spoilt.by(x, 0, dim, lane);
+        }
+        if (!spoilt.any()) continue;
         q.load(row_of_head(a.q, p.q0 + row, head), dim, lane, a.negative ? -a.c : a.c);
-        float m = -INFINITY, sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < kMostDim / 64; ++e) acc.x[e] = 0.f;
-        const int n = min(p.nk, row + 1 + p.nk - p.nq);
-        for (int j = 0; j < n; ++j) {
+        const float of_row = __shfl(lse2, row - row0, 64);
+        acc.clear();
+        for (int j = n - 1; j >= 0 && !spoilt.settled(acc); --j) {
             x.load(row_of_head(a.k, p.k0 + j, kv_head), dim, lane);
-            const float s = q.dot(x), top = fmaxf(m, s), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top), w = __builtin_amdgcn_exp2f(s - (top == -INFINITY ? 0.f : top));
-            m = top;
-            sum = fmaf(sum, f, w);
-#pragma unroll
-            for (int e = 0; e < kMostDim / 64; ++e) acc.x[e] *= f;
+            const float w = __builtin_amdgcn_exp2f(q.dot(x) - of_row);
             x.load(row_of_head(a.v, p.k0 + j, kv_head), dim, lane);
             acc.add(w, x);
         }
-        acc.store(row_of_head(a.out, p.q0 + row, head), dim, lane, sum == 0.f ? 0.f : 1.f / sum);
-        if (a.lse && lane == 0) a.lse[head * a.rows_q + p.q0 + row] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+        spoilt.store(acc, row_of_head(a.out, p.q0 + row, head), lane, 1.f);
     }
 }
 
@@ -183,7 +185,7 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
     }
     w.sum += other_half(w.sum);
     w.store(a, row, p.nq, p.q0, head);
-    if (odd) again<DT>(args_here(), p, head, row0, lane_here());
+    if (odd) again<DT>(args_here(), p, head, row0, (seen_wave + KT - 1) / KT * KT, w.m * w.c + __builtin_amdgcn_logf(w.sum), lane_here());
 #endif
 }
 
@@ -273,7 +275,7 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves(DP * AttnType<DT>::ES)) v
     odd = __syncthreads_or(odd);
     if (turn == 0) {
         w.store(a, row, p.nq, p.q0, head);
-        if (odd) again<DT>(args_here(), p, head, row0, lane_here());
+        if (odd) again<DT>(args_here(), p, head, row0, (seen_wave + 31) / 32 * 32, w.m * w.c + __builtin_amdgcn_logf(w.sum), lane_here());
     }
 #endif
 }
@@ -281,7 +283,9 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves(DP * AttnType<DT>::ES)) v
 template <int DT, int DP> static void launch_fwd(const AttnArgs& a, hipStream_t st) {
     const unsigned blocks = work_blocks(a, a.heads);
     // one block of 32 and eight waves, where those have registers enough, or four; or two that share tiles, and four waves for each
+    static_assert(FwdShape<DT, DP>::kLds <= 160 * 1024, "a compute unit has 160 KiB");
     constexpr int RB = DP * AttnType<DT>::ES, RG = share_tiles(DT, RB, false) ? 2 : 1, KS = RB > 512 ? 2 : 4, KS1 = RB > 128 ? KS : 8;
+    static_assert(FewShape<DT, DP, 1, KS1>::kLds + 1024 <= 160 * 1024 && FewShape<DT, DP, RG, KS>::kLds + 1024 <= 160 * 1024, "a compute unit has 160 KiB");
     if (a.few == 1) k_attention_few<DT, DP, 1, KS1><<<blocks, 64 * KS1, FewShape<DT, DP, 1, KS1>::kLds, st>>>(a);
     else if (a.few) k_attention_few<DT, DP, RG, KS><<<blocks, 64 * RG * KS, FewShape<DT, DP, RG, KS>::kLds, st>>>(a);
     else if (a.tile_rows == 64) k_attention<DT, DP, 2><<<blocks, 128, FwdShape<DT, DP>::kLds, st>>>(a);
@@ -449,7 +453,8 @@ static fx_status fill_args(const char* who, const fx_attention* d, AttnArgs* a, 
     a->order = k->longest <= 2048 ? kHeadsFirst : d->heads % 8 ? kTilesFirst : kHeadsApart;
     a->chunk = a->order == kHeadsFirst ? std::max(1, std::min(8, a->n_tiles / 64)) : 1;
     a->fold = 0;
-    if (tiles * heads * (d->dim > 128 ? kMostParts : 1) > (1ll << 32) / 256 - 8) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }
+    if (std::max(q->longest, k->longest) > 0x7FFFFFFFll - 1024) { set_error("%s: a sequence of more than 2^31-1025 rows", who); return FX_ERANGE; }
+    if ((tiles + tiles / 8 + 8) * heads * (d->dim > 128 ? kMostParts : 1) > (1ll << 32) / 256 - 8) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }
     return FX_OK;
 }
 

@@ -127,26 +127,31 @@ template <int DT, int DP, bool TINY = false> struct GqWave {
     }
 };
 
-// The wave's rows again, each over the keys that it sees and no others
-template <int DT> __device__ void gq_again(const AttnArgs& a, const Pair& p, int head, int row0, int lane) {
+// `count` elements from `from` on of the wave's rows again where keys that they do not see, up to `end`, are not finite.  off: the sum over
+// P dP less glse, of row0 + lane % 32
+template <int DT> __device__ void gq_again(const AttnArgs& a, const Pair& p, int head, int row0, int end, int from, int count, float off, int lane) {
     const int dim = a.dim_bytes / AttnType<DT>::ES, kv_head = head / a.group;
-    for (int row = row0; row < min(row0 + 32, p.nq); ++row) {
+    int unseen = min(end, p.nk);
+    Spoilt spoilt;
+    spoilt.clear();
+    for (int row = min(row0 + 32, p.nq) - 1; row >= row0; --row) {          // each row's unseen keys are those of the row behind it and one more
         LaneRow<DT> q, go, x, y, acc;
-        go.load(row_of_head(a.gout, p.q0 + row, head), dim, lane);
-        x.load(row_of_head(a.out, p.q0 + row, head), dim, lane);
-        const int64_t at = head * a.rows_q + p.q0 + row;
-        const float delta = (p.nk == 1 ? 0.f : go.dot(x)) - (a.glse ? a.glse[at] : 0.f), lse2 = a.lse[at] * kLog2e;
+        const int n = max(0, row + 1 + p.nk - p.nq);
+        while (unseen > n) {
+            x.load(row_of_head(a.k, p.k0 + --unseen, kv_head), dim, lane);
+            spoilt.by(x, from, min(from + count, dim), lane);
+        }
+        if (!spoilt.any()) continue;
+        const float lse2 = a.lse[head * a.rows_q + p.q0 + row] * kLog2e, of_row = __shfl(off, row - row0, 64);
         q.load(row_of_head(a.q, p.q0 + row, head), dim, lane, a.negative ? -a.c : a.c);
-#pragma unroll
-        for (int e = 0; e < kMostDim / 64; ++e) acc.x[e] = 0.f;
-        const int n = min(p.nk, row + 1 + p.nk - p.nq);
-        for (int j = 0; j < n; ++j) {
+        go.load(row_of_head(a.gout, p.q0 + row, head), dim, lane);
+        acc.clear();
+        for (int j = n - 1; j >= 0 && !spoilt.settled(acc); --j) {
             x.load(row_of_head(a.k, p.k0 + j, kv_head), dim, lane);
             y.load(row_of_head(a.v, p.k0 + j, kv_head), dim, lane);
-            acc.add(__builtin_amdgcn_exp2f(q.dot(x) - lse2) * ((p.nk == 1 ? 0.f : go.dot(y)) - delta), x);
+            acc.add(__builtin_amdgcn_exp2f(q.dot(x) - lse2) * ((p.nk == 1 ? 0.f : go.dot(y)) - of_row), x);
         }
-        if (lane == 0) *(f32x2*)(a.stats + 2 * at) = f32x2{lse2, delta};
-        if (a.gq.p) acc.store(row_of_head(a.gq, p.q0 + row, head), dim, lane, a.negative ? -a.scale : a.scale);
+        spoilt.store(acc, row_of_head(a.gq, p.q0 + row, head), lane, a.negative ? -a.scale : a.scale);
     }
 }
 
@@ -196,7 +201,7 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
         else w.template blocks<1>(kt, vt, key0, masked, last);
     }
     w.store(a, p, head, row);
-    if (odd && w.part == 0) gq_again<DT>(args_here(), p, head, row0, lane_here());
+    if (odd && a.gq.p) gq_again<DT>(args_here(), p, head, row0, (seen_wave + KT - 1) / KT * KT, w.part * S::COLS * 32, S::COLS * 32, w.delta - w.glse, lane_here());
 #endif
 }
 
@@ -270,7 +275,7 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves(DP * AttnType<DT>::ES)) v
     odd = __syncthreads_or(odd);
     if (turn == 0) {
         w.store(a, p, head, row);
-        if (odd && w.part == 0) gq_again<DT>(args_here(), p, head, row0, lane_here());
+        if (odd && a.gq.p) gq_again<DT>(args_here(), p, head, row0, (seen_wave + 31) / 32 * 32, w.part * S::COLS * 32, S::COLS * 32, w.delta - w.glse, lane_here());
     }
 #endif
 }
@@ -360,17 +365,31 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
     }
 };
 
-// The wave's keys again, each over the queries that see it and no others
-template <int DT> __device__ void gkv_again(const AttnArgs& a, const Pair& p, int kv_head, int key0, int lane) {
-    const int dim = a.dim_bytes / AttnType<DT>::ES;
-    for (int key = key0; key < min(key0 + 32, p.nk); ++key) {
+// `count` elements from `from` on of the wave's keys again where queries or output gradients, from row `begin` on, that do not see
+// them are not finite
+template <int DT> __device__ void gkv_again(const AttnArgs& a, const Pair& p, int kv_head, int key0, int begin, int from, int count, int lane) {
+    const int dim = a.dim_bytes / AttnType<DT>::ES, shift = p.nk - p.nq, first_head = kv_head * a.group;
+    int unseen = begin;
+    Spoilt spoilt_k, spoilt_v;
+    spoilt_k.clear();
+    spoilt_v.clear();
+    for (int key = key0; key < min(key0 + 32, p.nk); ++key) {               // each key's unseen queries are those of the key before it and one more
         LaneRow<DT> k, v, x, y, gk, gv;
+        const int first = max(0, key - shift);           // the first query that sees the key
+        for (; unseen < min(first, p.nq); ++unseen)
+            for (int head = first_head; head < first_head + a.group; ++head) {
+                x.load(row_of_head(a.q, p.q0 + unseen, head), dim, lane);
+                y.load(row_of_head(a.gout, p.q0 + unseen, head), dim, lane);
+                spoilt_k.by(x, from, min(from + count, dim), lane);
+                spoilt_v.by(y, from, min(from + count, dim), lane);
+            }
+        if (!spoilt_k.any() && !spoilt_v.any()) continue;
         k.load(row_of_head(a.k, p.k0 + key, kv_head), dim, lane, a.negative ? -a.c : a.c);
         v.load(row_of_head(a.v, p.k0 + key, kv_head), dim, lane);
-#pragma unroll
-        for (int e = 0; e < kMostDim / 64; ++e) gk.x[e] = gv.x[e] = 0.f;
-        for (int head = kv_head * a.group; head < (kv_head + 1) * a.group; ++head)
-            for (int row = max(0, key - (p.nk - p.nq)); row < p.nq; ++row) {
+        gk.clear();
+        gv.clear();
+        for (int head = first_head; head < first_head + a.group; ++head)
+            for (int row = first; row < p.nq && !(spoilt_k.settled(gk) && spoilt_v.settled(gv)); ++row) {
                 x.load(row_of_head(a.q, p.q0 + row, head), dim, lane);
                 y.load(row_of_head(a.gout, p.q0 + row, head), dim, lane);
                 const f32x2 stat = *(const f32x2*)(a.stats + 2 * (head * a.rows_q + p.q0 + row));
@@ -378,8 +397,8 @@ template <int DT> __device__ void gkv_again(const AttnArgs& a, const Pair& p, in
                 gv.add(w, y);
                 gk.add(w * ((p.nk == 1 ? 0.f : v.dot(y)) - stat[1]), x);
             }
-        if (a.gk.p) gk.store(row_of_head(a.gk, p.k0 + key, kv_head), dim, lane, a.negative ? -a.scale : a.scale);
-        if (a.gv.p) gv.store(row_of_head(a.gv, p.k0 + key, kv_head), dim, lane, 1.f);
+        if (a.gk.p) spoilt_k.store(gk, row_of_head(a.gk, p.k0 + key, kv_head), lane, a.negative ? -a.scale : a.scale);
+        if (a.gv.p) spoilt_v.store(gv, row_of_head(a.gv, p.k0 + key, kv_head), lane, 1.f);
     }
 }
 
@@ -450,7 +469,7 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
         }
     }
     w.store(a, p, kv_head, key);
-    if (odd && w.part == 0) gkv_again<DT>(args_here(), p, kv_head, key0, lane_here());
+    if (odd) gkv_again<DT>(args_here(), p, kv_head, key0, max(0, key0 - shift) / 32 * 32, w.part * S::COLS * 32, S::COLS * 32, lane_here());
 #endif
 }
 
@@ -514,7 +533,7 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves_of(DP * AttnType<DT>::ES,
     odd = __syncthreads_or(odd);
     if (turn == 0) {
         w.store(a, p, kv_head, key);
-        if (odd && w.part == 0) gkv_again<DT>(args_here(), p, kv_head, key0, lane_here());
+        if (odd) gkv_again<DT>(args_here(), p, kv_head, key0, max(0, key0 - shift) / 32 * 32, w.part * S::COLS * 32, S::COLS * 32, lane_here());
     }
 #endif
 }

@@ -465,7 +465,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_attention_join(StepArgs a) {
     __shared__ f32x4 sums[kJoinThreads];
     const int64_t item = blockIdx.x, b = item / a.heads;
     const int head = (int)(item % a.heads), tid = threadIdx.x;
-    const int len = (int)max((int64_t)0, min((int64_t)a.c.start[b], a.most)), chunk = chunk_of(a, len), n = (len + chunk - 1) / chunk;
+    const int len = (int)max((int64_t)0, min((int64_t)a.c.start[b], a.most)), chunk = chunk_of(a, len), n = len ? (len - 1) / chunk + 1 : 0;
     const float* stats = a.stats + 2 * item * a.splits;
     float top = -INFINITY;
     for (int i = tid; i < n; i += kJoinThreads) top = fmaxf(top, stats[2 * i]);
@@ -637,7 +637,7 @@ extern "C" fx_status fx_attention_step(const fx_cache* c, int64_t rows, const in
     if (rows > 0 && d_q == d_out) { set_error("%s: d_out is where d_q is", who); return FX_EINVAL; }
     if (rows > 0x7FFFFFFFll / 64 / heads) { set_error("%s: too many rows", who); return FX_ERANGE; }
     const int64_t all = (int64_t)a.t.cols * a.t.page_rows;
-    if (all > 0x7FFFFFFFll) { set_error("%s: a table of more than 2^31-1 positions", who); return FX_ERANGE; }
+    if (all > 0x7FFFFFFFll - 8192) { set_error("%s: a table of more than 2^31-8193 positions", who); return FX_ERANGE; }
     if (rows == 0) return FX_OK;
     a.start = d_len;
     StepArgs s{};

@@ -158,3 +158,64 @@ def test_sequences_by_size():
     run(lens, 3, 1, 32, "bf16", True, kv_lens=[900, 40, 7, 0, 300, 700, 1, 2, 0, 2000])
     run(lens, 8, 8, 32, "f16", True)
     run(lens, 8, 4, 64, "bf16", False)
+
+
+@pytest.mark.parametrize("dtype,d", [("f16", 200), ("f32", 140), ("bf16", 33)])
+def test_wide_rows_do_not_see_what_comes_later(dtype, d):
+    """One value of the last row of a causal sequence not finite, in each input: the rows and keys that do not see it against the formulas."""
+    n, heads, kvh = 75, 2, 1
+    seqs = fx.build_sequences([[0, n]])
+    make = lambda: [draw(s, n, h, d, dtype)[0] for s, h in ((1, heads), (2, kvh), (3, kvh), (4, heads))]
+    t = make()
+    f = [_f64(x) for x in t]
+    out, lse = fx.attention_fwd(seqs, *t[:3], causal=True)
+    ro, _, bo, _ = A.attention(*f[:3], [0, n], [0, n], True, d ** -0.5, dtype)
+    rg = A.attention_grad(*f, [0, n], [0, n], True, d ** -0.5, dtype)
+    for which in range(4):
+        for c in (0, d - 1):
+            u = make()
+            u[which][n - 1, 0, c] = float("nan")
+            o, _ = fx.attention_fwd(seqs, *u[:3], causal=True)
+            A.check(_f64(o)[:-1], ro[:-1], bo[:-1], dtype, f"out, {which}")
+            g = fx.attention_bwd(seqs, *u[:3], out, lse, u[3], causal=True)
+            if which in (1, 2):
+                A.check(_f64(g[0])[:-1], rg[0][:-1], rg[3][:-1], dtype, f"gq, {which}")
+            else:               # a row in the middle of a block: keys behind it do not see it
+                u = make()
+                u[which][40, 0, c] = float("inf")
+                g = fx.attention_bwd(seqs, *u[:3], out, lse, u[3], causal=True)
+                for i in (1, 2):
+                    A.check(_f64(g[i])[41:], rg[i][41:], rg[3 + i][41:], dtype, f"gradient {i}, {which}")
+
+
+def test_nothing_finite():
+    """A causal pass over NaN alone ends in about the time of any other, and is NaN; so is one with a channel of NaN, in that channel."""
+    n, heads, d = 16_384, 8, 64
+    seqs = fx.build_sequences([[0, n]])
+    x = torch.full((n, heads, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    out, lse = fx.attention_fwd(seqs, x, x, x, causal=True)
+    g = fx.attention_bwd(seqs, x, x, x, out, lse, x, causal=True)
+    assert all(torch.isnan(t).all() for t in (out, lse, *g))
+    q, k, v, go = (draw(s, n, heads, d, "bf16")[0] for s in range(4))
+    ref, _ = fx.attention_fwd(seqs, q, k, v, causal=True)
+    v[:, :, 5] = float("nan")
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    start.record()
+    out, lse = fx.attention_fwd(seqs, q, k, v, causal=True)
+    end.record()
+    torch.cuda.synchronize()
+    assert start.elapsed_time(end) < 500
+    clean = [c for c in range(d) if c != 5]
+    assert torch.isnan(out[:, :, 5]).all() and torch.equal(out[:, :, clean], ref[:, :, clean])
+    go[:, :, 7] = float("inf")
+    g = fx.attention_bwd(seqs, q, k, v, out, lse, go, causal=True)
+    assert not torch.isfinite(g[2][:, :, 7]).any() and torch.isfinite(g[2][:, :, clean[:5]]).all()
+
+
+def test_no_queries():
+    kv = fx.build_sequences([[0, 5], [5, 5]])
+    none = fx.build_sequences([[0, 0], [0, 0]])
+    q, k = torch.zeros((0, 4, 32), device="cuda"), torch.randn((5, 2, 32), device="cuda")
+    out, lse = fx.attention_fwd(none, q, k, k, kv_seqs=kv)
+    g = fx.attention_bwd(none, q, k, k, out, lse, q, kv_seqs=kv)
+    assert out.shape == (0, 4, 32) and lse.shape == (4, 0) and g[0].shape == q.shape and not g[1].any() and not g[2].any()
