@@ -5,6 +5,7 @@ one residual stream, from this library's operators with their gradients.
     x, n   = join(x, conv3(norm(x)), gate = conv1(norm(x)))           a convolution's reach: 3 x 3 x 3 voxels
     u | z  = conv1(n)
     x, n   = join(x, scan(u, z) + scan(u, z, reversed))               along all voxels of a scene, in index order
+    x, n   = join(x, conv1(attention(conv1(n))))                      inside windows of 512 voxels; with heads, left out without
     result = n . head
 
 ``python examples/voxel_mixer.py`` prints the loss of a few steps on indoor-like scenes (the target: how full a voxel's
@@ -83,6 +84,26 @@ class Scan(torch.autograd.Function):
         return torch.cat([gu, gz], 1), None, None
 
 
+class Attention(torch.autograd.Function):
+    """Takes queries, keys and values as they come out of one projection [N, (heads + 2 kv_heads) dim]."""
+
+    @staticmethod
+    def forward(ctx, packed, seqs, heads, kv_heads, causal):
+        q, k, v = packed.view(packed.shape[0], heads + 2 * kv_heads, -1).split([heads, kv_heads, kv_heads], 1)
+        out, lse = fx.attention_fwd(seqs, q, k, v, causal=causal)
+        ctx.args = seqs, heads, kv_heads, causal
+        ctx.save_for_backward(packed, out, lse)
+        return out.flatten(1)
+
+    @staticmethod
+    def backward(ctx, g):
+        packed, out, lse = ctx.saved_tensors
+        seqs, heads, kv_heads, causal = ctx.args
+        q, k, v = packed.view(packed.shape[0], heads + 2 * kv_heads, -1).split([heads, kv_heads, kv_heads], 1)
+        grads = fx.attention_bwd(seqs, q, k, v, out, lse, g.reshape(out.shape), causal=causal)
+        return torch.cat(grads, 1).flatten(1), None, None, None, None
+
+
 class Join(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, y, gate, post, scale, nxt, p, seed, offset):
@@ -100,7 +121,7 @@ class Join(torch.autograd.Function):
 
 # ------------------------------------------------------------------------------------------ the network
 class VoxelMixer(torch.nn.Module):
-    def __init__(self, c_in=8, c=64, p=0.1, seed=1):
+    def __init__(self, c_in=8, c=64, p=0.1, seed=1, heads=0, kv_heads=0):
         super().__init__()
         gen = torch.Generator().manual_seed(seed)
         def weight(*shape):
@@ -113,12 +134,15 @@ class VoxelMixer(torch.nn.Module):
         self.post2, self.scale2, self.w3 = ones(), ones(0.5), ones()
         # the first of the gate's channels forget within a few rows, the last remember for some thousand
         self.memory = torch.nn.Parameter(torch.linspace(-1.0, 7.0, c, device="cuda"))
-        self.p, self.seed = p, seed
+        self.p, self.seed, self.heads, self.kv_heads = p, seed, heads, kv_heads or heads
+        if heads:
+            self.attend = weight(1, c, (heads + 2 * self.kv_heads) * (c // heads))
+            self.mix, self.post3, self.scale3, self.w4 = weight(1, c, c), ones(), ones(0.5), ones()
 
     def forward(self, feat, grid_maps, step=0):
-        k3, k1, seqs = grid_maps
+        k3, k1, seqs, near = grid_maps
         p = self.p if self.training else 0.0
-        mask = lambda i: (p, self.seed, 4 * step + i)           # every call's mask has an offset of its own
+        mask = lambda i: (p, self.seed, 4 * step + i)           # every call's mask has an offset of its own (four a step)
         x = Dropout.apply(Conv.apply(feat, self.stem, k3), *mask(0))
         n = Norm.apply(x, self.w1)
         x, n = Join.apply(x, Conv.apply(n, self.conv, k3), Conv.apply(n, self.gate, k1), self.post1, self.scale1, self.w2, *mask(1))
@@ -126,7 +150,18 @@ class VoxelMixer(torch.nn.Module):
         both = torch.cat([both[:, :both.shape[1] // 2], both[:, both.shape[1] // 2:] + self.memory.to(both.dtype)], 1)
         y = Scan.apply(both, seqs, False) + Scan.apply(both, seqs, True)
         x, n = Join.apply(x, y, None, self.post2, self.scale2, self.w3, *mask(2))
+        if self.heads:
+            y = Attention.apply(Conv.apply(n, self.attend, k1), near, self.heads, self.kv_heads, False)
+            x, n = Join.apply(x, Conv.apply(y, self.mix, k1), None, self.post3, self.scale3, self.w4, *mask(3))
         return Conv.apply(n, self.head, k1)
+
+
+def windows(joffsets, size=512):
+    """Ranges of up to `size` rows of every range, in order."""
+    parts = [np.arange(a, b, size) for a, b in joffsets]
+    first = np.concatenate(parts) if parts else np.zeros(0, np.int64)
+    end = np.concatenate([np.minimum(p + size, b) for p, (_, b) in zip(parts, joffsets)]) if parts else first
+    return np.stack([first, end], 1)
 
 
 def scenes(name="indoor_small", dtype=torch.bfloat16):
@@ -134,7 +169,8 @@ def scenes(name="indoor_small", dtype=torch.bfloat16):
     w = G.workload(name)
     ijk, jo = w.jagged_ijk()
     grid = fx.build_index_grid(torch.from_numpy(ijk).cuda(), jo)
-    maps = (fx.build_kernel_map(grid, 3, 1), fx.build_kernel_map(grid, 1, 1), fx.build_sequences(grid.voxel_joffsets()))
+    maps = (fx.build_kernel_map(grid, 3, 1), fx.build_kernel_map(grid, 1, 1), fx.build_sequences(grid.voxel_joffsets()),
+            fx.build_sequences(windows(grid.voxel_joffsets())))
     n = grid.num_voxels
     full = (maps[0].dense() >= 0).sum(1, keepdim=True).float() / 27
     along = torch.cat([torch.linspace(-1, 1, int(b - a)) for a, b in grid.voxel_joffsets()])[:, None].cuda()
@@ -143,9 +179,9 @@ def scenes(name="indoor_small", dtype=torch.bfloat16):
     return feat, maps, torch.cat([full, along], 1)
 
 
-def train(steps=40, lr=3e-3, name="indoor_small", dtype=torch.bfloat16, report=None):
+def train(steps=40, lr=3e-3, name="indoor_small", dtype=torch.bfloat16, report=None, heads=0, kv_heads=0):
     feat, maps, target = scenes(name, dtype)
-    net = VoxelMixer(feat.shape[1])
+    net = VoxelMixer(feat.shape[1], heads=heads, kv_heads=kv_heads)
     opt = torch.optim.Adam(net.parameters(), lr=lr)
     losses = []
     for step in range(steps):
@@ -177,8 +213,34 @@ def stream(rows=1_000, c=64, chunk=300):
     return torch.cat(parts), whole
 
 
+def grow(rows=700, prompt=600, heads=8, kv_heads=2, d=64, page=16, dtype=torch.bfloat16, store=None, seqs=3):
+    """Scenes that grow row by row: attention inside what is there, its keys and values into a paged cache (of `store`, 8 bits
+    say), then one new row of each scene at a time.  Returns the rows and what one causal call over all of them gives."""
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    q, k, v = (torch.randn((seqs, rows, h, d), generator=gen, device="cuda").to(dtype) for h in (heads, kv_heads, kv_heads))
+    ranges = lambda n: [[s * n, (s + 1) * n] for s in range(seqs)]
+    whole, _ = fx.attention_fwd(fx.build_sequences(ranges(rows)), q.flatten(0, 1), k.flatten(0, 1), v.flatten(0, 1), causal=True)
+    columns = -(-rows // page)
+    cache = fx.KVCache.empty(seqs * columns, page, kv_heads, d, store or dtype)
+    table = torch.randperm(seqs * columns, generator=gen, device="cuda").to(torch.int32).view(seqs, columns)
+    lengths = torch.zeros(seqs, dtype=torch.int32, device="cuda")
+    first = fx.build_sequences(ranges(prompt))
+    out, _ = fx.attention_fwd(first, q[:, :prompt].flatten(0, 1), k[:, :prompt].flatten(0, 1), v[:, :prompt].flatten(0, 1), causal=True)
+    fx.cache_write(cache, table, lengths, k[:, :prompt].flatten(0, 1), v[:, :prompt].flatten(0, 1), seqs=first)
+    lengths += prompt
+    parts = [out.view(seqs, prompt, heads, d)]
+    for r in range(prompt, rows):
+        fx.cache_write(cache, table, lengths, k[:, r], v[:, r])
+        lengths += 1
+        parts.append(fx.attention_step(cache, table, lengths, q[:, r])[0][:, None])
+    return torch.cat(parts, 1), whole.view(seqs, rows, heads, d)
+
+
 if __name__ == "__main__":
     _, losses = train(report=print)
     print(f"loss {losses[0]:.4f} -> {np.mean(losses[-5:]):.4f}")
     got, whole = stream()
     print(f"streamed rows against one call: {float((got - whole).abs().max()):.1e}")
+    for store in (None, torch.float8_e4m3fn):
+        got, whole = grow(store=store)
+        print(f"rows over a cache of {store or 'their own type'} against one causal call: {float((got - whole).abs().max()):.1e}")
