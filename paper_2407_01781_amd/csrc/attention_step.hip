@@ -508,7 +508,10 @@ template <int DT, bool E4M3, int DP> static void launch_step(const StepArgs& a, 
     typedef StepShape<DT, E4M3, DP> S;
     constexpr int MANY = S::kMany;
     static_assert((MANY - MANY / 4) * SLOT <= 160 * 1024, "a compute unit has 160 KiB");
-    if (MANY == 4 || a.splits > 1) k_attention_step<DT, E4M3, DP, 4, S::kResident><<<(unsigned)blocks, 256, 3 * SLOT, st>>>(a);
+    // One workgroup with many waves for each sequence only where every one of them has a compute unit to itself; more are better served by
+    // four waves each, several workgroups on a unit (64 dimensions bf16, up to 300 positions, 1024 x 8 key heads: 218 -> 93 us, 256 x 4:
+    // 29 -> 15; 64 x 4 of up to 1000 positions the other way: 14.2 with sixteen waves, 17.2 with four).
+    if (MANY == 4 || a.splits > 1 || blocks > compute_units()) k_attention_step<DT, E4M3, DP, 4, S::kResident><<<(unsigned)blocks, 256, 3 * SLOT, st>>>(a);
     else k_attention_step<DT, E4M3, DP, MANY, 1><<<(unsigned)blocks, 64 * MANY, (MANY - MANY / 4) * SLOT, st>>>(a);
 }
 
@@ -635,7 +638,7 @@ extern "C" fx_status fx_attention_step(const fx_cache* c, int64_t rows, const in
     for (const HeadsTensor& x : t) FX_TRY(check_heads(who, x, c->dim, dtype_size(dt)));
     if (rows > 0 && (!d_len || (uintptr_t)d_len % 4 || (uintptr_t)d_lse % 4)) { set_error("%s: d_len is null, or it or d_lse is not aligned to its elements", who); return FX_EINVAL; }
     if (rows > 0 && d_q == d_out) { set_error("%s: d_out is where d_q is", who); return FX_EINVAL; }
-    if (rows > 0x7FFFFFFFll / 64 / heads) { set_error("%s: too many rows", who); return FX_ERANGE; }
+    if (rows > 0x7FFFFFFFll) { set_error("%s: more than 2^31-1 rows", who); return FX_ERANGE; }
     const int64_t all = (int64_t)a.t.cols * a.t.page_rows;
     if (all > 0x7FFFFFFFll - 8192) { set_error("%s: a table of more than 2^31-8193 positions", who); return FX_ERANGE; }
     if (rows == 0) return FX_OK;
@@ -654,15 +657,15 @@ extern "C" fx_status fx_attention_step(const fx_cache* c, int64_t rows, const in
     s.group = heads / c->kv_heads;
     s.groups = (s.group + kStepHeads - 1) / kStepHeads;
     s.scale2 = scale * kLog2e;
-    // Up to 1024 positions a workgroup of 8 or 16 waves takes them all and there is no second launch; beyond, every sequence is
+    // Up to 1024 positions one workgroup takes them all and there is no second launch; beyond, every sequence is
     // split into as many parts, such that there are about eight workgroups for a compute unit -- of one sequence, as many as a
     // unit holds at a time -- where that leaves the longest 256 positions at least.  (Parts of equal length, more of them in longer sequences: 327 us for 64 sequences of up to 32,768
     // positions, 8 bits x 128, as most of two rounds of workgroups are there and the second is half empty; 32 of them for a unit 402.)
     const int64_t items = rows * c->kv_heads * s.groups;
+    if (items >= (1ll << 32) / 256) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }       // threads of a launch are counted in 32 bits
     s.splits = 1;
     if (s.most > 1024)
         s.splits = (int32_t)std::max<int64_t>(1, std::min({(s.most + kLeastChunk - 1) / kLeastChunk, (int64_t)kMostSplits, (rows == 1 ? step_resident(dt, c->store == FX_E4M3, a.dim <= 64 ? 64 : a.dim <= 128 ? 128 : 256) : 8) * compute_units() / items}));
-    if (items * s.splits > 0x7FFFFFFFll / 64) { set_error("%s: too many rows", who); return FX_ERANGE; }
     void* part = nullptr;
     if (s.splits > 1) {
         FX_TRY(scratch_alloc(who, &part, ((size_t)rows * heads * s.splits) * (a.pitch + 2) * 4, st));

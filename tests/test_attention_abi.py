@@ -118,6 +118,12 @@ def test_rows_of_the_cache():
     _refused(-5, *_step(_cache(table_cols=1 << 28, ld_table=1 << 28)))
 
 
+def test_threads_of_a_step_are_counted_in_32_bits():
+    """2^24 workgroups of 256 threads would wrap to none; 34 heads that share a key head are three workgroups."""
+    for rows, heads in ((1 << 24, 4), (1 << 23, 4), (1 << 22, 68)):
+        _refused(-5, *_step(_cache(), rows=rows, heads=heads, ld=heads * 64))
+
+
 @pytest.mark.parametrize("struct,offsets", [(B._Attention, {"dt": 16, "heads": 20, "causal": 32, "scale": 36, "d_q": 40, "ld_q": 64, "hs_v": 104}),
                                             (B._Cache, {"d_k_exp": 16, "d_table": 32, "ld_table": 40, "table_cols": 48, "store": 60, "dim": 68})])
 def test_descriptions_lie_as_the_header_says(struct, offsets):

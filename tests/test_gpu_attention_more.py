@@ -219,3 +219,22 @@ def test_no_queries():
     out, lse = fx.attention_fwd(none, q, k, k, kv_seqs=kv)
     g = fx.attention_bwd(none, q, k, k, out, lse, q, kv_seqs=kv)
     assert out.shape == (0, 4, 32) and lse.shape == (4, 0) and g[0].shape == q.shape and not g[1].any() and not g[2].any()
+
+
+@pytest.mark.parametrize("n,heads,kv_heads,dim,dtype,store", [(300, 3, 1, 64, "bf16", "bf16"), (70, 8, 4, 40, "f32", "f32"), (260, 4, 2, 128, "f16", "e4m3")])
+def test_step_of_more_sequences_than_compute_units(n, heads, kv_heads, dim, dtype, store):
+    """One workgroup of four waves for each, several on a unit."""
+    rng = np.random.default_rng(n)
+    lens = rng.integers(0, 200, size=n).tolist()
+    lens[0], lens[-1] = 0, 1
+    bounds, jo = _joff(lens)
+    table, pages = _tables(rng, lens, 16)
+    cache = fx.KVCache.empty(pages, 16, kv_heads, dim, torch.float8_e4m3fn if store == "e4m3" else {"bf16": torch.bfloat16, "f32": torch.float32}[store])
+    k, k64 = draw(1, bounds[-1], kv_heads, dim, dtype)
+    v, v64 = draw(2, bounds[-1], kv_heads, dim, dtype)
+    q, q64 = draw(3, n, heads, dim, dtype, std=2.0)
+    fx.cache_write(cache, table, torch.zeros(n, dtype=torch.int32, device="cuda"), k, v, seqs=fx.build_sequences(jo))
+    out, lse = fx.attention_step(cache, table, torch.tensor(lens, dtype=torch.int32, device="cuda"), q)
+    ro, rl, bo, bl = A.attention(q64, _held(k64, store), _held(v64, store), np.arange(n + 1), bounds, False, dim ** -0.5, dtype)
+    A.check(_f64(out), ro, bo, dtype, "out")
+    A.check(_f64(lse), rl.T, bl.T, "f32", "lse")
