@@ -44,7 +44,11 @@ struct AttnArgs {
     const float* glse;
     int64_t rows_q;
     int32_t n_tiles, tile_rows, few, heads, kv_heads, group, dim_bytes;
-    int32_t causal, order, chunk, fold, negative;
+    int32_t causal, order, chunk, negative;
+    int32_t shares;                         // 2: two workgroups share a key's queries, and their sums are joined
+    float* sums;                            // [shares, kv_heads, rows_k, gk and gv, dim]
+    int32_t* odd;                           // [shares, kv_heads, parts, n_tiles, waves]: not finite what a wave's rows do not see
+    int64_t rows_k;
     float c;            // |scale| log2(e)
     float scale;        // |scale|
 };
@@ -334,14 +338,11 @@ __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 
 // takes `chunk` neighbouring tiles of each 8 chunk, all heads of a tile in a row where sequences are short (the heads' parts of
 // a row share lines, the tiles of a sequence its keys, in one L2), head after head where they are long (the L2 then has
 // one head's keys); or, with a multiple of eight heads, all tiles of its eighth of the heads.
-// fold: a launch whose workgroups are all resident at once is dealt out such that a compute unit's second is as light as its
-// first is heavy (gradients, 16,384 x 16 x 128 causal: 5.4 -> 5.25 ms, when their statistics still came through registers).
 enum Order { kTilesFirst = 0, kHeadsFirst = 1, kHeadsApart = 2 };
 struct Work { int tile, head; };            // head < 0: none
 __device__ __forceinline__ Work work_of(const AttnArgs& a, int heads) {
     const uint32_t xcd = blockIdx.x % 8, tiles = (uint32_t)a.n_tiles, chunk = (uint32_t)a.chunk, per_xcd = (tiles + 8 * chunk - 1) / (8 * chunk) * chunk;
-    uint32_t slot = blockIdx.x / 8;
-    if (a.fold) slot = 2 * slot < gridDim.x / 8 ? 2 * slot : 2 * (gridDim.x / 8 - 1 - slot) + 1;
+    const uint32_t slot = blockIdx.x / 8;
     Work w;
     if (a.order == kHeadsApart) {
         const uint32_t h = slot / tiles;
@@ -379,6 +380,8 @@ struct HeadsTensor {
 };
 fx_status check_heads(const char* who, const HeadsTensor& t, int32_t dim, int es);
 
+// workgroups that share the queries of a tile of keys
+int key_shares(const AttnArgs& a, int32_t n_tiles, int32_t few, int64_t queries, int dim, fx_dtype dt);
 // a: tiles of queries, b: those of keys
 void attention_bwd_launch(const AttnArgs& a, const AttnArgs& b, fx_dtype dt, int dim, bool keys, hipStream_t st);
 

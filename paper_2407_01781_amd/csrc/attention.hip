@@ -457,7 +457,8 @@ static fx_status fill_args(const char* who, const fx_attention* d, AttnArgs* a, 
     a->c = fmaxf(a->scale * kLog2e, 0x1p-149f);       // not 0: a masked score is -infinity and stays it
     a->order = k->longest <= 2048 ? kHeadsFirst : d->heads % 8 ? kTilesFirst : kHeadsApart;
     a->chunk = a->order == kHeadsFirst ? std::max(1, std::min(8, a->n_tiles / 64)) : 1;
-    a->fold = 0;
+    a->shares = 1;
+    a->sums = nullptr;
     if (std::max(q->longest, k->longest) > 0x7FFFFFFFll - 1024) { set_error("%s: a sequence of more than 2^31-1025 rows", who); return FX_ERANGE; }
     if ((tiles + tiles / 8 + 8) * heads * (d->dim > 128 ? kMostParts : 1) > (1ll << 32) / 256 - 8) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }
     return FX_OK;
@@ -537,6 +538,15 @@ extern "C" fx_status fx_attention_bwd(const fx_attention* d, const void* d_out, 
     a.lse = const_cast<float*>(d_lse);
     a.glse = d_glse;
     a.stats = (float*)stats;
+    a.rows_k = nk;
+    a.shares = key_shares(a, b.n_tiles, b.few, d->q_seqs->longest * (d->heads / d->kv_heads), dim, d->dt);
+    if (a.shares > 1) {
+        void* p = nullptr;
+        FX_TRY(scratch.get(who, &p, (size_t)a.shares * d->kv_heads * nk * 2 * dim * 4));
+        a.sums = (float*)p;
+        FX_TRY(scratch.get(who, &p, (size_t)a.shares * d->kv_heads * kMostParts * b.n_tiles * 4 * 4));
+        a.odd = (int32_t*)p;
+    }
     attention_bwd_launch(a, b, d->dt, dim, d_gk || d_gv, st);
     FX_TRY(back.run(who, d->dim, d->dim, dtype_size(d->dt), st));
     FX_HIP_TRY(hipGetLastError());

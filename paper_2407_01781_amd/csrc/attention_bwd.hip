@@ -5,8 +5,8 @@
 // the queries for a workgroup's keys (gk, gv).  Scores and dP are computed in both: seven products instead of five, for
 // results that do not depend on an order of atomics and need no fp32 copy of gq in memory.
 // P = exp(s - lse), dP = gout v^T, dS = P (dP - sum_j P dP + glse); gq = scale dS k, gk = scale dS^T q, gv = P^T gout.
-// 16,384 x 16 x 128 bf16 causal: 1.5 ms for gq (1.1 PFLOP/s) and 3.0 for gk and gv (0.72: LDS is read for as long as the matrix
-// instructions run, and workgroups of few queries leave their compute unit half empty); 131,072 x 4 x 64 f16 in windows of 1,024: 0.29 and 0.33 ms.
+// 16,384 x 16 x 128 bf16 causal: 1.5 ms for gq (1.1 PFLOP/s) and 2.0 for gk and gv with their join (1.1; LDS is read for as long as the matrix
+// instructions run); 131,072 x 4 x 64 f16 in windows of 1,024: 0.29 and 0.33 ms.
 #include "attention.h"
 
 #include <math.h>
@@ -310,7 +310,7 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
         for (int i = 0; i < S::COLS; ++i) gk[i] = gv[i] = f32x16(0.f);
     }
 
-    // 32 queries whose first that sees the lane's key is `first`, counted from the block's first (all do where not masked)
+    // 32 queries whose first that sees the block's first key is `first`, counted from the block's first (all do where not masked)
     __device__ __forceinline__ void block(const lds_byte* qt, const lds_byte* ot, const float* stats, bool masked, int first) {
         f32x16 p = f32x16(0.f), ds = f32x16(0.f);
 #pragma unroll
@@ -330,7 +330,8 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
             }
         }
         if (masked) {
-            first -= 4 * (lane_here() >> 5);
+            const int lane = lane_here();
+            first += (lane & 31) - 4 * (lane >> 5);
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 if (8 * (r >> 2) + (r & 3) < first) p[r] = ds[r] = 0.f;
@@ -352,18 +353,30 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
         }
     }
 
+    // the same of one share of the queries, in fp32
+    __device__ __forceinline__ void store_sums(const AttnArgs& a, const Pair& p, int kv_head, int key, int share) {
+        if (key >= p.nk) return;
+        const int dim_bytes = a.dim_bytes / AttnType<DT>::ES * 4;
+        unsigned char* to = (unsigned char*)a.sums + (((int64_t)share * a.kv_heads + kv_head) * a.rows_k + p.k0 + key) * 2 * dim_bytes;
+        const float f = a.negative ? -a.scale : a.scale;
+#pragma unroll
+        for (int i = 0; i < S::COLS; ++i) {
+            store_columns<FX_F32>(gk[i], f, to, part * S::COLS + i, dim_bytes, lane_here() >> 5);
+            store_columns<FX_F32>(gv[i], 1.f, to + dim_bytes, part * S::COLS + i, dim_bytes, lane_here() >> 5);
+        }
+    }
     __device__ __forceinline__ void store(const AttnArgs& a, const Pair& p, int kv_head, int key) {
         if (key >= p.nk) return;
         if (a.gk.p) {
             unsigned char* out = a.gk.p + (int64_t)(p.k0 + key) * a.gk.ld + kv_head * a.gk.hs;
             const float f = a.negative ? -a.scale : a.scale;
 #pragma unroll
-            for (int i = 0; i < S::COLS; ++i) store_columns<DT>(gk[i], f, out, part * S::COLS + i, a.dim_bytes, half);
+            for (int i = 0; i < S::COLS; ++i) store_columns<DT>(gk[i], f, out, part * S::COLS + i, a.dim_bytes, lane_here() >> 5);
         }
         if (a.gv.p) {
             unsigned char* out = a.gv.p + (int64_t)(p.k0 + key) * a.gv.ld + kv_head * a.gv.hs;
 #pragma unroll
-            for (int i = 0; i < S::COLS; ++i) store_columns<DT>(gv[i], 1.f, out, part * S::COLS + i, a.dim_bytes, half);
+            for (int i = 0; i < S::COLS; ++i) store_columns<DT>(gv[i], 1.f, out, part * S::COLS + i, a.dim_bytes, lane_here() >> 5);
         }
     }
 };
@@ -426,21 +439,24 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     lds_byte* lds = (lds_byte*)smem;
     lds_byte* stats = lds + 4 * S::kQueries;
-    const Work work = work_of(a, a.kv_heads * S::kParts);
+    const Work work = work_of(a, a.kv_heads * S::kParts * a.shares);
     if (work.head < 0) return;
-    const int kv_head = work.head / S::kParts;
+    const int share = work.head & (a.shares - 1), head_part = work.head >> (a.shares - 1), kv_head = head_part / S::kParts;
     const int wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63;
     const SeqTile st = a.tiles[work.tile];
     const Pair p = pair_of_keys(a, st);
     // the tile that most queries see is a causal sequence's first: it is begun first
     const int tile0 = a.causal ? (p.nk - 1) / (32 * W) * (32 * W) - st.row : st.row;
-    const int key0 = tile0 + wave * 32, key = key0 + (lane & 31), shift = p.nk - p.nq;
+    const int key0 = tile0 + wave * 32, shift = p.nk - p.nq;
     TileLoad<RB, QT, W> lq, lo;
     lq.init(wave, lane, a.q.ld, a.dim_bytes);
     lo.init(wave, lane, a.gout.ld, a.dim_bytes);
     // all heads of the group in turn; of each the tiles from the first on in which a query sees the workgroup's first key
     const int begin = a.causal ? max(0, tile0 - shift) / QT * QT : 0, n = begin < p.nq ? (p.nq - begin + QT - 1) / QT * a.group : 0;
-    int next_head = kv_head * a.group, next = begin;
+    const int j0 = share ? n / 2 : 0, j1 = share + 1 < a.shares ? n / 2 : n, per_head = max(1, n / a.group), items = j1 - j0;
+    const int before = uni(j0 / per_head);
+    int next_head = kv_head * a.group + before, next = begin + (j0 - before * per_head) * QT;
+    int r0 = next - QT;
     auto load = [&](int b) {
         lq.load(lds + b * S::kQueries, a.q.p + (int64_t)p.q0 * a.q.ld + next_head * a.q.hs, a.q.ld, next, p.nq, a.dim_bytes, wave);
         lo.load(lds + (2 + b) * S::kQueries, a.gout.p + (int64_t)p.q0 * a.gout.ld + next_head * a.gout.hs, a.gout.ld, next, p.nq, a.dim_bytes, wave);
@@ -448,18 +464,17 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
         next += QT;
         if (next >= p.nq) { next = begin; ++next_head; }
     };
-    if (n > 0) load(0);
+    if (items > 0) load(0);
     GkvWave<DT, DP, W == 2> w;
-    w.init(a, p, kv_head, work.head % S::kParts, key0, lane);
-    int r0 = begin - QT;
+    w.init(a, p, kv_head, head_part % S::kParts, key0, lane);
     bool odd = false;
-    for (int j = 0; j < n; ++j) {
+    for (int j = 0; j < items; ++j) {
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
         const int b = j & 1;
         r0 += QT;
         if (r0 >= p.nq) r0 = begin;
-        if (j + 1 < n) load(b ^ 1);
+        if (j + 1 < items) load(b ^ 1);
         const lds_byte *qt = lds + b * S::kQueries, *ot = lds + (2 + b) * S::kQueries;
         const float* st = (const float*)(smem + 4 * S::kQueries + b * S::kStats);
 #pragma unroll
@@ -468,11 +483,46 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
             if (key0 >= p.nk || r >= p.nq || (a.causal && r + 31 + shift < key0)) continue;
             const bool masked = a.causal && r + shift < key0 + 31;
             if (masked) odd |= block_not_finite<DT, RB>(qt, t) || block_not_finite<DT, RB>(ot, t);
-            w.block(qt + LdsRows<RB>::row_at(t), ot + LdsRows<RB>::row_at(t), st + 2 * t, masked, key - shift - r);
+            w.block(qt + LdsRows<RB>::row_at(t), ot + LdsRows<RB>::row_at(t), st + 2 * t, masked, key0 - shift - r);
         }
     }
-    w.store(a, p, kv_head, key);
+    if (a.shares > 1) {
+        w.store_sums(a, p, kv_head, key0 + (lane_here() & 31), share);
+        if (lane_here() == 0) a.odd[((int64_t)(share * a.kv_heads * S::kParts + head_part) * a.n_tiles + work.tile) * W + wave] = odd;
+        return;
+    }
+    w.store(a, p, kv_head, key0 + (lane_here() & 31));
     if (odd) gkv_again<DT>(args_here(), p, kv_head, key0, max(0, key0 - shift) / 32 * 32, w.part * S::COLS * 32, S::COLS * 32, lane_here());
+#endif
+}
+
+// The shares' sums of W blocks of 32 keys added, in their order; and what unseen rows have spoilt summed anew
+template <int DT, int PARTS, int W>
+__global__ __launch_bounds__(64 * W) void k_attention_join_keys(AttnArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef typename AttnType<DT>::T T;
+    const int tile = blockIdx.x % a.n_tiles, kv_head = blockIdx.x / a.n_tiles, wave = uni(threadIdx.x / 64), lane = threadIdx.x & 63;
+    const Pair p = pair_of_keys(a, a.tiles[tile]);
+    const int key0 = (a.causal ? (p.nk - 1) / (32 * W) * (32 * W) - a.tiles[tile].row : a.tiles[tile].row) + wave * 32, keys = min(32, p.nk - key0);
+    const int dim = a.dim_bytes / AttnType<DT>::ES, fours = dim / 4;
+    const int64_t share = a.rows_k * a.kv_heads * 2 * dim;
+    const float* sums = a.sums + ((int64_t)kv_head * a.rows_k + p.k0 + key0) * 2 * dim;
+    for (int i = lane; i < keys * 2 * fours; i += 64) {
+        const int row = i / (2 * fours), at = i - row * 2 * fours, which = at >= fours, d = (at - which * fours) * 4;
+        const HeadsView& out = which ? a.gv : a.gk;
+        if (!out.p) continue;
+        f32x4 x = *(const f32x4*)(sums + (int64_t)row * 2 * dim + at * 4);
+        for (int s = 1; s < a.shares; ++s) x += *(const f32x4*)(sums + s * share + (int64_t)row * 2 * dim + at * 4);
+        T* to = (T*)row_of_head(out, p.k0 + key0 + row, kv_head) + d;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[e] = (T)x[e];
+    }
+    bool odd = false;
+    for (int s = 0; s < a.shares; ++s)
+        for (int part = 0; part < PARTS; ++part)
+            odd |= a.odd[((int64_t)((s * a.kv_heads + kv_head) * PARTS + part) * a.n_tiles + tile) * W + wave] != 0;
+    __threadfence_block();
+    if (odd && keys > 0) gkv_again<DT>(a, p, kv_head, key0, max(0, key0 - (p.nk - p.nq)) / 32 * 32, 0, dim, lane);
 #endif
 }
 
@@ -491,7 +541,7 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves_of(DP * AttnType<DT>::ES,
     const SeqTile st = a.tiles[work.tile];
     const Pair p = pair_of_keys(a, st);
     const int tile0 = a.causal ? (p.nk - 1) / (32 * RG) * (32 * RG) - st.row : st.row;
-    const int key0 = tile0 + rg * 32, key = key0 + (lane & 31), shift = p.nk - p.nq;
+    const int key0 = tile0 + rg * 32, shift = p.nk - p.nq;
     TileLoad<RB, QT, RG> lq, lo;
     lq.init(rg, lane, a.q.ld, a.dim_bytes);
     lo.init(rg, lane, a.gout.ld, a.dim_bytes);
@@ -523,7 +573,7 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves_of(DP * AttnType<DT>::ES,
             const unsigned char* now = own + b * S::kOwn;
             const bool masked = a.causal && r0 + shift < key0 + 31;
             if (masked) odd |= block_not_finite<DT, RB>((const lds_byte*)now, 0) || block_not_finite<DT, RB>((const lds_byte*)now + S::kBlock, 0);
-            w.block((const lds_byte*)now, (const lds_byte*)now + S::kBlock, (const float*)(now + 2 * S::kBlock), masked, key - shift - r0);
+            w.block((const lds_byte*)now, (const lds_byte*)now + S::kBlock, (const float*)(now + 2 * S::kBlock), masked, key0 - shift - r0);
         }
         if (NB == 1) {
             __builtin_amdgcn_s_waitcnt(0);          // what is read there has been read
@@ -535,7 +585,7 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves_of(DP * AttnType<DT>::ES,
     add_results<RG, KS>(smem, w.gv, rg, turn, lane);
     odd = __syncthreads_or(odd);
     if (turn == 0) {
-        w.store(a, p, kv_head, key);
+        w.store(a, p, kv_head, key0 + (lane_here() & 31));
         if (odd) gkv_again<DT>(args_here(), p, kv_head, key0, max(0, key0 - shift) / 32 * 32, w.part * S::COLS * 32, S::COLS * 32, lane_here());
     }
 #endif
@@ -548,7 +598,7 @@ template <int DT, int DP> static void launch_bwd(const AttnArgs& a, const AttnAr
     constexpr int LDS = S::template lds_few<RG, KS>(), LDSK = S::template lds_few<RG, KSK>(), LDS1 = S::template lds_few<1, KS1>();
     static_assert(LDS + 1024 <= 160 * 1024 && LDSK + 1024 <= 160 * 1024 && LDS1 + 1024 <= 160 * 1024 && S::kLdsKeys <= 160 * 1024, "a compute unit has 160 KiB");
     static_assert(S::kParts <= kMostParts, "the launch is checked for them");
-    const unsigned nq = work_blocks(a, a.heads * S::kParts), nk = work_blocks(b, b.kv_heads * S::kParts);
+    const unsigned nq = work_blocks(a, a.heads * S::kParts), nk = work_blocks(b, b.kv_heads * S::kParts * b.shares);
     if (nq && a.few == 1) k_attention_gq_few<DT, DP, 1, KS1><<<nq, 64 * KS1, LDS1, st>>>(a);
     else if (nq && a.few) k_attention_gq_few<DT, DP, RG, KS><<<nq, 64 * RG * KS, LDS, st>>>(a);
     else if (nq && a.tile_rows == 64) k_attention_gq<DT, DP, 2><<<nq, 128, S::kLdsKeys, st>>>(a);
@@ -558,6 +608,8 @@ template <int DT, int DP> static void launch_bwd(const AttnArgs& a, const AttnAr
     else if (b.few) k_attention_gkv_few<DT, DP, RG, KSK><<<nk, 64 * RG * KSK, LDSK, st>>>(b);
     else if (b.tile_rows == 64) k_attention_gkv<DT, DP, 2><<<nk, 128, S::kLdsQueries, st>>>(b);
     else k_attention_gkv<DT, DP, 4><<<nk, 256, S::kLdsQueries, st>>>(b);
+    if (b.shares > 1 && b.tile_rows == 64) k_attention_join_keys<DT, S::kParts, 2><<<b.n_tiles * b.kv_heads, 128, 0, st>>>(b);
+    else if (b.shares > 1) k_attention_join_keys<DT, S::kParts, 4><<<b.n_tiles * b.kv_heads, 256, 0, st>>>(b);
 }
 
 template <int DT> static void launch_bwd_dim(const AttnArgs& a, const AttnArgs& b, int dim, bool keys, hipStream_t st) {
@@ -565,6 +617,15 @@ template <int DT> static void launch_bwd_dim(const AttnArgs& a, const AttnArgs& 
     else if (dim <= 64) launch_bwd<DT, 64>(a, b, keys, st);
     else if (dim <= 128) launch_bwd<DT, 128>(a, b, keys, st);
     else launch_bwd<DT, 256>(a, b, keys, st);
+}
+
+// A causal sequence's last keys have few queries.  Where all workgroups are resident at once those leave their compute unit half empty:
+// a second workgroup for each tile, in an order from long to short, fills it.  bf16 causal, both gradients' kernels: 16,384 x 16 / 4 x 128 4395 ->
+// 3465 us, 16,384 x 16 / 2 x 128 6600 -> 4614, 8,192 x 8 / 4 x 64 516 -> 363, 2,048 x 16 x 128 150 -> 139; with 1,024 queries for a key the join
+// costs more than it gives (1,024 x 32 x 128: 92 -> 103).
+int key_shares(const AttnArgs& a, int32_t n_tiles, int32_t few, int64_t queries, int dim, fx_dtype dt) {
+    const int parts = dim <= 128 ? 1 : dt == FX_F32 ? 4 : 2;
+    return a.causal && !few && queries >= 2048 && (a.gk.p || a.gv.p) && (int64_t)n_tiles * a.kv_heads * parts <= 2 * compute_units() ? 2 : 1;
 }
 
 void attention_bwd_launch(const AttnArgs& a, const AttnArgs& keys_tiles, fx_dtype dt, int dim, bool keys, hipStream_t st) {
@@ -575,9 +636,9 @@ void attention_bwd_launch(const AttnArgs& a, const AttnArgs& keys_tiles, fx_dtyp
     b.few = keys_tiles.few;
     if (b.order != kHeadsFirst) b.order = b.kv_heads % 8 ? kTilesFirst : kHeadsApart;
     b.chunk = b.order == kHeadsFirst ? std::max(1, std::min(8, b.n_tiles / 64)) : 1;
-    if (b.causal && (int64_t)b.n_tiles * b.kv_heads <= 2 * compute_units()) {
+    if (b.shares > 1) {         // the tiles with most queries first, over all heads and shares
         b.order = kHeadsFirst;
-        b.chunk = b.fold = 1;
+        b.chunk = 1;
     }
     if (dt == FX_F32) launch_bwd_dim<FX_F32>(a, b, dim, keys, st);
     else if (dt == FX_F16) launch_bwd_dim<FX_F16>(a, b, dim, keys, st);

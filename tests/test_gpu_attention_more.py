@@ -238,3 +238,23 @@ def test_step_of_more_sequences_than_compute_units(n, heads, kv_heads, dim, dtyp
     ro, rl, bo, bl = A.attention(q64, _held(k64, store), _held(v64, store), np.arange(n + 1), bounds, False, dim ** -0.5, dtype)
     A.check(_f64(out), ro, bo, dtype, "out")
     A.check(_f64(lse), rl.T, bl.T, "f32", "lse")
+
+
+@pytest.mark.parametrize("lens,d,dtype", [([4200] + [300] * 100, 128, "f16"), ([4200] + [300] * 100, 40, "f32"), ([4096] * 8, 200, "bf16")])
+def test_keys_whose_queries_two_workgroups_share(lens, d, dtype):
+    run(lens, 1, 1, d, dtype, True)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f16", 128)])
+def test_shared_queries_that_are_not_finite(dtype, d):
+    """A query and its gradient of NaN in one channel: keys behind them do not see it, whichever workgroup had them."""
+    n, at = 4200, 2000
+    seqs = fx.build_sequences(_joff([n] + [300] * 100)[1])
+    t = [draw(s, seqs.rows, 1, d, dtype)[0] for s in (1, 2, 3, 4)]
+    rg = A.attention_grad(*[_f64(x)[:n] for x in t], [0, n], [0, n], True, d ** -0.5, dtype)
+    out, lse = fx.attention_fwd(seqs, *t[:3], causal=True)
+    t[0][at, 0, 1] = t[3][at, 0, d - 1] = float("nan")
+    g = fx.attention_bwd(seqs, *t[:3], out, lse, t[3], causal=True)
+    for i in (1, 2):
+        A.check(_f64(g[i])[at + 1:n], rg[i][at + 1:], rg[3 + i][at + 1:], dtype, f"gradient {i}")
+        assert torch.isnan(g[i][:at + 1]).any() and torch.isfinite(g[i][n:]).all()
