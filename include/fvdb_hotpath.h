@@ -578,7 +578,8 @@ fx_status fx_dropout(const void* d_x, int64_t ld_x, fx_dtype dt, int64_t rows, i
  * Products, maxima and sums are fp32; in 16 bits exp(s - m) is rounded to the type before its product with v (m close to the
  * row's maximum, the sum of the weights is of the unrounded ones), every output once.  A row's results depend on the keys that it sees alone,
  * a key's gradients on the queries that see it: infinities and NaN of others, of a causal sequence's later rows too, add nothing.
- * (Where a causal sequence holds such a value, the elements that it would spoil of the rows around it are summed one by one.)
+ * (Where a causal sequence holds such a value, the rows around it take longer: a few microseconds for each such value near a row's own
+ * position, whatever the sequence's length.)
  *   q_seqs, kv_seqs  the rows' division into sequences, as many of both; kv_seqs NULL: q_seqs
  *   d_lse            [heads, rows of q_seqs] fp32, natural logarithm, or NULL
  * Backward: d_out and d_lse are what the forward call wrote, d_gout and d_glse ([heads, rows], NULL: zeros) the gradients of

@@ -6,6 +6,7 @@
 // a workgroup's chain of loads, two tiles and stores: 203,132 x 4 x 32 f16 in 3,400 sequences 67 us, 212 MB.
 #include "attention.h"
 
+#include <limits.h>
 #include <math.h>
 
 namespace fx {
@@ -103,30 +104,22 @@ template <int DT, int DP, bool TINY = false> struct FwdWave {
     }
 };
 
-// The wave's rows again where values that they do not see, up to key `end`, are not finite.  lse2: of row0 + lane % 32, base 2
-template <int DT> __device__ void again(const AttnArgs& a, const Pair& p, int head, int row0, int end, float lse2, int lane) {
-    const int dim = a.dim_bytes / AttnType<DT>::ES, kv_head = head / a.group;
-    int unseen = min(end, p.nk);
-    Spoilt spoilt;
-    spoilt.clear();
-    for (int row = min(row0 + 32, p.nq) - 1; row >= row0; --row) {          // each row's unseen keys are those of the row behind it and one more
-        LaneRow<DT> q, x, acc;
-        const int n = max(0, row + 1 + p.nk - p.nq);
-        while (unseen > n) {
-            x.load(row_of_head(a.v, p.k0 + --unseen, kv_head), dim, lane);
-            spoilt.by(x, 0, dim, lane);
-        }
-        if (!spoilt.any()) continue;
-        q.load(row_of_head(a.q, p.q0 + row, head), dim, lane, a.negative ? -a.c : a.c);
-        const float of_row = __shfl(lse2, row - row0, 64);
-        acc.clear();
-        for (int j = n - 1; j >= 0 && !spoilt.settled(acc); --j) {
-            x.load(row_of_head(a.k, p.k0 + j, kv_head), dim, lane);
-            const float w = __builtin_amdgcn_exp2f(q.dot(x) - of_row);
-            x.load(row_of_head(a.v, p.k0 + j, kv_head), dim, lane);
-            acc.add(w, x);
-        }
-        spoilt.store(acc, row_of_head(a.out, p.q0 + row, head), lane, 1.f);
+// The diagonal tiles' values that are not finite, from key `from` on, added for the rows that see them: a weight is positive, and such a
+// value times it is what it is itself
+template <int DT, int N> __device__ __forceinline__ void add_not_finite(f32x16 (&acc)[N], const unsigned char* vb, int64_t ld, int from, int end, int last, int dim_bytes, int lane) {
+    for (int key = from; key < end; ++key) {
+        const unsigned char* row = vb + key * ld;
+        if (!row_not_finite<DT>(row, dim_bytes, lane)) continue;
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                Four<DT> f;
+                f.load(row, k, g, dim_bytes, lane >> 5);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[k][4 * g + e] += key <= last && !finite(f.x[e]) ? f.x[e] : 0.f;
+                __builtin_amdgcn_sched_barrier(0);
+            }
     }
 }
 
@@ -135,7 +128,7 @@ template <int DT, int DP> struct FwdShape {
     static constexpr int RB = DP * AttnType<DT>::ES;
     static constexpr int KT = RB > 256 ? 32 : 64;
     static constexpr int kTile = LdsRows<RB>::bytes(KT);
-    static constexpr int kLds = 4 * kTile;
+    static constexpr int kFlagsAt = 4 * kTile, kLds = kFlagsAt + kFlags;
 };
 
 template <int DT, int DP, int W>
@@ -164,6 +157,7 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
     const int seen_wave = row0 >= p.nq ? 0 : a.causal ? max(0, min(p.nk, min(row0 + 32, p.nq) + shift)) : p.nk;
     const int last = a.causal ? min(p.nk - 1, row + shift) : p.nk - 1, unmasked = a.causal ? min(p.nk - 1, row0 + shift) : p.nk - 1;
     const int n = (seen + KT - 1) / KT;
+    const int diagonal = a.causal ? max(0, st.row + 1 + shift) / KT : INT_MAX;           // the first tile that is not seen whole by some row of the workgroup
     if (n > 0) {
         lk.load(lds, kb, a.k.ld, 0, p.nk, a.dim_bytes, wave);
         lv.load(lds + 2 * S::kTile, vb, a.v.ld, 0, p.nk, a.dim_bytes, wave);
@@ -182,15 +176,15 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
         }
         const lds_byte *kt = lds + b * S::kTile, *vt = lds + (2 + b) * S::kTile;
         const bool masked = key0 + KT - 1 > unmasked;
+        if (j >= diagonal) odd |= cleaned_rows<KT, W>(lds + S::kFlagsAt, clean_rows<DT, RB, KT, W>(lds + (2 + b) * S::kTile, wave), wave) != 0;
         if (key0 >= seen_wave) continue;
-        if (a.causal && masked) odd |= block_not_finite<DT, RB>(vt, 0) || (KT == 64 && block_not_finite<DT, RB>(vt, KT - 32));
         // half a tile by itself only where sequences are short: a second form of the loop's body costs registers
         if (KT == 64 && (W > 2 || key0 + 32 < seen_wave)) w.template blocks<2>(kt, vt, 0, key0, masked, last);
         else w.template blocks<1>(kt, vt, 0, key0, masked, last);
     }
     w.sum += other_half(w.sum);
+    if (odd) add_not_finite<DT>(w.acc, vb, a.v.ld, diagonal * KT, seen_wave, last, a.dim_bytes, lane_here());
     w.store(a, row, p.nq, p.q0, head);
-    if (odd) again<DT>(args_here(), p, head, row0, (seen_wave + KT - 1) / KT * KT, w.m * w.c + __builtin_amdgcn_logf(w.sum), lane_here());
 #endif
 }
 
@@ -201,7 +195,7 @@ template <int DT, int DP, int RG, int KS> struct FewShape {
     static constexpr int kTile = LdsRows<RB>::bytes(32);
     static constexpr int kBuffers = 4 * kTile * KS <= 128 * 1024 ? 2 : 1;
     static constexpr int kSlot = DP * 32 * 4 + 512;                 // a wave's result
-    static constexpr int kLds = std::max(2 * kBuffers * kTile * KS, KS / 2 * RG * kSlot);
+    static constexpr int kFlagsAt = std::max(2 * kBuffers * kTile * KS, KS / 2 * RG * kSlot), kLds = kFlagsAt + kFlags;
 };
 
 template <int DT, int DP, int RG, int KS>
@@ -227,6 +221,7 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves(DP * AttnType<DT>::ES)) v
     const int seen_wave = row0 >= p.nq ? 0 : a.causal ? max(0, min(p.nk, min(row0 + 32, p.nq) + shift)) : p.nk;
     const int last = a.causal ? min(p.nk - 1, row + shift) : p.nk - 1, unmasked = a.causal ? min(p.nk - 1, row0 + shift) : p.nk - 1;
     const int n = (seen + 31) / 32, rounds = (n + KS - 1) / KS;         // a wave without a block in the last round waits with the others
+    const int diagonal = a.causal ? max(0, st.row + 1 + shift) / 32 : INT_MAX;
     auto load = [&](int j, int b) {
         lk.load(lds + b * 2 * S::kTile, kb, a.k.ld, j * 32, p.nk, a.dim_bytes, rg);
         lv.load(lds + b * 2 * S::kTile + S::kTile, vb, a.v.ld, j * 32, p.nk, a.dim_bytes, rg);
@@ -241,11 +236,15 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves(DP * AttnType<DT>::ES)) v
         const int j = i * KS + turn, b = NB == 2 ? i & 1 : 0;
         __builtin_amdgcn_s_waitcnt(0);
         if (RG > 1) __syncthreads();
-        const lds_byte* at = lds + b * 2 * S::kTile;
+        lds_byte* at = lds + b * 2 * S::kTile;
+        if (i * KS + KS > diagonal) {           // one of the turns' blocks
+            uint32_t mine = j >= diagonal && j < n ? clean_rows<DT, RB, 32, RG>(at + S::kTile, rg) : 0;
+            if (RG > 1) mine = (uint32_t)cleaned_rows<32, RG>((lds_byte*)smem + S::kFlagsAt + turn * RG * 4, mine, rg);
+            odd |= mine != 0;
+        }
         if (NB == 2 && j + KS < n) load(j + KS, b ^ 1);
         if (j * 32 < seen_wave) {
             const bool masked = j * 32 + 31 > unmasked;
-            if (a.causal && masked) odd |= block_not_finite<DT, RB>(at + S::kTile, 0);
             w.template blocks<1>(at, at + S::kTile, 0, j * 32, masked, last);
         }
         if (NB == 1) {
@@ -279,8 +278,8 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves(DP * AttnType<DT>::ES)) v
     }
     odd = __syncthreads_or(odd);
     if (turn == 0) {
+        if (odd) add_not_finite<DT>(w.acc, vb, a.v.ld, diagonal * 32, seen_wave, last, a.dim_bytes, lane_here());
         w.store(a, row, p.nq, p.q0, head);
-        if (odd) again<DT>(args_here(), p, head, row0, (seen_wave + 31) / 32 * 32, w.m * w.c + __builtin_amdgcn_logf(w.sum), lane_here());
     }
 #endif
 }
@@ -544,8 +543,6 @@ extern "C" fx_status fx_attention_bwd(const fx_attention* d, const void* d_out, 
         void* p = nullptr;
         FX_TRY(scratch.get(who, &p, (size_t)a.shares * d->kv_heads * nk * 2 * dim * 4));
         a.sums = (float*)p;
-        FX_TRY(scratch.get(who, &p, (size_t)a.shares * d->kv_heads * kMostParts * b.n_tiles * 4 * 4));
-        a.odd = (int32_t*)p;
     }
     attention_bwd_launch(a, b, d->dt, dim, d_gk || d_gv, st);
     FX_TRY(back.run(who, d->dim, d->dim, dtype_size(d->dt), st));

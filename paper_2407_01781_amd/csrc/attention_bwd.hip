@@ -9,6 +9,7 @@
 // instructions run); 131,072 x 4 x 64 f16 in windows of 1,024: 0.29 and 0.33 ms.
 #include "attention.h"
 
+#include <limits.h>
 #include <math.h>
 
 namespace fx {
@@ -18,7 +19,8 @@ template <int DT, int DP> struct BwdShape {
     static constexpr int KT = RB > 128 ? 32 : 64;               // keys of a tile that streams by (two blocks' scores and dP are 64 registers)
     static constexpr int QT = RB > 128 ? 32 : 64;               // queries, a block of 32 after the other
     static constexpr int kKeys = LdsRows<RB>::bytes(KT), kQueries = LdsRows<RB>::bytes(QT), kStats = 2 * QT * 4;
-    static constexpr int kLdsKeys = 4 * kKeys, kLdsQueries = 4 * kQueries + 2 * kStats;
+    static constexpr int kFlagsKeys = 4 * kKeys, kFlagsQueries = 4 * kQueries + 2 * kStats;
+    static constexpr int kLdsKeys = kFlagsKeys + kFlags, kLdsQueries = kFlagsQueries + kFlags;
     // Parts that the output's columns are dealt out in, as heads of their own: above 128 dimensions a lane's results, its own rows and
     // their products would not fit 512 registers without spills.
     static constexpr int kParts = DP > 128 ? (DT == FX_F32 ? 4 : 2) : 1;
@@ -28,8 +30,17 @@ template <int DT, int DP> struct BwdShape {
     static constexpr int kBlock = LdsRows<RB>::bytes(32), kBlockStats = 32 * 8;
     static constexpr int kOwn = 2 * kBlock + kBlockStats;            // a wave's two tiles and what belongs to their rows
     template <int KS> static constexpr int buffers() { return 2 * kOwn * KS <= 128 * 1024 ? 2 : 1; }
-    template <int RG, int KS> static constexpr int lds_few() { return std::max(buffers<KS>() * kOwn * KS, KS / 2 * RG * COLS * 4096); }
+    template <int RG, int KS> static constexpr int flags_few() { return std::max(buffers<KS>() * kOwn * KS, KS / 2 * RG * COLS * 4096); }
+    template <int RG, int KS> static constexpr int lds_few() { return flags_few<RG, KS>() + kFlags; }
 };
+
+// zeros in the place of the rows of a 32x32 result that have a bit in `odd`
+__device__ __forceinline__ void without(uint64_t odd, int half, f32x16& x, f32x16& y) {
+    const uint32_t mine = (uint32_t)odd >> (4 * half);
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+        if (mine >> (8 * (r >> 2) + (r & 3)) & 1) x[r] = y[r] = 0.f;
+}
 
 // ------------------------------------------------------------------ gradients of the queries
 template <int DT, int DP, bool TINY = false> struct GqWave {
@@ -73,7 +84,8 @@ template <int DT, int DP, bool TINY = false> struct GqWave {
         for (int k = 0; k < S::COLS; ++k) acc[k] = f32x16(0.f);
     }
 
-    template <int NB> __device__ __forceinline__ void blocks(const lds_byte* kt, const lds_byte* vt, int key0, bool masked, int last) {
+    // odd: keys that are not finite, whose place in the tile has zeros (rows_again)
+    template <int NB> __device__ __forceinline__ void blocks(const lds_byte* kt, const lds_byte* vt, int key0, bool masked, int last, uint64_t odd) {
         f32x16 p[NB], dp[NB];
 #pragma unroll
         for (int t = 0; t < NB; ++t) {
@@ -93,6 +105,10 @@ template <int DT, int DP, bool TINY = false> struct GqWave {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (32 * t + 8 * (r >> 2) + (r & 3) > left) p[t][r] = dp[t][r] = 0.f;
+        }
+        if (odd) {
+#pragma unroll
+            for (int t = 0; t < NB; ++t) without(odd >> (32 * t), half, p[t], dp[t]);
         }
         if (one_tile && !one_key) {
             delta = 0.f;
@@ -119,6 +135,20 @@ template <int DT, int DP, bool TINY = false> struct GqWave {
         }
     }
 
+    // The keys from `from` on that are not finite, one by one: into the rows that see them (up to key `last`) alone
+    __device__ __forceinline__ void keys_again(const AttnArgs& a, const Pair& p, int head, int row, int from, int end, int last) {
+        const int lane = lane_here(), kv_head = head / a.group;
+        const int64_t mine = p.q0 + min(row, p.nq - 1);
+        for (int key = from; key < end; ++key) {
+            const unsigned char* kr = row_of_head(a.k, p.k0 + key, kv_head);
+            if (!row_not_finite<DT>(kr, a.dim_bytes, lane)) continue;
+            const float s = dot_rows<DT>(row_of_head(a.q, mine, head), kr, a.dim_bytes, lane >> 5);
+            const float dp = one_key ? 0.f : dot_rows<DT>(row_of_head(a.gout, mine, head), row_of_head(a.v, p.k0 + key, kv_head), a.dim_bytes, lane >> 5);
+            const float w = __builtin_amdgcn_exp2f(fmaf(s, a.negative ? -a.c : a.c, -lse2));
+            add_row<DT>(acc, kr, w * (dp - (delta - glse)), key <= last, part * S::COLS, a.dim_bytes, lane >> 5);
+        }
+    }
+
     __device__ __forceinline__ void store(const AttnArgs& a, const Pair& p, int head, int row) {
         if (row >= p.nq) return;
         if (half == 0 && part == 0) *(f32x2*)(a.stats + 2 * (head * a.rows_q + p.q0 + row)) = f32x2{lse2, delta - glse};
@@ -129,34 +159,6 @@ template <int DT, int DP, bool TINY = false> struct GqWave {
         for (int k = 0; k < S::COLS; ++k) store_columns<DT>(acc[k], f, out, part * S::COLS + k, a.dim_bytes, half);
     }
 };
-
-// `count` elements from `from` on of the wave's rows again where keys that they do not see, up to `end`, are not finite.  off: the sum over
-// P dP less glse, of row0 + lane % 32
-template <int DT> __device__ void gq_again(const AttnArgs& a, const Pair& p, int head, int row0, int end, int from, int count, float off, int lane) {
-    const int dim = a.dim_bytes / AttnType<DT>::ES, kv_head = head / a.group;
-    int unseen = min(end, p.nk);
-    Spoilt spoilt;
-    spoilt.clear();
-    for (int row = min(row0 + 32, p.nq) - 1; row >= row0; --row) {          // each row's unseen keys are those of the row behind it and one more
-        LaneRow<DT> q, go, x, y, acc;
-        const int n = max(0, row + 1 + p.nk - p.nq);
-        while (unseen > n) {
-            x.load(row_of_head(a.k, p.k0 + --unseen, kv_head), dim, lane);
-            spoilt.by(x, from, min(from + count, dim), lane);
-        }
-        if (!spoilt.any()) continue;
-        const float lse2 = a.lse[head * a.rows_q + p.q0 + row] * kLog2e, of_row = __shfl(off, row - row0, 64);
-        q.load(row_of_head(a.q, p.q0 + row, head), dim, lane, a.negative ? -a.c : a.c);
-        go.load(row_of_head(a.gout, p.q0 + row, head), dim, lane);
-        acc.clear();
-        for (int j = n - 1; j >= 0 && !spoilt.settled(acc); --j) {
-            x.load(row_of_head(a.k, p.k0 + j, kv_head), dim, lane);
-            y.load(row_of_head(a.v, p.k0 + j, kv_head), dim, lane);
-            acc.add(__builtin_amdgcn_exp2f(q.dot(x) - lse2) * ((p.nk == 1 ? 0.f : go.dot(y)) - of_row), x);
-        }
-        spoilt.store(acc, row_of_head(a.gq, p.q0 + row, head), lane, a.negative ? -a.scale : a.scale);
-    }
-}
 
 template <int DT, int DP, int W>
 __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_attention_gq(AttnArgs a) {
@@ -181,6 +183,7 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
     const int seen_wave = row0 >= p.nq ? 0 : a.causal ? max(0, min(p.nk, min(row0 + 32, p.nq) + shift)) : p.nk;
     const int last = a.causal ? min(p.nk - 1, row + shift) : p.nk - 1, unmasked = a.causal ? min(p.nk - 1, row0 + shift) : p.nk - 1;
     const int n = a.gq.p || p.nk <= KT ? (seen + KT - 1) / KT : 0;          // without gq the sums alone, where they are made of the tile
+    const int diagonal = a.causal ? max(0, st.row + 1 + shift) / KT : INT_MAX;      // the first tile that is not seen whole by some row of the workgroup
     if (n > 0) {
         lk.load(lds, kb, a.k.ld, 0, p.nk, a.dim_bytes, wave);
         lv.load(lds + 2 * S::kKeys, vb, a.v.ld, 0, p.nk, a.dim_bytes, wave);
@@ -196,15 +199,19 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
             lk.load(lds + (b ^ 1) * S::kKeys, kb, a.k.ld, key0 + KT, p.nk, a.dim_bytes, wave);
             lv.load(lds + (2 + (b ^ 1)) * S::kKeys, vb, a.v.ld, key0 + KT, p.nk, a.dim_bytes, wave);
         }
+        uint64_t odd_keys = 0;
+        if (j >= diagonal) {
+            odd_keys = cleaned_rows<KT, W>(lds + S::kFlagsKeys, clean_rows<DT, RB, KT, W>(lds + b * S::kKeys, wave), wave);
+            odd |= odd_keys != 0;
+        }
         if (key0 >= seen_wave) continue;
         const lds_byte *kt = lds + b * S::kKeys, *vt = lds + (2 + b) * S::kKeys;
         const bool masked = key0 + KT - 1 > unmasked;
-        if (a.causal && masked) odd |= block_not_finite<DT, RB>(kt, 0) || (KT == 64 && block_not_finite<DT, RB>(kt, KT - 32));
-        if (KT == 64 && (W > 2 || key0 + 32 < seen_wave)) w.template blocks<2>(kt, vt, key0, masked, last);
-        else w.template blocks<1>(kt, vt, key0, masked, last);
+        if (KT == 64 && (W > 2 || key0 + 32 < seen_wave)) w.template blocks<2>(kt, vt, key0, masked, last, odd_keys);
+        else w.template blocks<1>(kt, vt, key0, masked, last, odd_keys);
     }
+    if (odd) w.keys_again(args_here(), p, head, row, diagonal * KT, seen_wave, last);
     w.store(a, p, head, row);
-    if (odd && a.gq.p) gq_again<DT>(args_here(), p, head, row0, (seen_wave + KT - 1) / KT * KT, w.part * S::COLS * 32, S::COLS * 32, w.delta - w.glse, lane_here());
 #endif
 }
 
@@ -249,6 +256,7 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves(DP * AttnType<DT>::ES)) v
     const int seen_wave = row0 >= p.nq ? 0 : a.causal ? max(0, min(p.nk, min(row0 + 32, p.nq) + shift)) : p.nk;
     const int last = a.causal ? min(p.nk - 1, row + shift) : p.nk - 1, unmasked = a.causal ? min(p.nk - 1, row0 + shift) : p.nk - 1;
     const int n = a.gq.p || p.nk <= 32 ? (seen + 31) / 32 : 0, rounds = (n + KS - 1) / KS;
+    const int diagonal = a.causal ? max(0, st.row + 1 + shift) / 32 : INT_MAX;
     auto load = [&](int j, int b) {
         lk.load(lds + b * S::kOwn, kb, a.k.ld, j * 32, p.nk, a.dim_bytes, rg);
         lv.load(lds + b * S::kOwn + S::kBlock, vb, a.v.ld, j * 32, p.nk, a.dim_bytes, rg);
@@ -261,13 +269,15 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves(DP * AttnType<DT>::ES)) v
         const int j = i * KS + turn, b = NB == 2 ? i & 1 : 0;
         __builtin_amdgcn_s_waitcnt(0);
         if (RG > 1) __syncthreads();
-        const lds_byte* at = lds + b * S::kOwn;
-        if (NB == 2 && j + KS < n) load(j + KS, b ^ 1);
-        if (j * 32 < seen_wave) {
-            const bool masked = j * 32 + 31 > unmasked;
-            if (a.causal && masked) odd |= block_not_finite<DT, RB>(at, 0);
-            w.template blocks<1>(at, at + S::kBlock, j * 32, masked, last);
+        lds_byte* at = lds + b * S::kOwn;
+        uint32_t odd_keys = 0;
+        if (i * KS + KS > diagonal) {           // one of the turns' blocks
+            odd_keys = j >= diagonal && j < n ? clean_rows<DT, RB, 32, RG>(at, rg) : 0;
+            if (RG > 1) odd_keys = (uint32_t)cleaned_rows<32, RG>((lds_byte*)smem + S::template flags_few<RG, KS>() + turn * RG * 4, odd_keys, rg);
+            odd |= odd_keys != 0;
         }
+        if (NB == 2 && j + KS < n) load(j + KS, b ^ 1);
+        if (j * 32 < seen_wave) w.template blocks<1>(at, at + S::kBlock, j * 32, j * 32 + 31 > unmasked, last, odd_keys);
         if (NB == 1) {
             __builtin_amdgcn_s_waitcnt(0);          // what is read there has been read
             if (RG > 1) __syncthreads();
@@ -277,8 +287,8 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves(DP * AttnType<DT>::ES)) v
     add_results<RG, KS>(smem, w.acc, rg, turn, lane);
     odd = __syncthreads_or(odd);
     if (turn == 0) {
+        if (odd) w.keys_again(args_here(), p, head, row, diagonal * 32, seen_wave, last);
         w.store(a, p, head, row);
-        if (odd && a.gq.p) gq_again<DT>(args_here(), p, head, row0, (seen_wave + 31) / 32 * 32, w.part * S::COLS * 32, S::COLS * 32, w.delta - w.glse, lane_here());
     }
 #endif
 }
@@ -311,7 +321,8 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
     }
 
     // 32 queries whose first that sees the block's first key is `first`, counted from the block's first (all do where not masked)
-    __device__ __forceinline__ void block(const lds_byte* qt, const lds_byte* ot, const float* stats, bool masked, int first) {
+    // odd: rows that are not finite, whose places in the tiles have zeros (rows_again)
+    __device__ __forceinline__ void block(const lds_byte* qt, const lds_byte* ot, const float* stats, bool masked, int first, uint32_t odd) {
         f32x16 p = f32x16(0.f), ds = f32x16(0.f);
 #pragma unroll
         for (int i = 0; i < S::STEPS; ++i) p = Elem<T>::mma(rows_of(qt, 0, i), k.x[i], p);
@@ -336,6 +347,7 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
             for (int r = 0; r < 16; ++r)
                 if (8 * (r >> 2) + (r & 3) < first) p[r] = ds[r] = 0.f;
         }
+        if (odd) without(odd, half, p, ds);
         Weights<DT> wp, wd;
         wp.set(p);
         wd.set(ds);
@@ -353,7 +365,24 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
         }
     }
 
-    // the same of one share of the queries, in fp32
+    // Rows row0 .. end - 1 of a head that are not finite, one by one: into the keys that they see alone
+    __device__ __forceinline__ void rows_again(const AttnArgs& a, const Pair& p, int head, int key, int row0, int end) {
+        const int lane = lane_here(), kv_head = head / a.group;
+        const int64_t mine = p.k0 + min(key, p.nk - 1);
+        for (int row = row0; row < end; ++row) {
+            const unsigned char *qr = row_of_head(a.q, p.q0 + row, head), *gr = row_of_head(a.gout, p.q0 + row, head);
+            if (!row_not_finite<DT>(qr, a.dim_bytes, lane) && !row_not_finite<DT>(gr, a.dim_bytes, lane)) continue;
+            const f32x2 stat = *(const f32x2*)(a.stats + 2 * (head * a.rows_q + p.q0 + row));
+            const float s = dot_rows<DT>(row_of_head(a.k, mine, kv_head), qr, a.dim_bytes, lane >> 5);
+            const float dp = one_key ? 0.f : dot_rows<DT>(row_of_head(a.v, mine, kv_head), gr, a.dim_bytes, lane >> 5);
+            const float w = __builtin_amdgcn_exp2f(fmaf(s, a.negative ? -a.c : a.c, -stat[0]));
+            const bool sees = row + p.nk - p.nq >= key;
+            add_row<DT>(gk, qr, w * (dp - stat[1]), sees, part * S::COLS, a.dim_bytes, lane >> 5);
+            add_row<DT>(gv, gr, w, sees, part * S::COLS, a.dim_bytes, lane >> 5);
+        }
+    }
+
+    // the results of one share of the queries, in fp32
     __device__ __forceinline__ void store_sums(const AttnArgs& a, const Pair& p, int kv_head, int key, int share) {
         if (key >= p.nk) return;
         const int dim_bytes = a.dim_bytes / AttnType<DT>::ES * 4;
@@ -381,43 +410,6 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
     }
 };
 
-// `count` elements from `from` on of the wave's keys again where queries or output gradients, from row `begin` on, that do not see
-// them are not finite
-template <int DT> __device__ void gkv_again(const AttnArgs& a, const Pair& p, int kv_head, int key0, int begin, int from, int count, int lane) {
-    const int dim = a.dim_bytes / AttnType<DT>::ES, shift = p.nk - p.nq, first_head = kv_head * a.group;
-    int unseen = begin;
-    Spoilt spoilt_k, spoilt_v;
-    spoilt_k.clear();
-    spoilt_v.clear();
-    for (int key = key0; key < min(key0 + 32, p.nk); ++key) {               // each key's unseen queries are those of the key before it and one more
-        LaneRow<DT> k, v, x, y, gk, gv;
-        const int first = max(0, key - shift);           // the first query that sees the key
-        for (; unseen < min(first, p.nq); ++unseen)
-            for (int head = first_head; head < first_head + a.group; ++head) {
-                x.load(row_of_head(a.q, p.q0 + unseen, head), dim, lane);
-                y.load(row_of_head(a.gout, p.q0 + unseen, head), dim, lane);
-                spoilt_k.by(x, from, min(from + count, dim), lane);
-                spoilt_v.by(y, from, min(from + count, dim), lane);
-            }
-        if (!spoilt_k.any() && !spoilt_v.any()) continue;
-        k.load(row_of_head(a.k, p.k0 + key, kv_head), dim, lane, a.negative ? -a.c : a.c);
-        v.load(row_of_head(a.v, p.k0 + key, kv_head), dim, lane);
-        gk.clear();
-        gv.clear();
-        for (int head = first_head; head < first_head + a.group; ++head)
-            for (int row = first; row < p.nq && !(spoilt_k.settled(gk) && spoilt_v.settled(gv)); ++row) {
-                x.load(row_of_head(a.q, p.q0 + row, head), dim, lane);
-                y.load(row_of_head(a.gout, p.q0 + row, head), dim, lane);
-                const f32x2 stat = *(const f32x2*)(a.stats + 2 * (head * a.rows_q + p.q0 + row));
-                const float w = __builtin_amdgcn_exp2f(k.dot(x) - stat[0]);
-                gv.add(w, y);
-                gk.add(w * ((p.nk == 1 ? 0.f : v.dot(y)) - stat[1]), x);
-            }
-        if (a.gk.p) spoilt_k.store(gk, row_of_head(a.gk, p.k0 + key, kv_head), lane, a.negative ? -a.scale : a.scale);
-        if (a.gv.p) spoilt_v.store(gv, row_of_head(a.gv, p.k0 + key, kv_head), lane, 1.f);
-    }
-}
-
 // lse (base 2) and delta of ROWS rows, as the first kernel left them, into LDS; zeros for a row that does not exist, whose query and
 // gradient are zeros too: it adds nothing
 template <int ROWS> __device__ __forceinline__ void load_stats(const AttnArgs& a, lds_byte* to, int head, int q0, int row0, int nq, int lane) {
@@ -432,7 +424,7 @@ template <int ROWS> __device__ __forceinline__ void load_stats(const AttnArgs& a
 }
 
 template <int DT, int DP, int W>
-__global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 4)) void k_attention_gkv(AttnArgs a) {
+__global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES <= 128 ? 3 : least_waves_of(DP * AttnType<DT>::ES, W == 4)) void k_attention_gkv(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef BwdShape<DT, DP> S;
     constexpr int RB = S::RB, QT = S::QT;
@@ -451,6 +443,7 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
     TileLoad<RB, QT, W> lq, lo;
     lq.init(wave, lane, a.q.ld, a.dim_bytes);
     lo.init(wave, lane, a.gout.ld, a.dim_bytes);
+    const int diagonal = a.causal ? tile0 + 32 * W - 1 - shift : 0;         // rows before this one do not see all of the workgroup's keys
     // all heads of the group in turn; of each the tiles from the first on in which a query sees the workgroup's first key
     const int begin = a.causal ? max(0, tile0 - shift) / QT * QT : 0, n = begin < p.nq ? (p.nq - begin + QT - 1) / QT * a.group : 0;
     const int j0 = share ? n / 2 : 0, j1 = share + 1 < a.shares ? n / 2 : n, per_head = max(1, n / a.group), items = j1 - j0;
@@ -476,28 +469,36 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
         if (r0 >= p.nq) r0 = begin;
         if (j + 1 < items) load(b ^ 1);
         const lds_byte *qt = lds + b * S::kQueries, *ot = lds + (2 + b) * S::kQueries;
+        uint64_t odd_rows = 0;
+        if (r0 < diagonal) {
+            const uint32_t mine = clean_rows<DT, RB, QT, W>(lds + b * S::kQueries, wave) | clean_rows<DT, RB, QT, W>(lds + (2 + b) * S::kQueries, wave);
+            odd_rows = cleaned_rows<QT, W>(lds + S::kFlagsQueries, mine, wave);
+            odd |= odd_rows != 0;
+        }
         const float* st = (const float*)(smem + 4 * S::kQueries + b * S::kStats);
 #pragma unroll
         for (int t = 0; t < QT; t += 32) {
             const int r = r0 + t;
             if (key0 >= p.nk || r >= p.nq || (a.causal && r + 31 + shift < key0)) continue;
             const bool masked = a.causal && r + shift < key0 + 31;
-            if (masked) odd |= block_not_finite<DT, RB>(qt, t) || block_not_finite<DT, RB>(ot, t);
-            w.block(qt + LdsRows<RB>::row_at(t), ot + LdsRows<RB>::row_at(t), st + 2 * t, masked, key0 - shift - r);
+            w.block(qt + LdsRows<RB>::row_at(t), ot + LdsRows<RB>::row_at(t), st + 2 * t, masked, key0 - shift - r, (uint32_t)(odd_rows >> t));
         }
     }
+    if (odd)            // the same tiles of the workgroup's items
+        for (int j = j0; j < j1; ++j) {
+            const int of_head = j / per_head, row = begin + (j - of_head * per_head) * QT;
+            if (row < diagonal) w.rows_again(args_here(), p, kv_head * a.group + of_head, key0 + (lane_here() & 31), row, min(row + QT, p.nq));
+        }
     if (a.shares > 1) {
         w.store_sums(a, p, kv_head, key0 + (lane_here() & 31), share);
-        if (lane_here() == 0) a.odd[((int64_t)(share * a.kv_heads * S::kParts + head_part) * a.n_tiles + work.tile) * W + wave] = odd;
         return;
     }
     w.store(a, p, kv_head, key0 + (lane_here() & 31));
-    if (odd) gkv_again<DT>(args_here(), p, kv_head, key0, max(0, key0 - shift) / 32 * 32, w.part * S::COLS * 32, S::COLS * 32, lane_here());
 #endif
 }
 
-// The shares' sums of W blocks of 32 keys added, in their order; and what unseen rows have spoilt summed anew
-template <int DT, int PARTS, int W>
+// The shares' sums of W blocks of 32 keys added, in their order
+template <int DT, int W>
 __global__ __launch_bounds__(64 * W) void k_attention_join_keys(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef typename AttnType<DT>::T T;
@@ -517,18 +518,12 @@ __global__ __launch_bounds__(64 * W) void k_attention_join_keys(AttnArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) to[e] = (T)x[e];
     }
-    bool odd = false;
-    for (int s = 0; s < a.shares; ++s)
-        for (int part = 0; part < PARTS; ++part)
-            odd |= a.odd[((int64_t)((s * a.kv_heads + kv_head) * PARTS + part) * a.n_tiles + tile) * W + wave] != 0;
-    __threadfence_block();
-    if (odd && keys > 0) gkv_again<DT>(a, p, kv_head, key0, max(0, key0 - (p.nk - p.nq)) / 32 * 32, 0, dim, lane);
 #endif
 }
 
 // For few keys: RG blocks of 32, for each of which KS waves take the blocks of 32 queries of all heads in turn
 template <int DT, int DP, int RG, int KS>
-__global__ __launch_bounds__(64 * RG * KS, least_waves_of(DP * AttnType<DT>::ES, false)) void k_attention_gkv_few(AttnArgs a) {
+__global__ __launch_bounds__(64 * RG * KS, RG * KS == 4 && DP * AttnType<DT>::ES <= 128 ? 3 : least_waves_of(DP * AttnType<DT>::ES, false)) void k_attention_gkv_few(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef BwdShape<DT, DP> S;
     constexpr int RB = S::RB, QT = 32, NB = S::template buffers<KS>();
@@ -547,6 +542,7 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves_of(DP * AttnType<DT>::ES,
     lo.init(rg, lane, a.gout.ld, a.dim_bytes);
     const int begin = a.causal ? max(0, tile0 - shift) / QT * QT : 0, per_head = begin < p.nq ? (p.nq - begin + QT - 1) / QT : 0;
     const int n = per_head * a.group, rounds = (n + KS - 1) / KS;
+    const int diagonal = a.causal ? tile0 + 32 * RG - 1 - shift : 0;        // rows before this one do not see all of the workgroup's keys
     int head = kv_head * a.group, at = turn;            // the next block of the wave's turn: the at-th of the head
     auto load = [&](int b) {
         while (at >= per_head) { at -= per_head; ++head; }
@@ -568,12 +564,18 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves_of(DP * AttnType<DT>::ES,
         __builtin_amdgcn_s_waitcnt(0);
         if (RG > 1) __syncthreads();
         r0 = next;
+        uint32_t odd_rows = 0;
+        if (begin < diagonal) {
+            lds_byte* now = (lds_byte*)own + b * S::kOwn;
+            if (j < n && r0 < diagonal) odd_rows = clean_rows<DT, RB, QT, RG>(now, rg) | clean_rows<DT, RB, QT, RG>(now + S::kBlock, rg);
+            if (RG > 1) odd_rows = (uint32_t)cleaned_rows<QT, RG>((lds_byte*)smem + S::template flags_few<RG, KS>() + turn * RG * 4, odd_rows, rg);
+            odd |= odd_rows != 0;
+        }
         if (NB == 2 && j + KS < n) next = load(b ^ 1);
         if (j < n && key0 < p.nk && !(a.causal && r0 + 31 + shift < key0)) {
             const unsigned char* now = own + b * S::kOwn;
             const bool masked = a.causal && r0 + shift < key0 + 31;
-            if (masked) odd |= block_not_finite<DT, RB>((const lds_byte*)now, 0) || block_not_finite<DT, RB>((const lds_byte*)now + S::kBlock, 0);
-            w.block((const lds_byte*)now, (const lds_byte*)now + S::kBlock, (const float*)(now + 2 * S::kBlock), masked, key0 - shift - r0);
+            w.block((const lds_byte*)now, (const lds_byte*)now + S::kBlock, (const float*)(now + 2 * S::kBlock), masked, key0 - shift - r0, odd_rows);
         }
         if (NB == 1) {
             __builtin_amdgcn_s_waitcnt(0);          // what is read there has been read
@@ -585,8 +587,10 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves_of(DP * AttnType<DT>::ES,
     add_results<RG, KS>(smem, w.gv, rg, turn, lane);
     odd = __syncthreads_or(odd);
     if (turn == 0) {
+        if (odd)
+            for (int h = 0; h < a.group; ++h)
+                w.rows_again(args_here(), p, kv_head * a.group + h, key0 + (lane_here() & 31), begin, min((diagonal - begin + QT - 1) / QT * QT + begin, p.nq));
         w.store(a, p, kv_head, key0 + (lane_here() & 31));
-        if (odd) gkv_again<DT>(args_here(), p, kv_head, key0, max(0, key0 - shift) / 32 * 32, w.part * S::COLS * 32, S::COLS * 32, lane_here());
     }
 #endif
 }
@@ -608,8 +612,8 @@ template <int DT, int DP> static void launch_bwd(const AttnArgs& a, const AttnAr
     else if (b.few) k_attention_gkv_few<DT, DP, RG, KSK><<<nk, 64 * RG * KSK, LDSK, st>>>(b);
     else if (b.tile_rows == 64) k_attention_gkv<DT, DP, 2><<<nk, 128, S::kLdsQueries, st>>>(b);
     else k_attention_gkv<DT, DP, 4><<<nk, 256, S::kLdsQueries, st>>>(b);
-    if (b.shares > 1 && b.tile_rows == 64) k_attention_join_keys<DT, S::kParts, 2><<<b.n_tiles * b.kv_heads, 128, 0, st>>>(b);
-    else if (b.shares > 1) k_attention_join_keys<DT, S::kParts, 4><<<b.n_tiles * b.kv_heads, 256, 0, st>>>(b);
+    if (b.shares > 1 && b.tile_rows == 64) k_attention_join_keys<DT, 2><<<b.n_tiles * b.kv_heads, 128, 0, st>>>(b);
+    else if (b.shares > 1) k_attention_join_keys<DT, 4><<<b.n_tiles * b.kv_heads, 256, 0, st>>>(b);
 }
 
 template <int DT> static void launch_bwd_dim(const AttnArgs& a, const AttnArgs& b, int dim, bool keys, hipStream_t st) {
