@@ -1,6 +1,8 @@
 """Compile the HIP sources into paper_2407_01781_amd/libfvdb_hotpath.so (gfx950 only)."""
 from __future__ import annotations
 
+import glob
+import importlib.util
 import os
 import subprocess
 
@@ -17,6 +19,11 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
 NO_SCRATCH = {"scan.hip", "block.hip"}
 # Here scalar registers may be kept in lanes of vector registers (and a frame be reserved for it), vector registers may not.
 NO_VECTOR_SPILL = {"attention.hip", "attention_bwd.hip", "attention_step.hip"}
+
+# by its path: this file is run without its package, too, which loads the library
+_spec = importlib.util.spec_from_file_location("_matrix_waits", os.path.join(HERE, "matrix_waits.py"))
+_matrix_waits = importlib.util.module_from_spec(_spec)
+_spec.loader.exec_module(_matrix_waits)
 
 
 def _spills(src: str, lines) -> list:
@@ -58,14 +65,22 @@ def build(force: bool = True, verbose: bool = False) -> str:
         cmd = [hipcc] + compile_flags + ["-c", os.path.join(CSRC, src), "-o", obj]
         if src in NO_SCRATCH or src in NO_VECTOR_SPILL:
             cmd.append("-Rpass-analysis=kernel-resource-usage")
+        cmd.append("-save-temps=obj")
         if verbose:
             print(" ".join(cmd))
-        return obj, subprocess.run(cmd, capture_output=True, text=True)
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        early, temps = None, [t for e in ("-h*", ".hip-h*") for t in glob.glob(obj[:-2] + e)]
+        for t in temps:
+            if res.returncode == 0 and t.endswith("gfx950.s"):
+                with open(t) as f:
+                    early = _matrix_waits.early_reads(f.read())
+            os.remove(t)
+        return obj, res, early
 
     with ThreadPoolExecutor(min(8, len(SOURCES))) as ex:
         results = list(ex.map(compile_one, SOURCES))
     errs = []
-    for src, (obj, res) in zip(SOURCES, results):
+    for src, (obj, res, early) in zip(SOURCES, results):
         lines = [l for l in res.stderr.splitlines() if "packed-fp32-ops" not in l]
         if (src in NO_SCRATCH or src in NO_VECTOR_SPILL) and res.returncode == 0:
             spills = _spills(src, lines)
@@ -75,9 +90,11 @@ def build(force: bool = True, verbose: bool = False) -> str:
         err = "\n".join(lines)
         if res.returncode != 0:
             raise RuntimeError("hipcc failed:\n" + err)
+        if early is None or early:
+            raise RuntimeError(f"{src}: matrix results are read too early, or there is no assembly to look at\n" + "\n".join(early or []))
         if err.strip():
             errs.append(err)
-    link = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + [obj for obj, _ in results] + ["-o", LIB]
+    link = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + [obj for obj, _, _ in results] + ["-o", LIB]
     if verbose:
         print(" ".join(link))
     res = subprocess.run(link, capture_output=True, text=True)

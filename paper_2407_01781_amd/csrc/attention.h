@@ -225,6 +225,14 @@ template <int DT> __device__ __forceinline__ uint32_t not_finite(uint32_t w) {  
     if (DT == FX_F16) return ((w & 0x7C007C00u) + 0x04000400u) & 0x80008000u;
     return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
 }
+// As many wait states as any matrix instruction needs before its result is read.  Behind a loop, whose end and branches meet: the
+// compiler has counted the states of one such path and not of a shorter one.
+__device__ __forceinline__ void matrix_results_ready() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_nop 15\n\ts_nop 2");
+#endif
+    __builtin_amdgcn_sched_barrier(0);
+}
 // The lane's number, made where it is used: what hangs on it is not kept in registers through the loop
 __device__ __forceinline__ int lane_here() {
     int lane = threadIdx.x & 63;

@@ -182,6 +182,7 @@ __global__ __launch_bounds__(64 * W, least_waves_of(DP * AttnType<DT>::ES, W == 
         if (KT == 64 && (W > 2 || key0 + 32 < seen_wave)) w.template blocks<2>(kt, vt, 0, key0, masked, last);
         else w.template blocks<1>(kt, vt, 0, key0, masked, last);
     }
+    matrix_results_ready();
     w.sum += other_half(w.sum);
     if (odd) add_not_finite<DT>(w.acc, vb, a.v.ld, diagonal * KT, seen_wave, last, a.dim_bytes, lane_here());
     w.store(a, row, p.nq, p.q0, head);
@@ -253,6 +254,7 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves(DP * AttnType<DT>::ES)) v
             if (j + KS < n) load(j + KS, 0);
         }
     }
+    matrix_results_ready();
     w.sum += other_half(w.sum);
 #pragma unroll
     for (int h = KS / 2; h >= 1; h /= 2) {

@@ -210,6 +210,7 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
         if (KT == 64 && (W > 2 || key0 + 32 < seen_wave)) w.template blocks<2>(kt, vt, key0, masked, last, odd_keys);
         else w.template blocks<1>(kt, vt, key0, masked, last, odd_keys);
     }
+    matrix_results_ready();
     if (odd) w.keys_again(args_here(), p, head, row, diagonal * KT, seen_wave, last);
     w.store(a, p, head, row);
 #endif
@@ -284,6 +285,7 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves(DP * AttnType<DT>::ES)) v
             if (j + KS < n) load(j + KS, 0);
         }
     }
+    matrix_results_ready();
     add_results<RG, KS>(smem, w.acc, rg, turn, lane);
     odd = __syncthreads_or(odd);
     if (turn == 0) {
@@ -484,6 +486,7 @@ __global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES <= 128 ? 3 : least_wa
             w.block(qt + LdsRows<RB>::row_at(t), ot + LdsRows<RB>::row_at(t), st + 2 * t, masked, key0 - shift - r, (uint32_t)(odd_rows >> t));
         }
     }
+    matrix_results_ready();
     if (odd)            // the same tiles of the workgroup's items
         for (int j = j0; j < j1; ++j) {
             const int of_head = j / per_head, row = begin + (j - of_head * per_head) * QT;
@@ -583,6 +586,7 @@ __global__ __launch_bounds__(64 * RG * KS, RG * KS == 4 && DP * AttnType<DT>::ES
             if (j + KS < n) next = load(0);
         }
     }
+    matrix_results_ready();
     add_results<RG, KS>(smem, w.gk, rg, turn, lane);
     add_results<RG, KS>(smem, w.gv, rg, turn, lane);
     odd = __syncthreads_or(odd);
