@@ -42,6 +42,28 @@ __device__ __forceinline__ void without(uint64_t odd, int half, f32x16& x, f32x1
         if (mine >> (8 * (r >> 2) + (r & 3)) & 1) x[r] = y[r] = 0.f;
 }
 
+// ------------------------------------------------------------------ small gradients of scores in fp16
+// A gradient of a score, P dP, is about the loss gradient's size over the number of keys: in fp16, whose least number is 2^-24, it
+// would lose its digits or be 0 where gq and gk are far above that.  A row (of gq; a key of gk) takes its gradients of scores times a power of
+// two, 2^lift, that follows the largest so far: at least 2^11 and at most 2^15, so that what is lost is 2^-36 of the largest; its sums are
+// divided by it at their end.  The other types have fp32's exponents and no factor.  (131,072 x 4 x 64 in windows of 1,024: 617 us without, 674.)
+constexpr float kMostLifted = 0x1p15f;
+template <int DT> constexpr int first_lift() { return DT == FX_F16 ? 60 : 0; }
+
+// The gradients of scores of which one is too large for its lane's factor: by how much that comes down, as a power of two.  Infinities
+// stay what they are and are not followed.
+template <int NB> __device__ __forceinline__ int lower_by(const f32x16* x) {
+    float big = 0.f;
+#pragma unroll
+    for (int t = 0; t < NB; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) big = fmaxf(big, finite(x[t][r]) ? fabsf(x[t][r]) : 0.f);
+    const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(big), __float_as_uint(big), false, false);
+    big = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
+    return big > kMostLifted ? (int)(__float_as_uint(big) >> 23) - 127 - 11 : 0;
+}
+__device__ __forceinline__ float two_to(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }       // -126 .. 127
+
 // ------------------------------------------------------------------ gradients of the queries
 template <int DT, int DP, bool TINY = false> struct GqWave {
     typedef BwdShape<DT, DP> S;
@@ -52,7 +74,7 @@ template <int DT, int DP, bool TINY = false> struct GqWave {
     OwnRows<DT, S::STEPS> q, go;
     f32x16 acc[S::COLS];
     float lse2, glse, delta, c;
-    int half, part;
+    int half, part, lift;
     bool one_key, one_tile, tiny;
 
     // A row that sees one key has dS = glse whatever it holds; the rounding of out would leave something.  Where a sequence's keys
@@ -78,6 +100,7 @@ template <int DT, int DP, bool TINY = false> struct GqWave {
         one_key = p.nk == 1;
         one_tile = p.nk <= tile_keys;
         tiny = p.nk <= kTinyRows;
+        lift = first_lift<DT>();
         if (one_key) delta = 0.f;
         q.load(a.q.p + (int64_t)p.q0 * a.q.ld + head * a.q.hs, a.q.ld, row0, p.nq, a.dim_bytes, lane, a.negative);
 #pragma unroll
@@ -87,6 +110,7 @@ template <int DT, int DP, bool TINY = false> struct GqWave {
     // odd: keys that are not finite, whose place in the tile has zeros (rows_again)
     template <int NB> __device__ __forceinline__ void blocks(const lds_byte* kt, const lds_byte* vt, int key0, bool masked, int last, uint64_t odd) {
         f32x16 p[NB], dp[NB];
+        const float from = DT == FX_F16 ? (float)lift - lse2 : -lse2;         // the factor is the weights'
 #pragma unroll
         for (int t = 0; t < NB; ++t) {
             p[t] = dp[t] = f32x16(0.f);
@@ -96,7 +120,7 @@ template <int DT, int DP, bool TINY = false> struct GqWave {
             for (int i = 0; i < S::STEPS; ++i) dp[t] = Elem<T>::mma(rows_of(vt, t * 32, i), go.x[i], dp[t]);
             if (one_key) dp[t] = f32x16(0.f);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) p[t][r] = __builtin_amdgcn_exp2f(fmaf(p[t][r], c, -lse2));
+            for (int r = 0; r < 16; ++r) p[t][r] = __builtin_amdgcn_exp2f(fmaf(p[t][r], c, from));
         }
         if (masked) {
             const int left = last - key0 - 4 * half;
@@ -117,13 +141,35 @@ template <int DT, int DP, bool TINY = false> struct GqWave {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) delta = fmaf(p[t][r], dp[t][r], delta);
             delta += other_half(delta);
+            if (DT == FX_F16) delta *= two_to(-lift);
         }
         const float off = delta - glse;
+        if constexpr (DT == FX_F16) {
+            float big = 0.f;
+#pragma unroll
+            for (int t = 0; t < NB; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    p[t][r] *= dp[t][r] - off;
+                    big = fmaxf(big, fabsf(p[t][r]));
+                }
+            if (__any(big > kMostLifted)) {
+                const int by = lower_by<NB>(p);
+                const float f = two_to(-by);
+                lift -= by;
+#pragma unroll
+                for (int t = 0; t < NB; ++t) p[t] *= f;
+#pragma unroll
+                for (int k = 0; k < S::COLS; ++k) acc[k] *= f;
+            }
+        }
 #pragma unroll
         for (int t = 0; t < NB; ++t) {
             Weights<DT> w;
+            if constexpr (DT != FX_F16) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) p[t][r] *= dp[t][r] - off;
+                for (int r = 0; r < 16; ++r) p[t][r] *= dp[t][r] - off;
+            }
             w.set(p[t]);
 #pragma unroll
             for (int k = 0; k < S::COLS; ++k) columns(acc[k], kt + part * S::kPart, t * 32, k, w);
@@ -146,6 +192,14 @@ template <int DT, int DP, bool TINY = false> struct GqWave {
             const float dp = one_key ? 0.f : dot_rows<DT>(row_of_head(a.gout, mine, head), row_of_head(a.v, p.k0 + key, kv_head), a.dim_bytes, lane >> 5);
             const float w = __builtin_amdgcn_exp2f(fmaf(s, a.negative ? -a.c : a.c, -lse2));
             add_row<DT>(acc, kr, w * (dp - (delta - glse)), key <= last, part * S::COLS, a.dim_bytes, lane >> 5);
+        }
+    }
+
+    // behind the last block
+    __device__ __forceinline__ void end() {
+        if constexpr (DT == FX_F16) {
+#pragma unroll
+            for (int k = 0; k < S::COLS; ++k) acc[k] *= two_to(-lift);
         }
     }
 
@@ -211,6 +265,7 @@ __global__ __launch_bounds__(64 * W, least_waves(DP * AttnType<DT>::ES)) void k_
         else w.template blocks<1>(kt, vt, key0, masked, last, odd_keys);
     }
     matrix_results_ready();
+    w.end();
     if (odd) w.keys_again(args_here(), p, head, row, diagonal * KT, seen_wave, last);
     w.store(a, p, head, row);
 #endif
@@ -286,6 +341,7 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves(DP * AttnType<DT>::ES)) v
         }
     }
     matrix_results_ready();
+    w.end();
     add_results<RG, KS>(smem, w.acc, rg, turn, lane);
     odd = __syncthreads_or(odd);
     if (turn == 0) {
@@ -304,7 +360,7 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
     ColumnProduct<DT, RB> columns;
     OwnRows<DT, S::STEPS> k, v;
     f32x16 gk[S::COLS], gv[S::COLS];
-    float c;
+    float c, lift;
     int half, part;
     bool one_key, tiny;
 
@@ -314,6 +370,7 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
         c = a.c;
         one_key = p.nk == 1;
         tiny = p.nq * a.group <= kTinyRows;
+        lift = two_to(first_lift<DT>());
         k.load(a.k.p + (int64_t)p.k0 * a.k.ld + kv_head * a.k.hs, a.k.ld, key0, p.nk, a.dim_bytes, lane, a.negative);
         v.load(a.v.p + (int64_t)p.k0 * a.v.ld + kv_head * a.v.hs, a.v.ld, key0, p.nk, a.dim_bytes, lane);
         rows_of.init(lane);
@@ -350,6 +407,21 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
                 if (8 * (r >> 2) + (r & 3) < first) p[r] = ds[r] = 0.f;
         }
         if (odd) without(odd, half, p, ds);
+        if constexpr (DT == FX_F16) {
+            float big = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                ds[r] *= lift;
+                big = fmaxf(big, fabsf(ds[r]));
+            }
+            if (__any(big > kMostLifted)) {
+                const float f = two_to(-lower_by<1>(&ds));
+                lift *= f;
+                ds *= f;
+#pragma unroll
+                for (int i = 0; i < S::COLS; ++i) gk[i] *= f;
+            }
+        }
         Weights<DT> wp, wd;
         wp.set(p);
         wd.set(ds);
@@ -381,6 +453,14 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
             const bool sees = row + p.nk - p.nq >= key;
             add_row<DT>(gk, qr, w * (dp - stat[1]), sees, part * S::COLS, a.dim_bytes, lane >> 5);
             add_row<DT>(gv, gr, w, sees, part * S::COLS, a.dim_bytes, lane >> 5);
+        }
+    }
+
+    // behind the last block
+    __device__ __forceinline__ void end() {
+        if constexpr (DT == FX_F16) {
+#pragma unroll
+            for (int i = 0; i < S::COLS; ++i) gk[i] *= 1.f / lift;
         }
     }
 
@@ -426,7 +506,7 @@ template <int ROWS> __device__ __forceinline__ void load_stats(const AttnArgs& a
 }
 
 template <int DT, int DP, int W>
-__global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES <= 128 ? 3 : least_waves_of(DP * AttnType<DT>::ES, W == 4)) void k_attention_gkv(AttnArgs a) {
+__global__ __launch_bounds__(64 * W, W == 4 && DP * AttnType<DT>::ES <= 128 ? 3 : least_waves_of(DP * AttnType<DT>::ES, W == 4)) void k_attention_gkv(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef BwdShape<DT, DP> S;
     constexpr int RB = S::RB, QT = S::QT;
@@ -487,6 +567,7 @@ __global__ __launch_bounds__(64 * W, DP * AttnType<DT>::ES <= 128 ? 3 : least_wa
         }
     }
     matrix_results_ready();
+    w.end();
     if (odd)            // the same tiles of the workgroup's items
         for (int j = j0; j < j1; ++j) {
             const int of_head = j / per_head, row = begin + (j - of_head * per_head) * QT;
@@ -526,7 +607,7 @@ __global__ __launch_bounds__(64 * W) void k_attention_join_keys(AttnArgs a) {
 
 // For few keys: RG blocks of 32, for each of which KS waves take the blocks of 32 queries of all heads in turn
 template <int DT, int DP, int RG, int KS>
-__global__ __launch_bounds__(64 * RG * KS, RG * KS == 4 && DP * AttnType<DT>::ES <= 128 ? 3 : least_waves_of(DP * AttnType<DT>::ES, false)) void k_attention_gkv_few(AttnArgs a) {
+__global__ __launch_bounds__(64 * RG * KS, least_waves_of(DP * AttnType<DT>::ES, false)) void k_attention_gkv_few(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef BwdShape<DT, DP> S;
     constexpr int RB = S::RB, QT = 32, NB = S::template buffers<KS>();
@@ -587,6 +668,7 @@ __global__ __launch_bounds__(64 * RG * KS, RG * KS == 4 && DP * AttnType<DT>::ES
         }
     }
     matrix_results_ready();
+    w.end();
     add_results<RG, KS>(smem, w.gk, rg, turn, lane);
     add_results<RG, KS>(smem, w.gv, rg, turn, lane);
     odd = __syncthreads_or(odd);
