@@ -48,6 +48,9 @@ __device__ __forceinline__ void without(uint64_t odd, int half, f32x16& x, f32x1
 // two, 2^lift, that follows the largest so far: at least 2^11 and at most 2^15, so that what is lost is 2^-36 of the largest; its sums are
 // divided by it at their end.  The other types have fp32's exponents and no factor.  (131,072 x 4 x 64 in windows of 1,024: 617 us without, 674.)
 constexpr float kMostLifted = 0x1p15f;
+// A weight of gv is at most 1 and about 1 / keys: the statistics' lse is less by 15, so that weights and with them both gradients are
+// 2^15 of themselves until they are stored, and what is lost of a weight is 2^-40
+template <int DT> constexpr int weight_lift() { return DT == FX_F16 ? 15 : 0; }
 template <int DT> constexpr int first_lift() { return DT == FX_F16 ? 60 : 0; }
 
 // The gradients of scores of which one is too large for its lane's factor: by how much that comes down, as a power of two.  Infinities
@@ -205,7 +208,7 @@ template <int DT, int DP, bool TINY = false> struct GqWave {
 
     __device__ __forceinline__ void store(const AttnArgs& a, const Pair& p, int head, int row) {
         if (row >= p.nq) return;
-        if (half == 0 && part == 0) *(f32x2*)(a.stats + 2 * (head * a.rows_q + p.q0 + row)) = f32x2{lse2, delta - glse};
+        if (half == 0 && part == 0) *(f32x2*)(a.stats + 2 * (head * a.rows_q + p.q0 + row)) = f32x2{lse2 - weight_lift<DT>(), delta - glse};
         if (!a.gq.p) return;
         unsigned char* out = a.gq.p + (int64_t)(p.q0 + row) * a.gq.ld + head * a.gq.hs;
         const float f = a.negative ? -a.scale : a.scale;
@@ -356,6 +359,8 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
     typedef BwdShape<DT, DP> S;
     typedef typename AttnType<DT>::T T;
     static constexpr int RB = S::RB;
+    static constexpr float kDown = DT == FX_F16 ? 0x1p-15f : 1.f;
+    static_assert(weight_lift<FX_F16>() == 15, "kDown undoes it");
     RowReader<DT, RB> rows_of;
     ColumnProduct<DT, RB> columns;
     OwnRows<DT, S::STEPS> k, v;
@@ -469,30 +474,30 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
         if (key >= p.nk) return;
         const int dim_bytes = a.dim_bytes / AttnType<DT>::ES * 4;
         unsigned char* to = (unsigned char*)a.sums + (((int64_t)share * a.kv_heads + kv_head) * a.rows_k + p.k0 + key) * 2 * dim_bytes;
-        const float f = a.negative ? -a.scale : a.scale;
+        const float f = (a.negative ? -a.scale : a.scale) * kDown;
 #pragma unroll
         for (int i = 0; i < S::COLS; ++i) {
             store_columns<FX_F32>(gk[i], f, to, part * S::COLS + i, dim_bytes, lane_here() >> 5);
-            store_columns<FX_F32>(gv[i], 1.f, to + dim_bytes, part * S::COLS + i, dim_bytes, lane_here() >> 5);
+            store_columns<FX_F32>(gv[i], kDown, to + dim_bytes, part * S::COLS + i, dim_bytes, lane_here() >> 5);
         }
     }
     __device__ __forceinline__ void store(const AttnArgs& a, const Pair& p, int kv_head, int key) {
         if (key >= p.nk) return;
         if (a.gk.p) {
             unsigned char* out = a.gk.p + (int64_t)(p.k0 + key) * a.gk.ld + kv_head * a.gk.hs;
-            const float f = a.negative ? -a.scale : a.scale;
+            const float f = (a.negative ? -a.scale : a.scale) * kDown;
 #pragma unroll
             for (int i = 0; i < S::COLS; ++i) store_columns<DT>(gk[i], f, out, part * S::COLS + i, a.dim_bytes, lane_here() >> 5);
         }
         if (a.gv.p) {
             unsigned char* out = a.gv.p + (int64_t)(p.k0 + key) * a.gv.ld + kv_head * a.gv.hs;
 #pragma unroll
-            for (int i = 0; i < S::COLS; ++i) store_columns<DT>(gv[i], 1.f, out, part * S::COLS + i, a.dim_bytes, lane_here() >> 5);
+            for (int i = 0; i < S::COLS; ++i) store_columns<DT>(gv[i], kDown, out, part * S::COLS + i, a.dim_bytes, lane_here() >> 5);
         }
     }
 };
 
-// lse (base 2) and delta of ROWS rows, as the first kernel left them, into LDS; zeros for a row that does not exist, whose query and
+// lse (base 2, less weight_lift) and delta of ROWS rows, as the first kernel left them, into LDS; zeros for a row that does not exist, whose query and
 // gradient are zeros too: it adds nothing
 template <int ROWS> __device__ __forceinline__ void load_stats(const AttnArgs& a, lds_byte* to, int head, int q0, int row0, int nq, int lane) {
 #if defined(__HIP_DEVICE_COMPILE__)

@@ -32,3 +32,20 @@ def test_small_gradients_of_the_output(lens, heads, kv_heads, d, causal, std):
     for name, x, y, e in list(zip(("gq", "gk", "gv"), got, ref[:3], ref[3:])):
         if name != "gv":            # there it is the weight's own, below
             A.check(_f64(x), y, e, "f16", name)
+
+
+@pytest.mark.parametrize("queries,keys,heads,kv_heads,d,causal", [([64], [262_144], 1, 1, 64, False), ([40, 3], [90_000, 150_000], 2, 1, 32, True), ([130], [70_000], 2, 2, 128, True)])
+def test_small_weights_of_the_gradients(queries, keys, heads, kv_heads, d, causal):
+    """Weights of some 2^-18: what the kernels lose of one is 2^-40 at most, and of a gradient of a score 2^-36 of its row's largest, here 2^-10."""
+    bq, jq = _joff(queries)
+    bk, jk = _joff(keys)
+    seqs, kv = fx.build_sequences(jq), fx.build_sequences(jk)
+    q, q64 = draw(1, bq[-1], heads, d, "f16")
+    (k, k64), (v, v64) = (draw(s, bk[-1], kv_heads, d, "f16") for s in (2, 3))
+    go, go64 = draw(4, bq[-1], heads, d, "f16", std=50.0)
+    out, lse = fx.attention_fwd(seqs, q, k, v, causal=causal, kv_seqs=kv)
+    got = fx.attention_bwd(seqs, q, k, v, out, lse, go, causal=causal, kv_seqs=kv)
+    with mock.patch.dict(A.LEAST, f16=2.0 ** -40):
+        ref = A.attention_grad(q64, k64, v64, go64, bq, bk, causal, d ** -0.5, "f16")
+    for name, x, y, e in zip(("gq", "gk", "gv"), got, ref[:3], ref[3:]):
+        A.check(_f64(x), y, e, "f16", name)
