@@ -576,7 +576,8 @@ fx_status fx_dropout(const void* d_x, int64_t ld_x, fx_dtype dt, int64_t rows, i
  * j runs over the keys of i's sequence.  With `causal` the last query stands at the last key and each before it one key earlier:
  * query i of n sees key j of m where n - i <= m - j.  A row that sees no key gets out = 0, lse = -inf, and gradients of 0.
  * Products, maxima and sums are fp32; in 16 bits exp(s - m) is rounded to the type before its product with v (m close to the
- * row's maximum, the sum of the weights is of the unrounded ones), every output once.  A row's results depend on the keys that it sees alone,
+ * row's maximum, the sum of the weights is of the unrounded ones; in FX_F16 times a power of two, so that a weight of less than 2^-25 of the largest loses
+ * 2^-36 of that at most), every output once.  A row's results depend on the keys that it sees alone,
  * a key's gradients on the queries that see it: infinities and NaN of others, of a causal sequence's later rows too, add nothing.
  * (Where a causal sequence holds such a value, the rows around it take longer: a few microseconds for each such value near a row's own
  * position, whatever the sequence's length.)

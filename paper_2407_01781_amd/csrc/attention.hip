@@ -17,6 +17,9 @@ namespace fx {
 template <int DT, int DP, bool TINY = false> struct FwdWave {
     typedef typename AttnType<DT>::T T;
     static constexpr int RB = DP * AttnType<DT>::ES, STEPS = RB / 32, COLS = DP / 32;
+    // By how many powers of two a weight may pass the reference's before that follows, and how many lie between the reference's own weight and 1.
+    // fp16 ends at 2^-24: its largest weights are 2^11 to 2^15, and what a smaller one loses is 2^-36 of them.
+    static constexpr float kLag = DT == FX_F16 ? 4.f : 8.f, kUp = DT == FX_F16 ? 11.f : 0.f;
     RowReader<DT, RB> rows_of;
     ColumnProduct<DT, RB> columns;
     OwnRows<DT, STEPS> q;
@@ -61,10 +64,10 @@ template <int DT, int DP, bool TINY = false> struct FwdWave {
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
         top = fmaxf(top, other_half(top));
-        // The maximum that weights are relative to follows the row's own only when that has grown by a factor of 2^8: acc and
-        // sum are exact in whichever they are, a weight is at most 2^8, and few tiles have to scale what is there.
-        if (__any(top * c > m * c + 8.f)) rescale(fmaxf(m, top));
-        const float mc = m == -INFINITY ? 0.f : m * c;
+        // The maximum that weights are relative to follows the row's own only when that has grown by a factor of 2^kLag: acc and
+        // sum are exact in whichever they are, a weight is at most 2^(kLag + kUp), and few tiles have to scale what is there.
+        if (__any(top * c > m * c + kLag)) rescale(fmaxf(m, top));
+        const float mc = m == -INFINITY ? 0.f : base(m);
         float part = 0.f;
 #pragma unroll
         for (int t = 0; t < NB; ++t) {
@@ -86,6 +89,8 @@ template <int DT, int DP, bool TINY = false> struct FwdWave {
         sum += part;
     }
 
+    // the exponent of a weight of 1 (base 2), where the reference is x
+    __device__ __forceinline__ float base(float x) const { return DT == FX_F16 ? fmaf(x, c, -kUp) : x * c; }
     __device__ __forceinline__ void rescale(float to) {
         const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - to) * c);
         m = to;
@@ -94,13 +99,14 @@ template <int DT, int DP, bool TINY = false> struct FwdWave {
         for (int k = 0; k < COLS; ++k) acc[k] *= f;
     }
 
+    __device__ __forceinline__ float lse() const { return DT == FX_F16 ? (base(m) + kUp) + __builtin_amdgcn_logf(sum * 0x1p-11f) : m * c + __builtin_amdgcn_logf(sum); }
     __device__ __forceinline__ void store(const AttnArgs& a, int row, int nq, int q0, int head) {
         if (row >= nq) return;
         const float f = sum == 0.f ? 0.f : 1.f / sum;
         unsigned char* out = a.out.p + (int64_t)(q0 + row) * a.out.ld + head * a.out.hs;
 #pragma unroll
         for (int k = 0; k < COLS; ++k) store_columns<DT>(acc[k], f, out, k, a.dim_bytes, half);
-        if (a.lse && half == 0) a.lse[head * a.rows_q + q0 + row] = sum == 0.f ? -INFINITY : (m * c + __builtin_amdgcn_logf(sum)) * kLn2;
+        if (a.lse && half == 0) a.lse[head * a.rows_q + q0 + row] = sum == 0.f ? -INFINITY : lse() * kLn2;
     }
 };
 

@@ -49,3 +49,27 @@ def test_small_weights_of_the_gradients(queries, keys, heads, kv_heads, d, causa
         ref = A.attention_grad(q64, k64, v64, go64, bq, bk, causal, d ** -0.5, "f16")
     for name, x, y, e in zip(("gq", "gk", "gv"), got, ref[:3], ref[3:]):
         A.check(_f64(x), y, e, "f16", name)
+
+
+def _one_leads(n, heads, d, nats, dtype, rows=1):
+    """Queries and keys of which key 5 leads the others by so many nats, all in a channel of their own; values of about 1, its own 0."""
+    q, _ = draw(1, rows, heads, d, dtype, std=0.02)
+    k, _ = draw(2, n, 1, d, dtype, std=0.02)
+    v, _ = draw(3, n, 1, d, dtype, std=0.1)
+    q[..., 0], k[..., 0], k[5, :, 0] = d ** 0.5, 0.0, nats
+    v += 1
+    v[5] = 0
+    return q, k, v
+
+
+@pytest.mark.parametrize("n,nats,heads,d,rows", [(100_000, 15.0, 1, 64, 40), (100_000, 17.0, 2, 32, 200), (60_000, 19.0, 1, 128, 300), (3_000, 16.0, 4, 64, 2_000), (60, 14.0, 2, 64, 3)])
+def test_one_key_leads(n, nats, heads, d, rows):
+    """What a weight loses below fp16's normal numbers is 2^-36 of the row's largest at most, however many keys there are."""
+    q, k, v = _one_leads(n, heads, d, nats, "f16", rows)
+    f = [_f64(x) for x in (q, k, v)]
+    seqs, kv = fx.build_sequences([[0, rows]]), fx.build_sequences([[0, n]])
+    out, lse = fx.attention_fwd(seqs, q, k, v, kv_seqs=kv)
+    with mock.patch.dict(A.LEAST, f16=2.0 ** -36 / 256):            # the bound takes 256 of it, of the row's largest
+        ro, rl, bo, bl = A.attention(*f, [0, rows], [0, n], False, d ** -0.5, "f16")
+    A.check(_f64(lse), rl, bl, "f32", "lse")
+    A.check(_f64(out), ro, bo, "f16", "out")
