@@ -623,7 +623,8 @@ fx_status fx_attention_bwd(const fx_attention* a, const void* d_out, int64_t ld_
  * FX_E4M3, none otherwise).
  * fx_attention_step: out_b = attention of query row b over positions 0 .. d_len[b]-1 of sequence b (no key: 0 and lse = -inf), d_lse
  * [rows, heads] or NULL.  `most` bounds the lengths on the host (longer ones are cut there), 0: table_cols * page_rows; the split of the work goes by it.
- * The weights exp(s - m) have 16 bits at least where they meet values (22 in FX_F16, 24 where q is FX_F32).
+ * The weights exp(s - m) have 16 bits at least where they meet values (24 where q is FX_F32; over FX_F16 22 down to 2^-18 of the largest, and below that
+ * what a weight loses is 2^-40 of the largest).
  * FX_ERANGE beyond 2^31-1 rows of pages and heads, 2^31-1 rows of a call, 2^31-8193 positions of a step's table, 2^24-1 rows
  * times key heads of a step (times the sixteens of query heads that share one), 65535 heads.
  * None of the calls waits for the stream; lengths, starts and the table are read when the kernels run, so that a captured step follows them. */

@@ -140,7 +140,8 @@ __global__ __launch_bounds__(256) void k_cache_read(CacheArgs c, CacheRows a) {
 // Bound by HBM: 986,880 positions x 2 key heads x 64 bf16 in 92 us (5.5 TB/s), and 6 for the join; 64 sequences of up to 32,768 positions,
 // 4 x 128 in 8 bits, in 235 us with the join (4.4 TB/s).
 // Weights are split into a leading and a trailing part (three for fp32 queries over 8 bits), so that the product with 16-bit
-// values loses nothing that the output would show.
+// values loses nothing that the output would show.  fp16 ends at 2^-24: over values in it weights are taken times 2^15, and what both parts lose is 2^-40 of
+// the largest.
 constexpr int kStepTile = 32, kStepHeads = 16;
 
 struct StepArgs {
@@ -166,6 +167,7 @@ template <int DT, bool E4M3, int DP> struct StepShape {
     static constexpr int KL = DP * SB / 64;                        // 16-byte loads of a key by a lane
     static constexpr int QP = !E4M3 || DT == FX_BF16 ? 1 : DT == FX_F16 ? 2 : 3;    // parts of a query
     static constexpr int PP = E4M3 && DT == FX_F32 ? 3 : 2;                        // parts of a weight
+    static constexpr float kUp = DT == FX_F16 && !E4M3 ? 0x1p15f : 1.f;            // of a weight, whose own is at most 1
     static constexpr int kResident = step_resident(DT, E4M3, DP);
     // waves of a workgroup that has a sequence to itself: as many as the registers hold without spills
     static constexpr int kMany = DP > 128 ? 4 : DP > 64 || kWide || (E4M3 && DT != FX_BF16) ? 8 : 16;
@@ -365,7 +367,7 @@ __global__ __launch_bounds__(64 * W, RESIDENT) void k_attention_step(StepArgs a)
         const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            s[i] = __builtin_amdgcn_exp2f(s[i] - base);
+            s[i] = __builtin_amdgcn_exp2f(s[i] - base) * S::kUp;
             sum += s[i];
         }
         if constexpr (S::kWide) {
@@ -408,6 +410,11 @@ __global__ __launch_bounds__(64 * W, RESIDENT) void k_attention_step(StepArgs a)
     }
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
+    if (S::kUp != 1.f) {
+        sum *= 1.f / S::kUp;
+#pragma unroll
+        for (int j = 0; j < VE; ++j) acc[j] *= 1.f / S::kUp;
+    }
     // the waves' results joined: three quarters of them put theirs into LDS, the others take three each
     float* shared = (float*)smem;
     constexpr int SLOT = DP * kStepHeads + 2 * kStepHeads;

@@ -73,3 +73,57 @@ def test_one_key_leads(n, nats, heads, d, rows):
         ro, rl, bo, bl = A.attention(*f, [0, rows], [0, n], False, d ** -0.5, "f16")
     A.check(_f64(lse), rl, bl, "f32", "lse")
     A.check(_f64(out), ro, bo, "f16", "out")
+
+
+def _cached(k, v, dtype, store=None, page=256):
+    """Rows of one sequence in a cache, and its table."""
+    n, kvh, d = k.shape
+    pages = -(-n // page)
+    cache = fx.KVCache.empty(pages, page, kvh, d, store or k.dtype)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").flip(0)[None].contiguous()
+    fx.cache_write(cache, table, torch.zeros(1, dtype=torch.int32, device="cuda"), k, v, seqs=fx.build_sequences([[0, n]]))
+    return cache, table
+
+
+# half units of what a step's weights keep where they meet values: two parts of the cache's type, three of bf16 with fp32 queries over 8 bits
+STEP = {("bf16", None): 2.0 ** -16, ("f16", None): 2.0 ** -22, ("f32", None): 2.0 ** -24, ("bf16", "e4m3"): 2.0 ** -16, ("f16", "e4m3"): 2.0 ** -16, ("f32", "e4m3"): 2.0 ** -24}
+
+
+def _step_bounds(q, k, v, bounds, dtype, store):
+    """Of one row over all keys of its sequence: weights as the step has them; where they are fp16 they lose 2^-40 of the largest beside that."""
+    with mock.patch.dict(A.HALF, step=STEP[dtype, store]), mock.patch.dict(A.LEAST, step=2.0 ** -40 / 256 if dtype == "f16" and not store else 0.0):
+        return A.attention(q, k, v, np.arange(len(bounds)), bounds, False, q.shape[2] ** -0.5, "step")
+
+
+@pytest.mark.parametrize("n,nats,heads,d,dtype", [(986_880, 15.0, 1, 64, "f16"), (986_880, 17.0, 2, 16, "f16"), (100_000, 20.0, 1, 64, "f16"), (900, 15.0, 8, 128, "f16"), (100_000, 20.0, 1, 64, "bf16"), (5_000, 17.0, 2, 200, "f16")])
+def test_one_key_leads_a_step(n, nats, heads, d, dtype):
+    q, k, v = _one_leads(n, heads, d, nats, dtype)
+    cache, table = _cached(k, v, dtype)
+    out, lse = fx.attention_step(cache, table, torch.tensor([n], dtype=torch.int32, device="cuda"), q)
+    ro, rl, bo, bl = _step_bounds(_f64(q), _f64(k), _f64(v), [0, n], dtype, None)
+    A.check(_f64(lse), rl.T, bl.T, "f32", "lse")
+    A.check(_f64(out), ro, bo, dtype, "out")
+
+
+@pytest.mark.parametrize("dtype,store", list(STEP))
+@pytest.mark.parametrize("n,heads,d", [(2, 1, 64), (7, 2, 64), (40, 3, 128), (300, 1, 33), (3000, 2, 256), (9, 16, 16)])
+def test_digits_of_a_step(n, heads, d, dtype, store):
+    """Values that nearly cancel show what the weights are rounded to: in one part it would be 2^-9 or 2^-12 of the sum's size."""
+    seqs = 5
+    bounds, jo = _joff([n] * seqs)
+    (q, q64), (k, k64), (v, v64) = (draw(s, m, h, d, dtype) for s, m, h in ((1, seqs, heads), (2, n * seqs, 1), (3, n * seqs, 1)))
+    to = torch.float8_e4m3fn if store else v.dtype
+    held = lambda x: A.quantised(x) if store else x
+    for i in range(seqs):               # the last value of each sequence cancels the others under the first head's weights
+        part = slice(i * n, i * n + n)
+        p = np.exp(d ** -0.5 * (held(k64[part, 0]) @ q64[i, 0]))
+        v64[i * n + n - 1, 0] = -(p[:-1] @ held(v64[part, 0])[:-1]) / p[-1]
+    v = torch.from_numpy(v64).to(v.dtype).cuda()
+    v64 = _f64(v)
+    page = 16
+    cache = fx.KVCache.empty(seqs * -(-n // page), page, 1, d, to)
+    table = torch.randperm(cache.k.shape[0], generator=torch.Generator().manual_seed(1)).to(torch.int32).view(seqs, -1).cuda()
+    fx.cache_write(cache, table, torch.zeros(seqs, dtype=torch.int32, device="cuda"), k, v, seqs=fx.build_sequences(jo))
+    out, _ = fx.attention_step(cache, table, torch.full((seqs,), n, dtype=torch.int32, device="cuda"), q)
+    ro, _, bo, _ = _step_bounds(q64, held(k64), held(v64), bounds, dtype, store)
+    A.check(_f64(out), ro, bo, dtype, "out")
