@@ -225,6 +225,11 @@ template <int DT> __device__ __forceinline__ uint32_t not_finite(uint32_t w) {  
     if (DT == FX_F16) return ((w & 0x7C007C00u) + 0x04000400u) & 0x80008000u;
     return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
 }
+// zeros in the place of values that are not finite
+template <int DT> __device__ __forceinline__ uint32_t finite_only(uint32_t w) {
+    const uint32_t bad = not_finite<DT>(w);
+    return w & ~(DT == FX_F32 ? (uint32_t)((int)bad >> 31) : (bad >> 15) * 0xFFFFu);
+}
 // As many wait states as any matrix instruction needs before its result is read.  Behind a loop, whose end and branches meet: the
 // compiler has counted the states of one such path and not of a shorter one.
 __device__ __forceinline__ void matrix_results_ready() {
@@ -254,13 +259,11 @@ template <int DT, int RB, int ROWS, int WAVES> __device__ __forceinline__ uint32
 #pragma unroll 1
     for (int piece = lane / R; piece < RB / 16; piece += LANES) {
         __attribute__((address_space(3))) u32x4* at = (__attribute__((address_space(3))) u32x4*)(tile + L::place(row, piece));
-        u32x4 w = *at, bad;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) bad[i] = not_finite<DT>(w[i]);
-        if (!(bad[0] | bad[1] | bad[2] | bad[3])) continue;
+        u32x4 w = *at;
+        if (!(not_finite<DT>(w[0]) | not_finite<DT>(w[1]) | not_finite<DT>(w[2]) | not_finite<DT>(w[3]))) continue;
         any = true;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] &= ~(DT == FX_F32 ? (uint32_t)((int)bad[i] >> 31) : (bad[i] >> 15) * 0xFFFFu);
+        for (int i = 0; i < 4; ++i) w[i] = finite_only<DT>(w[i]);
         *at = w;
     }
     asm volatile("" ::: "memory");

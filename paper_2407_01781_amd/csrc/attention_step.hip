@@ -3,6 +3,7 @@
 #include "cache_rows.h"
 
 #include <math.h>
+#include <type_traits>
 
 namespace fx {
 
@@ -162,12 +163,13 @@ constexpr int step_resident(int dt, bool e4m3, int dp) {
 
 template <int DT, bool E4M3, int DP> struct StepShape {
     static constexpr bool kWide = DT == FX_F32 && !E4M3;           // fp32 keys and values
+    static constexpr bool kF16 = DT == FX_F16 && !E4M3;            // products of fp16, of bf16 otherwise
     static constexpr int SB = E4M3 ? 1 : AttnType<DT>::ES;         // bytes of a stored element
     static constexpr int VE = DP / 16;                             // dimensions of a value's row that a lane loads
     static constexpr int KL = DP * SB / 64;                        // 16-byte loads of a key by a lane
     static constexpr int QP = !E4M3 || DT == FX_BF16 ? 1 : DT == FX_F16 ? 2 : 3;    // parts of a query
     static constexpr int PP = E4M3 && DT == FX_F32 ? 3 : 2;                        // parts of a weight
-    static constexpr float kUp = DT == FX_F16 && !E4M3 ? 0x1p15f : 1.f;            // of a weight, whose own is at most 1
+    static constexpr float kUp = kF16 ? 0x1p15f : 1.f;            // of a weight, whose own is at most 1
     static constexpr int kResident = step_resident(DT, E4M3, DP);
     // waves of a workgroup that has a sequence to itself: as many as the registers hold without spills
     static constexpr int kMany = DP > 128 ? 4 : DP > 64 || kWide || (E4M3 && DT != FX_BF16) ? 8 : 16;
@@ -206,7 +208,7 @@ __global__ __launch_bounds__(64 * W, RESIDENT) void k_attention_step(StepArgs a)
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef StepShape<DT, E4M3, DP> S;
     typedef typename AttnType<DT>::T T;
-    typedef Mma16<DT == FX_F16 && !E4M3> M;
+    typedef Mma16<S::kF16> M;
     constexpr int VE = S::VE, KL = S::KL, SB = S::SB, QP = S::QP, PP = S::PP;
     constexpr int VW = VE * SB >= 4 ? VE * SB / 4 : 1;             // words of a value's piece
     constexpr int KF = S::kWide ? KL : E4M3 ? 2 * KL : KL;         // operands of a key
@@ -276,6 +278,9 @@ __global__ __launch_bounds__(64 * W, RESIDENT) void k_attention_step(StepArgs a)
         const int page = col < (uint32_t)a.c.t.cols ? table[col] : -1;        // does not wait for the length
         return (int)pos < end ? row_in_page(a.c.t, page, pos, col, kv) : -1;
     };
+    // Once; and again where the sums are not finite: an infinity among the values that are seen, times a weight's trailing part, which may
+    // be 0 or negative, is not what it is times the weight.  `careful`: trailing parts meet zeros in such places.
+    auto sum_up = [&](auto careful) {
     int t = (int)from + wave * kStepTile;
     int row = row_of(t);
     for (; t < end; t += W * kStepTile) {
@@ -400,12 +405,32 @@ __global__ __launch_bounds__(64 * W, RESIDENT) void k_attention_step(StepArgs a)
                     u32x4 w;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], h ? 0x07060302 : 0x05040100);
-                    typename M::vec v;
+                    typename M::vec v, trailing;
                     __builtin_memcpy(&v, &w, 16);
+                    if (decltype(careful)::value)
 #pragma unroll
-                    for (int k = PP - 1; k >= 0; --k) acc[j + h] = M::mma(v, p[k], acc[j + h]);
+                        for (int e = 0; e < 4; ++e) w[e] = finite_only<S::kF16 ? FX_F16 : FX_BF16>(w[e]);
+                    __builtin_memcpy(&trailing, &w, 16);
+#pragma unroll
+                    for (int k = PP - 1; k >= 0; --k) acc[j + h] = M::mma(k ? trailing : v, p[k], acc[j + h]);
                 }
             }
+        }
+    }
+    };
+    sum_up(std::false_type{});
+    if constexpr (!S::kWide) {
+        bool odd = false;
+#pragma unroll
+        for (int j = 0; j < VE; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) odd |= !finite(acc[j][r]);
+        if (__any(odd)) {
+#pragma unroll
+            for (int j = 0; j < VE; ++j) acc[j] = f32x4(0.f);
+            top = -INFINITY;
+            sum = 0.f;
+            sum_up(std::true_type{});
         }
     }
     sum += __shfl_xor(sum, 16, 64);

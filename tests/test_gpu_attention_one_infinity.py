@@ -99,3 +99,37 @@ def test_seen_and_unseen(lens, kv_lens, heads, kv_heads, d, dtype, bad):
                     want = rg[2][k0:last].copy()
                     want[:, head // g, c] = bad
                     A.check(got[2][k0:last], want, rg[5][k0:last], dtype, "gv of keys that see it")
+
+
+def _seen(dtype, d, n, bad):
+    """Two queries over n keys each, values of which some are not finite, what comes of them and its bound."""
+    heads, kvh, seqs = 4, 2, 2
+    b, jo = _joff([n] * seqs)
+    (q, q64), (k, k64), (v, v64) = (draw(s, m, h, d, dtype) for s, m, h in ((1, seqs, heads), (2, n * seqs, kvh), (3, n * seqs, kvh)))
+    ro, _, bo, _ = A.attention(q64, k64, v64, np.arange(seqs + 1), b, False, d ** -0.5, dtype)
+    at = np.random.default_rng(n).integers(n, size=4)
+    want = ro.copy()
+    for i, c in enumerate((1, d - 1)):
+        v[at[i], 1, c] = bad
+        want[0, 2:, c] = bad
+    if n > 1:
+        v[n + (at[2] + 1) % n, 0, 2], v[n + at[2], 0, 2] = float("inf"), float("-inf")
+        want[1, :2, 2] = np.nan
+    return q, k, v, fx.build_sequences(jo), want, bo
+
+
+SEEN = [pytest.mark.parametrize("dtype,d", [("f16", 64), ("bf16", 40), ("f32", 64), ("bf16", 200), ("f16", 128)]),
+        pytest.mark.parametrize("n", [1, 2, 16, 17, 33, 700, 5000]), pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])]
+
+
+@SEEN[0]
+@SEEN[1]
+@SEEN[2]
+def test_values_that_a_step_sees(dtype, d, n, bad):
+    """An infinity in a value is what every row that sees it has there; two that differ in sign, or a NaN, are a NaN; the other channels are as without."""
+    q, k, v, keys, want, bound = _seen(dtype, d, n, bad)
+    cache = fx.KVCache.empty(2 * -(-n // 16), 16, 2, d, k.dtype)
+    table = torch.randperm(cache.k.shape[0], generator=torch.Generator().manual_seed(1)).to(torch.int32).view(2, -1).cuda()
+    fx.cache_write(cache, table, torch.zeros(2, dtype=torch.int32, device="cuda"), k, v, seqs=keys)
+    out, _ = fx.attention_step(cache, table, torch.full((2,), n, dtype=torch.int32, device="cuda"), q)
+    A.check(_f64(out), want, bound, dtype, "step")
