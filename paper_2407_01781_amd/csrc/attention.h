@@ -131,6 +131,17 @@ template <int DT, int STEPS> struct OwnRows {
     }
 };
 
+// Of one word of a tensor: the sign bits of the values that are not finite
+template <int DT> __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+    if (DT == FX_F32) return ((w & 0x7F800000u) + 0x00800000u) & 0x80000000u;
+    if (DT == FX_F16) return ((w & 0x7C007C00u) + 0x04000400u) & 0x80008000u;
+    return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+}
+// zeros in the place of values that are not finite
+template <int DT> __device__ __forceinline__ uint32_t finite_only(uint32_t w) {
+    const uint32_t bad = not_finite<DT>(w);
+    return w & ~(DT == FX_F32 ? (uint32_t)((int)bad >> 31) : (bad >> 15) * 0xFFFFu);
+}
 // A 32x32 result in its registers as the right operand of a product over its rows
 template <int DT> struct Weights;
 template <> struct Weights<FX_F32> {
@@ -150,11 +161,14 @@ template <int DT> struct Weights16 {
             __builtin_memcpy(&p[t], &w, 16);
         }
     }
-    // what the rounding of x left
+    // what the rounding of x left, of an infinity nothing
     __device__ __forceinline__ f32x16 rest(const f32x16& x) const {
         f32x16 y;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) y[r] = x[r] - (float)p[r >> 3][r & 7];
+        for (int r = 0; r < 16; ++r) {
+            const float rounded = (float)p[r >> 3][r & 7];
+            y[r] = fabsf(rounded) < INFINITY ? x[r] - rounded : 0.f;
+        }
         return y;
     }
 };
@@ -162,7 +176,8 @@ template <> struct Weights<FX_F16> : Weights16<FX_F16> {};
 template <> struct Weights<FX_BF16> : Weights16<FX_BF16> {};
 
 // A sum over up to so many rows takes along what the rounding of its weights left: over more their errors cancel as good as ever, in
-// a product with one or two they are the result's own, beside its rounding.
+// a product with one or two they are the result's own, beside its rounding.  What is left of a weight may be 0 or negative and meets zeros
+// in the place of infinities: those are in the product with the weight itself.
 constexpr int kTinyRows = 16;
 
 // acc += (columns 32 col .. 32 col + 31 of the 32 rows from row0 on)^T w, the result's rows the tile's columns
@@ -179,7 +194,8 @@ template <int DT, int RB> struct ColumnProduct {
             else a[e] = L::place(8 * e + 4 * half + (i >> 2), (lane >> 4 & 1) * 2 + ((i & 3) >> 1)) + (i & 1) * 8;
         }
     }
-    __device__ __forceinline__ void operator()(f32x16& acc, const lds_byte* tile, int row0, int col, const Weights<DT>& w) const {
+    // FINITE: with zeros in the place of what is not
+    template <bool FINITE = false> __device__ __forceinline__ void operator()(f32x16& acc, const lds_byte* tile, int row0, int col, const Weights<DT>& w) const {
         if constexpr (DT == FX_F32) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -193,7 +209,14 @@ template <int DT, int RB> struct ColumnProduct {
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
                     h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(tile + a[e] + L::row_at(row0 + 16 * t) + col * L::kSegment));
-                const s16x8 x = __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                s16x8 x = __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                if (FINITE) {
+                    u32x4 words;
+                    __builtin_memcpy(&words, &x, 16);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) words[e] = finite_only<DT>(words[e]);
+                    __builtin_memcpy(&x, &words, 16);
+                }
                 typename Elem<typename AttnType<DT>::T>::vec8 f;
                 __builtin_memcpy(&f, &x, 16);
                 acc = Elem<typename AttnType<DT>::T>::mma(f, w.p[t], acc);
@@ -220,16 +243,6 @@ __device__ __forceinline__ Pair pair_of_keys(const AttnArgs& a, const SeqTile& t
 // look into those tiles before they multiply, put zeros in the place of what is not finite, and go over the rows that had it
 // again behind the loop, for those alone that see them: at most the diagonal tiles' rows, whatever the length.  (16,384 x 4 x 64 f16 with
 // two infinities among the values: 0.37 ms as without; 138 where what they had spoilt was summed anew over all keys.)
-template <int DT> __device__ __forceinline__ uint32_t not_finite(uint32_t w) {       // the sign bit of every value that is not
-    if (DT == FX_F32) return ((w & 0x7F800000u) + 0x00800000u) & 0x80000000u;
-    if (DT == FX_F16) return ((w & 0x7C007C00u) + 0x04000400u) & 0x80008000u;
-    return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
-}
-// zeros in the place of values that are not finite
-template <int DT> __device__ __forceinline__ uint32_t finite_only(uint32_t w) {
-    const uint32_t bad = not_finite<DT>(w);
-    return w & ~(DT == FX_F32 ? (uint32_t)((int)bad >> 31) : (bad >> 15) * 0xFFFFu);
-}
 // As many wait states as any matrix instruction needs before its result is read.  Behind a loop, whose end and branches meet: the
 // compiler has counted the states of one such path and not of a shorter one.
 __device__ __forceinline__ void matrix_results_ready() {

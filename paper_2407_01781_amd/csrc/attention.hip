@@ -83,7 +83,7 @@ template <int DT, int DP, bool TINY = false> struct FwdWave {
             if (TINY && DT != FX_F32 && tiny) {
                 w.set(w.rest(s[t]));
 #pragma unroll
-                for (int k = 0; k < COLS; ++k) columns(acc[k], vt, row0 + t * 32, k, w);
+                for (int k = 0; k < COLS; ++k) columns.template operator()<true>(acc[k], vt, row0 + t * 32, k, w);
             }
         }
         sum += part;

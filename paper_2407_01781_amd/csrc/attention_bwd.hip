@@ -179,7 +179,7 @@ template <int DT, int DP, bool TINY = false> struct GqWave {
             if (TINY && DT != FX_F32 && tiny) {
                 w.set(w.rest(p[t]));
 #pragma unroll
-                for (int k = 0; k < S::COLS; ++k) columns(acc[k], kt + part * S::kPart, t * 32, k, w);
+                for (int k = 0; k < S::COLS; ++k) columns.template operator()<true>(acc[k], kt + part * S::kPart, t * 32, k, w);
             }
         }
     }
@@ -438,9 +438,9 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
             wp.set(wp.rest(p));
             wd.set(wd.rest(ds));
 #pragma unroll
-            for (int i = 0; i < S::COLS; ++i) columns(gv[i], ot + part * S::kPart, 0, i, wp);
+            for (int i = 0; i < S::COLS; ++i) columns.template operator()<true>(gv[i], ot + part * S::kPart, 0, i, wp);
 #pragma unroll
-            for (int i = 0; i < S::COLS; ++i) columns(gk[i], qt + part * S::kPart, 0, i, wd);
+            for (int i = 0; i < S::COLS; ++i) columns.template operator()<true>(gk[i], qt + part * S::kPart, 0, i, wd);
         }
     }
 

@@ -52,7 +52,8 @@ def test_time(heads, kv_heads, d, dtype, bad, which):
 
 @pytest.mark.parametrize("lens,kv_lens,heads,kv_heads,d,dtype", [
     ([700], None, 2, 1, 64, "bf16"), ([500, 300], None, 4, 2, 128, "f16"), ([300], [420], 3, 1, 40, "f32"), ([150] * 30, None, 4, 4, 32, "bf16"),
-    ([2000, 90], None, 16, 8, 64, "f16"), ([900], None, 8, 8, 128, "bf16"), ([70], [33], 2, 2, 200, "bf16"), ([330], None, 2, 2, 200, "f32"), ([4300] + [300] * 100, None, 1, 1, 64, "bf16")])
+    ([2000, 90], None, 16, 8, 64, "f16"), ([900], None, 8, 8, 128, "bf16"), ([70], [33], 2, 2, 200, "bf16"), ([330], None, 2, 2, 200, "f32"), ([4300] + [300] * 100, None, 1, 1, 64, "bf16"),
+    ([12, 60, 33, 9], None, 4, 2, 64, "f16"), ([1, 2, 5, 16, 17, 3], None, 3, 1, 32, "bf16"), ([16, 4], [7, 30], 2, 2, 128, "bf16"), ([15], None, 1, 1, 200, "f16")])
 @pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
 def test_seen_and_unseen(lens, kv_lens, heads, kv_heads, d, dtype, bad):
     """Every element of out and gv against the formula where a value, or an output's gradient, is not finite: what does not see it is
@@ -133,3 +134,30 @@ def test_values_that_a_step_sees(dtype, d, n, bad):
     fx.cache_write(cache, table, torch.zeros(2, dtype=torch.int32, device="cuda"), k, v, seqs=keys)
     out, _ = fx.attention_step(cache, table, torch.full((2,), n, dtype=torch.int32, device="cuda"), q)
     A.check(_f64(out), want, bound, dtype, "step")
+
+
+@SEEN[0]
+@SEEN[1]
+@SEEN[2]
+def test_values_that_rows_see(dtype, d, n, bad):
+    q, k, v, keys, want, bound = _seen(dtype, d, n, bad)
+    A.check(_f64(fx.attention_fwd(fx.build_sequences([[0, 1], [1, 2]]), q, k, v, kv_seqs=keys)[0]), want, bound, dtype, "forward")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("lens", [[1, 2, 8, 16, 30], [1, 2, 9, 16, 40, 200]])
+def test_gradients_of_few_rows(dtype, bad, lens):
+    """An infinity in an output's gradient is what the values that its row sees have there, over few rows and many."""
+    heads, kvh, d = 2, 1, 64
+    b, jo = _joff(lens)
+    seqs = fx.build_sequences(jo)
+    t = [draw(s, b[-1], h, d, dtype)[0] for s, h in ((1, heads), (2, kvh), (3, kvh), (4, heads))]
+    ref = A.attention_grad(*[_f64(x) for x in t], b, b, False, d ** -0.5, dtype)
+    out, lse = fx.attention_fwd(seqs, *t[:3])
+    want = ref[2].copy()
+    for s in range(len(lens)):
+        t[3][int(b[s]) + lens[s] // 2, 1, 5] = bad
+        want[b[s]:b[s + 1], 0, 5] = bad
+    _, _, gv = fx.attention_bwd(seqs, *t[:3], out, lse, t[3])
+    A.check(_f64(gv), want, ref[5], dtype, "gv")
