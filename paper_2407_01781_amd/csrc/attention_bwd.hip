@@ -105,6 +105,10 @@ template <int DT, int DP, bool TINY = false> struct GqWave {
         tiny = p.nk <= kTinyRows;
         lift = first_lift<DT>();
         if (one_key) delta = 0.f;
+        if (lse2 == -INFINITY) {            // a row without a weight: whatever its gradients hold, they go nowhere
+            lse2 = INFINITY;
+            delta = glse = 0.f;
+        }
         q.load(a.q.p + (int64_t)p.q0 * a.q.ld + head * a.q.hs, a.q.ld, row0, p.nq, a.dim_bytes, lane, a.negative);
 #pragma unroll
         for (int k = 0; k < S::COLS; ++k) acc[k] = f32x16(0.f);
