@@ -34,6 +34,8 @@ template <int DT, int DP> struct BwdShape {
     template <int RG, int KS> static constexpr int lds_few() { return flags_few<RG, KS>() + kFlags; }
 };
 
+// a block's rows of 32 that do not exist: their queries are zeros, but zero times a key's infinity is none
+__device__ __forceinline__ uint32_t rows_behind(int left) { return left < 32 ? ~0u << left : 0u; }
 // zeros in the place of the rows of a 32x32 result that have a bit in `odd`
 __device__ __forceinline__ void without(uint64_t odd, int half, f32x16& x, f32x16& y) {
     const uint32_t mine = (uint32_t)odd >> (4 * half);
@@ -389,7 +391,7 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
     }
 
     // 32 queries whose first that sees the block's first key is `first`, counted from the block's first (all do where not masked)
-    // odd: rows that are not finite, whose places in the tiles have zeros (rows_again)
+    // odd: rows that are not finite, whose places in the tiles have zeros (rows_again), and those that do not exist
     __device__ __forceinline__ void block(const lds_byte* qt, const lds_byte* ot, const float* stats, bool masked, int first, uint32_t odd) {
         f32x16 p = f32x16(0.f), ds = f32x16(0.f);
 #pragma unroll
@@ -501,8 +503,7 @@ template <int DT, int DP, bool TINY = false> struct GkvWave {
     }
 };
 
-// lse (base 2, less weight_lift) and delta of ROWS rows, as the first kernel left them, into LDS; zeros for a row that does not exist, whose query and
-// gradient are zeros too: it adds nothing
+// lse (base 2, less weight_lift) and delta of ROWS rows, as the first kernel left them, into LDS; zeros for a row that does not exist
 template <int ROWS> __device__ __forceinline__ void load_stats(const AttnArgs& a, lds_byte* to, int head, int q0, int row0, int nq, int lane) {
 #if defined(__HIP_DEVICE_COMPILE__)
     const uint64_t from = (uint64_t)(a.stats + 2 * (head * a.rows_q + q0 + row0));
@@ -572,7 +573,7 @@ __global__ __launch_bounds__(64 * W, W == 4 && DP * AttnType<DT>::ES <= 128 ? 3 
             const int r = r0 + t;
             if (key0 >= p.nk || r >= p.nq || (a.causal && r + 31 + shift < key0)) continue;
             const bool masked = a.causal && r + shift < key0 + 31;
-            w.block(qt + LdsRows<RB>::row_at(t), ot + LdsRows<RB>::row_at(t), st + 2 * t, masked, key0 - shift - r, (uint32_t)(odd_rows >> t));
+            w.block(qt + LdsRows<RB>::row_at(t), ot + LdsRows<RB>::row_at(t), st + 2 * t, masked, key0 - shift - r, (uint32_t)(odd_rows >> t) | rows_behind(p.nq - r));
         }
     }
     matrix_results_ready();
@@ -668,7 +669,7 @@ __global__ __launch_bounds__(64 * RG * KS, least_waves_of(DP * AttnType<DT>::ES,
         if (j < n && key0 < p.nk && !(a.causal && r0 + 31 + shift < key0)) {
             const unsigned char* now = own + b * S::kOwn;
             const bool masked = a.causal && r0 + shift < key0 + 31;
-            w.block((const lds_byte*)now, (const lds_byte*)now + S::kBlock, (const float*)(now + 2 * S::kBlock), masked, key0 - shift - r0, odd_rows);
+            w.block((const lds_byte*)now, (const lds_byte*)now + S::kBlock, (const float*)(now + 2 * S::kBlock), masked, key0 - shift - r0, odd_rows | rows_behind(p.nq - r0));
         }
         if (NB == 1) {
             __builtin_amdgcn_s_waitcnt(0);          // what is read there has been read
