@@ -615,7 +615,7 @@ fx_status fx_attention_bwd(const fx_attention* a, const void* d_out, int64_t ld_
  *   store             FX_F32, FX_F16, FX_BF16, or FX_E4M3: 8 bits (OCP e4m3) and one exponent for every row and head,
  *                     value = code * 2^(exponent - 127).  The exponent is the least of 0 .. 255 with which no finite value of the row passes
  *                     448 (0 for a row of zeros), so that the division is exact and codes are rounded once, to nearest even;
- *                     an infinity is stored as NaN.
+ *                     an infinity is stored as NaN.  (248 is the largest that it makes; rows with 255 are NaN to a step.)
  *   d_k_exp, d_v_exp  [pages, kv_heads, page_rows] bytes, for FX_E4M3 alone
  * fx_cache_write puts row r of sequence b of `q` at position d_start[b] + r; with q NULL there are `rows` sequences of one row each.
  * Rows have dtype dt, `store` is dt or FX_E4M3 (FX_EUNSUPPORTED).  No two rows of a call may have one place.

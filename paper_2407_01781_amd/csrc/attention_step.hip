@@ -355,6 +355,7 @@ __global__ __launch_bounds__(64 * W, RESIDENT) void k_attention_step(StepArgs a)
             for (int i = 0; i < 8; ++i)
                 if (!(there >> (16 * (i >> 2) + 4 * g + (i & 3)) & 1)) {
                     s[i] = -INFINITY;
+                    if (E4M3) v_scale[i] = 1.f;          // an exponent of 255 would make NaN of zeros
 #pragma unroll
                     for (int w = 0; w < VW; ++w) vw[i][w] = 0;
                 }
