@@ -755,6 +755,10 @@ def dropout(x: torch.Tensor, p: float, seed: int, offset: int, residual: Optiona
 
 
 # ------------------------------------------------------------------------------------------ attention
+class _Broadcast(AssertionError):
+    """Rows, heads or elements lie on each other, as in the gradient of a sum: inputs are copied then."""
+
+
 def _heads(t: torch.Tensor, shape, dtype: torch.dtype, device: int, name: str):
     """Address and strides from row to row and head to head of a tensor of heads [rows, heads, dim]: any order of rows and
     heads, a head's elements next to each other."""
@@ -762,8 +766,9 @@ def _heads(t: torch.Tensor, shape, dtype: torch.dtype, device: int, name: str):
         raise AssertionError(f"{name}: {tuple(shape)} {dtype} on the current GPU expected")
     ld, hs, one = t.stride()
     rows, heads, dim = shape
-    if one != 1 and dim > 1 and rows:
-        raise AssertionError(f"{name}: a head's elements have to lie next to each other")
+    if rows and (one != 1 and dim > 1 or ld == 0 and rows > 1 or hs == 0 and heads > 1):
+        kind = _Broadcast if one == 0 and dim > 1 or ld == 0 and rows > 1 or hs == 0 and heads > 1 else AssertionError
+        raise kind(f"{name}: a head's elements have to lie next to each other, rows and heads apart")
     # the stride of a single row or head says nothing
     if heads <= 1:
         hs = dim
@@ -806,10 +811,14 @@ def attention_fwd(seqs: Sequences, q: torch.Tensor, k: torch.Tensor, v: torch.Te
                   kv_seqs: Optional[Sequences] = None, out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Softmax attention of every row over the rows of its sequence: q [rows, heads, dim], k and v [rows, kv_heads, dim] (query
     head h reads key head h // (heads / kv_heads)), or rows of kv_seqs, as many sequences.  causal: the last query stands at the last
-    key, and none sees a later one.  scale: dim ** -0.5 without.  Returns out [rows, heads, dim] and lse [heads, rows] float32, the
+    key, and none sees a later one.  scale: dim ** -0.5 without.  A head's elements lie next to each other; inputs that are broadcast
+    are copied first.  Returns out [rows, heads, dim] and lse [heads, rows] float32, the
     logarithm of the sum of exp(scale q . k); 0 and -inf for a row that sees no key."""
     device = torch.cuda.current_device()
-    a = _attention(seqs, kv_seqs, q, k, v, causal, scale, device)
+    try:
+        a = _attention(seqs, kv_seqs, q, k, v, causal, scale, device)
+    except _Broadcast:
+        return attention_fwd(seqs, q.contiguous(), k.contiguous(), v.contiguous(), causal, scale, kv_seqs, out)
     out, *op = _new_heads(q) if out is None else (out, *_heads(out, q.shape, q.dtype, device, "out"))
     lse = torch.empty((a.heads, seqs.rows), dtype=torch.float32, device=q.device)
     _check(lib.fx_attention_fwd(a, *op, lse.data_ptr(), _stream()))
@@ -821,8 +830,11 @@ def attention_bwd(seqs: Sequences, q: torch.Tensor, k: torch.Tensor, v: torch.Te
                   kv_seqs: Optional[Sequences] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """Gradients of attention_fwd's q, k and v; out and lse are its outputs, grad_lse the gradient of the second (zeros without)."""
     device = torch.cuda.current_device()
-    a = _attention(seqs, kv_seqs, q, k, v, causal, scale, device)
-    op, gp = _heads(out, q.shape, q.dtype, device, "out"), _heads(grad_out, q.shape, q.dtype, device, "grad_out")
+    try:
+        a = _attention(seqs, kv_seqs, q, k, v, causal, scale, device)
+        op, gp = _heads(out, q.shape, q.dtype, device, "out"), _heads(grad_out, q.shape, q.dtype, device, "grad_out")
+    except _Broadcast:
+        return attention_bwd(seqs, *(t.contiguous() for t in (q, k, v, out)), lse, grad_out.contiguous(), grad_lse, causal, scale, kv_seqs)
     stats = (q.shape[1], q.shape[0])
     lp, glp = _floats(lse, stats, "lse"), _floats(grad_lse, stats, "grad_lse")
     (gq, *gqp), (gk, *gkp), (gv, *gvp) = _new_heads(q), _new_heads(k), _new_heads(v)
@@ -877,8 +889,11 @@ def cache_write(cache: KVCache, table: torch.Tensor, start: torch.Tensor, k: tor
     c = cache._with(table, n, device)
     assert k.dtype in _TORCH_DT, "k and v: float32, float16 or bfloat16"
     shape = rows, cache.kv_heads, cache.dim
-    _check(lib.fx_cache_write(c, None if seqs is None else seqs._h, rows, _numbers(start, n, "start"), _TORCH_DT[k.dtype],
-                              *_heads(k, shape, k.dtype, device, "k"), *_heads(v, shape, k.dtype, device, "v"), _stream()))
+    try:
+        kp, vp = _heads(k, shape, k.dtype, device, "k"), _heads(v, shape, k.dtype, device, "v")
+    except _Broadcast:
+        return cache_write(cache, table, start, k.contiguous(), v.contiguous(), seqs)
+    _check(lib.fx_cache_write(c, None if seqs is None else seqs._h, rows, _numbers(start, n, "start"), _TORCH_DT[k.dtype], *kp, *vp, _stream()))
 
 
 def cache_read(cache: KVCache, table: torch.Tensor, start: torch.Tensor, seqs: Sequences,
@@ -907,7 +922,10 @@ def attention_step(cache: KVCache, table: torch.Tensor, lengths: torch.Tensor, q
     device = torch.cuda.current_device()
     c = cache._with(table, n, device)
     assert dim == cache.dim, f"q: {cache.dim} dimensions expected"
-    qp = _heads(q, shape, q.dtype, device, "q")
+    try:
+        qp = _heads(q, shape, q.dtype, device, "q")
+    except _Broadcast:
+        return attention_step(cache, table, lengths, q.contiguous(), scale, longest, out)
     out, *op = _new_heads(q) if out is None else (out, *_heads(out, shape, q.dtype, device, "out"))
     lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
     _check(lib.fx_attention_step(c, n, _numbers(lengths, n, "lengths"), longest, _TORCH_DT[q.dtype], heads, dim ** -0.5 if scale is None else scale,
