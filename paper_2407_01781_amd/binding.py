@@ -782,16 +782,16 @@ def _new_heads(like: torch.Tensor):
     return t, t.data_ptr(), max(heads, 1) * dim, dim
 
 
-def _floats(t: Optional[torch.Tensor], shape, name: str):
+def _floats(t: Optional[torch.Tensor], shape, device: int, name: str):
     if t is None:
         return None
-    assert t.is_cuda and t.dtype is torch.float32 and t.shape == shape and t.is_contiguous(), \
-        f"{name}: contiguous float32 {tuple(shape)} on the GPU expected"
+    assert t.get_device() == device and t.dtype is torch.float32 and t.shape == shape and t.is_contiguous(), \
+        f"{name}: contiguous float32 {tuple(shape)} on the current GPU expected"
     return t.data_ptr()
 
 
-def _numbers(t: torch.Tensor, n: int, name: str) -> int:
-    assert t.is_cuda and t.dtype is torch.int32 and t.shape == (n,) and t.is_contiguous(), f"{name}: contiguous int32 ({n},) on the GPU expected"
+def _numbers(t: torch.Tensor, n: int, device: int, name: str) -> int:
+    assert t.get_device() == device and t.dtype is torch.int32 and t.shape == (n,) and t.is_contiguous(), f"{name}: contiguous int32 ({n},) on the current GPU expected"
     return t.data_ptr()
 
 
@@ -836,7 +836,7 @@ def attention_bwd(seqs: Sequences, q: torch.Tensor, k: torch.Tensor, v: torch.Te
     except _Broadcast:
         return attention_bwd(seqs, *(t.contiguous() for t in (q, k, v, out)), lse, grad_out.contiguous(), grad_lse, causal, scale, kv_seqs)
     stats = (q.shape[1], q.shape[0])
-    lp, glp = _floats(lse, stats, "lse"), _floats(grad_lse, stats, "grad_lse")
+    lp, glp = _floats(lse, stats, device, "lse"), _floats(grad_lse, stats, device, "grad_lse")
     (gq, *gqp), (gk, *gkp), (gv, *gvp) = _new_heads(q), _new_heads(k), _new_heads(v)
     _check(lib.fx_attention_bwd(a, *op, lp, *gp, glp, *gqp, *gkp, *gvp, _stream()))
     return gq, gk, gv
@@ -893,7 +893,7 @@ def cache_write(cache: KVCache, table: torch.Tensor, start: torch.Tensor, k: tor
         kp, vp = _heads(k, shape, k.dtype, device, "k"), _heads(v, shape, k.dtype, device, "v")
     except _Broadcast:
         return cache_write(cache, table, start, k.contiguous(), v.contiguous(), seqs)
-    _check(lib.fx_cache_write(c, None if seqs is None else seqs._h, rows, _numbers(start, n, "start"), _TORCH_DT[k.dtype], *kp, *vp, _stream()))
+    _check(lib.fx_cache_write(c, None if seqs is None else seqs._h, rows, _numbers(start, n, device, "start"), _TORCH_DT[k.dtype], *kp, *vp, _stream()))
 
 
 def cache_read(cache: KVCache, table: torch.Tensor, start: torch.Tensor, seqs: Sequences,
@@ -908,7 +908,7 @@ def cache_read(cache: KVCache, table: torch.Tensor, start: torch.Tensor, seqs: S
     k = torch.empty(shape, dtype=dtype, device=cache.k.device)
     v = torch.empty_like(k)
     ld, hs = max(shape[1] * shape[2], 1), shape[2]
-    _check(lib.fx_cache_read(c, seqs._h, _numbers(start, seqs.batch_size, "start"), _TORCH_DT[dtype], k.data_ptr(), ld, hs, v.data_ptr(), ld, hs, _stream()))
+    _check(lib.fx_cache_read(c, seqs._h, _numbers(start, seqs.batch_size, device, "start"), _TORCH_DT[dtype], k.data_ptr(), ld, hs, v.data_ptr(), ld, hs, _stream()))
     return k, v
 
 
@@ -928,6 +928,6 @@ def attention_step(cache: KVCache, table: torch.Tensor, lengths: torch.Tensor, q
         return attention_step(cache, table, lengths, q.contiguous(), scale, longest, out)
     out, *op = _new_heads(q) if out is None else (out, *_heads(out, shape, q.dtype, device, "out"))
     lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
-    _check(lib.fx_attention_step(c, n, _numbers(lengths, n, "lengths"), longest, _TORCH_DT[q.dtype], heads, dim ** -0.5 if scale is None else scale,
+    _check(lib.fx_attention_step(c, n, _numbers(lengths, n, device, "lengths"), longest, _TORCH_DT[q.dtype], heads, dim ** -0.5 if scale is None else scale,
                                  *qp, *op, lse.data_ptr(), _stream()))
     return out, lse
