@@ -642,30 +642,6 @@ static fx_status run_scan(ScanArgs& a, fx_dtype dt, bool up, hipStream_t st) {
     return launch_scan_kind<FX_BF16, BWD>(a, up, st);
 }
 
-// Lists the tiles of every kind (fx_sequences::d_tiles): sequences from long to short (by the power of two of their
-// lengths), and a sequence's tiles from its last on.  Returns the longest length.
-static int64_t list_tiles(const int64_t* h_joffsets, int32_t B, SeqTile* out, const int64_t* n_tiles) {
-    int64_t count[33] = {}, longest = 0;
-    auto cls = [](int64_t len) { return len ? 64 - __builtin_clzll((unsigned long long)len) : 0; };
-    for (int t = 0; t < kSeqTileKinds; ++t) {
-        const int64_t T = kSeqTileRows[t];
-        for (int64_t& c : count) c = 0;
-        for (int32_t b = 0; b < B; ++b) {
-            const int64_t len = h_joffsets[2 * b + 1] - h_joffsets[2 * b];
-            count[cls(len)] += (len + T - 1) / T;
-            longest = std::max(longest, len);
-        }
-        for (int64_t c = 32, at = 0; c >= 0; --c) { const int64_t n = count[c]; count[c] = at; at += n; }
-        for (int32_t b = 0; b < B; ++b) {
-            const int64_t len = h_joffsets[2 * b + 1] - h_joffsets[2 * b];
-            int64_t& at = count[cls(len)];
-            for (int64_t r = (len + T - 1) / T * T - T; r >= 0; r -= T) out[at++] = SeqTile{b, (int32_t)r, (int32_t)h_joffsets[2 * b], (int32_t)len};
-        }
-        out += n_tiles[t];
-    }
-    return longest;
-}
-
 }  // namespace fx
 
 using namespace fx;
@@ -673,27 +649,28 @@ using namespace fx;
 extern "C" fx_status fx_build_sequences(const int64_t* h_joffsets, int32_t B, int64_t rows, void* stream, fx_sequences** out) {
     const char* who = "fx_build_sequences";
     if (!out || B < 0 || rows < 0 || (B > 0 && !h_joffsets)) { set_error("%s: null pointer or negative size", who); return FX_EINVAL; }
-    int64_t at = 0;
+    int64_t at = 0, longest = 0, n_tiles[kSeqTileKinds] = {};
     for (int32_t b = 0; b < B; ++b) {
         if (h_joffsets[2 * b] != at || h_joffsets[2 * b + 1] < at) {
             set_error("%s: sequence %d does not begin where the one before it ends", who, b);
             return FX_EINVAL;
         }
+        const int64_t len = h_joffsets[2 * b + 1] - at;
+        longest = std::max(longest, len);
+        for (int t = 0; t < kSeqTileKinds; ++t) n_tiles[t] += (len + kSeqTileRows[t] - 1) / (uint64_t)kSeqTileRows[t];
         at = h_joffsets[2 * b + 1];
     }
     if (at != rows) { set_error("%s: the sequences do not end at the last row", who); return FX_EINVAL; }
     if (rows > 0x7FFFFFFFll) { set_error("%s: more than 2^31-1 rows", who); return FX_ERANGE; }
     hipStream_t st = (hipStream_t)stream;
     const int64_t words = rows / 64 + 2;
-    int64_t n_tiles[kSeqTileKinds], all_tiles = 0;
-    for (int t = 0; t < kSeqTileKinds; all_tiles += n_tiles[t++]) {
-        n_tiles[t] = 0;
-        for (int32_t b = 0; b < B; ++b) n_tiles[t] += (h_joffsets[2 * b + 1] - h_joffsets[2 * b] + kSeqTileRows[t] - 1) / kSeqTileRows[t];
-    }
+    int64_t all_tiles = 0;
+    for (int64_t n : n_tiles) all_tiles += n;
     const size_t lists = ((size_t)words * 12 + (size_t)B * 8 + 4 + 15) / 16 * 16, bytes = lists + (size_t)all_tiles * sizeof(SeqTile);
+    const size_t on_host = tiles_on_host(n_tiles), upload = lists + on_host * sizeof(SeqTile);
     void* staging = nullptr;
     FX_HIP_TRY(hipStreamSynchronize(st));           // an upload before this one may still read the staging area
-    FX_TRY(host_staging(&staging, bytes, 1));
+    FX_TRY(host_staging(&staging, upload, 1));
     uint64_t* begin = (uint64_t*)staging;
     int32_t* rank = (int32_t*)(begin + words);
     int32_t* ids = rank + words;                    // the sequences with rows, then those without
@@ -710,19 +687,11 @@ extern "C" fx_status fx_build_sequences(const int64_t* h_joffsets, int32_t B, in
     int32_t* first = ids + B;
     for (int32_t b = 0; b < B; ++b) first[b] = (int32_t)h_joffsets[2 * b];
     first[B] = (int32_t)rows;
-    SeqTile* tiles = (SeqTile*)((char*)staging + lists);
-    const int64_t longest = list_tiles(h_joffsets, B, tiles, n_tiles);
+    if (on_host) list_tiles_on_host(h_joffsets, B, n_tiles, (SeqTile*)((char*)staging + lists));
     fx_sequences* q = new (std::nothrow) fx_sequences;
     if (!q) { set_error("%s: out of host memory", who); return FX_ENOMEM; }
     const fx_status s = dev_alloc(&q->buf, bytes, st);
     if (s != FX_OK) { delete q; return s; }
-    const hipError_t e = hipMemcpyAsync(q->buf, staging, bytes, hipMemcpyHostToDevice, st);
-    if (e != hipSuccess || hipStreamSynchronize(st) != hipSuccess) {
-        dev_free(q->buf, st);
-        delete q;
-        set_error("%s: upload failed: %s", who, hipGetErrorString(e));
-        return FX_EDEVICE;
-    }
     q->rows = rows;
     q->B = B;
     q->n_empty = empty;
@@ -735,6 +704,15 @@ extern "C" fx_status fx_build_sequences(const int64_t* h_joffsets, int32_t B, in
     const SeqTile* d_tiles = (const SeqTile*)((const char*)q->buf + lists);
     for (int t = 0; t < kSeqTileKinds; d_tiles += n_tiles[t++]) { q->d_tiles[t] = d_tiles; q->n_tiles[t] = n_tiles[t]; }
     q->longest = longest;
+    const hipError_t e = hipMemcpyAsync(q->buf, staging, upload, hipMemcpyHostToDevice, st);
+    const fx_status listed = e != hipSuccess ? FX_EDEVICE : all_tiles == (int64_t)on_host ? FX_OK : list_tiles(who, q, some, st);
+    const hipError_t end = hipStreamSynchronize(st);
+    if (listed != FX_OK || end != hipSuccess) {
+        if (e != hipSuccess || end != hipSuccess) set_error("%s: upload failed: %s", who, hipGetErrorString(e != hipSuccess ? e : end));
+        dev_free(q->buf, st);
+        delete q;
+        return listed != FX_OK ? listed : FX_EDEVICE;
+    }
     *out = q;
     return FX_OK;
 }

@@ -28,3 +28,13 @@ struct fx_sequences {
     const fx::SeqTile* d_tiles[fx::kSeqTileKinds] = {};
     int64_t n_tiles[fx::kSeqTileKinds] = {};
 };
+
+namespace fx {
+
+// How many tiles the host lists: all, or none where they are many
+size_t tiles_on_host(const int64_t* n_tiles);
+void list_tiles_on_host(const int64_t* h_joffsets, int32_t B, const int64_t* n_tiles, SeqTile* out);
+// Fills q's lists on the GPU; `some` sequences have rows
+fx_status list_tiles(const char* who, const fx_sequences* q, int32_t some, hipStream_t st);
+
+}  // namespace fx
