@@ -766,9 +766,11 @@ def _heads(t: torch.Tensor, shape, dtype: torch.dtype, device: int, name: str):
         raise AssertionError(f"{name}: {tuple(shape)} {dtype} on the current GPU expected")
     ld, hs, one = t.stride()
     rows, heads, dim = shape
-    if rows and (one != 1 and dim > 1 or ld == 0 and rows > 1 or hs == 0 and heads > 1):
-        kind = _Broadcast if one == 0 and dim > 1 or ld == 0 and rows > 1 or hs == 0 and heads > 1 else AssertionError
-        raise kind(f"{name}: a head's elements have to lie next to each other, rows and heads apart")
+    if not (ld and hs and one == 1) and rows:
+        if ld == 0 and rows > 1 or hs == 0 and heads > 1 or one == 0 and dim > 1:
+            raise _Broadcast(f"{name}: rows, heads and elements have to lie apart")
+        if one != 1 and dim > 1:
+            raise AssertionError(f"{name}: a head's elements have to lie next to each other")
     # the stride of a single row or head says nothing
     if heads <= 1:
         hs = dim
