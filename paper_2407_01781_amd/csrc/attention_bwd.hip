@@ -47,8 +47,9 @@ __device__ __forceinline__ void without(uint64_t odd, int half, f32x16& x, f32x1
 // ------------------------------------------------------------------ small gradients of scores in fp16
 // A gradient of a score, P dP, is about the loss gradient's size over the number of keys: in fp16, whose least number is 2^-24, it
 // would lose its digits or be 0 where gq and gk are far above that.  A row (of gq; a key of gk) takes its gradients of scores times a power of
-// two, 2^lift, that follows the largest so far: at least 2^11 and at most 2^15, so that what is lost is 2^-36 of the largest; its sums are
-// divided by it at their end.  The other types have fp32's exponents and no factor.  (131,072 x 4 x 64 in windows of 1,024: 617 us without, 674.)
+// two, 2^lift, that follows the largest so far: at least 2^7 and at most 2^15, so that what is lost is 2^-32 of the largest; its sums are
+// divided by it at their end.  The other types have fp32's exponents and no factor.  (131,072 x 4 x 64 in windows of 1,024: 612 us without, 631; 660 from 2^11 on,
+// as it then has to come down in every other tile.)
 constexpr float kMostLifted = 0x1p15f;
 // A weight of gv is at most 1 and about 1 / keys: the statistics' lse is less by 15, so that weights and with them both gradients are
 // 2^15 of themselves until they are stored, and what is lost of a weight is 2^-40
@@ -65,7 +66,7 @@ template <int NB> __device__ __forceinline__ int lower_by(const f32x16* x) {
         for (int r = 0; r < 16; ++r) big = fmaxf(big, finite(x[t][r]) ? fabsf(x[t][r]) : 0.f);
     const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(big), __float_as_uint(big), false, false);
     big = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
-    return big > kMostLifted ? (int)(__float_as_uint(big) >> 23) - 127 - 11 : 0;
+    return big > kMostLifted ? (int)(__float_as_uint(big) >> 23) - 127 - 7 : 0;
 }
 __device__ __forceinline__ float two_to(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }       // -126 .. 127
 
@@ -720,8 +721,8 @@ template <int DT> static void launch_bwd_dim(const AttnArgs& a, const AttnArgs& 
 }
 
 // A causal sequence's last keys have few queries.  Where all workgroups are resident at once those leave their compute unit half empty:
-// a second workgroup for each tile, in an order from long to short, fills it.  bf16 causal, both gradients' kernels: 16,384 x 16 / 4 x 128 4395 ->
-// 3465 us, 16,384 x 16 / 2 x 128 6600 -> 4614, 8,192 x 8 / 4 x 64 516 -> 363, 2,048 x 16 x 128 150 -> 139; with 1,024 queries for a key the join
+// a second workgroup for each tile, in an order from long to short, fills it.  bf16 causal, both gradients' kernels: 16,384 x 16 / 4 x 128 4996 ->
+// 3626 us, 16,384 x 16 / 2 x 128 6325 -> 4348, 8,192 x 8 / 4 x 64 517 -> 363, 2,048 x 16 x 128 143 -> 137; with 1,024 queries for a key the join
 // costs more than it gives (1,024 x 32 x 128: 92 -> 103).
 int key_shares(const AttnArgs& a, int32_t n_tiles, int32_t few, int64_t queries, int dim, fx_dtype dt) {
     const int parts = dim <= 128 ? 1 : dt == FX_F32 ? 4 : 2;

@@ -695,7 +695,9 @@ extern "C" fx_status fx_attention_step(const fx_cache* c, int64_t rows, const in
     // Up to 1024 positions one workgroup takes them all and there is no second launch; beyond, every sequence is
     // split into as many parts, such that there are about eight workgroups for a compute unit -- of one sequence, as many as a
     // unit holds at a time -- where that leaves the longest 256 positions at least.  (Parts of equal length, more of them in longer sequences: 327 us for 64 sequences of up to 32,768
-    // positions, 8 bits x 128, as most of two rounds of workgroups are there and the second is half empty; 32 of them for a unit 402.)
+    // positions, 8 bits x 128, as most of two rounds of workgroups are there and the second is half empty; 32 of them for a unit 402.)  One sequence of
+    // 986,880 positions x 2 x 64 bf16: 102 us with as many as are resident, 106 with eight.  A few of equal length would gain too (four of 100,000 x 4 x 128 in 8 bits 100 ->
+    // 84, two of 400,000 x 2 x 64 bf16 85 -> 82), but their lengths are not known here, and of unequal ones the longest decides.
     const int64_t items = rows * c->kv_heads * s.groups;
     if (items >= (1ll << 32) / 256) { set_error("%s: too many rows for one launch", who); return FX_ERANGE; }       // threads of a launch are counted in 32 bits
     s.splits = 1;

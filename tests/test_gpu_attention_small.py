@@ -36,7 +36,7 @@ def test_small_gradients_of_the_output(lens, heads, kv_heads, d, causal, std):
 
 @pytest.mark.parametrize("queries,keys,heads,kv_heads,d,causal", [([64], [262_144], 1, 1, 64, False), ([40, 3], [90_000, 150_000], 2, 1, 32, True), ([130], [70_000], 2, 2, 128, True)])
 def test_small_weights_of_the_gradients(queries, keys, heads, kv_heads, d, causal):
-    """Weights of some 2^-18: what the kernels lose of one is 2^-40 at most, and of a gradient of a score 2^-36 of its row's largest, here 2^-10."""
+    """Weights of some 2^-18: what the kernels lose of one is 2^-40 at most, and of a gradient of a score 2^-32 of its row's largest, here 2^-10."""
     bq, jq = _joff(queries)
     bk, jk = _joff(keys)
     seqs, kv = fx.build_sequences(jq), fx.build_sequences(jk)
