@@ -586,8 +586,8 @@ fx_status fx_dropout(const void* d_x, int64_t ld_x, fx_dtype dt, int64_t rows, i
  * Backward: d_out and d_lse are what the forward call wrote, d_gout and d_glse ([heads, rows], NULL: zeros) the gradients of
  * both outputs.  With P_ij = exp(s_ij - lse_i), dP_ij = gout_i . v_j and dS_ij = P_ij (dP_ij - sum_j P_ij dP_ij + glse_i):
  *     gq_i = scale sum_j dS_ij k_j,   gk_j = scale sum_i dS_ij q_i,   gv_j = sum_i P_ij gout_i
- * over all query heads of a key head.  In 16 bits P and dS are rounded to the type before their products (not in sums over up to
- * 16 rows); in FX_F16 P times 2^15, so that what is lost of one is 2^-40 at most, and dS times a power of two for each row of gq and each key of gk, so that what falls below the type's least number is
+ * over all query heads of a key head.  In 16 bits P and dS are rounded to the type before their products (where all sequences of a call
+ * are short, sums over up to 16 rows take along what that left); in FX_F16 P times 2^15, so that what is lost of one is 2^-40 at most, and dS times a power of two for each row of gq and each key of gk, so that what falls below the type's least number is
  * 2^-32 of the row's or key's largest, however small the gradients are.  The sum over P dP is taken as gout . out, of a sequence's few keys as it stands.  gq, gk and gv may be NULL (not computed).  No atomics: the same bits from every call.
  * Scratch: 8 bytes a row and head, and where two workgroups share a key's queries 16 bytes for each element of gk (few long causal sequences).
  * An output must not be where an input or another output is (FX_EINVAL) nor overlap them, and its rows and heads must not

@@ -177,7 +177,8 @@ template <> struct Weights<FX_BF16> : Weights16<FX_BF16> {};
 
 // A sum over up to so many rows takes along what the rounding of its weights left: over more their errors cancel as good as ever, in
 // a product with one or two they are the result's own, beside its rounding.  What is left of a weight may be 0 or negative and meets zeros
-// in the place of infinities: those are in the product with the weight itself.
+// in the place of infinities: those are in the product with the weight itself.  In the kernels of two waves alone, which calls of short sequences
+// take: in the others it costs registers that they do not have.
 constexpr int kTinyRows = 16;
 
 // acc += (columns 32 col .. 32 col + 31 of the 32 rows from row0 on)^T w, the result's rows the tile's columns

@@ -3,7 +3,7 @@
 // out_i = sum_j exp(s_ij - lse_i) v_j, s = scale q k^T, lse_i = log sum_j exp(s_ij), in one pass over the keys with the running maximum and
 // sum of each row.  Long sequences are bound by the matrix instructions and the exponentials between them: 32,768 x 16 x 128 bf16
 // causal 4.2 ms, 1.04 PFLOP/s (a library product 1.38), 65,536 x 8 x 64 causal in four sequences 1.65 ms, 0.93.  Short ones are bound by
-// a workgroup's chain of loads, two tiles and stores: 203,132 x 4 x 32 f16 in 3,400 sequences 67 us, 212 MB.
+// a workgroup's chain of loads, two tiles and stores: 203,132 x 4 x 32 f16 in 3,400 sequences 65 us, 212 MB.
 #include "attention.h"
 
 #include <limits.h>

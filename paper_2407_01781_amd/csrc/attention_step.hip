@@ -138,8 +138,8 @@ __global__ __launch_bounds__(256) void k_cache_read(CacheArgs c, CacheRows a) {
 //   out        dimensions as rows, heads as columns, over the 32 keys in the order in which the lanes hold their weights.  A lane loads
 //              VE neighbouring dimensions of each of its eight keys -- sixteen lanes a whole row -- and turns the 8 x VE block by byte
 //              permutes into VE operands, dimension VE (l % 16) + j for the j-th.  Nothing of keys or values passes through LDS.
-// Bound by HBM: 986,880 positions x 2 key heads x 64 bf16 in 92 us (5.5 TB/s), and 6 for the join; 64 sequences of up to 32,768 positions,
-// 4 x 128 in 8 bits, in 235 us with the join (4.4 TB/s).
+// Bound by HBM: 986,880 positions x 2 key heads x 64 bf16 in 93 us (5.4 TB/s), and 7 for the join; 64 sequences of up to 32,768 positions,
+// 4 x 128 in 8 bits, in 237 us with the join (4.4 TB/s).
 // Weights are split into a leading and a trailing part (three for fp32 queries over 8 bits), so that the product with 16-bit
 // values loses nothing that the output would show.  fp16 ends at 2^-24: over values in it weights are taken times 2^15, and what both parts lose is 2^-40 of
 // the largest.
