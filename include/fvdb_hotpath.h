@@ -579,6 +579,7 @@ fx_status fx_dropout(const void* d_x, int64_t ld_x, fx_dtype dt, int64_t rows, i
  * row's maximum, the sum of the weights is of the unrounded ones; in FX_F16 times a power of two, so that a weight of less than 2^-25 of the largest loses
  * 2^-36 of that at most), every output once.  A row's results depend on the keys that it sees alone,
  * a key's gradients on the queries that see it: infinities and NaN of others, of a causal sequence's later rows too, add nothing.
+ * An infinity among the values that a row sees is in its result, as long as its weight is not lost to the type.
  * (Where a causal sequence holds such a value, the rows around it take longer: a few microseconds for each such value near a row's own
  * position, whatever the sequence's length.)
  *   q_seqs, kv_seqs  the rows' division into sequences, as many of both; kv_seqs NULL: q_seqs
