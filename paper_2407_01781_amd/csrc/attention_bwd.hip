@@ -117,7 +117,7 @@ template <int DT, int DP, bool TINY = false> struct GqWave {
         for (int k = 0; k < S::COLS; ++k) acc[k] = f32x16(0.f);
     }
 
-    // odd: keys that are not finite, whose place in the tile has zeros (rows_again)
+    // odd: keys that are not finite, whose place in the tile has zeros (keys_again)
     template <int NB> __device__ __forceinline__ void blocks(const lds_byte* kt, const lds_byte* vt, int key0, bool masked, int last, uint64_t odd) {
         f32x16 p[NB], dp[NB];
         const float from = DT == FX_F16 ? (float)lift - lse2 : -lse2;         // the factor is the weights'
